@@ -84,10 +84,14 @@ typedef enum {
   UAD_E_HIP = 5,         /* a HIP runtime call failed (message has hipGetErrorString) */
   UAD_E_OOM = 6,         /* device allocation failed */
   UAD_E_UNSUPPORTED = 7, /* model dimensions the kernels do not support */
-  UAD_E_RANGE = 8        /* (from uad_synchronize) an fp16 operand of the enqueued work was not finite */
+  UAD_E_RANGE = 8,       /* (from uad_synchronize) an fp16 operand of the enqueued work was not finite */
+  UAD_E_PAGE = 9         /* (from uad_kv_synchronize, uad_synchronize) a page id, a length or a row of the
+                            enqueued work on a paged cache could not be used */
 } uad_status;
 
-enum { UAD_DTYPE_F32 = 0, UAD_DTYPE_BF16 = 1 };
+/* UAD_DTYPE_F8: e4m3 (4 exponent and 3 mantissa bits, largest value 448, no
+ * infinities), for the pools of a paged cache only. */
+enum { UAD_DTYPE_F32 = 0, UAD_DTYPE_BF16 = 1, UAD_DTYPE_F8 = 2 };
 
 typedef struct {
   int32_t n_layers;   /* L */
@@ -297,11 +301,137 @@ uad_status uad_build_schedule(const int32_t *budgets, int32_t batch, int32_t chu
  * action j measured from the request.  Pure host code. */
 uad_status uad_aal(const double *release, int32_t n, double t_act, double *aal_out);
 
+/* ---------------------------------------------------------------------------
+ * Paged K/V cache of the vision-language model that the expert's prefix comes
+ * from: the model appends the keys and values of new tokens, attends to them one
+ * token per sequence while it decodes, and the expert takes its prefix straight
+ * from the pages (uad_set_prefix_paged).
+ *
+ * Pools.  The caller owns two device arrays for the life of the handle, of
+ * UAD_DTYPE_BF16 or UAD_DTYPE_F8, 16-byte aligned, with one slot per token:
+ *   k  [n_layers][n_pages][n_kv_heads][page_size][head_dim]
+ *   v  [n_layers][n_pages][n_kv_heads][head_dim][page_size]   (transposed pages)
+ * An 8-bit pool holds x / scale (k_scale, v_scale), cut to +-448 and rounded to
+ * nearest-even once; a NaN stays one.  A bf16 pool rounds to nearest-even once.
+ * Slots that no call has written may hold anything, NaN included.
+ *
+ * Sequences.  Calls take int32 device arrays: a page table [n_seqs][pages_per_seq]
+ * (cache position p of sequence b lies in page page_table[b][p / page_size] at
+ * offset p % page_size, the same ids in every layer; entries behind a sequence's
+ * last page are not read) and lens [n_seqs], the tokens that the cache holds for
+ * each sequence, the new ones of this call included: a decoding step raises lens
+ * once and hands the same array to uad_kv_append and uad_kv_attend of every
+ * layer.  The device checks what it reads there: a page id outside 0..n_pages-1,
+ * a length below 0, beyond the table or below the sequence's new rows, and a
+ * row_start that does not rise within 0..n_rows raise UAD_E_PAGE, reported by
+ * uad_kv_synchronize; such an entry touches no memory, and the results of that
+ * work are invalid.  Pages may be shared between sequences for reading; two
+ * tokens of one call that go to the same slot leave either's value there.
+ *
+ * Rotation.  With rope_dim > 0, elements (i, i + rope_dim/2) of a head, or
+ * neighbours (2i, 2i+1) with rope_pairs, are turned by position * w_i,
+ * w_i = rope_theta^(-2i/rope_dim), i < rope_dim/2: (a, b) becomes
+ * (a cos - b sin, b cos + a sin).  Angles are held in 64 bits (positions may be
+ * far).  uad_kv_append turns keys, uad_kv_attend the query.
+ *
+ * Work is enqueued on the handle's stream, allocates nothing and can be captured
+ * into a HIP graph.  Work of one handle shares the handle's workspace and must
+ * not overlap on the device: use a handle per stream (several handles may share
+ * pools), and do not replay two graphs of one handle at once.  A handle is not
+ * thread-safe.  The calling thread's current device is left as it was.
+ * ------------------------------------------------------------------------- */
+typedef struct uad_kv uad_kv; /* opaque, owned by the library */
+
+typedef struct {
+  int32_t n_layers;
+  int32_t n_heads;    /* query heads, a multiple of n_kv_heads; head j reads KV head floor(j*n_kv_heads/n_heads) */
+  int32_t n_kv_heads;
+  int32_t head_dim;   /* 64, 128 or 256 */
+  int32_t page_size;  /* 16, 32, 64, 128 or 256 tokens */
+  int32_t n_pages;
+  int32_t max_seqs;   /* largest n_seqs of any later call */
+  int32_t dtype;      /* of the pools: UAD_DTYPE_BF16 or UAD_DTYPE_F8 */
+  int32_t rope_dim;   /* 0 (no rotation) or a multiple of 16 up to head_dim */
+  int32_t rope_pairs; /* 0: halves (i, i + rope_dim/2); 1: neighbours */
+  double rope_theta;  /* > 0 (unused with rope_dim 0) */
+  float k_scale, v_scale; /* finite and > 0; 1 with UAD_DTYPE_BF16 */
+  void *k, *v;        /* the pools, device memory of the handle's device */
+} uad_kv_config;
+
+/* Create a handle on HIP device `device` that enqueues on `hip_stream` (NULL:
+ * the null stream) and allocates the workspace of its calls.  Errors:
+ * UAD_E_INVALID (null or negative fields, unaligned pools, bad dtype or scale),
+ * UAD_E_UNSUPPORTED (head_dim, page_size, rope_dim or head counts the kernels do
+ * not take), UAD_E_SHAPE (a pool's allocation ends before the pool does, or is
+ * not device memory of this device), UAD_E_OOM, UAD_E_HIP.  On error *out is set
+ * to NULL. */
+uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_stream, uad_kv **out);
+
+/* Free the handle's workspace (after synchronising its stream); the pools stay the caller's. */
+void uad_kv_destroy(uad_kv *kv);
+
+/* Message for the last non-OK status of this handle; kv == NULL: of the last
+ * failed uad_kv_create on this thread. */
+const char *uad_kv_last_error(const uad_kv *kv);
+
+/* Re-target the handle at another stream of the same device, after its queued work is done. */
+uad_status uad_kv_set_stream(uad_kv *kv, void *hip_stream);
+
+/* Append keys and values of new tokens to one layer's pages; keys are rotated on
+ * the way.
+ *   k, v        device [n_rows][n_kv_heads][head_dim] of dtype F32 or BF16, rows
+ *               ldk / ldv elements apart (at least n_kv_heads * head_dim), aligned
+ *               to their type (to 16 bytes is faster)
+ *   row_start   int32 [n_seqs + 1], rising from 0: rows row_start[b] ..
+ *               row_start[b+1]-1 are sequence b's new tokens in order (none is
+ *               fine), and rows from row_start[n_seqs] on are ignored; NULL: one
+ *               row per sequence (n_rows == n_seqs)
+ *   positions   int32 [n_rows] rotation positions, or NULL: the cache positions.
+ *               Row j of sequence b's n new rows takes cache position
+ *               lens[b] - n + j.
+ * Errors: UAD_E_INVALID (null pointer, bad layer, dtype or row length),
+ * UAD_E_SHAPE (n_seqs beyond max_seqs, n_rows != n_seqs without row_start),
+ * UAD_E_HIP. */
+uad_status uad_kv_append(uad_kv *kv, int32_t layer, const void *k, const void *v, int32_t dtype, int64_t ldk,
+                         int64_t ldv, int32_t n_rows, const int32_t *row_start, const int32_t *lens,
+                         const int32_t *positions, const int32_t *page_table, int32_t pages_per_seq, int32_t n_seqs);
+
+/* Attention of one query token per sequence over the lens[b] tokens of its pages
+ * in one layer: out = softmax(scale * q K^T) V per head, in fp32, rounded once to
+ * the type of q.  A sequence of length 0 gives zeros.
+ *   q, out      device [n_seqs][n_heads][head_dim] of dtype F32 or BF16, sequences
+ *               ldq / ldo elements apart, aligned to their type; out may not
+ *               overlap q or the pools
+ *   positions   int32 [n_seqs] rotation positions of the queries, or NULL: lens[b] - 1
+ *   scale       softmax scale, finite (1/sqrt(head_dim) as a rule)
+ * Errors as uad_kv_append. */
+uad_status uad_kv_attend(uad_kv *kv, int32_t layer, const void *q, void *out, int32_t dtype, int64_t ldq, int64_t ldo,
+                         const int32_t *lens, const int32_t *positions, const int32_t *page_table,
+                         int32_t pages_per_seq, int32_t n_seqs, float scale);
+
+/* uad_set_prefix_kv from a paged cache: environment b's prefix is the first
+ * prefix_len tokens of sequence b, in every layer (values of an 8-bit pool are
+ * rounded to bf16).  The cache must have the expert's n_layers, n_kv_heads and
+ * head_dim.  Unlike uad_set_prefix_kv it is enqueued on the context's stream,
+ * ordered after the work queued on the cache's stream, which goes on after it.
+ *   lens        int32 device [batch]: a length below prefix_len raises UAD_E_PAGE
+ *               (from both handles' synchronize), as do the ids checked there
+ * Errors: UAD_E_INVALID, UAD_E_SHAPE (batch > max_batch, prefix_len > max_prefix
+ * or beyond the page table, another model or device), UAD_E_HIP (after work was
+ * enqueued: no prefix is set then). */
+uad_status uad_set_prefix_paged(uad_ctx *ctx, uad_kv *kv, const int32_t *lens, const int32_t *page_table,
+                                int32_t pages_per_seq, int32_t batch, int32_t prefix_len);
+
+/* Block the host until the handle's queued work is done, then read and clear its
+ * status word.  Errors: UAD_E_PAGE, UAD_E_HIP. */
+uad_status uad_kv_synchronize(uad_kv *kv);
+
 /* Block the host until all work enqueued on the context's stream is done,
  * then read and clear the context's device status word: UAD_E_RANGE when a
  * GEMM or attention operand rounded to fp16 was not finite (|value| > 65504,
- * or NaN) since the last call, UAD_E_HIP when an in-kernel wait gave up; the
- * results of that work are then invalid.  Errors: UAD_E_HIP, UAD_E_RANGE. */
+ * or NaN) since the last call, UAD_E_PAGE when a prefix from pages met an id or
+ * length that cannot be used, UAD_E_HIP when an in-kernel wait gave up; the
+ * results of that work are then invalid.  Errors: UAD_E_HIP, UAD_E_RANGE, UAD_E_PAGE. */
 uad_status uad_synchronize(uad_ctx *ctx);
 
 /* Device wall-clock tick rate (Hz) of the counter written to step_ticks. */

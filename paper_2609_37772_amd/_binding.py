@@ -21,20 +21,24 @@ __all__ = [
     "uad_denoise_budgets", "uad_denoise_release", "uad_build_schedule", "uad_aal", "uad_synchronize", "uad_tick_rate_hz",
     "uad_debug_velocity_field", "uad_profile_enable", "uad_profile_read", "UAD_DTYPE_F32", "UAD_DTYPE_BF16", "STATUS_NAMES",
     "UAD_RELEASE_UAER", "UAD_RELEASE_TR", "UAD_FLAG_ADARMS",
+    "uad_kv_create", "uad_kv_destroy", "uad_kv_last_error", "uad_kv_set_stream", "uad_kv_append", "uad_kv_attend",
+    "uad_kv_synchronize", "uad_set_prefix_paged", "UAD_DTYPE_F8",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libuad.so")
-UAD_DTYPE_F32, UAD_DTYPE_BF16 = 0, 1
+UAD_DTYPE_F32, UAD_DTYPE_BF16, UAD_DTYPE_F8 = 0, 1, 2
 UAD_RELEASE_UAER, UAD_RELEASE_TR = 0, 1
 UAD_FLAG_ADARMS = 1
 STATUS_NAMES = {0: "UAD_OK", 1: "UAD_E_INVALID", 2: "UAD_E_SHAPE", 3: "UAD_E_STATE", 4: "UAD_E_MISSING",
-                5: "UAD_E_HIP", 6: "UAD_E_OOM", 7: "UAD_E_UNSUPPORTED", 8: "UAD_E_RANGE"}
+                5: "UAD_E_HIP", 6: "UAD_E_OOM", 7: "UAD_E_UNSUPPORTED", 8: "UAD_E_RANGE", 9: "UAD_E_PAGE"}
 EXPORTED_SYMBOLS = [
     "uad_create", "uad_destroy", "uad_last_error", "uad_set_stream", "uad_load_weights",
     "uad_set_prefix_kv", "uad_denoise_step", "uad_denoise_step_static", "uad_denoise_schedule", "uad_denoise_budgets",
     "uad_denoise_release",
     "uad_build_schedule", "uad_aal", "uad_synchronize", "uad_tick_rate_hz", "uad_debug_velocity_field",
     "uad_profile_enable", "uad_profile_read",
+    "uad_kv_create", "uad_kv_destroy", "uad_kv_last_error", "uad_kv_set_stream", "uad_kv_append", "uad_kv_attend",
+    "uad_kv_synchronize", "uad_set_prefix_paged",
 ]
 
 
@@ -56,6 +60,14 @@ class uad_tensor(ctypes.Structure):
                 ("ndim", ctypes.c_int32), ("shape", ctypes.c_int64 * 4), ("on_device", ctypes.c_int32)]
 
 
+class uad_kv_config(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_seqs", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rope_dim", ctypes.c_int32),
+                ("rope_pairs", ctypes.c_int32), ("rope_theta", ctypes.c_double), ("k_scale", ctypes.c_float),
+                ("v_scale", ctypes.c_float), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -67,7 +79,7 @@ def load_library() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise RuntimeError(f"{LIB_PATH} is not built; run `python -m paper_2609_37772_amd.build`")
     lib = ctypes.CDLL(LIB_PATH)
-    P, I32, F32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
+    P, I32, I64, F32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
     sig = {
         "uad_create": ([ctypes.POINTER(uad_model_config), I32, P, ctypes.POINTER(P)], I32),
         "uad_destroy": ([P], None),
@@ -87,6 +99,14 @@ def load_library() -> ctypes.CDLL:
         "uad_debug_velocity_field": ([P, I32, F32, F32], I32),
         "uad_profile_enable": ([P, I32], I32),
         "uad_profile_read": ([P, I32, ctypes.c_char_p, I32, P, P], I32),
+        "uad_kv_create": ([ctypes.POINTER(uad_kv_config), I32, P, ctypes.POINTER(P)], I32),
+        "uad_kv_destroy": ([P], None),
+        "uad_kv_last_error": ([P], ctypes.c_char_p),
+        "uad_kv_set_stream": ([P, P], I32),
+        "uad_kv_append": ([P, I32, P, P, I32, I64, I64, I32, P, P, P, P, I32, I32], I32),
+        "uad_kv_attend": ([P, I32, P, P, I32, I64, I64, P, P, P, I32, I32, F32], I32),
+        "uad_kv_synchronize": ([P], I32),
+        "uad_set_prefix_paged": ([P, P, P, P, I32, I32, I32], I32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -106,11 +126,14 @@ def _check(ctx, st: int, what: str):
         raise UadError(st, f"{what}: {msg.decode() if msg else ''}")
 
 
-def _dev_ptr(t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...], name: str) -> Optional[int]:
+def _dev_ptr(t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...], name: str,
+             device: Optional[int] = None) -> Optional[int]:
     if t is None:
         return None
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{name} must be on device {device}, got {t.get_device()}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if tuple(t.shape) != tuple(shape):
@@ -381,3 +404,120 @@ def uad_profile_read(ctx: int) -> Dict[str, Tuple[float, int]]:
         out[name.value.decode()] = (ms.value, n.value)
         i += 1
     return out
+
+
+# ----------------------------------------------------------------------------
+# Paged K/V cache
+# ----------------------------------------------------------------------------
+_ROW_TYPES = {torch.float32: UAD_DTYPE_F32, torch.bfloat16: UAD_DTYPE_BF16}
+
+
+def _check_kv(kv, st: int, what: str):
+    if st != 0:
+        raise UadError(st, f"{what}: {uad_kv_last_error(kv)}")
+
+
+def _rows(t: torch.Tensor, shape: Tuple[int, ...], name: str, device: int) -> Tuple[int, int, int]:
+    """(pointer, uad dtype, elements between rows) of a device tensor of rows [n][heads][head_dim], each row dense."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != device:
+        raise ValueError(f"{name} must be a tensor on device {device}")
+    dt = _ROW_TYPES.get(t.dtype)
+    if dt is None:
+        raise ValueError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    if t.dim() != 3 or t.shape[1:] != shape:
+        raise ValueError(f"{name} must be [rows][{shape[0]}][{shape[1]}], got {tuple(t.shape)}")
+    ld, heads, inner = t.stride()
+    row = shape[0] * shape[1]
+    if t.shape[0] < 2:
+        ld = row  # the stride of a dimension of one says nothing
+    if t.numel() and (inner != 1 or (heads != shape[1] and shape[0] > 1) or ld < row):
+        raise ValueError(f"{name} must have dense rows that do not overlap, got strides {t.stride()}")
+    return t.data_ptr(), dt, max(ld, row)
+
+
+def _ints(t: Optional[torch.Tensor], shape: Tuple[int, ...], name: str, device: int) -> Optional[int]:
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.shape != shape or not t.is_cuda \
+            or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on device {device}")
+    return t.data_ptr()
+
+
+def _table(page_table: torch.Tensor, lens: torch.Tensor, device: int) -> Tuple[int, int, int, int]:
+    """(page table, pages per sequence, lens, sequences) of a call."""
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be an int32 device tensor [n_seqs][pages_per_seq]")
+    n, wide = page_table.shape
+    return _ints(page_table, (n, wide), "page_table", device), wide, _ints(lens, (n,), "lens", device), n
+
+
+def uad_kv_create(n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int,
+                  max_seqs: int, dtype: int, rope_dim: int, rope_pairs: int, rope_theta: float, k_scale: float,
+                  v_scale: float, k: torch.Tensor, v: torch.Tensor, device: int = 0,
+                  stream: Optional[torch.cuda.Stream] = None) -> int:
+    """Create a paged-cache handle over the pools ``k`` and ``v`` (kept by the caller); returns it."""
+    cfg = uad_kv_config(n_layers, n_heads, n_kv_heads, head_dim, page_size, n_pages, max_seqs, dtype, rope_dim,
+                        rope_pairs, float(rope_theta), float(k_scale), float(v_scale), k.data_ptr(), v.data_ptr())
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    out = ctypes.c_void_p()
+    st = load_library().uad_kv_create(ctypes.byref(cfg), device, ctypes.c_void_p(stream.cuda_stream), ctypes.byref(out))
+    _check_kv(None, st, "uad_kv_create")
+    return out.value
+
+
+def uad_kv_destroy(kv: int) -> None:
+    load_library().uad_kv_destroy(kv)
+
+
+def uad_kv_last_error(kv: Optional[int]) -> str:
+    m = load_library().uad_kv_last_error(kv)
+    return m.decode() if m else ""
+
+
+def uad_kv_set_stream(kv: int, stream: Optional[torch.cuda.Stream]) -> None:
+    _check_kv(kv, load_library().uad_kv_set_stream(kv, None if stream is None else stream.cuda_stream), "uad_kv_set_stream")
+
+
+def uad_kv_append(kv: int, layer: int, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor,
+                  row_start: Optional[torch.Tensor], positions: Optional[torch.Tensor], row_shape: Tuple[int, int],
+                  device: int = 0) -> None:
+    """Append rows k, v [n_rows][Hkv][hd] (rows may be slices of wider ones) to a layer's pages."""
+    pk, dk, ldk = _rows(k, row_shape, "k", device)
+    pv, dv, ldv = _rows(v, row_shape, "v", device)
+    n = k.shape[0]
+    if dk != dv or v.shape[0] != n:
+        raise ValueError("k and v must share dtype and rows")
+    pt, wide, pl, seqs = _table(page_table, lens, device)
+    ps = _ints(row_start, (seqs + 1,), "row_start", device)
+    pp = _ints(positions, (n,), "positions", device)
+    st = load_library().uad_kv_append(kv, layer, pk, pv, dk, ldk, ldv, n, ps, pl, pp, pt, wide, seqs)
+    if st:
+        _check_kv(kv, st, "uad_kv_append")
+
+
+def uad_kv_attend(kv: int, layer: int, q: torch.Tensor, out: torch.Tensor, page_table: torch.Tensor,
+                  lens: torch.Tensor, positions: Optional[torch.Tensor], scale: float, row_shape: Tuple[int, int],
+                  device: int = 0) -> None:
+    """Attention of q [n_seqs][Hq][hd], one token per sequence, over a layer's pages into out (q's type and shape)."""
+    pt, wide, pl, seqs = _table(page_table, lens, device)
+    pq, dq, ldq = _rows(q, row_shape, "q", device)
+    po, do, ldo = _rows(out, row_shape, "out", device)
+    if dq != do or q.shape[0] != seqs or out.shape[0] != seqs:
+        raise ValueError("q and out must share dtype and have a row per sequence")
+    pp = _ints(positions, (seqs,), "positions", device)
+    st = load_library().uad_kv_attend(kv, layer, pq, po, dq, ldq, ldo, pl, pp, pt, wide, seqs, scale)
+    if st:
+        _check_kv(kv, st, "uad_kv_attend")
+
+
+def uad_kv_synchronize(kv: int) -> None:
+    _check_kv(kv, load_library().uad_kv_synchronize(kv), "uad_kv_synchronize")
+
+
+def uad_set_prefix_paged(ctx: int, kv: int, page_table: torch.Tensor, lens: torch.Tensor, prefix_len: int,
+                         device: int = 0) -> None:
+    """The first prefix_len tokens of each sequence of a paged cache become the expert's prefix K/V."""
+    pt, wide, pl, seqs = _table(page_table, lens, device)
+    _check(ctx, load_library().uad_set_prefix_paged(ctx, kv, pl, pt, wide, seqs, prefix_len), "uad_set_prefix_paged")

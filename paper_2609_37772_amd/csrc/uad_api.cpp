@@ -1439,6 +1439,9 @@ uad_status uad_synchronize(uad_ctx *c) {
   if (e != hipSuccess) return hip_fail(c, e, "uad_synchronize: status word");
   if (w & kStatusTimeout)
     return fail(c, UAD_E_HIP, "uad_synchronize: an in-kernel wait gave up (results of that work are invalid)");
+  if (w & kStatusPage)
+    return fail(c, UAD_E_PAGE, "uad_synchronize: a prefix from pages met a page id or a length that cannot be used "
+                               "(results of that work are invalid)");
   return fail(c, UAD_E_RANGE,
               "uad_synchronize: an fp16 GEMM / attention operand was not finite (|value| > 65504 or NaN); "
               "results of that work are invalid");

@@ -57,10 +57,12 @@ constexpr size_t kKxPartialFloats = 128 * 128;
 constexpr int kBlockElems = kTileN * kTileK;  // 512 fp16 = 1 KiB
 
 // Device status word of a context (bits, cleared and reported by
-// uad_synchronize): an fp16 operand that was not finite after rounding, and an
-// in-kernel wait that gave up.
+// uad_synchronize): an fp16 operand that was not finite after rounding, an
+// in-kernel wait that gave up, and a page id, length or row of a paged cache that
+// cannot be used (a uad_kv has a status word of its own, with that bit only).
 constexpr unsigned kStatusRange = 1u;
 constexpr unsigned kStatusTimeout = 2u;
+constexpr unsigned kStatusPage = 4u;
 
 __device__ __forceinline__ void raise_status(unsigned *status, unsigned bit) {
   __hip_atomic_fetch_or(status, bit, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

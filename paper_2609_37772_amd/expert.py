@@ -36,6 +36,10 @@ class ActionExpert:
     def set_prefix_kv(self, k, v, batch: int, prefix_len: int) -> None:
         B.uad_set_prefix_kv(self.ctx, k, v, batch, prefix_len)
 
+    def set_prefix_paged(self, cache, page_table, lens, prefix_len: int) -> None:
+        """The prefix of one environment per row of ``page_table`` from a :class:`PagedKV` cache."""
+        B.uad_set_prefix_paged(self.ctx, cache.handle, page_table, lens, prefix_len, self.device)
+
     def step(self, x, t, dt, mask, v_out=None) -> None:
         B.uad_denoise_step(self.ctx, x, t, dt, mask, v_out)
 
