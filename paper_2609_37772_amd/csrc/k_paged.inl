@@ -4,6 +4,12 @@
 
 namespace uad {
 
+// The running maximum of a query is raised only when a tile passes it by more than
+// this (a power of two), which spares most tiles the rescaling.
+constexpr float kKvRescale = 8.0f;
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
 // ---------------------------------------------------------------------------
 // Element types
 // ---------------------------------------------------------------------------
@@ -124,88 +130,472 @@ hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_
 }
 
 // ---------------------------------------------------------------------------
-// Attention of one token: one workgroup per sequence and query head, four waves
-// that take every fourth key with a running maximum and sum, joined in LDS.
+// Attention of one token per sequence.
+//
+// Bound by reading K and V once.  A unit is a KV head of a sequence with up to 16 of
+// its query heads, the 16 columns of the matrix instruction: S^T = K Q^T and
+// O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, whose time is a tenth of the read's, so
+// that operands can be split into bf16 terms (a value = hi + lo [+ rest], each the bf16
+// of what is left): the rotated query and the weights keep 16 bits with bf16 results
+// and 24 with fp32 ones.
+//
+// A wave takes tiles of kTileKeys keys.  Row i of the t-th 16-key product is key
+// KPL * (i / 4) + 4 t + i % 4, so that lane group g ends with the scores of the
+// KPL = 4 * kTileKeys / 16 consecutive keys KPL * g.., which are the k index of its
+// operand of the P V product, and the keys of one 16-byte load of a transposed V page:
+// K and V go from memory to the matrix instructions' registers, with no LDS between.
+// Loads of the next K tile are issued when this one's scores are done, of the next V
+// tile when this one's products are.  The four waves take every fourth tile with
+// running maxima and sums of their own and meet in LDS at the end of a unit; units that
+// several workgroups share are joined from their slots by kv_join_kernel, in the order
+// of the keys.
 // ---------------------------------------------------------------------------
+constexpr int kAttendWaves = 4;
+constexpr int kAttendMinTiles = kAttendWaves;  // tiles of a workgroup's share, where there are as many
+
+// Workgroups per CU: the tiles in flight, the outputs and their operands take a wave
+// 120 - 234 registers, at head dim 256 more than half a SIMD's 512.
+template <int HD>
+constexpr int kAttendPerCu = HD == 256 ? 1 : 2;
+
+template <bool F8>
+constexpr int kTileKeys = F8 ? 64 : 32;  // keys of 16-byte V^T loads by the four lane groups
+
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+
+template <bool F8>
+__device__ __forceinline__ bf16x8 operand_of(u32x4_t r, int u) {  // 8 bf16 of a 16-byte load (u: which half, 8-bit)
+  union {
+    bf16x8 v;
+    bf16x2 p[4];
+    uint32_t w[4];
+  } o;
+  if constexpr (F8) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      o.p[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r[2 * u + i], 1.0f, false);
+      o.p[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r[2 * u + i], 1.0f, true);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o.w[i] = r[i];
+  }
+  return o.v;
+}
+
+// A workgroup's place in the row of tiles: its run [lo, hi), and the sequence that lo
+// falls into with that sequence's first tile.
+struct Run {
+  int64_t total, lo, hi, start;
+  int b, wgs;
+};
+
+// Lengths of all sequences, by whole waves: lane i adds up a run of them, a scan over
+// the lanes gives where each run starts.
+template <int TILE>
+__device__ __forceinline__ int64_t tiles_before(const KvAttendArgs &a, int units, int lane, int64_t *mine, bool *bad) {
+  const int per = (a.n_seqs + 63) / 64;
+  int64_t n = 0;
+  for (int i = 0; i < per; ++i) {
+    const int b = lane * per + i;
+    if (b < a.n_seqs) n += tiles_of_length(usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, bad), TILE);
+  }
+  n *= units;
+  *mine = n;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t up = __shfl_up(n, d);
+    if (lane >= d) n += up;
+  }
+  return n;  // inclusive
+}
+
+__device__ __forceinline__ int64_t from_lane(int64_t v, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)v, lane), hi = __builtin_amdgcn_readlane((uint32_t)(v >> 32), lane);
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+template <int TILE>
+__device__ __forceinline__ Run run_of(const KvAttendArgs &a, int units, int w) {
+  const int lane = threadIdx.x & 63, per = (a.n_seqs + 63) / 64;
+  bool bad = false;
+  int64_t mine;
+  const int64_t upto = tiles_before<TILE>(a, units, lane, &mine, &bad);
+  if (bad && w == 0) raise_status(a.status, kStatusPage);
+  Run r;
+  r.total = from_lane(upto, 63);
+  r.wgs = sharing_wgs(r.total, a.grid, kAttendMinTiles);
+  r.lo = r.hi = 0;
+  if (w >= r.wgs) return r;
+  r.lo = share_begin(r.total, r.wgs, w);
+  r.hi = share_begin(r.total, r.wgs, w + 1);
+  const int at = __builtin_ctzll(__ballot(upto > r.lo));  // the last lane holds the total
+  r.b = at * per;
+  r.start = from_lane(upto - mine, at);
+  return r;
+}
+
+__device__ __forceinline__ int length_of(const KvAttendArgs &a, int b) {
+  bool bad = false;
+  return usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad);
+}
+
+// LDS of the attention: the query's bf16 terms while a unit is read, then the waves'
+// outputs; behind them the waves' maxima and sums.
+template <int HD>
+constexpr int attend_lds_floats() {
+  return kAttendWaves * 16 * HD + kAttendWaves * 16 * 2;
+}
+
 template <int HD, bool F32, bool F8>
-__global__ __launch_bounds__(256) void kv_attend_kernel(KvAttendArgs a) {
-  constexpr int E = HD / 64;
-  __shared__ float qs[HD], o_s[4][HD], ml[4][2];
-  const int b = blockIdx.x, head = blockIdx.y, g = head / a.group;
+__global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD>) void kv_attend_kernel(KvAttendArgs a) {
+  constexpr int TILE = kTileKeys<F8>, NT = TILE / 16, KPL = 4 * NT;
+  constexpr int KS = HD / 32;           // k steps of Q K^T
+  constexpr int KL = F8 ? HD / 64 : KS; // 16-byte loads of a key row per lane
+  constexpr int NTO = HD / 16;          // 16-column tiles of the output
+  constexpr int TERMS = F32 ? 3 : 2;
+  constexpr int NW = kAttendWaves;
+  extern __shared__ __align__(16) float lds[];
+  __bf16 *qf = (__bf16 *)lds;                      // [TERMS][KS][64][8]
+  f32x4 *obuf = (f32x4 *)lds;                      // [NW][NTO][64]
+  float *ml = lds + NW * 16 * HD;                  // [NW][16][2]
+  static_assert(TERMS * KS * 64 * 8 * 2 <= NW * 16 * HD * 4, "the query's terms fit the waves' outputs");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  const int runs = (a.group + 15) / 16, units = a.d.n_kv_heads * runs;
+  const int rows_max = a.group < 16 ? a.group : 16;
+  Run run = run_of<TILE>(a, units, blockIdx.x);
+  const int mask = (1 << a.d.page_shift) - 1;
+  bool bad = false;
+
+  while (run.lo < run.hi) {
+    int len = length_of(a, run.b), tiles = tiles_of_length(len, TILE);
+    while (run.start + (int64_t)tiles * units <= run.lo) {  // within a lane's sequences
+      run.start += (int64_t)tiles * units;
+      if (++run.b >= a.n_seqs) return;  // only if the lengths change while this runs
+      len = length_of(a, run.b);
+      tiles = tiles_of_length(len, TILE);
+    }
+    const int64_t in_seq = run.lo - run.start;
+    const int unit = (int)(in_seq / tiles), t0 = (int)(in_seq - (int64_t)unit * tiles);
+    const int t1 = (int)(run.hi - run.lo < tiles - t0 ? t0 + (run.hi - run.lo) : tiles);
+    const int kvh = unit / runs, head0 = kvh * a.group + (unit - kvh * runs) * 16;
+    const int rows = min(16, (kvh + 1) * a.group - head0);
+    const int b = run.b, last = len - 1;
+    const int32_t *table = a.table + (int64_t)b * a.pages_per_seq;
+
+    // page ids of a tile's keys as this lane needs them for K and for V
+    auto page_ids = [&](int tile, int &kp, int &vp) {
+      kp = table[min(tile * TILE + KPL * (c >> 2), last) >> a.d.page_shift];
+      vp = table[min(tile * TILE + KPL * g, last) >> a.d.page_shift];
+    };
+    auto checked = [&](int page) {
+      const bool ok = page_ok(a.d, page);
+      bad |= !ok;
+      return ok ? page : 0;
+    };
+    u32x4_t kr[NT][KL], vr[NTO];
+    auto load_k = [&](int tile, int page) {
+      const size_t esz = F8 ? 1 : 2;
+      const char *p = (const char *)a.kp + (page_base(a.d, checked(page), kvh) + (F8 ? 16 : 8) * g) * esz;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int off = min(tile * TILE + KPL * (c >> 2) + 4 * t + (c & 3), last) & mask;
+#pragma unroll
+        for (int j = 0; j < KL; ++j) kr[t][j] = *(const u32x4_t *)(p + (size_t)off * HD * esz + j * 64);
+      }
+    };
+    auto load_v = [&](int tile, int page) {
+      const size_t esz = F8 ? 1 : 2;
+      const int off = min(tile * TILE + KPL * g, last & ~(KPL - 1)) & mask;
+      const char *p = (const char *)a.vp + (page_base(a.d, checked(page), kvh) + off + ((size_t)c << a.d.page_shift)) * esz;
+#pragma unroll
+      for (int n = 0; n < NTO; ++n) vr[n] = *(const u32x4_t *)(p + (((size_t)n * 16) << a.d.page_shift) * esz);
+    };
+
+    int tile = t0 + wave;
+    const bool any = last >= 0;
+    int next_kp = 0, next_vp = 0;
+    if (any && tile < t1) {
+      int kp, vp;
+      page_ids(tile, kp, vp);
+      if (tile + NW < t1) page_ids(tile + NW, next_kp, next_vp);
+      load_k(tile, kp);
+      load_v(tile, vp);
+    }
+
+    // the query, rotated, as bf16 terms in operand order; rows past the group are zero
+    {
+      constexpr int HP = HD / 2, RS = 64 * NW / HP;
+      const int p = threadIdx.x % HP;
+      int ea, eb;
+      rope_pair(p, a.rope_dim, a.rope_pairs != 0, &ea, &eb);
+      const bool turned = p < a.rope_dim / 2;
+      float sn = 0.f, cs = 1.f;
+      if (turned) turn_of(a.turns[p], a.positions ? a.positions[b] : last, &sn, &cs);
+      auto at = [&](int e, int row) {  // operand element of column e
+        if constexpr (F8) return (((e >> 6) * 2 + ((e >> 3) & 1)) * 64 + ((e >> 4) & 3) * 16 + row) * 8 + (e & 7);
+        else return ((e >> 5) * 64 + ((e >> 3) & 3) * 16 + row) * 8 + (e & 7);
+      };
+      for (int row = threadIdx.x / HP; row < 16; row += RS) {
+        float x = 0.f, y = 0.f;
+        if (row < rows) {
+          const int64_t qi = b * a.ldq + (int64_t)(head0 + row) * HD;
+          x = load_elem<F32>(a.q, qi + ea);
+          y = load_elem<F32>(a.q, qi + eb);
+        }
+        float v0 = turned ? x * cs - y * sn : x, v1 = turned ? y * cs + x * sn : y;
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+          const __bf16 h0 = (__bf16)v0, h1 = (__bf16)v1;
+          qf[t * KS * 512 + at(ea, row)] = h0;
+          qf[t * KS * 512 + at(eb, row)] = h1;
+          v0 -= (float)h0;
+          v1 -= (float)h1;
+        }
+      }
+    }
+    __syncthreads();
+
+    f32x4 o[NTO];
+#pragma unroll
+    for (int n = 0; n < NTO; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    for (; any && tile < t1; tile += NW) {
+      f32x4 s[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kb = 0; kb < KS; ++kb) {
+        bf16x8 qt[TERMS];
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i) qt[i] = *(const bf16x8 *)(qf + ((i * KS + kb) * 64 + lane) * 8);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const bf16x8 kf = operand_of<F8>(kr[t][F8 ? kb / 2 : kb], kb & 1);
+#pragma unroll
+          for (int i = TERMS - 1; i >= 0; --i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qt[i], s[t], 0, 0, 0);
+        }
+      }
+      const int vp = next_vp;
+      const bool more = tile + NW < t1;
+      if (more) {
+        const int kp = next_kp;
+        if (tile + 2 * NW < t1) page_ids(tile + 2 * NW, next_kp, next_vp);
+        load_k(tile + NW, kp);
+      }
+      // scores in powers of two, keys from the end on masked
+      const int key0 = tile * TILE + KPL * g;
+      const bool tail = tile * TILE + TILE > len;
+      float mt = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float v = s[t][r] * a.scale_log2;
+          if (tail && key0 + 4 * t + r > last) v = -INFINITY;
+          s[t][r] = v;
+          mt = fmaxf(mt, v);
+        }
+      mt = max_pair32(max_pair16(mt));
+      // the running maximum is raised when it is passed by more than 2^8 (the weights
+      // stay below that); all lanes of a query agree
+      if (__ballot(mt > m + kKvRescale || m == -INFINITY)) {
+        const float m1 = fmaxf(m, mt), f = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
+        m = m1;
+        l *= f;
+#pragma unroll
+        for (int n = 0; n < NTO; ++n) o[n] *= f;
+      }
+      union {
+        bf16x8 v[TERMS][NT / 2];
+        __bf16 e[TERMS][4 * NT];
+      } pf;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float p = __builtin_amdgcn_exp2f(s[t][r] - m);
+          l += p;
+#pragma unroll
+          for (int i = 0; i < TERMS; ++i) {
+            pf.e[i][4 * t + r] = (__bf16)p;
+            p -= (float)pf.e[i][4 * t + r];
+          }
+        }
+      if (tail) {  // what lies behind the last key may be anything, NaN included
+        constexpr int PER = F8 ? 4 : 2;  // elements of a register
+        const int keep = max(len - key0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int n = min(max(keep - i * PER, 0), PER);
+          const uint32_t bits = n == PER ? 0xFFFFFFFFu : (1u << (n * (32 / PER))) - 1;
+#pragma unroll
+          for (int k = 0; k < NTO; ++k) vr[k][i] &= bits;
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NTO; ++n)
+#pragma unroll
+        for (int u = 0; u < NT / 2; ++u) {
+          const bf16x8 vf = operand_of<F8>(vr[n], u);
+#pragma unroll
+          for (int i = TERMS - 1; i >= 0; --i) o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf.v[i][u], o[n], 0, 0, 0);
+        }
+      if (more) load_v(tile + NW, vp);
+    }
+
+    // the waves meet: maxima and sums, then outputs in units of the common maximum
+    l = sum_pair32(sum_pair16(l));
+    if (g == 0) {
+      ml[(wave * 16 + c) * 2] = m;
+      ml[(wave * 16 + c) * 2 + 1] = l;
+    }
+    __syncthreads();  // also: every wave is past its last read of the query
+    float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) mx = fmaxf(mx, ml[(w * 16 + c) * 2]);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float lw = ml[(w * 16 + c) * 2 + 1];
+      if (lw != 0.f) sum += lw * __builtin_amdgcn_exp2f(ml[(w * 16 + c) * 2] - mx);
+    }
+    const float f = l != 0.f ? __builtin_amdgcn_exp2f(m - mx) : 0.f;
+#pragma unroll
+    for (int n = 0; n < NTO; ++n) obuf[(wave * NTO + n) * 64 + lane] = o[n] * f;
+    __syncthreads();
+    const bool whole = t0 == 0 && t1 == tiles;
+    const size_t slot = 2 * (size_t)blockIdx.x + (t0 == 0);
+    const float scale = sum != 0.f ? a.v_scale / sum : 0.f;
+    if (c < rows) {
+#pragma unroll
+      for (int i = 0; i < NTO / NW; ++i) {
+        const int n = wave * (NTO / NW) + i;
+        f32x4 v = obuf[n * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) v += obuf[(w * NTO + n) * 64 + lane];
+        if (whole) {
+          const int64_t oi = b * a.ldo + (int64_t)(head0 + c) * HD + 16 * n + 4 * g;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) store_elem<F32>(a.out, oi + r, v[r] * scale);
+        } else {
+          *(f32x4 *)(a.part + (slot * rows_max + c) * HD + 16 * n + 4 * g) = v;
+        }
+      }
+      if (!whole && wave == 0 && g == 0) {
+        a.part_ml[(slot * rows_max + c) * 2] = mx;
+        a.part_ml[(slot * rows_max + c) * 2 + 1] = sum;
+      }
+    }
+    __syncthreads();  // the outputs are read before the next unit's query takes their place
+    run.lo += t1 - t0;
+  }
+  if (bad) raise_status(a.status, kStatusPage);
+}
+
+// One workgroup per row of a unit: the slots of the workgroups that share it, in the
+// order of the keys, each wave a quarter of them.
+template <int HD, bool F32, bool F8>
+__global__ __launch_bounds__(64 * kAttendWaves) void kv_join_kernel(KvAttendArgs a) {
+  constexpr int TILE = kTileKeys<F8>, NW = kAttendWaves, E = HD / 64;
+  __shared__ float acc_s[NW][HD], ml[NW][2];
+  const int runs = (a.group + 15) / 16, units = a.d.n_kv_heads * runs;
+  const int rows_max = a.group < 16 ? a.group : 16;
+  const int b = blockIdx.x / units, unit = blockIdx.x - b * units, row = blockIdx.y;
+  const int kvh = unit / runs, head = kvh * a.group + (unit - kvh * runs) * 16 + row;
+  if (head >= (kvh + 1) * a.group) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   bool bad = false;
-  const int len = usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad);
-  const int64_t qi = b * a.ldq + (int64_t)head * HD;
-  for (int p = threadIdx.x; p < HD / 2; p += 256) {
-    int ea, eb;
-    rope_pair(p, a.rope_dim, a.rope_pairs != 0, &ea, &eb);
-    const float x = load_elem<F32>(a.q, qi + ea), y = load_elem<F32>(a.q, qi + eb);
-    float s = 0.f, c = 1.f;
-    const bool turned = p < a.rope_dim / 2;
-    if (turned) turn_of(a.turns[p], a.positions ? a.positions[b] : len - 1, &s, &c);
-    qs[ea] = turned ? x * c - y * s : x;
-    qs[eb] = turned ? y * c + x * s : y;
-  }
-  __syncthreads();
-  float q[E], o[E], m = -INFINITY, l = 0.f;
+  int64_t mine;
+  const int64_t upto = tiles_before<TILE>(a, units, lane, &mine, &bad);
+  const int64_t total = from_lane(upto, 63);
+  const int wgs = sharing_wgs(total, a.grid, kAttendMinTiles), per = (a.n_seqs + 63) / 64;
+  int64_t start = from_lane(upto - mine, b / per);
+  for (int i = b / per * per; i < b; ++i) start += (int64_t)tiles_of_length(length_of(a, i), TILE) * units;
+  const int tiles = tiles_of_length(length_of(a, b), TILE);
+  start += (int64_t)unit * tiles;
+  const int w0 = share_holding(total, wgs, start), w1 = share_holding(total, wgs, start + tiles - 1);
+  if (w0 == w1) return;  // written by its only workgroup
+  float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    q[e] = qs[lane * E + e];
-    o[e] = 0.f;
-  }
-  for (int key = wave; key < len; key += 4) {
-    const int page = a.table[(int64_t)b * a.pages_per_seq + (key >> a.d.page_shift)];
-    if (!page_ok(a.d, page)) {
-      bad = true;
-      continue;
-    }
-    const int off = key & ((1 << a.d.page_shift) - 1);
-    const size_t base = page_base(a.d, page, g);
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s += q[e] * load_pool<F8>(a.kp, base + k_in_page(a.d, off, lane * E + e));
-    s = sum_wave64(s) * a.scale_log2;
-    const float m1 = fmaxf(m, s), f = exp2f(m - m1), p = exp2f(s - m1);
-    l = l * f + p;
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      o[e] = o[e] * f + p * load_pool<F8>(a.vp, base + v_in_page(a.d, off, lane * E + e));
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  for (int w = w0 + wave; w <= w1; w += NW) {
+    const size_t at = (2 * (size_t)w + (w == w0)) * rows_max + row;
+    const float mw = a.part_ml[at * 2], lw = a.part_ml[at * 2 + 1];
+    const float m1 = fmaxf(m, mw), f0 = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
+    const float f1 = lw != 0.f ? __builtin_amdgcn_exp2f(mw - m1) : 0.f;
     m = m1;
+    l = l * f0 + lw * f1;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = o[e] * f0 + a.part[at * HD + e * 64 + lane] * f1;
   }
-  if (bad && lane == 0) raise_status(a.status, kStatusPage);
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc_s[wave][e * 64 + lane] = o[e];
   if (lane == 0) {
     ml[wave][0] = m;
     ml[wave][1] = l;
   }
-#pragma unroll
-  for (int e = 0; e < E; ++e) o_s[wave][lane * E + e] = o[e];
   __syncthreads();
-  float mx = -INFINITY;
-  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, ml[w][0]);
-  for (int c = threadIdx.x; c < HD; c += 256) {
-    float num = 0.f, den = 0.f;
-    for (int w = 0; w < 4; ++w)
-      if (ml[w][1] > 0.f) {
-        const float f = exp2f(ml[w][0] - mx);
-        num += f * o_s[w][c];
-        den += f * ml[w][1];
-      }
-    store_elem<F32>(a.out, b * a.ldo + (int64_t)head * HD + c, den > 0.f ? num / den * a.v_scale : 0.f);
+  float mx = -INFINITY, sum = 0.f, f[NW];
+#pragma unroll
+  for (int w = 0; w < NW; ++w) mx = fmaxf(mx, ml[w][0]);
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    f[w] = ml[w][1] != 0.f ? __builtin_amdgcn_exp2f(ml[w][0] - mx) : 0.f;
+    sum += ml[w][1] * f[w];
   }
+  for (int col = threadIdx.x; col < HD; col += 64 * NW) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) v += acc_s[w][col] * f[w];
+    store_elem<F32>(a.out, b * a.ldo + (int64_t)head * HD + col, sum != 0.f ? v * (a.v_scale / sum) : 0.f);
+  }
+}
+
+int kv_attend_max_grid(int n_cu, int head_dim) { return n_cu * (head_dim == 256 ? kAttendPerCu<256> : kAttendPerCu<64>); }
+
+template <int HD, bool F32, bool F8>
+static hipError_t attend_attr() {
+  return hipFuncSetAttribute((const void *)kv_attend_kernel<HD, F32, F8>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                             attend_lds_floats<HD>() * 4);
+}
+template <int HD>
+static hipError_t attend_attrs() {
+  hipError_t e = attend_attr<HD, true, true>();
+  if (e == hipSuccess) e = attend_attr<HD, true, false>();
+  if (e == hipSuccess) e = attend_attr<HD, false, true>();
+  if (e == hipSuccess) e = attend_attr<HD, false, false>();
+  return e;
+}
+hipError_t kv_attend_init(int head_dim) {
+  return head_dim == 64 ? attend_attrs<64>() : head_dim == 128 ? attend_attrs<128>() : attend_attrs<256>();
+}
+
+template <int HD, bool F32, bool F8>
+static hipError_t launch_attend_type(KvAttendArgs a, hipStream_t s) {
+  const int runs = (a.group + 15) / 16, units = a.d.n_kv_heads * runs;
+  // no more workgroups than the page table could give work
+  const int64_t tiles = (((int64_t)a.pages_per_seq << a.d.page_shift) + kTileKeys<F8> - 1) / kTileKeys<F8>;
+  const int64_t most = tiles < ((int64_t)1 << 40) / units / a.n_seqs ? tiles * units * a.n_seqs : (int64_t)1 << 40;
+  a.grid = sharing_wgs(most, a.grid, kAttendMinTiles);
+  const dim3 wg(64 * kAttendWaves);
+  hipLaunchKernelGGL((kv_attend_kernel<HD, F32, F8>), dim3(a.grid), wg, attend_lds_floats<HD>() * 4, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.grid == 1) return e;
+  hipLaunchKernelGGL((kv_join_kernel<HD, F32, F8>), dim3(a.n_seqs * units, a.group < 16 ? a.group : 16), wg, 0, s, a);
+  return hipGetLastError();
 }
 
 template <int HD>
 static hipError_t launch_attend_hd(const KvAttendArgs &a, bool f32, bool f8, hipStream_t s) {
-  const dim3 grid(a.n_seqs, a.n_heads), wg(256);
-  if (f32 && f8) hipLaunchKernelGGL((kv_attend_kernel<HD, true, true>), grid, wg, 0, s, a);
-  else if (f32) hipLaunchKernelGGL((kv_attend_kernel<HD, true, false>), grid, wg, 0, s, a);
-  else if (f8) hipLaunchKernelGGL((kv_attend_kernel<HD, false, true>), grid, wg, 0, s, a);
-  else hipLaunchKernelGGL((kv_attend_kernel<HD, false, false>), grid, wg, 0, s, a);
-  return hipGetLastError();
+  if (f32) return f8 ? launch_attend_type<HD, true, true>(a, s) : launch_attend_type<HD, true, false>(a, s);
+  return f8 ? launch_attend_type<HD, false, true>(a, s) : launch_attend_type<HD, false, false>(a, s);
 }
 
 hipError_t launch_kv_attend(const KvAttendArgs &a, bool f32, bool f8, hipStream_t s) {
-  if (a.n_seqs < 1 || a.group < 1 || a.n_heads != a.group * a.d.n_kv_heads) return hipErrorInvalidValue;
+  if (a.n_seqs < 1 || a.group < 1 || a.n_heads != a.group * a.d.n_kv_heads || a.pages_per_seq < 1 || a.grid < 1 ||
+      a.d.page_shift < 4)
+    return hipErrorInvalidValue;
   if (a.d.head_dim == 64) return launch_attend_hd<64>(a, f32, f8, s);
   if (a.d.head_dim == 128) return launch_attend_hd<128>(a, f32, f8, s);
   if (a.d.head_dim == 256) return launch_attend_hd<256>(a, f32, f8, s);

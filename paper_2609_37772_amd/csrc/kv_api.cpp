@@ -1,10 +1,10 @@
 // C ABI of the paged K/V cache: handle, argument checks, kernel arguments.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <new>
 #include <string>
-#include <vector>
 
 #include "kv_internal.h"
 
@@ -173,13 +173,19 @@ uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_str
   hipError_t e = hipDeviceGetAttribute(&kv->n_cu, hipDeviceAttributeMultiprocessorCount, device);
   if (e != hipSuccess) return cerr(UAD_E_HIP, "hipDeviceGetAttribute", e);
   const size_t o_turns = 256, n_turns = m.rope_dim / 2;
-  const size_t total = o_turns + n_turns * sizeof(double);
+  const size_t o_ml = o_turns + 128 * sizeof(double);
+  const size_t rows = std::min(16, m.n_heads / m.n_kv_heads), slots = 2 * (size_t)kv_attend_max_grid(kv->n_cu, kv->cfg.head_dim);
+  const size_t o_part = o_ml + slots * rows * 2 * sizeof(float);
+  const size_t total = o_part + slots * rows * m.head_dim * sizeof(float);
   e = hipMalloc(&kv->buf, total);
   if (e != hipSuccess) return cerr(UAD_E_OOM, "hipMalloc(workspace)", e);
-  e = hipMemset(kv->buf, 0, total);
+  e = hipMemset(kv->buf, 0, o_ml);
   if (e == hipSuccess) e = hipEventCreateWithFlags(&kv->ev, hipEventDisableTiming);
   kv->status = (unsigned *)kv->buf;
   kv->turns = (double *)((char *)kv->buf + o_turns);
+  kv->part_ml = (float *)((char *)kv->buf + o_ml);
+  kv->part = (float *)((char *)kv->buf + o_part);
+  if (e == hipSuccess) e = kv_attend_init(m.head_dim);
   if (n_turns) {
     // turns (angle / 2 pi) per position of pair i: theta^(-2i/rope_dim) / 2 pi
     double turns[128];
@@ -267,6 +273,8 @@ uad_status uad_kv_attend(uad_kv *kv, int32_t layer, const void *q, void *out, in
   a.scale_log2 = (float)((double)scale * kv->cfg.k_scale * 1.4426950408889634);
   a.v_scale = kv->cfg.v_scale;
   a.status = kv->status;
+  a.part = kv->part; a.part_ml = kv->part_ml;
+  a.grid = kv_attend_max_grid(kv->n_cu, kv->cfg.head_dim);
   const hipError_t e = launch_kv_attend(a, dtype == UAD_DTYPE_F32, kv->cfg.dtype == UAD_DTYPE_F8, kv->stream);
   return e == hipSuccess ? UAD_OK : kv_hip_fail(kv, e, fn, "launch");
 }

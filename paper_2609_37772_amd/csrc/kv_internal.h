@@ -39,6 +39,10 @@ struct KvAttendArgs {
   float scale_log2;       // log2(e) * softmax scale * K scale
   float v_scale;
   unsigned *status;
+  // joins of units that several workgroups share: two slots per workgroup, of
+  // min(16, group) rows of unnormalised outputs [rows][head_dim] and (max, sum) per row
+  float *part, *part_ml;
+  int grid;               // workgroups of the launch
 };
 
 // The expert's prefix from the pages (stores as in PrefixArgs).
@@ -55,6 +59,10 @@ struct KvPrefixArgs {
   unsigned *status, *ctx_status;
 };
 
+// Workgroups that an attention launch may have at most (the workspace holds two
+// slots for each), and the kernels' LDS limits raised (once per handle).
+int kv_attend_max_grid(int n_cu, int head_dim);
+hipError_t kv_attend_init(int head_dim);
 hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_t s);
 hipError_t launch_kv_attend(const KvAttendArgs &a, bool f32, bool f8, hipStream_t s);
 hipError_t launch_kv_prefix(const KvPrefixArgs &a, int batch, int n_layers, bool f8, hipStream_t s);
@@ -71,5 +79,6 @@ struct uad_kv {
   void *buf = nullptr;     // status word, turns, workspace
   unsigned *status = nullptr;
   double *turns = nullptr;
+  float *part = nullptr, *part_ml = nullptr;
   hipEvent_t ev = nullptr;  // orders the cache's stream and an expert's
 };

@@ -60,4 +60,29 @@ UAD_HD void rope_pair(int p, int rope_dim, bool neighbours, int *a, int *b) {
   }
 }
 
+// ---------------------------------------------------------------------------
+// The attention's work: unit u of sequence b is (KV head, run of up to 16 query heads)
+// u, read in tiles of `tile` keys; a sequence without keys counts one tile, so that
+// somebody writes its zeros.  All tiles of all units stand in one row, sequences
+// outermost, and each workgroup takes an equal run of it, whatever the lengths are.
+// ---------------------------------------------------------------------------
+UAD_HD int tiles_of_length(int len, int tile) { return len > tile ? (int)(((int64_t)len + tile - 1) / tile) : 1; }
+
+// Workgroups that take part: at least min_tiles tiles each, where there are as many.
+UAD_HD int sharing_wgs(int64_t total, int grid, int min_tiles) {
+  const int64_t n = (total + min_tiles - 1) / min_tiles;
+  return n < grid ? (int)n : grid;
+}
+// First tile of workgroup w (and, for w + 1, the end of w's run).
+UAD_HD int64_t share_begin(int64_t total, int wgs, int w) {
+  if (total < ((int64_t)1 << 32) / 4096 && wgs <= 4096) return (uint32_t)total * (uint32_t)w / (uint32_t)wgs;
+  return total * w / wgs;
+}
+// The workgroup whose run holds tile t.
+UAD_HD int share_holding(int64_t total, int wgs, int64_t t) {
+  if (total < ((int64_t)1 << 32) / 4096 && wgs <= 4096)
+    return (int)(((uint32_t)(t + 1) * (uint32_t)wgs - 1) / (uint32_t)total);
+  return (int)(((t + 1) * wgs - 1) / total);
+}
+
 }  // namespace uad
