@@ -362,7 +362,8 @@ typedef struct {
  * the null stream) and allocates the workspace of its calls.  Errors:
  * UAD_E_INVALID (null or negative fields, unaligned pools, bad dtype or scale),
  * UAD_E_UNSUPPORTED (head_dim, page_size, rope_dim or head counts the kernels do
- * not take), UAD_E_SHAPE (a pool's allocation ends before the pool does, or is
+ * not take; max_seqs * n_kv_heads * ceil(n_heads / n_kv_heads / 16) above 2^22),
+ * UAD_E_SHAPE (a pool's allocation ends before the pool does, or is
  * not device memory of this device), UAD_E_OOM, UAD_E_HIP.  On error *out is set
  * to NULL. */
 uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_stream, uad_kv **out);

@@ -145,18 +145,19 @@ hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_
 // operand of the P V product, and the keys of one 16-byte load of a transposed V page:
 // K and V go from memory to the matrix instructions' registers, with no LDS between.
 // Loads of the next K tile are issued when this one's scores are done, of the next V
-// tile when this one's products are.  The four waves take every fourth tile with
-// running maxima and sums of their own and meet in LDS at the end of a unit; units that
-// several workgroups share are joined from their slots by kv_join_kernel, in the order
-// of the keys.
+// tile when this one's products are.  The waves of a workgroup take every
+// kAttendWaves<HD>-th tile with running maxima and sums of their own and meet in LDS.  A
+// unit's splits meet in slots of the workspace: the last workgroup to arrive joins
+// them, in the order of the keys.
 // ---------------------------------------------------------------------------
-constexpr int kAttendWaves = 4;
-constexpr int kAttendMinTiles = kAttendWaves;  // tiles of a workgroup's share, where there are as many
+constexpr int kAttendMinTiles = 4;  // tiles of a split, where a unit has as many
 
-// Workgroups per CU: the tiles in flight, the outputs and their operands take a wave
-// 120 - 234 registers, at head dim 256 more than half a SIMD's 512.
+// Waves of a workgroup, and workgroups per CU: the tiles in flight, the outputs and
+// their operands take a wave up to 256 registers at head dim 256, 170 at 128, 128 at 64.
 template <int HD>
-constexpr int kAttendPerCu = HD == 256 ? 1 : 2;
+constexpr int kAttendWaves = HD == 128 ? 4 : 8;
+template <int HD>
+constexpr int kAttendPerCu = HD == 256 ? 1 : HD == 128 ? 3 : 2;
 
 template <bool F8>
 constexpr int kTileKeys = F8 ? 64 : 32;  // keys of 16-byte V^T loads by the four lane groups
@@ -183,376 +184,466 @@ __device__ __forceinline__ bf16x8 operand_of(u32x4_t r, int u) {  // 8 bf16 of a
   return o.v;
 }
 
-// A workgroup's place in the row of tiles: its run [lo, hi), and the sequence that lo
-// falls into with that sequence's first tile.
-struct Run {
-  int64_t total, lo, hi, start;
-  int b, wgs;
+// Inclusive sum over the lanes of a wave, by DPP: within rows of 16, then across them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_i(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, true);
+}
+__device__ __forceinline__ int scan_wave64(int v) {
+  v += dpp_i<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
+  v += dpp_i<0x112, 0xF>(v);
+  v += dpp_i<0x114, 0xF>(v);
+  v += dpp_i<0x118, 0xF>(v);
+  v += dpp_i<0x142, 0xA>(v);  // the last lane of rows 0 and 2 to rows 1 and 3
+  v += dpp_i<0x143, 0xC>(v);  // lane 31 to rows 2 and 3
+  return v;
+}
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
+
+// What a workgroup does: tiles t0 .. t1-1 of a unit of sequence b; split `split` of
+// `splits`, whose slots start at `slot`.
+struct AttendWork {
+  int b, unit, len, t0, t1, split, splits, slot;
 };
 
-// Lengths of all sequences, by whole waves: lane i adds up a run of them, a scan over
-// the lanes gives where each run starts.
+// The plan (see paged.h), by whole waves: lane i looks after sequences i * per ..
 template <int TILE>
-__device__ __forceinline__ int64_t tiles_before(const KvAttendArgs &a, int units, int lane, int64_t *mine, bool *bad) {
-  const int per = (a.n_seqs + 63) / 64;
-  int64_t n = 0;
-  for (int i = 0; i < per; ++i) {
-    const int b = lane * per + i;
-    if (b < a.n_seqs) n += tiles_of_length(usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, bad), TILE);
-  }
-  n *= units;
-  *mine = n;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t up = __shfl_up(n, d);
-    if (lane >= d) n += up;
-  }
-  return n;  // inclusive
-}
-
-__device__ __forceinline__ int64_t from_lane(int64_t v, int lane) {
-  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)v, lane), hi = __builtin_amdgcn_readlane((uint32_t)(v >> 32), lane);
-  return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-
-template <int TILE>
-__device__ __forceinline__ Run run_of(const KvAttendArgs &a, int units, int w) {
+__device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, int wg, AttendWork *w) {
   const int lane = threadIdx.x & 63, per = (a.n_seqs + 63) / 64;
   bool bad = false;
-  int64_t mine;
-  const int64_t upto = tiles_before<TILE>(a, units, lane, &mine, &bad);
-  if (bad && w == 0) raise_status(a.status, kStatusPage);
-  Run r;
-  r.total = from_lane(upto, 63);
-  r.wgs = sharing_wgs(r.total, a.grid, kAttendMinTiles);
-  r.lo = r.hi = 0;
-  if (w >= r.wgs) return r;
-  r.lo = share_begin(r.total, r.wgs, w);
-  r.hi = share_begin(r.total, r.wgs, w + 1);
-  const int at = __builtin_ctzll(__ballot(upto > r.lo));  // the last lane holds the total
-  r.b = at * per;
-  r.start = from_lane(upto - mine, at);
-  return r;
+  auto length = [&](int b) { return usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad); };
+  int my_len = 0;
+  int64_t n = 0;
+  for (int i = 0; i < per; ++i)
+    if (lane * per + i < a.n_seqs) {
+      my_len = length(lane * per + i);
+      n += tiles_of_length(my_len, TILE);
+    }
+  if (bad && wg == 0) raise_status(a.status, kStatusPage);
+  n *= units;
+  const int64_t total = ((int64_t)last_lane(scan_wave64((int)(n >> 24))) << 24) + last_lane(scan_wave64((int)(n & 0xFFFFFF)));
+  int share = first_share(total, a.target, kAttendMinTiles);
+  int mine, upto;
+  auto count = [&]() {  // workgroups of this lane's sequences, and up to them
+    mine = 0;
+    if (per == 1) {
+      if (lane < a.n_seqs) mine = splits_of(tiles_of_length(my_len, TILE), share) * units;
+    } else {
+      for (int i = 0; i < per; ++i)
+        if (lane * per + i < a.n_seqs) mine += splits_of(tiles_of_length(length(lane * per + i), TILE), share) * units;
+    }
+    upto = scan_wave64(mine);
+    return last_lane(upto);
+  };
+  int wgs = count();
+  if ((int64_t)a.n_seqs * units < a.target)
+    for (int i = 0; i < kShareTries && wgs > a.target; ++i) {
+      share = next_share(share);
+      wgs = count();
+    }
+  if (wg >= wgs) return false;
+  const int at = __builtin_ctzll(__ballot(upto > wg));
+  // workgroups in split units, for the slots
+  int split_mine = 0;
+  if (per == 1) {
+    split_mine = mine > units ? mine : 0;
+  } else {
+    for (int i = 0; i < per; ++i)
+      if (lane * per + i < a.n_seqs) {
+        const int s = splits_of(tiles_of_length(length(lane * per + i), TILE), share);
+        if (s > 1) split_mine += s * units;
+      }
+  }
+  const int split_upto = scan_wave64(split_mine);
+  int start = __builtin_amdgcn_readlane(upto - mine, at), slot = __builtin_amdgcn_readlane(split_upto - split_mine, at);
+  int b = at * per, len = __builtin_amdgcn_readlane(my_len, at);
+  int tiles, splits;
+  for (;;) {
+    if (per > 1) len = __builtin_amdgcn_readfirstlane(length(b));
+    tiles = tiles_of_length(len, TILE);
+    splits = splits_of(tiles, share);
+    if (per == 1 || start + splits * units > wg) break;
+    start += splits * units;
+    if (splits > 1) slot += splits * units;
+    if (++b >= a.n_seqs) return false;  // only if the lengths change while this runs
+  }
+  w->b = b;
+  w->len = len;
+  w->unit = (unsigned)(wg - start) / (unsigned)splits;
+  if (w->unit >= units) return false;  // likewise
+  w->split = wg - start - w->unit * splits;
+  w->splits = splits;
+  w->slot = slot + w->unit * splits;
+  if (splits > 1 && w->slot + splits > a.slots) return false;  // likewise
+  w->t0 = split_begin(tiles, splits, w->split);
+  w->t1 = split_begin(tiles, splits, w->split + 1);
+  return true;
 }
 
-__device__ __forceinline__ int length_of(const KvAttendArgs &a, int b) {
-  bool bad = false;
-  return usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad);
+// A slot's values cross the XCDs' L2 caches: written through and read past them.
+__device__ __forceinline__ void put_slot(float *p, f32x4 v) {
+  union {
+    f32x4 f;
+    uint64_t u[2];
+  } x{v};
+  __hip_atomic_store((uint64_t *)p, x.u[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store((uint64_t *)p + 1, x.u[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x4 get_slot(const float *p) {
+  union {
+    uint64_t u[2];
+    f32x4 f;
+  } x;
+  x.u[0] = __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  x.u[1] = __hip_atomic_load((const uint64_t *)p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return x.f;
+}
+__device__ __forceinline__ uint64_t pair_of(float m, float l) {
+  return (uint64_t)__float_as_uint(m) | ((uint64_t)__float_as_uint(l) << 32);
 }
 
-// LDS of the attention: the query's bf16 terms while a unit is read, then the waves'
-// outputs; behind them the waves' maxima and sums.
+// LDS of the attention: the query's bf16 terms while the keys are read, then the waves'
+// outputs; behind them the waves' (or slots') maxima and sums and a word.
+constexpr int kAttendMl = 2 * kJoinFan * 16 * 2;  // floats
 template <int HD>
 constexpr int attend_lds_floats() {
-  return kAttendWaves * 16 * HD + kAttendWaves * 16 * 2;
+  return kAttendWaves<HD> * 16 * HD + kAttendMl + 16 * 2 + 4;
+}
+
+// The last of `n` workgroups to get here carries on; all of this workgroup's slot
+// values have arrived in memory by then.
+__device__ __forceinline__ bool last_to_arrive(unsigned *counter, int n, float *word) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(n - 1);
+    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *(int *)word = last;
+  }
+  __syncthreads();
+  return *(int *)word != 0;
+}
+
+// Joins slots first, first + step, .. (n of them, at most 2 * kJoinFan): outputs go to
+// `put(row, column, value, 1 / sum)`; m_s, l_s [16]: the joint maximum and sum per row.
+template <int HD, class Put>
+__device__ __forceinline__ void join_slots(const KvAttendArgs &a, int rows, int rows_max, int first, int step, int n,
+                                           float *ml, float *top, Put put) {
+  constexpr int VEC = HD / 4, THREADS = 64 * kAttendWaves<HD>;
+  const int items = rows * VEC;
+  // the first values are on their way while the weights are worked out
+  f32x4 v[kJoinFan];
+  int item = threadIdx.x;
+  auto fetch = [&](int it, int i0) {
+    const int row = it / VEC, col = it % VEC * 4;
+#pragma unroll
+    for (int i = 0; i < kJoinFan; ++i)
+      if (i0 + i < n) v[i] = get_slot(a.part + ((size_t)(first + (i0 + i) * step) * rows_max + row) * HD + col);
+  };
+  for (int i = threadIdx.x; i < n * 16; i += THREADS) {
+    const int row = i & 15;
+    uint64_t p = pair_of(-INFINITY, 0.f);
+    if (row < rows)
+      p = __hip_atomic_load(a.part_ml + (size_t)(first + (i >> 4) * step) * rows_max + row, __ATOMIC_RELAXED,
+                            __HIP_MEMORY_SCOPE_AGENT);
+    *(uint64_t *)(ml + 2 * i) = p;
+  }
+  if (item < items) fetch(item, 0);
+  __syncthreads();
+  if (threadIdx.x < 16) {
+    float mx = -INFINITY, sum = 0.f;
+    for (int i = 0; i < n; ++i) mx = fmaxf(mx, ml[2 * (i * 16 + threadIdx.x)]);
+    for (int i = 0; i < n; ++i) {
+      const float l = ml[2 * (i * 16 + threadIdx.x) + 1];
+      const float f = l != 0.f ? __builtin_amdgcn_exp2f(ml[2 * (i * 16 + threadIdx.x)] - mx) : 0.f;
+      sum += l * f;
+      ml[2 * (i * 16 + threadIdx.x)] = f;
+    }
+    top[2 * threadIdx.x] = mx;
+    top[2 * threadIdx.x + 1] = sum;
+  }
+  __syncthreads();
+  for (; item < items; item += THREADS) {
+    const int row = item / VEC;
+    if (item != (int)threadIdx.x) fetch(item, 0);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < n; i0 += kJoinFan) {
+      if (i0) fetch(item, i0);
+#pragma unroll
+      for (int i = 0; i < kJoinFan; ++i)
+        if (i0 + i < n) o += v[i] * ml[2 * ((i0 + i) * 16 + row)];
+    }
+    put(row, item % VEC * 4, o, top[2 * row + 1]);
+  }
 }
 
 template <int HD, bool F32, bool F8>
-__global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD>) void kv_attend_kernel(KvAttendArgs a) {
+__global__ __launch_bounds__(64 * kAttendWaves<HD>, kAttendPerCu<HD> * kAttendWaves<HD> / 4) void kv_attend_kernel(KvAttendArgs a) {
   constexpr int TILE = kTileKeys<F8>, NT = TILE / 16, KPL = 4 * NT;
   constexpr int KS = HD / 32;           // k steps of Q K^T
   constexpr int KL = F8 ? HD / 64 : KS; // 16-byte loads of a key row per lane
   constexpr int NTO = HD / 16;          // 16-column tiles of the output
   constexpr int TERMS = F32 ? 3 : 2;
-  constexpr int NW = kAttendWaves;
+  constexpr int NW = kAttendWaves<HD>;
+  constexpr int ESZ = F8 ? 1 : 2;
   extern __shared__ __align__(16) float lds[];
   __bf16 *qf = (__bf16 *)lds;                      // [TERMS][KS][64][8]
   f32x4 *obuf = (f32x4 *)lds;                      // [NW][NTO][64]
-  float *ml = lds + NW * 16 * HD;                  // [NW][16][2]
+  float *ml = lds + NW * 16 * HD;                  // [NW or slots][16][2]
+  float *top = ml + kAttendMl, *word = top + 32;
   static_assert(TERMS * KS * 64 * 8 * 2 <= NW * 16 * HD * 4, "the query's terms fit the waves' outputs");
+  static_assert(NW * 16 * 2 <= kAttendMl, "the waves' maxima fit the slots'");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
   const int runs = (a.group + 15) / 16, units = a.d.n_kv_heads * runs;
   const int rows_max = a.group < 16 ? a.group : 16;
-  Run run = run_of<TILE>(a, units, blockIdx.x);
-  const int mask = (1 << a.d.page_shift) - 1;
+  // the turns per position of this thread's pair of columns
+  constexpr int HP = HD / 2, RS = 64 * NW / HP, QN = (16 + RS - 1) / RS;
+  const int p = threadIdx.x % HP;
+  int ea, eb;
+  rope_pair(p, a.rope_dim, a.rope_pairs != 0, &ea, &eb);
+  const bool turned = p < a.rope_dim / 2;
+  const double turns = turned ? a.turns[p] : 0.0;
+
+  AttendWork w;
+  if (!plan_attend<TILE>(a, units, blockIdx.x, &w)) return;
+  const int kvh = w.unit / runs, head0 = kvh * a.group + (w.unit - kvh * runs) * 16;
+  const int rows = min(16, (kvh + 1) * a.group - head0);
+  const int last = w.len - 1, mask = (1 << a.d.page_shift) - 1;
+  const int32_t *table = a.table + (int64_t)w.b * a.pages_per_seq;
   bool bad = false;
 
-  while (run.lo < run.hi) {
-    int len = length_of(a, run.b), tiles = tiles_of_length(len, TILE);
-    while (run.start + (int64_t)tiles * units <= run.lo) {  // within a lane's sequences
-      run.start += (int64_t)tiles * units;
-      if (++run.b >= a.n_seqs) return;  // only if the lengths change while this runs
-      len = length_of(a, run.b);
-      tiles = tiles_of_length(len, TILE);
+  // Loads are waited for in the order of their issue: page ids and the query's values
+  // first, then the keys and values, which arrive while the query is rotated.
+  auto page_ids = [&](int tile, int &kp, int &vp) {
+    kp = table[min(tile * TILE + KPL * (c >> 2), last) >> a.d.page_shift];
+    vp = table[min(tile * TILE + KPL * g, last) >> a.d.page_shift];
+  };
+  auto checked = [&](int page) {
+    const bool ok = page_ok(a.d, page);
+    bad |= !ok;
+    return ok ? page : 0;
+  };
+  u32x4_t kr[NT][KL], vr[NTO];
+  auto load_k = [&](int tile, int page) {
+    const char *src = (const char *)a.kp + (page_base(a.d, checked(page), kvh) + (F8 ? 16 : 8) * g) * ESZ;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int off = min(tile * TILE + KPL * (c >> 2) + 4 * t + (c & 3), last) & mask;
+#pragma unroll
+      for (int j = 0; j < KL; ++j) kr[t][j] = *(const u32x4_t *)(src + (unsigned)(off * HD * ESZ) + j * 64);
     }
-    const int64_t in_seq = run.lo - run.start;
-    const int unit = (int)(in_seq / tiles), t0 = (int)(in_seq - (int64_t)unit * tiles);
-    const int t1 = (int)(run.hi - run.lo < tiles - t0 ? t0 + (run.hi - run.lo) : tiles);
-    const int kvh = unit / runs, head0 = kvh * a.group + (unit - kvh * runs) * 16;
-    const int rows = min(16, (kvh + 1) * a.group - head0);
-    const int b = run.b, last = len - 1;
-    const int32_t *table = a.table + (int64_t)b * a.pages_per_seq;
+  };
+  auto load_v = [&](int tile, int page) {
+    const int off = min(tile * TILE + KPL * g, last & ~(KPL - 1)) & mask;
+    const char *src = (const char *)a.vp + (page_base(a.d, checked(page), kvh) + off + (c << a.d.page_shift)) * ESZ;
+#pragma unroll
+    for (int n = 0; n < NTO; ++n) vr[n] = *(const u32x4_t *)(src + (unsigned)((n * 16 << a.d.page_shift) * ESZ));
+  };
 
-    // page ids of a tile's keys as this lane needs them for K and for V
-    auto page_ids = [&](int tile, int &kp, int &vp) {
-      kp = table[min(tile * TILE + KPL * (c >> 2), last) >> a.d.page_shift];
-      vp = table[min(tile * TILE + KPL * g, last) >> a.d.page_shift];
-    };
-    auto checked = [&](int page) {
-      const bool ok = page_ok(a.d, page);
-      bad |= !ok;
-      return ok ? page : 0;
-    };
-    u32x4_t kr[NT][KL], vr[NTO];
-    auto load_k = [&](int tile, int page) {
-      const size_t esz = F8 ? 1 : 2;
-      const char *p = (const char *)a.kp + (page_base(a.d, checked(page), kvh) + (F8 ? 16 : 8) * g) * esz;
+  int tile = w.t0 + wave;
+  const int t1 = last >= 0 ? w.t1 : 0;
+  int kp = 0, vp = 0, next_kp = 0, next_vp = 0;
+  if (tile < t1) page_ids(tile, kp, vp);
+  if (tile + NW < t1) page_ids(tile + NW, next_kp, next_vp);
+  int position = last;
+  if (a.positions) position = a.positions[w.b];
+  float qx[QN], qy[QN];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const int off = min(tile * TILE + KPL * (c >> 2) + 4 * t + (c & 3), last) & mask;
-#pragma unroll
-        for (int j = 0; j < KL; ++j) kr[t][j] = *(const u32x4_t *)(p + (size_t)off * HD * esz + j * 64);
-      }
-    };
-    auto load_v = [&](int tile, int page) {
-      const size_t esz = F8 ? 1 : 2;
-      const int off = min(tile * TILE + KPL * g, last & ~(KPL - 1)) & mask;
-      const char *p = (const char *)a.vp + (page_base(a.d, checked(page), kvh) + off + ((size_t)c << a.d.page_shift)) * esz;
-#pragma unroll
-      for (int n = 0; n < NTO; ++n) vr[n] = *(const u32x4_t *)(p + (((size_t)n * 16) << a.d.page_shift) * esz);
-    };
-
-    int tile = t0 + wave;
-    const bool any = last >= 0;
-    int next_kp = 0, next_vp = 0;
-    if (any && tile < t1) {
-      int kp, vp;
-      page_ids(tile, kp, vp);
-      if (tile + NW < t1) page_ids(tile + NW, next_kp, next_vp);
-      load_k(tile, kp);
-      load_v(tile, vp);
+  for (int i = 0; i < QN; ++i) {
+    const int row = threadIdx.x / HP + i * RS;
+    qx[i] = qy[i] = 0.f;
+    if (row < rows) {
+      const int64_t qi = w.b * a.ldq + (int64_t)(head0 + row) * HD;
+      qx[i] = load_elem<F32>(a.q, qi + ea);
+      qy[i] = load_elem<F32>(a.q, qi + eb);
     }
-
-    // the query, rotated, as bf16 terms in operand order; rows past the group are zero
-    {
-      constexpr int HP = HD / 2, RS = 64 * NW / HP;
-      const int p = threadIdx.x % HP;
-      int ea, eb;
-      rope_pair(p, a.rope_dim, a.rope_pairs != 0, &ea, &eb);
-      const bool turned = p < a.rope_dim / 2;
-      float sn = 0.f, cs = 1.f;
-      if (turned) turn_of(a.turns[p], a.positions ? a.positions[b] : last, &sn, &cs);
-      auto at = [&](int e, int row) {  // operand element of column e
-        if constexpr (F8) return (((e >> 6) * 2 + ((e >> 3) & 1)) * 64 + ((e >> 4) & 3) * 16 + row) * 8 + (e & 7);
-        else return ((e >> 5) * 64 + ((e >> 3) & 3) * 16 + row) * 8 + (e & 7);
-      };
-      for (int row = threadIdx.x / HP; row < 16; row += RS) {
-        float x = 0.f, y = 0.f;
-        if (row < rows) {
-          const int64_t qi = b * a.ldq + (int64_t)(head0 + row) * HD;
-          x = load_elem<F32>(a.q, qi + ea);
-          y = load_elem<F32>(a.q, qi + eb);
-        }
-        float v0 = turned ? x * cs - y * sn : x, v1 = turned ? y * cs + x * sn : y;
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-          const __bf16 h0 = (__bf16)v0, h1 = (__bf16)v1;
-          qf[t * KS * 512 + at(ea, row)] = h0;
-          qf[t * KS * 512 + at(eb, row)] = h1;
-          v0 -= (float)h0;
-          v1 -= (float)h1;
-        }
-      }
-    }
-    __syncthreads();
-
-    f32x4 o[NTO];
-#pragma unroll
-    for (int n = 0; n < NTO; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-    for (; any && tile < t1; tile += NW) {
-      f32x4 s[NT];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kb = 0; kb < KS; ++kb) {
-        bf16x8 qt[TERMS];
-#pragma unroll
-        for (int i = 0; i < TERMS; ++i) qt[i] = *(const bf16x8 *)(qf + ((i * KS + kb) * 64 + lane) * 8);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const bf16x8 kf = operand_of<F8>(kr[t][F8 ? kb / 2 : kb], kb & 1);
-#pragma unroll
-          for (int i = TERMS - 1; i >= 0; --i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qt[i], s[t], 0, 0, 0);
-        }
-      }
-      const int vp = next_vp;
-      const bool more = tile + NW < t1;
-      if (more) {
-        const int kp = next_kp;
-        if (tile + 2 * NW < t1) page_ids(tile + 2 * NW, next_kp, next_vp);
-        load_k(tile + NW, kp);
-      }
-      // scores in powers of two, keys from the end on masked
-      const int key0 = tile * TILE + KPL * g;
-      const bool tail = tile * TILE + TILE > len;
-      float mt = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float v = s[t][r] * a.scale_log2;
-          if (tail && key0 + 4 * t + r > last) v = -INFINITY;
-          s[t][r] = v;
-          mt = fmaxf(mt, v);
-        }
-      mt = max_pair32(max_pair16(mt));
-      // the running maximum is raised when it is passed by more than 2^8 (the weights
-      // stay below that); all lanes of a query agree
-      if (__ballot(mt > m + kKvRescale || m == -INFINITY)) {
-        const float m1 = fmaxf(m, mt), f = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
-        m = m1;
-        l *= f;
-#pragma unroll
-        for (int n = 0; n < NTO; ++n) o[n] *= f;
-      }
-      union {
-        bf16x8 v[TERMS][NT / 2];
-        __bf16 e[TERMS][4 * NT];
-      } pf;
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float p = __builtin_amdgcn_exp2f(s[t][r] - m);
-          l += p;
-#pragma unroll
-          for (int i = 0; i < TERMS; ++i) {
-            pf.e[i][4 * t + r] = (__bf16)p;
-            p -= (float)pf.e[i][4 * t + r];
-          }
-        }
-      if (tail) {  // what lies behind the last key may be anything, NaN included
-        constexpr int PER = F8 ? 4 : 2;  // elements of a register
-        const int keep = max(len - key0, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int n = min(max(keep - i * PER, 0), PER);
-          const uint32_t bits = n == PER ? 0xFFFFFFFFu : (1u << (n * (32 / PER))) - 1;
-#pragma unroll
-          for (int k = 0; k < NTO; ++k) vr[k][i] &= bits;
-        }
-      }
-#pragma unroll
-      for (int n = 0; n < NTO; ++n)
-#pragma unroll
-        for (int u = 0; u < NT / 2; ++u) {
-          const bf16x8 vf = operand_of<F8>(vr[n], u);
-#pragma unroll
-          for (int i = TERMS - 1; i >= 0; --i) o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf.v[i][u], o[n], 0, 0, 0);
-        }
-      if (more) load_v(tile + NW, vp);
-    }
-
-    // the waves meet: maxima and sums, then outputs in units of the common maximum
-    l = sum_pair32(sum_pair16(l));
-    if (g == 0) {
-      ml[(wave * 16 + c) * 2] = m;
-      ml[(wave * 16 + c) * 2 + 1] = l;
-    }
-    __syncthreads();  // also: every wave is past its last read of the query
-    float mx = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) mx = fmaxf(mx, ml[(w * 16 + c) * 2]);
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float lw = ml[(w * 16 + c) * 2 + 1];
-      if (lw != 0.f) sum += lw * __builtin_amdgcn_exp2f(ml[(w * 16 + c) * 2] - mx);
-    }
-    const float f = l != 0.f ? __builtin_amdgcn_exp2f(m - mx) : 0.f;
-#pragma unroll
-    for (int n = 0; n < NTO; ++n) obuf[(wave * NTO + n) * 64 + lane] = o[n] * f;
-    __syncthreads();
-    const bool whole = t0 == 0 && t1 == tiles;
-    const size_t slot = 2 * (size_t)blockIdx.x + (t0 == 0);
-    const float scale = sum != 0.f ? a.v_scale / sum : 0.f;
-    if (c < rows) {
-#pragma unroll
-      for (int i = 0; i < NTO / NW; ++i) {
-        const int n = wave * (NTO / NW) + i;
-        f32x4 v = obuf[n * 64 + lane];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) v += obuf[(w * NTO + n) * 64 + lane];
-        if (whole) {
-          const int64_t oi = b * a.ldo + (int64_t)(head0 + c) * HD + 16 * n + 4 * g;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) store_elem<F32>(a.out, oi + r, v[r] * scale);
-        } else {
-          *(f32x4 *)(a.part + (slot * rows_max + c) * HD + 16 * n + 4 * g) = v;
-        }
-      }
-      if (!whole && wave == 0 && g == 0) {
-        a.part_ml[(slot * rows_max + c) * 2] = mx;
-        a.part_ml[(slot * rows_max + c) * 2 + 1] = sum;
-      }
-    }
-    __syncthreads();  // the outputs are read before the next unit's query takes their place
-    run.lo += t1 - t0;
   }
-  if (bad) raise_status(a.status, kStatusPage);
-}
-
-// One workgroup per row of a unit: the slots of the workgroups that share it, in the
-// order of the keys, each wave a quarter of them.
-template <int HD, bool F32, bool F8>
-__global__ __launch_bounds__(64 * kAttendWaves) void kv_join_kernel(KvAttendArgs a) {
-  constexpr int TILE = kTileKeys<F8>, NW = kAttendWaves, E = HD / 64;
-  __shared__ float acc_s[NW][HD], ml[NW][2];
-  const int runs = (a.group + 15) / 16, units = a.d.n_kv_heads * runs;
-  const int rows_max = a.group < 16 ? a.group : 16;
-  const int b = blockIdx.x / units, unit = blockIdx.x - b * units, row = blockIdx.y;
-  const int kvh = unit / runs, head = kvh * a.group + (unit - kvh * runs) * 16 + row;
-  if (head >= (kvh + 1) * a.group) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  bool bad = false;
-  int64_t mine;
-  const int64_t upto = tiles_before<TILE>(a, units, lane, &mine, &bad);
-  const int64_t total = from_lane(upto, 63);
-  const int wgs = sharing_wgs(total, a.grid, kAttendMinTiles), per = (a.n_seqs + 63) / 64;
-  int64_t start = from_lane(upto - mine, b / per);
-  for (int i = b / per * per; i < b; ++i) start += (int64_t)tiles_of_length(length_of(a, i), TILE) * units;
-  const int tiles = tiles_of_length(length_of(a, b), TILE);
-  start += (int64_t)unit * tiles;
-  const int w0 = share_holding(total, wgs, start), w1 = share_holding(total, wgs, start + tiles - 1);
-  if (w0 == w1) return;  // written by its only workgroup
-  float m = -INFINITY, l = 0.f, o[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int w = w0 + wave; w <= w1; w += NW) {
-    const size_t at = (2 * (size_t)w + (w == w0)) * rows_max + row;
-    const float mw = a.part_ml[at * 2], lw = a.part_ml[at * 2 + 1];
-    const float m1 = fmaxf(m, mw), f0 = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
-    const float f1 = lw != 0.f ? __builtin_amdgcn_exp2f(mw - m1) : 0.f;
-    m = m1;
-    l = l * f0 + lw * f1;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * f0 + a.part[at * HD + e * 64 + lane] * f1;
+  if (tile < t1) {
+    load_k(tile, kp);
+    load_v(tile, vp);
   }
+
+  // the query, rotated, as bf16 terms in operand order; rows past the group are zero
+  {
+    float sn = 0.f, cs = 1.f;
+    if (turned) turn_of(turns, position, &sn, &cs);
+    auto at = [&](int e, int row) {  // operand element of column e
+      if constexpr (F8) return (((e >> 6) * 2 + ((e >> 3) & 1)) * 64 + ((e >> 4) & 3) * 16 + row) * 8 + (e & 7);
+      else return ((e >> 5) * 64 + ((e >> 3) & 3) * 16 + row) * 8 + (e & 7);
+    };
 #pragma unroll
-  for (int e = 0; e < E; ++e) acc_s[wave][e * 64 + lane] = o[e];
-  if (lane == 0) {
-    ml[wave][0] = m;
-    ml[wave][1] = l;
+    for (int i = 0; i < QN; ++i) {
+      const int row = threadIdx.x / HP + i * RS;
+      if (row >= 16) break;
+      const float x = qx[i], y = qy[i];
+      float v0 = turned ? x * cs - y * sn : x, v1 = turned ? y * cs + x * sn : y;
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t) {
+        const __bf16 h0 = (__bf16)v0, h1 = (__bf16)v1;
+        qf[t * KS * 512 + at(ea, row)] = h0;
+        qf[t * KS * 512 + at(eb, row)] = h1;
+        v0 -= (float)h0;
+        v1 -= (float)h1;
+      }
+    }
   }
   __syncthreads();
-  float mx = -INFINITY, sum = 0.f, f[NW];
+
+  f32x4 o[NTO];
 #pragma unroll
-  for (int w = 0; w < NW; ++w) mx = fmaxf(mx, ml[w][0]);
+  for (int n = 0; n < NTO; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  for (; tile < t1; tile += NW) {
+    // the query's operands are read anew for every tile: kept, they would take up to 96
+    // registers from the tiles in flight
+    asm volatile("" ::: "memory");
+    f32x4 s[NT];
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    f[w] = ml[w][1] != 0.f ? __builtin_amdgcn_exp2f(ml[w][0] - mx) : 0.f;
-    sum += ml[w][1] * f[w];
+    for (int t = 0; t < NT; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < KS; ++kb) {
+      bf16x8 qt[TERMS];
+#pragma unroll
+      for (int i = 0; i < TERMS; ++i) qt[i] = *(const bf16x8 *)(qf + ((i * KS + kb) * 64 + lane) * 8);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const bf16x8 kf = operand_of<F8>(kr[t][F8 ? kb / 2 : kb], kb & 1);
+#pragma unroll
+        for (int i = TERMS - 1; i >= 0; --i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qt[i], s[t], 0, 0, 0);
+      }
+    }
+    vp = next_vp;
+    const bool more = tile + NW < t1;
+    if (more) {
+      kp = next_kp;
+      if (tile + 2 * NW < t1) page_ids(tile + 2 * NW, next_kp, next_vp);
+      load_k(tile + NW, kp);
+    }
+    // scores in powers of two, keys from the end on masked
+    const int key0 = tile * TILE + KPL * g;
+    const bool tail = tile * TILE + TILE > w.len;
+    float mt = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float v = s[t][r] * a.scale_log2;
+        if (tail && key0 + 4 * t + r > last) v = -INFINITY;
+        s[t][r] = v;
+        mt = fmaxf(mt, v);
+      }
+    mt = max_pair32(max_pair16(mt));
+    // the running maximum is raised when it is passed by more than 2^8 (the weights
+    // stay below that); all lanes of a query agree
+    if (__ballot(mt > m + kKvRescale || m == -INFINITY)) {
+      const float m1 = fmaxf(m, mt), f = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
+      m = m1;
+      l *= f;
+#pragma unroll
+      for (int n = 0; n < NTO; ++n) o[n] *= f;
+    }
+    union {
+      bf16x8 v[TERMS][NT / 2];
+      __bf16 e[TERMS][4 * NT];
+    } pf;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float q = __builtin_amdgcn_exp2f(s[t][r] - m);
+        l += q;
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i) {
+          pf.e[i][4 * t + r] = (__bf16)q;
+          q -= (float)pf.e[i][4 * t + r];
+        }
+      }
+    if (tail) {  // what lies behind the last key may be anything, NaN included
+      constexpr int PER = F8 ? 4 : 2;  // elements of a register
+      const int keep = max(w.len - key0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int n = min(max(keep - i * PER, 0), PER);
+        const uint32_t bits = n == PER ? 0xFFFFFFFFu : (1u << (n * (32 / PER))) - 1;
+#pragma unroll
+        for (int k = 0; k < NTO; ++k) vr[k][i] &= bits;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NTO; ++n)
+#pragma unroll
+      for (int u = 0; u < NT / 2; ++u) {
+        const bf16x8 vf = operand_of<F8>(vr[n], u);
+#pragma unroll
+        for (int i = TERMS - 1; i >= 0; --i) o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf.v[i][u], o[n], 0, 0, 0);
+      }
+    if (more) load_v(tile + NW, vp);
   }
-  for (int col = threadIdx.x; col < HD; col += 64 * NW) {
-    float v = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) v += acc_s[w][col] * f[w];
-    store_elem<F32>(a.out, b * a.ldo + (int64_t)head * HD + col, sum != 0.f ? v * (a.v_scale / sum) : 0.f);
+  if (bad) raise_status(a.status, kStatusPage);
+
+  // the waves meet: maxima and sums, then outputs in units of the common maximum
+  l = sum_pair32(sum_pair16(l));
+  if (g == 0) {
+    ml[(wave * 16 + c) * 2] = m;
+    ml[(wave * 16 + c) * 2 + 1] = l;
   }
+  __syncthreads();  // also: every wave is past its last read of the query
+  float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) mx = fmaxf(mx, ml[(i * 16 + c) * 2]);
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    const float li = ml[(i * 16 + c) * 2 + 1];
+    if (li != 0.f) sum += li * __builtin_amdgcn_exp2f(ml[(i * 16 + c) * 2] - mx);
+  }
+  const float f = l != 0.f ? __builtin_amdgcn_exp2f(m - mx) : 0.f;
+#pragma unroll
+  for (int n = 0; n < NTO; ++n) obuf[(wave * NTO + n) * 64 + lane] = o[n] * f;
+  __syncthreads();
+  auto put_out = [&](int row, int col, f32x4 v, float total) {
+    const float scale = total != 0.f ? a.v_scale / total : 0.f;
+    const int64_t oi = w.b * a.ldo + (int64_t)(head0 + row) * HD + col;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) store_elem<F32>(a.out, oi + r, v[r] * scale);
+  };
+  const int slot = w.slot + w.split;
+  if (c < rows) {
+    for (int n = wave; n < NTO; n += NW) {
+      f32x4 v = obuf[n * 64 + lane];
+#pragma unroll
+      for (int i = 1; i < NW; ++i) v += obuf[(i * NTO + n) * 64 + lane];
+      if (w.splits == 1) put_out(c, 16 * n + 4 * g, v, sum);
+      else put_slot(a.part + ((size_t)slot * rows_max + c) * HD + 16 * n + 4 * g, v);
+    }
+    if (w.splits > 1 && wave == 0 && g == 0)
+      __hip_atomic_store(a.part_ml + (size_t)slot * rows_max + c, pair_of(mx, sum), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  if (w.splits == 1) return;
+
+  int first = w.slot, step = 1, n = w.splits;
+  if (w.splits > 2 * kJoinFan) {  // runs of kJoinFan splits first, into the first slot of each
+    const int run = w.split / kJoinFan;
+    first = w.slot + run * kJoinFan;
+    n = min(kJoinFan, w.splits - run * kJoinFan);
+    if (!last_to_arrive(a.arrived + first, n, word)) return;
+    join_slots<HD>(a, rows, rows_max, first, 1, n, ml, top, [&](int row, int col, f32x4 v, float) {
+      put_slot(a.part + ((size_t)first * rows_max + row) * HD + col, v);
+    });
+    if (threadIdx.x < rows)
+      __hip_atomic_store(a.part_ml + (size_t)first * rows_max + threadIdx.x, pair_of(top[2 * threadIdx.x], top[2 * threadIdx.x + 1]),
+                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    first = w.slot;
+    step = kJoinFan;
+    n = (w.splits + kJoinFan - 1) / kJoinFan;
+  }
+  if (!last_to_arrive(a.arrived + a.slots + w.slot, n, word)) return;
+  join_slots<HD>(a, rows, rows_max, first, step, n, ml, top, put_out);
 }
 
-int kv_attend_max_grid(int n_cu, int head_dim) { return n_cu * (head_dim == 256 ? kAttendPerCu<256> : kAttendPerCu<64>); }
+int kv_attend_target(int n_cu, int head_dim) {
+  return n_cu * (head_dim == 256 ? kAttendPerCu<256> : head_dim == 128 ? kAttendPerCu<128> : kAttendPerCu<64>);
+}
 
 template <int HD, bool F32, bool F8>
 static hipError_t attend_attr() {
@@ -572,17 +663,15 @@ hipError_t kv_attend_init(int head_dim) {
 }
 
 template <int HD, bool F32, bool F8>
-static hipError_t launch_attend_type(KvAttendArgs a, hipStream_t s) {
-  const int runs = (a.group + 15) / 16, units = a.d.n_kv_heads * runs;
-  // no more workgroups than the page table could give work
-  const int64_t tiles = (((int64_t)a.pages_per_seq << a.d.page_shift) + kTileKeys<F8> - 1) / kTileKeys<F8>;
-  const int64_t most = tiles < ((int64_t)1 << 40) / units / a.n_seqs ? tiles * units * a.n_seqs : (int64_t)1 << 40;
-  a.grid = sharing_wgs(most, a.grid, kAttendMinTiles);
-  const dim3 wg(64 * kAttendWaves);
-  hipLaunchKernelGGL((kv_attend_kernel<HD, F32, F8>), dim3(a.grid), wg, attend_lds_floats<HD>() * 4, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.grid == 1) return e;
-  hipLaunchKernelGGL((kv_join_kernel<HD, F32, F8>), dim3(a.n_seqs * units, a.group < 16 ? a.group : 16), wg, 0, s, a);
+static hipError_t launch_attend_type(const KvAttendArgs &a, hipStream_t s) {
+  const int64_t units = (int64_t)a.n_seqs * a.d.n_kv_heads * ((a.group + 15) / 16);
+  // the plan's workgroups: one for each unit, more where units are split, which are no
+  // more than the slots, nor than the page table gives tiles
+  const int64_t tiles = tiles_of_length((int)std::min<int64_t>((int64_t)a.pages_per_seq << a.d.page_shift, 0x7FFFFFFF), kTileKeys<F8>);
+  const int64_t splits = splits_of((int)tiles, kAttendMinTiles);
+  const int64_t grid = std::min(units * splits, units + a.slots);
+  hipLaunchKernelGGL((kv_attend_kernel<HD, F32, F8>), dim3((unsigned)grid), dim3(64 * kAttendWaves<HD>), attend_lds_floats<HD>() * 4,
+                     s, a);
   return hipGetLastError();
 }
 
@@ -593,8 +682,8 @@ static hipError_t launch_attend_hd(const KvAttendArgs &a, bool f32, bool f8, hip
 }
 
 hipError_t launch_kv_attend(const KvAttendArgs &a, bool f32, bool f8, hipStream_t s) {
-  if (a.n_seqs < 1 || a.group < 1 || a.n_heads != a.group * a.d.n_kv_heads || a.pages_per_seq < 1 || a.grid < 1 ||
-      a.d.page_shift < 4)
+  if (a.n_seqs < 1 || a.group < 1 || a.n_heads != a.group * a.d.n_kv_heads || a.pages_per_seq < 1 || a.target < 1 ||
+      a.slots < max_slots(a.target) || a.d.page_shift < 4)
     return hipErrorInvalidValue;
   if (a.d.head_dim == 64) return launch_attend_hd<64>(a, f32, f8, s);
   if (a.d.head_dim == 128) return launch_attend_hd<128>(a, f32, f8, s);

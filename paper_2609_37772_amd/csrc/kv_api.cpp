@@ -151,7 +151,8 @@ uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_str
     return cerr(UAD_E_UNSUPPORTED, "page_size must be 16, 32, 64, 128 or 256");
   if (m.rope_dim % 16) return cerr(UAD_E_UNSUPPORTED, "rope_dim must be a multiple of 16");
   if (m.n_heads % m.n_kv_heads) return cerr(UAD_E_UNSUPPORTED, "n_kv_heads must divide n_heads");
-  if (m.n_heads > 65535) return cerr(UAD_E_UNSUPPORTED, "n_heads must be at most 65535");
+  if ((int64_t)m.n_kv_heads * ((m.n_heads / m.n_kv_heads + 15) / 16) * m.max_seqs > (1 << 22))
+    return cerr(UAD_E_UNSUPPORTED, "max_seqs * n_kv_heads * ceil(n_heads / n_kv_heads / 16) must be at most 2^22");
   if (!m.k || !m.v) return cerr(UAD_E_INVALID, "null pool");
   if (!aligned(m.k, 16) || !aligned(m.v, 16)) return cerr(UAD_E_INVALID, "the pools must be 16-byte aligned");
 
@@ -173,17 +174,19 @@ uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_str
   hipError_t e = hipDeviceGetAttribute(&kv->n_cu, hipDeviceAttributeMultiprocessorCount, device);
   if (e != hipSuccess) return cerr(UAD_E_HIP, "hipDeviceGetAttribute", e);
   const size_t o_turns = 256, n_turns = m.rope_dim / 2;
-  const size_t o_ml = o_turns + 128 * sizeof(double);
-  const size_t rows = std::min(16, m.n_heads / m.n_kv_heads), slots = 2 * (size_t)kv_attend_max_grid(kv->n_cu, kv->cfg.head_dim);
-  const size_t o_part = o_ml + slots * rows * 2 * sizeof(float);
-  const size_t total = o_part + slots * rows * m.head_dim * sizeof(float);
+  const size_t rows = std::min(16, m.n_heads / m.n_kv_heads);
+  kv->slots = max_slots(kv_attend_target(kv->n_cu, m.head_dim));
+  const size_t o_arrived = o_turns + 128 * sizeof(double), o_ml = o_arrived + 2 * (size_t)kv->slots * sizeof(unsigned);
+  const size_t o_part = o_ml + kv->slots * rows * sizeof(uint64_t);
+  const size_t total = o_part + kv->slots * rows * m.head_dim * sizeof(float);
   e = hipMalloc(&kv->buf, total);
   if (e != hipSuccess) return cerr(UAD_E_OOM, "hipMalloc(workspace)", e);
   e = hipMemset(kv->buf, 0, o_ml);
   if (e == hipSuccess) e = hipEventCreateWithFlags(&kv->ev, hipEventDisableTiming);
   kv->status = (unsigned *)kv->buf;
   kv->turns = (double *)((char *)kv->buf + o_turns);
-  kv->part_ml = (float *)((char *)kv->buf + o_ml);
+  kv->arrived = (unsigned *)((char *)kv->buf + o_arrived);
+  kv->part_ml = (uint64_t *)((char *)kv->buf + o_ml);
   kv->part = (float *)((char *)kv->buf + o_part);
   if (e == hipSuccess) e = kv_attend_init(m.head_dim);
   if (n_turns) {
@@ -273,8 +276,8 @@ uad_status uad_kv_attend(uad_kv *kv, int32_t layer, const void *q, void *out, in
   a.scale_log2 = (float)((double)scale * kv->cfg.k_scale * 1.4426950408889634);
   a.v_scale = kv->cfg.v_scale;
   a.status = kv->status;
-  a.part = kv->part; a.part_ml = kv->part_ml;
-  a.grid = kv_attend_max_grid(kv->n_cu, kv->cfg.head_dim);
+  a.part = kv->part; a.part_ml = kv->part_ml; a.arrived = kv->arrived; a.slots = kv->slots;
+  a.target = kv_attend_target(kv->n_cu, kv->cfg.head_dim);
   const hipError_t e = launch_kv_attend(a, dtype == UAD_DTYPE_F32, kv->cfg.dtype == UAD_DTYPE_F8, kv->stream);
   return e == hipSuccess ? UAD_OK : kv_hip_fail(kv, e, fn, "launch");
 }

@@ -39,10 +39,14 @@ struct KvAttendArgs {
   float scale_log2;       // log2(e) * softmax scale * K scale
   float v_scale;
   unsigned *status;
-  // joins of units that several workgroups share: two slots per workgroup, of
-  // min(16, group) rows of unnormalised outputs [rows][head_dim] and (max, sum) per row
-  float *part, *part_ml;
-  int grid;               // workgroups of the launch
+  // joins of units that several workgroups share: a slot for each, of min(16, group)
+  // rows of unnormalised outputs [rows][head_dim] and a (max, sum) pair per row, and
+  // two arrival counters (zero between launches: the last to arrive clears them)
+  float *part;
+  uint64_t *part_ml;
+  unsigned *arrived;      // [2][slots]
+  int slots;
+  int target;             // workgroups that run at once
 };
 
 // The expert's prefix from the pages (stores as in PrefixArgs).
@@ -59,9 +63,9 @@ struct KvPrefixArgs {
   unsigned *status, *ctx_status;
 };
 
-// Workgroups that an attention launch may have at most (the workspace holds two
-// slots for each), and the kernels' LDS limits raised (once per handle).
-int kv_attend_max_grid(int n_cu, int head_dim);
+// Attention workgroups that run at once, and the kernels' LDS limits raised (once per
+// handle).
+int kv_attend_target(int n_cu, int head_dim);
 hipError_t kv_attend_init(int head_dim);
 hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_t s);
 hipError_t launch_kv_attend(const KvAttendArgs &a, bool f32, bool f8, hipStream_t s);
@@ -79,6 +83,9 @@ struct uad_kv {
   void *buf = nullptr;     // status word, turns, workspace
   unsigned *status = nullptr;
   double *turns = nullptr;
-  float *part = nullptr, *part_ml = nullptr;
+  float *part = nullptr;
+  uint64_t *part_ml = nullptr;
+  unsigned *arrived = nullptr;
+  int slots = 0;
   hipEvent_t ev = nullptr;  // orders the cache's stream and an expert's
 };

@@ -61,28 +61,37 @@ UAD_HD void rope_pair(int p, int rope_dim, bool neighbours, int *a, int *b) {
 }
 
 // ---------------------------------------------------------------------------
-// The attention's work: unit u of sequence b is (KV head, run of up to 16 query heads)
-// u, read in tiles of `tile` keys; a sequence without keys counts one tile, so that
-// somebody writes its zeros.  All tiles of all units stand in one row, sequences
-// outermost, and each workgroup takes an equal run of it, whatever the lengths are.
+// The attention's work.  Unit u of sequence b is a KV head with up to 16 of its query
+// heads, read in tiles of `tile` keys; a sequence without keys counts one tile, so that
+// somebody writes its zeros.  Every unit of a sequence is cut into the same number of
+// splits of at most `share` tiles, one workgroup each.  The lengths are known on the
+// device alone, and every workgroup works the plan out for itself.
 // ---------------------------------------------------------------------------
+constexpr int kMaxSplits = 512;   // of a unit
+constexpr int kJoinFan = 16;      // splits that one workgroup joins; above 2 * kJoinFan of them in two levels
+
 UAD_HD int tiles_of_length(int len, int tile) { return len > tile ? (int)(((int64_t)len + tile - 1) / tile) : 1; }
 
-// Workgroups that take part: at least min_tiles tiles each, where there are as many.
-UAD_HD int sharing_wgs(int64_t total, int grid, int min_tiles) {
-  const int64_t n = (total + min_tiles - 1) / min_tiles;
-  return n < grid ? (int)n : grid;
+// Tiles of a workgroup for `total` tiles on `target` workgroups that run at once.
+UAD_HD int first_share(int64_t total, int target, int min_tiles) {
+  const int64_t s = (total + target - 1) / target;
+  return s < min_tiles ? min_tiles : s > (1 << 30) ? 1 << 30 : (int)s;
 }
-// First tile of workgroup w (and, for w + 1, the end of w's run).
-UAD_HD int64_t share_begin(int64_t total, int wgs, int w) {
-  if (total < ((int64_t)1 << 32) / 4096 && wgs <= 4096) return (uint32_t)total * (uint32_t)w / (uint32_t)wgs;
-  return total * w / wgs;
+// With fewer units than workgroups that run at once, the splits' remainders may take
+// more than those: then the next larger share is tried, a few times (what is over
+// runs in a second round).
+constexpr int kShareTries = 6;
+UAD_HD int next_share(int share) { return share + (share >> 4) + 1; }
+
+UAD_HD int splits_of(int tiles, int share) {
+  const int s = (int)(((uint32_t)tiles + (uint32_t)share - 1) / (uint32_t)share);
+  return s < kMaxSplits ? s : kMaxSplits;
 }
-// The workgroup whose run holds tile t.
-UAD_HD int share_holding(int64_t total, int wgs, int64_t t) {
-  if (total < ((int64_t)1 << 32) / 4096 && wgs <= 4096)
-    return (int)(((uint32_t)(t + 1) * (uint32_t)wgs - 1) / (uint32_t)total);
-  return (int)(((t + 1) * wgs - 1) / total);
-}
+// First tile of split s of n (and, for s + 1, the end of s).
+UAD_HD int split_begin(int tiles, int n, int s) { return (int)((int64_t)tiles * s / n); }
+
+// Workgroups in units that are split: a unit of more than `share` tiles has fewer than
+// twice tiles / share, and total / share is at most `target`.
+UAD_HD int max_slots(int target) { return 2 * target; }
 
 }  // namespace uad

@@ -24,7 +24,7 @@ hipError_t kv_set_device(int d) { g_current = d; return hipSuccess; }
 }  // extern "C"
 
 namespace uad {
-int kv_attend_max_grid(int n_cu, int) { return n_cu; }
+int kv_attend_target(int n_cu, int) { return n_cu; }
 hipError_t kv_attend_init(int) { return hipSuccess; }
 hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_t) {
   char t[160];

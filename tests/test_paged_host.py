@@ -161,7 +161,7 @@ def kv(lib):
     (dict(dtype=2, k_scale=1e-45), INVALID), (dict(k_scale=2.0), INVALID), (dict(v_scale=0.5), INVALID),
     (dict(head_dim=96), UNSUPPORTED), (dict(head_dim=512), UNSUPPORTED), (dict(page_size=8), UNSUPPORTED),
     (dict(page_size=48), UNSUPPORTED), (dict(page_size=512), UNSUPPORTED), (dict(rope_dim=24), UNSUPPORTED),
-    (dict(n_heads=3), UNSUPPORTED), (dict(n_heads=65536), UNSUPPORTED), (dict(k=None), INVALID), (dict(v=None), INVALID),
+    (dict(n_heads=3), UNSUPPORTED), (dict(n_heads=2 ** 26), UNSUPPORTED), (dict(max_seqs=2 ** 22), UNSUPPORTED), (dict(k=None), INVALID), (dict(v=None), INVALID),
     (dict(n_pages=4), SHAPE), (dict(n_layers=3), SHAPE), (dict(n_pages=2 ** 31 - 1, n_layers=2 ** 31 - 1), SHAPE),
 ])
 def test_create_refuses(lib, change, status):
@@ -287,3 +287,71 @@ def test_prefix_from_another_models_pages_is_refused(lib, ctx, change):
     assert lib.uad_set_prefix_paged(ctx, h, X, X, 3, 2, 16) == SHAPE and lib.kv_stub_calls() == b""
     lib.uad_kv_destroy(h)
     pools.close()
+
+
+# ------------------------------------------------------------------------------------------------ the attention's plan
+PLAN = r"""
+#include "%s/paged.h"
+using namespace uad;
+extern "C" {
+int tiles_of(int len, int tile) { return tiles_of_length(len, tile); }
+int share_of(long long total, int target, int least) { return first_share(total, target, least); }
+int larger(int share) { return next_share(share); }
+int splits(int tiles, int share) { return splits_of(tiles, share); }
+int begin(int tiles, int n, int s) { return split_begin(tiles, n, s); }
+int slots(int target) { return max_slots(target); }
+int tries() { return kShareTries; }
+int fan() { return kJoinFan; }
+int most() { return kMaxSplits; }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    d = tmp_path_factory.mktemp("plan")
+    (d / "p.cpp").write_text(PLAN % CSRC)
+    subprocess.run(["g++", "-O1", "-Wall", "-Werror", "-std=c++17", "-shared", "-fPIC", str(d / "p.cpp"), "-o", str(d / "p.so")], check=True)
+    lib = ctypes.CDLL(str(d / "p.so"))
+    lib.share_of.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
+    return lib
+
+
+def plan_of(lib, lens, units, tile, target, least=4):
+    tiles = [lib.tiles_of(n, tile) for n in lens]
+    total = sum(tiles) * units
+    share = lib.share_of(total, target, least)
+    count = lambda: sum(lib.splits(t, share) * units for t in tiles)  # noqa: E731
+    if len(lens) * units < target:
+        for _ in range(lib.tries()):
+            if count() <= target:
+                break
+            share = lib.larger(share)
+    return tiles, share, [lib.splits(t, share) for t in tiles]
+
+
+def test_plan_covers_every_tile_within_the_slots_and_the_grid(plan):
+    r = np.random.default_rng(3)
+    for _ in range(400):
+        n, units, target = int(2 ** r.uniform(0, 8)), int(2 ** r.uniform(0, 5)), int(r.choice([1, 64, 256, 304, 512, 768]))
+        tile, pages, shift = int(r.choice([32, 64])), int(2 ** r.uniform(0, 14)), int(r.integers(4, 9))
+        cap = min(pages << shift, 2 ** 31 - 1)
+        lens = [int(x) for x in np.minimum(2 ** r.uniform(0, r.choice([3, 12, 22, 31]), n) - 1, cap)]
+        tiles, share, splits = plan_of(plan, lens, units, tile, target)
+        wgs, slots = sum(splits) * units, sum(s * units for s in splits if s > 1)
+        assert slots <= plan.slots(target) and max(splits) <= plan.most() and -(-max(splits) // plan.fan()) <= 2 * plan.fan()
+        # the launch: as many workgroups as the lengths could need
+        most = plan.splits(plan.tiles_of(cap, tile), 4)
+        assert wgs <= min(n * units * most, n * units + plan.slots(target))
+        for t, s in zip(tiles, splits):
+            ends = [plan.begin(t, s, i) for i in range(s + 1)]
+            assert ends[0] == 0 and ends[-1] == t and all(b > a for a, b in zip(ends, ends[1:]))
+            assert s == plan.most() or max(b - a for a, b in zip(ends, ends[1:])) <= share
+
+
+def test_plan_fills_the_workgroups_that_run_at_once(plan):
+    for n, units, length in ((1, 1, 817), (64, 1, 900), (1, 8, 131071), (8, 16, 4001), (1, 1, 1 << 20)):
+        tiles, share, splits = plan_of(plan, [length] * n, units, 32, 256)
+        wgs = sum(splits) * units
+        assert wgs <= 256 and (wgs >= 200 or share == 4)
+    assert plan_of(plan, [0], 4, 32, 256)[2] == [1]
