@@ -280,6 +280,14 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
   return true;
 }
 
+__device__ __forceinline__ float max_row16(float v) {
+  v = fmaxf(v, dpp_f<0xB1>(v));
+  v = fmaxf(v, dpp_f<0x4E>(v));
+  v = fmaxf(v, dpp_f<0x141>(v));
+  v = fmaxf(v, dpp_f<0x140>(v));
+  return v;
+}
+
 // A slot's values cross the XCDs' L2 caches: written through and read past them.
 __device__ __forceinline__ void put_slot(float *p, f32x4 v) {
   union {
@@ -303,8 +311,9 @@ __device__ __forceinline__ uint64_t pair_of(float m, float l) {
 }
 
 // LDS of the attention: the query's bf16 terms while the keys are read, then the waves'
-// outputs; behind them the waves' (or slots') maxima and sums and a word.
-constexpr int kAttendMl = 2 * kJoinFan * 16 * 2;  // floats
+// outputs; behind them the waves' maxima and sums (later the slots' weights), the joint
+// ones and a word.
+constexpr int kAttendMl = 2 * kJoinFan * 16;  // floats
 template <int HD>
 constexpr int attend_lds_floats() {
   return kAttendWaves<HD> * 16 * HD + kAttendMl + 16 * 2 + 4;
@@ -324,56 +333,57 @@ __device__ __forceinline__ bool last_to_arrive(unsigned *counter, int n, float *
   return *(int *)word != 0;
 }
 
-// Joins slots first, first + step, .. (n of them, at most 2 * kJoinFan): outputs go to
-// `put(row, column, value, 1 / sum)`; m_s, l_s [16]: the joint maximum and sum per row.
+// Joins slots first, first + step, .. (n of them, at most 2 * kJoinFan): sums go to
+// put(row, column, sum of outputs, sum of weights); top [16][2] holds the joint maximum
+// and sum of each row.  The outputs are on their way while 16 lanes a row work the
+// weights out.
 template <int HD, class Put>
 __device__ __forceinline__ void join_slots(const KvAttendArgs &a, int rows, int rows_max, int first, int step, int n,
-                                           float *ml, float *top, Put put) {
-  constexpr int VEC = HD / 4, THREADS = 64 * kAttendWaves<HD>;
+                                           float *weight, float *top, Put put) {
+  constexpr int VEC = HD / 4, THREADS = 64 * kAttendWaves<HD>, RUN = 8;
   const int items = rows * VEC;
-  // the first values are on their way while the weights are worked out
-  f32x4 v[kJoinFan];
-  int item = threadIdx.x;
-  auto fetch = [&](int it, int i0) {
-    const int row = it / VEC, col = it % VEC * 4;
+  const size_t slot_floats = (size_t)rows_max * HD;
+  f32x4 v[RUN];
+  auto fetch = [&](int item, int i0) {
+    const float *p = a.part + (size_t)first * slot_floats + (size_t)item * 4;
 #pragma unroll
-    for (int i = 0; i < kJoinFan; ++i)
-      if (i0 + i < n) v[i] = get_slot(a.part + ((size_t)(first + (i0 + i) * step) * rows_max + row) * HD + col);
+    for (int i = 0; i < RUN; ++i) v[i] = get_slot(p + (size_t)(min(i0 + i, n - 1) * step) * slot_floats);
   };
-  for (int i = threadIdx.x; i < n * 16; i += THREADS) {
-    const int row = i & 15;
-    uint64_t p = pair_of(-INFINITY, 0.f);
-    if (row < rows)
-      p = __hip_atomic_load(a.part_ml + (size_t)(first + (i >> 4) * step) * rows_max + row, __ATOMIC_RELAXED,
-                            __HIP_MEMORY_SCOPE_AGENT);
-    *(uint64_t *)(ml + 2 * i) = p;
-  }
-  if (item < items) fetch(item, 0);
-  __syncthreads();
-  if (threadIdx.x < 16) {
-    float mx = -INFINITY, sum = 0.f;
-    for (int i = 0; i < n; ++i) mx = fmaxf(mx, ml[2 * (i * 16 + threadIdx.x)]);
-    for (int i = 0; i < n; ++i) {
-      const float l = ml[2 * (i * 16 + threadIdx.x) + 1];
-      const float f = l != 0.f ? __builtin_amdgcn_exp2f(ml[2 * (i * 16 + threadIdx.x)] - mx) : 0.f;
-      sum += l * f;
-      ml[2 * (i * 16 + threadIdx.x)] = f;
-    }
-    top[2 * threadIdx.x] = mx;
-    top[2 * threadIdx.x + 1] = sum;
-  }
-  __syncthreads();
-  for (; item < items; item += THREADS) {
-    const int row = item / VEC;
-    if (item != (int)threadIdx.x) fetch(item, 0);
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = 0; i0 < n; i0 += kJoinFan) {
-      if (i0) fetch(item, i0);
+  const int row = threadIdx.x >> 4, i = threadIdx.x & 15;
+  uint64_t pair[2] = {pair_of(-INFINITY, 0.f), pair_of(-INFINITY, 0.f)};
+  if (row < rows)
 #pragma unroll
-      for (int i = 0; i < kJoinFan; ++i)
-        if (i0 + i < n) o += v[i] * ml[2 * ((i0 + i) * 16 + row)];
+    for (int k = 0; k < 2; ++k)
+      if (i + 16 * k < n)
+        pair[k] = __hip_atomic_load(a.part_ml + (size_t)(first + (i + 16 * k) * step) * rows_max + row, __ATOMIC_RELAXED,
+                                    __HIP_MEMORY_SCOPE_AGENT);
+  if ((int)threadIdx.x < items) fetch(threadIdx.x, 0);
+  if (row < 16) {
+    const float m0 = __uint_as_float((uint32_t)pair[0]), m1 = __uint_as_float((uint32_t)pair[1]);
+    const float l0 = __uint_as_float((uint32_t)(pair[0] >> 32)), l1 = __uint_as_float((uint32_t)(pair[1] >> 32));
+    const float mx = max_row16(fmaxf(m0, m1));
+    const float f0 = l0 != 0.f ? __builtin_amdgcn_exp2f(m0 - mx) : 0.f, f1 = l1 != 0.f ? __builtin_amdgcn_exp2f(m1 - mx) : 0.f;
+    const float sum = sum_row16(l0 * f0 + l1 * f1);
+    weight[i * 16 + row] = f0;
+    weight[(i + 16) * 16 + row] = f1;
+    if (i == 0) {
+      top[2 * row] = mx;
+      top[2 * row + 1] = sum;
     }
-    put(row, item % VEC * 4, o, top[2 * row + 1]);
+  }
+  __syncthreads();
+  for (int item = threadIdx.x; item < items; item += THREADS) {
+    const int r = item / VEC;
+    if (item >= THREADS) fetch(item, 0);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0;;) {
+#pragma unroll
+      for (int k = 0; k < RUN; ++k) o += v[k] * weight[(i0 + k) * 16 + r];
+      i0 += RUN;
+      if (i0 >= n) break;
+      fetch(item, i0);
+    }
+    put(r, item % VEC * 4, o, top[2 * r + 1]);
   }
 }
 
@@ -582,37 +592,50 @@ __global__ __launch_bounds__(64 * kAttendWaves<HD>, kAttendPerCu<HD> * kAttendWa
   }
   if (bad) raise_status(a.status, kStatusPage);
 
-  // the waves meet: maxima and sums, then outputs in units of the common maximum
+  // The waves meet: maxima and sums, then outputs in units of the common maximum, of
+  // half the waves where no others had a tile.
   l = sum_pair32(sum_pair16(l));
   if (g == 0) {
     ml[(wave * 16 + c) * 2] = m;
     ml[(wave * 16 + c) * 2 + 1] = l;
   }
   __syncthreads();  // also: every wave is past its last read of the query
+  const bool all = t1 - w.t0 > NW / 2;
   float mx = -INFINITY, sum = 0.f;
 #pragma unroll
   for (int i = 0; i < NW; ++i) mx = fmaxf(mx, ml[(i * 16 + c) * 2]);
 #pragma unroll
   for (int i = 0; i < NW; ++i) {
     const float li = ml[(i * 16 + c) * 2 + 1];
-    if (li != 0.f) sum += li * __builtin_amdgcn_exp2f(ml[(i * 16 + c) * 2] - mx);
+    sum += li != 0.f ? li * __builtin_amdgcn_exp2f(ml[(i * 16 + c) * 2] - mx) : 0.f;
   }
   const float f = l != 0.f ? __builtin_amdgcn_exp2f(m - mx) : 0.f;
+  if (c < rows && (all || wave < NW / 2))
 #pragma unroll
-  for (int n = 0; n < NTO; ++n) obuf[(wave * NTO + n) * 64 + lane] = o[n] * f;
+    for (int n = 0; n < NTO; ++n) obuf[(wave * NTO + n) * 64 + lane] = o[n] * f;
   __syncthreads();
+  const bool vec = a.out_vec;
   auto put_out = [&](int row, int col, f32x4 v, float total) {
     const float scale = total != 0.f ? a.v_scale / total : 0.f;
     const int64_t oi = w.b * a.ldo + (int64_t)(head0 + row) * HD + col;
+    v *= scale;
+    if (vec) {
+      if constexpr (F32) *(f32x4 *)((float *)a.out + oi) = v;
+      else *(bf16x4 *)((__bf16 *)a.out + oi) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+    } else {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) store_elem<F32>(a.out, oi + r, v[r] * scale);
+      for (int r = 0; r < 4; ++r) store_elem<F32>(a.out, oi + r, v[r]);
+    }
   };
   const int slot = w.slot + w.split;
   if (c < rows) {
     for (int n = wave; n < NTO; n += NW) {
       f32x4 v = obuf[n * 64 + lane];
 #pragma unroll
-      for (int i = 1; i < NW; ++i) v += obuf[(i * NTO + n) * 64 + lane];
+      for (int i = 1; i < NW / 2; ++i) v += obuf[(i * NTO + n) * 64 + lane];
+      if (all)
+#pragma unroll
+        for (int i = NW / 2; i < NW; ++i) v += obuf[(i * NTO + n) * 64 + lane];
       if (w.splits == 1) put_out(c, 16 * n + 4 * g, v, sum);
       else put_slot(a.part + ((size_t)slot * rows_max + c) * HD + 16 * n + 4 * g, v);
     }
@@ -621,24 +644,23 @@ __global__ __launch_bounds__(64 * kAttendWaves<HD>, kAttendPerCu<HD> * kAttendWa
   }
   if (w.splits == 1) return;
 
-  int first = w.slot, step = 1, n = w.splits;
-  if (w.splits > 2 * kJoinFan) {  // runs of kJoinFan splits first, into the first slot of each
-    const int run = w.split / kJoinFan;
-    first = w.slot + run * kJoinFan;
-    n = min(kJoinFan, w.splits - run * kJoinFan);
-    if (!last_to_arrive(a.arrived + first, n, word)) return;
-    join_slots<HD>(a, rows, rows_max, first, 1, n, ml, top, [&](int row, int col, f32x4 v, float) {
-      put_slot(a.part + ((size_t)first * rows_max + row) * HD + col, v);
+  // many splits: runs of kJoinFan first, into the first slot of each
+  bool final = w.splits <= 2 * kJoinFan;
+  for (;;) {
+    const int run = w.split / kJoinFan * kJoinFan;
+    const int first = final ? w.slot : w.slot + run, step = final && w.splits > 2 * kJoinFan ? kJoinFan : 1;
+    const int n = !final ? min(kJoinFan, w.splits - run) : (w.splits + step - 1) / step;
+    if (!last_to_arrive(a.arrived + (final ? a.slots : 0) + first, n, word)) return;
+    join_slots<HD>(a, rows, rows_max, first, step, n, ml, top, [&](int row, int col, f32x4 v, float total) {
+      if (final) put_out(row, col, v, total);
+      else put_slot(a.part + ((size_t)first * rows_max + row) * HD + col, v);
     });
-    if (threadIdx.x < rows)
-      __hip_atomic_store(a.part_ml + (size_t)first * rows_max + threadIdx.x, pair_of(top[2 * threadIdx.x], top[2 * threadIdx.x + 1]),
-                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    first = w.slot;
-    step = kJoinFan;
-    n = (w.splits + kJoinFan - 1) / kJoinFan;
+    if (final) return;
+    if ((int)threadIdx.x < rows)
+      __hip_atomic_store(a.part_ml + (size_t)first * rows_max + threadIdx.x,
+                         pair_of(top[2 * threadIdx.x], top[2 * threadIdx.x + 1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    final = true;
   }
-  if (!last_to_arrive(a.arrived + a.slots + w.slot, n, word)) return;
-  join_slots<HD>(a, rows, rows_max, first, step, n, ml, top, put_out);
 }
 
 int kv_attend_target(int n_cu, int head_dim) {

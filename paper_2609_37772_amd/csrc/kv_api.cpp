@@ -278,6 +278,8 @@ uad_status uad_kv_attend(uad_kv *kv, int32_t layer, const void *q, void *out, in
   a.status = kv->status;
   a.part = kv->part; a.part_ml = kv->part_ml; a.arrived = kv->arrived; a.slots = kv->slots;
   a.target = kv_attend_target(kv->n_cu, kv->cfg.head_dim);
+  const size_t four = dtype == UAD_DTYPE_F32 ? 16 : 8;
+  a.out_vec = aligned(out, four) && ldo % 4 == 0;
   const hipError_t e = launch_kv_attend(a, dtype == UAD_DTYPE_F32, kv->cfg.dtype == UAD_DTYPE_F8, kv->stream);
   return e == hipSuccess ? UAD_OK : kv_hip_fail(kv, e, fn, "launch");
 }

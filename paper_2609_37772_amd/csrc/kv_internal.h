@@ -47,6 +47,7 @@ struct KvAttendArgs {
   unsigned *arrived;      // [2][slots]
   int slots;
   int target;             // workgroups that run at once
+  bool out_vec;           // four outputs can be stored at once
 };
 
 // The expert's prefix from the pages (stores as in PrefixArgs).

@@ -74,7 +74,7 @@ UAD_HD int tiles_of_length(int len, int tile) { return len > tile ? (int)(((int6
 
 // Tiles of a workgroup for `total` tiles on `target` workgroups that run at once.
 UAD_HD int first_share(int64_t total, int target, int min_tiles) {
-  const int64_t s = (total + target - 1) / target;
+  const int64_t s = total < (1 << 30) ? ((uint32_t)total + (uint32_t)target - 1) / (uint32_t)target : (total + target - 1) / target;
   return s < min_tiles ? min_tiles : s > (1 << 30) ? 1 << 30 : (int)s;
 }
 // With fewer units than workgroups that run at once, the splits' remainders may take
