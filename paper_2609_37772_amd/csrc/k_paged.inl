@@ -18,6 +18,16 @@ __device__ __forceinline__ float load_elem(const void *p, int64_t i) {
   if constexpr (F32) return ((const float *)p)[i];
   else return __uint_as_float((uint32_t)((const uint16_t *)p)[i] << 16);
 }
+// The same in two steps, so that a load can be in flight before it is looked at.
+template <bool F32>
+__device__ __forceinline__ uint32_t load_raw(const void *p, int64_t i) {
+  if constexpr (F32) return ((const uint32_t *)p)[i];
+  else return ((const uint16_t *)p)[i];
+}
+template <bool F32>
+__device__ __forceinline__ float value_of(uint32_t raw) {
+  return __uint_as_float(F32 ? raw : raw << 16);
+}
 template <bool F32>
 __device__ __forceinline__ void store_elem(void *p, int64_t i, float v) {
   if constexpr (F32) ((float *)p)[i] = v;
@@ -146,18 +156,19 @@ hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_
 // K and V go from memory to the matrix instructions' registers, with no LDS between.
 // Loads of the next K tile are issued when this one's scores are done, of the next V
 // tile when this one's products are.  The waves of a workgroup take every
-// kAttendWaves<HD>-th tile with running maxima and sums of their own and meet in LDS.  A
+// kAttendWaves-th tile with running maxima and sums of their own and meet in LDS.  A
 // unit's splits meet in slots of the workspace: the last workgroup to arrive joins
 // them, in the order of the keys.
 // ---------------------------------------------------------------------------
 constexpr int kAttendMinTiles = 4;  // tiles of a split, where a unit has as many
 
-// Waves of a workgroup, and workgroups per CU: the tiles in flight, the outputs and
-// their operands take a wave up to 256 registers at head dim 256, 170 at 128, 128 at 64.
+constexpr int kAttendWaves = 8;
+// Workgroups per CU: the tiles in flight, the outputs and their operands take a wave up
+// to 256 registers at head dim 256 (two waves per SIMD) and 160 at 128; for 128, three
+// workgroups of four waves, which fit too, spilled or read slower (131071 keys, 32/8
+// heads: 108.9 us, two of them 104.1, one of eight waves 100.8).
 template <int HD>
-constexpr int kAttendWaves = HD == 128 ? 4 : 8;
-template <int HD>
-constexpr int kAttendPerCu = HD == 256 ? 1 : HD == 128 ? 3 : 2;
+constexpr int kAttendPerCu = HD == 64 ? 2 : 1;
 
 template <bool F8>
 constexpr int kTileKeys = F8 ? 64 : 32;  // keys of 16-byte V^T loads by the four lane groups
@@ -316,7 +327,7 @@ __device__ __forceinline__ uint64_t pair_of(float m, float l) {
 constexpr int kAttendMl = 2 * kJoinFan * 16;  // floats
 template <int HD>
 constexpr int attend_lds_floats() {
-  return kAttendWaves<HD> * 16 * HD + kAttendMl + 16 * 2 + 4;
+  return kAttendWaves * 16 * HD + kAttendMl + 16 * 2 + 4;
 }
 
 // The last of `n` workgroups to get here carries on; all of this workgroup's slot
@@ -340,7 +351,7 @@ __device__ __forceinline__ bool last_to_arrive(unsigned *counter, int n, float *
 template <int HD, class Put>
 __device__ __forceinline__ void join_slots(const KvAttendArgs &a, int rows, int rows_max, int first, int step, int n,
                                            float *weight, float *top, Put put) {
-  constexpr int VEC = HD / 4, THREADS = 64 * kAttendWaves<HD>, RUN = 8;
+  constexpr int VEC = HD / 4, THREADS = 64 * kAttendWaves, RUN = 8;
   const int items = rows * VEC;
   const size_t slot_floats = (size_t)rows_max * HD;
   f32x4 v[RUN];
@@ -388,13 +399,13 @@ __device__ __forceinline__ void join_slots(const KvAttendArgs &a, int rows, int 
 }
 
 template <int HD, bool F32, bool F8>
-__global__ __launch_bounds__(64 * kAttendWaves<HD>, kAttendPerCu<HD> * kAttendWaves<HD> / 4) void kv_attend_kernel(KvAttendArgs a) {
+__global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves / 4) void kv_attend_kernel(KvAttendArgs a) {
   constexpr int TILE = kTileKeys<F8>, NT = TILE / 16, KPL = 4 * NT;
   constexpr int KS = HD / 32;           // k steps of Q K^T
   constexpr int KL = F8 ? HD / 64 : KS; // 16-byte loads of a key row per lane
   constexpr int NTO = HD / 16;          // 16-column tiles of the output
   constexpr int TERMS = F32 ? 3 : 2;
-  constexpr int NW = kAttendWaves<HD>;
+  constexpr int NW = kAttendWaves;
   constexpr int ESZ = F8 ? 1 : 2;
   extern __shared__ __align__(16) float lds[];
   __bf16 *qf = (__bf16 *)lds;                      // [TERMS][KS][64][8]
@@ -413,7 +424,7 @@ __global__ __launch_bounds__(64 * kAttendWaves<HD>, kAttendPerCu<HD> * kAttendWa
   int ea, eb;
   rope_pair(p, a.rope_dim, a.rope_pairs != 0, &ea, &eb);
   const bool turned = p < a.rope_dim / 2;
-  const double turns = turned ? a.turns[p] : 0.0;
+  const double turns = a.turns[p];  // 128 of them are allocated
 
   AttendWork w;
   if (!plan_attend<TILE>(a, units, blockIdx.x, &w)) return;
@@ -458,16 +469,13 @@ __global__ __launch_bounds__(64 * kAttendWaves<HD>, kAttendPerCu<HD> * kAttendWa
   if (tile + NW < t1) page_ids(tile + NW, next_kp, next_vp);
   int position = last;
   if (a.positions) position = a.positions[w.b];
-  float qx[QN], qy[QN];
+  uint32_t qx[QN], qy[QN];
 #pragma unroll
   for (int i = 0; i < QN; ++i) {
-    const int row = threadIdx.x / HP + i * RS;
-    qx[i] = qy[i] = 0.f;
-    if (row < rows) {
-      const int64_t qi = w.b * a.ldq + (int64_t)(head0 + row) * HD;
-      qx[i] = load_elem<F32>(a.q, qi + ea);
-      qy[i] = load_elem<F32>(a.q, qi + eb);
-    }
+    const int row = min((int)threadIdx.x / HP + i * RS, rows - 1);
+    const int64_t qi = w.b * a.ldq + (int64_t)(head0 + row) * HD;
+    qx[i] = load_raw<F32>(a.q, qi + ea);
+    qy[i] = load_raw<F32>(a.q, qi + eb);
   }
   if (tile < t1) {
     load_k(tile, kp);
@@ -486,7 +494,7 @@ __global__ __launch_bounds__(64 * kAttendWaves<HD>, kAttendPerCu<HD> * kAttendWa
     for (int i = 0; i < QN; ++i) {
       const int row = threadIdx.x / HP + i * RS;
       if (row >= 16) break;
-      const float x = qx[i], y = qy[i];
+      const float x = row < rows ? value_of<F32>(qx[i]) : 0.f, y = row < rows ? value_of<F32>(qy[i]) : 0.f;
       float v0 = turned ? x * cs - y * sn : x, v1 = turned ? y * cs + x * sn : y;
 #pragma unroll
       for (int t = 0; t < TERMS; ++t) {
@@ -692,7 +700,7 @@ static hipError_t launch_attend_type(const KvAttendArgs &a, hipStream_t s) {
   const int64_t tiles = tiles_of_length((int)std::min<int64_t>((int64_t)a.pages_per_seq << a.d.page_shift, 0x7FFFFFFF), kTileKeys<F8>);
   const int64_t splits = splits_of((int)tiles, kAttendMinTiles);
   const int64_t grid = std::min(units * splits, units + a.slots);
-  hipLaunchKernelGGL((kv_attend_kernel<HD, F32, F8>), dim3((unsigned)grid), dim3(64 * kAttendWaves<HD>), attend_lds_floats<HD>() * 4,
+  hipLaunchKernelGGL((kv_attend_kernel<HD, F32, F8>), dim3((unsigned)grid), dim3(64 * kAttendWaves), attend_lds_floats<HD>() * 4,
                      s, a);
   return hipGetLastError();
 }
