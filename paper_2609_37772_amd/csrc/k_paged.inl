@@ -9,6 +9,7 @@ namespace uad {
 constexpr float kKvRescale = 8.0f;
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 
 // ---------------------------------------------------------------------------
 // Element types
@@ -57,6 +58,22 @@ __device__ __forceinline__ void turn_of(double turns, int position, float *s, fl
   const double t = turns * (double)position;
   sincospif(2.0f * (float)(t - rint(t)), s, c);
 }
+
+// Inclusive sum over the lanes of a wave, by DPP: within rows of 16, then across them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_i(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, true);
+}
+__device__ __forceinline__ int scan_wave64(int v) {
+  v += dpp_i<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
+  v += dpp_i<0x112, 0xF>(v);
+  v += dpp_i<0x114, 0xF>(v);
+  v += dpp_i<0x118, 0xF>(v);
+  v += dpp_i<0x142, 0xA>(v);  // the last lane of rows 0 and 2 to rows 1 and 3
+  v += dpp_i<0x143, 0xC>(v);  // lane 31 to rows 2 and 3
+  return v;
+}
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
 // The sequence of a new row: how many of row_start[0 .. n_seqs] are at most r, minus
 // one.  Called by whole waves; r is the same in all lanes.
@@ -122,21 +139,289 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
   }
 }
 
-hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_t s) {
-  if (a.n_rows < 1 || a.n_seqs < 1 || a.d.head_dim > 512 || a.d.head_dim < 2) return hipErrorInvalidValue;
-  constexpr int kMaxRows = 1 << 23;  // work items of a grid stay below 2^32
-  for (int64_t r = 0; r < a.n_rows; r += kMaxRows) {
+// ---------------------------------------------------------------------------
+// Append of many rows: one workgroup per tile (see paged.h), KV head and pool, so that
+// pages are written 16 bytes at a time: bound by memory, a row by itself would scatter
+// its values over a transposed page two bytes at a time.  K: a thread rotates 16
+// elements of a row, the pieces of 8 that are turned with each other.  V: through LDS,
+// whose 16-byte pieces are swizzled by the token's chunk, so that the lanes that read 8
+// (or 16) tokens of a column do not meet in a bank.
+// ---------------------------------------------------------------------------
+struct AppendTile {
+  int b, first, last;  // tile's cache positions that get a row: first .. last
+  int row;             // row of the first
+};
+
+__device__ __forceinline__ bool plan_append(const KvAppendArgs &a, int wg, AppendTile *t) {
+  const int lane = threadIdx.x & 63, per = (a.n_seqs + 63) / 64, shift = append_tile_shift(a.d.page_shift);
+  bool bad = false;
+  // positions [from, to) and rows of a sequence; none where they cannot be used
+  auto span = [&](int b, int *from, int *to, int *row) {
+    const int lo = a.row_start ? a.row_start[b] : b, hi = a.row_start ? a.row_start[b + 1] : b + 1;
+    const int len = usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad);
+    const bool ok = rows_ok(lo, hi, a.n_rows) && hi - lo <= len && (b > 0 || lo == 0);
+    bad |= !ok;
+    *row = lo;
+    *to = ok ? len : 0;
+    *from = ok ? len - (hi - lo) : 0;
+  };
+  int mine = 0, from = 0, to = 0, row = 0;
+  for (int i = 0; i < per; ++i)
+    if (lane * per + i < a.n_seqs) {
+      span(lane * per + i, &from, &to, &row);
+      mine += append_tiles(from, to, shift);
+    }
+  if (bad && wg == 0) raise_status(a.status, kStatusPage);
+  const int upto = scan_wave64(mine);
+  if (wg >= last_lane(upto)) return false;
+  const int at = __builtin_ctzll(__ballot(upto > wg));
+  int start = __builtin_amdgcn_readlane(upto - mine, at), b = at * per;
+  from = __builtin_amdgcn_readlane(from, at);
+  to = __builtin_amdgcn_readlane(to, at);
+  row = __builtin_amdgcn_readlane(row, at);
+  if (per > 1)
+    for (;; ++b) {
+      if (b >= a.n_seqs) return false;  // only if the caller's arrays change while this runs
+      span(b, &from, &to, &row);
+      const int n = append_tiles(from, to, shift);
+      if (start + n > wg) break;
+      start += n;
+    }
+  const int tile = (from >> shift) + wg - start;
+  t->b = b;
+  t->first = max(from, tile << shift);
+  t->last = min(to, (tile + 1) << shift) - 1;
+  t->row = row + t->first - from;
+  return t->first <= t->last;
+}
+
+// 8 consecutive elements of a row as they are loaded; values of them.
+template <bool F32>
+struct Raw8 {
+  u32x4_t r[F32 ? 2 : 1];
+  __device__ __forceinline__ void load(const void *p, int64_t i, bool vec) {
+    if (vec) {
+#pragma unroll
+      for (int k = 0; k < (F32 ? 2 : 1); ++k) r[k] = ((const u32x4_t *)((const char *)p + i * (F32 ? 4 : 2)))[k];
+    } else if constexpr (F32) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e / 4][e % 4] = ((const uint32_t *)p)[i + e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        r[0][e] = ((const uint16_t *)p)[i + 2 * e] | (uint32_t)((const uint16_t *)p)[i + 2 * e + 1] << 16;
+    }
+  }
+  __device__ __forceinline__ float value(int e) const {
+    if constexpr (F32) return __uint_as_float(r[e / 4][e % 4]);
+    else return __uint_as_float(e & 1 ? r[0][e / 2] & 0xFFFF0000u : r[0][e / 2] << 16);
+  }
+};
+
+// 8 pool elements: 16 bytes of bf16, 8 of e4m3.
+template <bool F8>
+struct Pool8 {
+  uint32_t w[F8 ? 2 : 4];
+  __device__ __forceinline__ void set(const float *v) {
+#pragma unroll
+    for (int i = 0; i < (F8 ? 2 : 4); ++i) {
+      if constexpr (F8) {
+        int x = __builtin_amdgcn_cvt_pk_fp8_f32(cut_f8(v[4 * i]), cut_f8(v[4 * i + 1]), 0, false);
+        w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(cut_f8(v[4 * i + 2]), cut_f8(v[4 * i + 3]), x, true);
+      } else {
+        union {
+          bf16x2 h;
+          uint32_t u;
+        } x{bf16x2{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]}};
+        w[i] = x.u;
+      }
+    }
+  }
+  __device__ __forceinline__ void put(void *p) const {
+    if constexpr (F8) *(uint64_t *)p = (uint64_t)w[0] | (uint64_t)w[1] << 32;
+    else *(u32x4_t *)p = u32x4_t{w[0], w[1], w[2], w[3]};
+  }
+};
+
+template <int HD, bool F32, bool F8>
+__global__ __launch_bounds__(256) void kv_append_tile_kernel(KvAppendArgs a) {
+  constexpr int ESZ = F8 ? 1 : 2;
+  constexpr int PIECES = HD / 8;                      // of 8 elements in a row
+  constexpr int ROUNDS = kAppendTile * PIECES / 2 / 256;  // of 256 threads with two pieces each, at most
+  constexpr int N = ROUNDS > 1 ? ROUNDS : 1;
+  __shared__ __align__(16) uint8_t lds[kAppendTile * HD * ESZ];
+  AppendTile t;
+  if (!plan_append(a, blockIdx.x, &t)) return;
+  const int head = blockIdx.y, mask = (1 << a.d.page_shift) - 1;
+  const int page = a.table[(int64_t)t.b * a.pages_per_seq + (t.first >> a.d.page_shift)];
+  if (!page_ok(a.d, page)) {
+    if (threadIdx.x == 0) raise_status(a.status, kStatusPage);
+    return;
+  }
+  const size_t base = page_base(a.d, page, head);
+  const int tokens = t.last - t.first + 1, items = tokens * (PIECES / 2);
+  const int tile_off = (t.first & mask) & ~(kAppendTile - 1);  // offset in the page of the tile's first slot
+  const bool is_v = blockIdx.z != 0;
+  const void *src = is_v ? a.v : a.k;
+  const int64_t ld = is_v ? a.ldv : a.ldk;
+  // an item: pieces x and y of a token; for K the ones that are turned with each other
+  // (piece p with p + rope_dim / 16, or neighbours, as which all pieces count for V, for
+  // rotated neighbours and behind rope_dim)
+  const int half = a.rope_dim / 16;
+  auto pieces = [&](int i, int *x, int *y) {
+    if (!is_v && !a.rope_pairs && i < half) {
+      *x = i;
+      *y = i + half;
+    } else {
+      *x = 2 * i;
+      *y = 2 * i + 1;
+    }
+  };
+  Raw8<F32> rx[N], ry[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int item = min((int)threadIdx.x + n * 256, items - 1), token = item / (PIECES / 2);
+    int x, y;
+    pieces(item % (PIECES / 2), &x, &y);
+    const int64_t at = (t.row + token) * ld + (int64_t)head * HD;
+    rx[n].load(src, at + 8 * x, a.in_vec);
+    ry[n].load(src, at + 8 * y, a.in_vec);
+  }
+  if (!is_v) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int item = threadIdx.x + n * 256, token = item / (PIECES / 2), i = item % (PIECES / 2);
+      if (item >= items) break;
+      float u[8], w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        u[e] = rx[n].value(e);
+        w[e] = ry[n].value(e);
+      }
+      int x, y;
+      pieces(i, &x, &y);
+      if (i < half) {
+        const int position = a.positions ? a.positions[t.row + token] : t.first + token;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float s, c;
+          turn_of(a.turns[8 * i + e], position, &s, &c);
+          if (a.rope_pairs) {  // elements 16 i + 2 e and the next
+            float &p = e < 4 ? u[2 * e] : w[2 * e - 8], &q = e < 4 ? u[2 * e + 1] : w[2 * e - 7];
+            const float p0 = p, q0 = q;
+            p = p0 * c - q0 * s;
+            q = q0 * c + p0 * s;
+          } else {
+            const float p0 = u[e], q0 = w[e];
+            u[e] = p0 * c - q0 * s;
+            w[e] = q0 * c + p0 * s;
+          }
+        }
+      }
+      if constexpr (F8)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          u[e] *= a.k_inv;
+          w[e] *= a.k_inv;
+        }
+      char *dst = (char *)a.kp + (base + k_in_page(a.d, (t.first & mask) + token, 0)) * ESZ;
+      Pool8<F8> o;
+      o.set(u);
+      o.put(dst + 8 * x * ESZ);
+      o.set(w);
+      o.put(dst + 8 * y * ESZ);
+    }
+    return;
+  }
+  // V: tokens x HD in pool type, a token's 8-element piece p at place p ^ (token / RUN)
+  constexpr int RUN = F8 ? 16 : 8;  // tokens of a 16-byte store
+  const int lead = (t.first & mask) - tile_off;  // slots of the tile before the first row
+  auto place = [&](int slot, int piece) { return (slot * PIECES + (piece ^ ((slot / RUN) & (PIECES - 1)))) * 8 * ESZ; };
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int item = threadIdx.x + n * 256, token = item / (PIECES / 2), i = item % (PIECES / 2);
+    if (item >= items) break;
+    float u[8], w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      u[e] = rx[n].value(e) * (F8 ? a.v_inv : 1.f);
+      w[e] = ry[n].value(e) * (F8 ? a.v_inv : 1.f);
+    }
+    Pool8<F8> o;
+    o.set(u);
+    o.put(lds + place(lead + token, 2 * i));
+    o.set(w);
+    o.put(lds + place(lead + token, 2 * i + 1));
+  }
+  __syncthreads();
+  // columns in words (2 of bf16, 4 of e4m3), runs of RUN slots
+  constexpr int COLS = 4 / ESZ, WORDS = HD / COLS;
+  const int run0 = lead / RUN, runs = (lead + tokens - 1) / RUN - run0 + 1;
+  char *vp = (char *)a.vp + (base + tile_off) * ESZ;
+  for (int item = threadIdx.x; item < WORDS * runs; item += 256) {
+    const int run = run0 + item % runs, word = item / runs, slot0 = run * RUN;
+    uint32_t v[RUN];
+#pragma unroll
+    for (int e = 0; e < RUN; ++e)
+      v[e] = *(const uint32_t *)(lds + place(slot0 + e, word * COLS / 8) + (word * COLS % 8) * ESZ);
+    const bool whole = slot0 >= lead && slot0 + RUN <= lead + tokens;
+#pragma unroll
+    for (int col = 0; col < COLS; ++col) {
+      char *dst = vp + (((size_t)(word * COLS + col) << a.d.page_shift) + slot0) * ESZ;
+      if (whole) {
+        u32x4_t o;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if constexpr (F8)
+            o[k] = (v[4 * k] >> (8 * col) & 0xFF) | (v[4 * k + 1] >> (8 * col) & 0xFF) << 8 |
+                   (v[4 * k + 2] >> (8 * col) & 0xFF) << 16 | (v[4 * k + 3] >> (8 * col)) << 24;
+          else
+            o[k] = (v[2 * k] >> (16 * col) & 0xFFFF) | (v[2 * k + 1] >> (16 * col)) << 16;
+        }
+        *(u32x4_t *)dst = o;
+      } else {
+#pragma unroll
+        for (int e = 0; e < RUN; ++e)
+          if (slot0 + e >= lead && slot0 + e < lead + tokens) {
+            if constexpr (F8) ((uint8_t *)dst)[e] = (uint8_t)(v[e] >> (8 * col));
+            else ((uint16_t *)dst)[e] = (uint16_t)(v[e] >> (16 * col));
+          }
+      }
+    }
+  }
+}
+
+// Mean rows per sequence from which an append goes by tiles.
+constexpr int kAppendTileRows = 4;
+
+template <bool F32, bool F8>
+static hipError_t launch_append_type(const KvAppendArgs &a, hipStream_t s) {
+  constexpr int kMaxWgs = 1 << 23;  // work items of a grid stay below 2^32
+  const int64_t tiles = append_grid(a.n_rows, a.n_seqs, append_tile_shift(a.d.page_shift));
+  if ((int64_t)a.n_seqs * kAppendTileRows <= a.n_rows && tiles <= kMaxWgs && a.d.n_kv_heads <= 65535) {
+    const dim3 grid((unsigned)tiles, a.d.n_kv_heads, 2), wg(256);
+    if (a.d.head_dim == 64) hipLaunchKernelGGL((kv_append_tile_kernel<64, F32, F8>), grid, wg, 0, s, a);
+    else if (a.d.head_dim == 128) hipLaunchKernelGGL((kv_append_tile_kernel<128, F32, F8>), grid, wg, 0, s, a);
+    else hipLaunchKernelGGL((kv_append_tile_kernel<256, F32, F8>), grid, wg, 0, s, a);
+    return hipGetLastError();
+  }
+  for (int64_t r = 0; r < a.n_rows; r += kMaxWgs) {
     KvAppendArgs p = a;
     p.row0 = (int)r;
-    const dim3 grid((unsigned)(a.n_rows - r < kMaxRows ? a.n_rows - r : kMaxRows)), wg(256);
-    if (f32 && f8) hipLaunchKernelGGL((kv_append_kernel<true, true>), grid, wg, 0, s, p);
-    else if (f32) hipLaunchKernelGGL((kv_append_kernel<true, false>), grid, wg, 0, s, p);
-    else if (f8) hipLaunchKernelGGL((kv_append_kernel<false, true>), grid, wg, 0, s, p);
-    else hipLaunchKernelGGL((kv_append_kernel<false, false>), grid, wg, 0, s, p);
+    const dim3 grid((unsigned)(a.n_rows - r < kMaxWgs ? a.n_rows - r : kMaxWgs)), wg(256);
+    hipLaunchKernelGGL((kv_append_kernel<F32, F8>), grid, wg, 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_t s) {
+  if (a.n_rows < 1 || a.n_seqs < 1 || (a.d.head_dim != 64 && a.d.head_dim != 128 && a.d.head_dim != 256) ||
+      a.d.page_shift < 4 || a.rope_dim % 16 || a.rope_dim > a.d.head_dim)
+    return hipErrorInvalidValue;
+  if (f32) return f8 ? launch_append_type<true, true>(a, s) : launch_append_type<true, false>(a, s);
+  return f8 ? launch_append_type<false, true>(a, s) : launch_append_type<false, false>(a, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -173,8 +458,6 @@ constexpr int kAttendPerCu = HD == 64 ? 2 : 1;
 template <bool F8>
 constexpr int kTileKeys = F8 ? 64 : 32;  // keys of 16-byte V^T loads by the four lane groups
 
-typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
-
 template <bool F8>
 __device__ __forceinline__ bf16x8 operand_of(u32x4_t r, int u) {  // 8 bf16 of a 16-byte load (u: which half, 8-bit)
   union {
@@ -194,22 +477,6 @@ __device__ __forceinline__ bf16x8 operand_of(u32x4_t r, int u) {  // 8 bf16 of a
   }
   return o.v;
 }
-
-// Inclusive sum over the lanes of a wave, by DPP: within rows of 16, then across them.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_i(int v) {
-  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, true);
-}
-__device__ __forceinline__ int scan_wave64(int v) {
-  v += dpp_i<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
-  v += dpp_i<0x112, 0xF>(v);
-  v += dpp_i<0x114, 0xF>(v);
-  v += dpp_i<0x118, 0xF>(v);
-  v += dpp_i<0x142, 0xA>(v);  // the last lane of rows 0 and 2 to rows 1 and 3
-  v += dpp_i<0x143, 0xC>(v);  // lane 31 to rows 2 and 3
-  return v;
-}
-__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
 // What a workgroup does: tiles t0 .. t1-1 of a unit of sequence b; split `split` of
 // `splits`, whose slots start at `slot`.

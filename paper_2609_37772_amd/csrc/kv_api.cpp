@@ -246,6 +246,8 @@ uad_status uad_kv_append(uad_kv *kv, int32_t layer, const void *k, const void *v
   a.row_start = row_start; a.lens = lens; a.positions = positions; a.table = page_table;
   a.n_rows = n_rows; a.n_seqs = n_seqs; a.pages_per_seq = pages_per_seq;
   a.turns = kv->turns; a.rope_dim = kv->cfg.rope_dim; a.rope_pairs = kv->cfg.rope_pairs;
+  const int64_t per16 = dtype == UAD_DTYPE_F32 ? 4 : 8;
+  a.in_vec = aligned(k, 16) && aligned(v, 16) && ldk % per16 == 0 && ldv % per16 == 0;
   a.k_inv = 1.f / kv->cfg.k_scale; a.v_inv = 1.f / kv->cfg.v_scale;
   a.status = kv->status;
   const hipError_t e = launch_kv_append(a, dtype == UAD_DTYPE_F32, kv->cfg.dtype == UAD_DTYPE_F8, kv->stream);

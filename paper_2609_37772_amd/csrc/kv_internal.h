@@ -20,6 +20,7 @@ struct KvAppendArgs {
   const int32_t *table;      // [n_seqs][pages_per_seq]
   int n_rows, n_seqs, pages_per_seq;
   int row0;               // first row of this launch
+  bool in_vec;            // rows can be loaded 16 bytes at a time
   const double *turns;    // [rope_dim / 2] turns per position
   int rope_dim, rope_pairs;
   float k_inv, v_inv;     // 1 / scale (8-bit pools)

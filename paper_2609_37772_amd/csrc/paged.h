@@ -61,6 +61,24 @@ UAD_HD void rope_pair(int p, int rope_dim, bool neighbours, int *a, int *b) {
 }
 
 // ---------------------------------------------------------------------------
+// Appends of many rows go by tiles: runs of up to kAppendTile cache positions that start
+// at a multiple of their size and lie in one page.
+// ---------------------------------------------------------------------------
+constexpr int kAppendTile = 64;
+
+UAD_HD int append_tile_shift(int page_shift) { return page_shift < 6 ? page_shift : 6; }
+// Tiles that positions [from, to) touch.
+UAD_HD int append_tiles(int from, int to, int shift) { return to > from ? ((to - 1) >> shift) - (from >> shift) + 1 : 0; }
+// At most as many workgroups: every tile holds a row, and a sequence's first and last
+// tile may be shorter than the others.
+UAD_HD int64_t append_grid(int n_rows, int n_seqs, int shift) {
+  const int64_t most = ((int64_t)n_rows >> shift) + 2 * (int64_t)n_seqs;
+  return most < n_rows ? most : n_rows;
+}
+// New rows of a sequence at row_start[b] .. row_start[b + 1]: usable, or an error.
+UAD_HD bool rows_ok(int from, int to, int n_rows) { return from >= 0 && from <= to && to <= n_rows; }
+
+// ---------------------------------------------------------------------------
 // The attention's work.  Unit u of sequence b is a KV head with up to 16 of its query
 // heads, read in tiles of `tile` keys; a sequence without keys counts one tile, so that
 // somebody writes its zeros.  Every unit of a sequence is cut into the same number of

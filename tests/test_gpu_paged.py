@@ -86,6 +86,11 @@ APPENDS = [
     (8, 256, 64, [70, 3], [60, 64], BF16, F8, 256, False),
     (1, 64, 16, [2] * 130, [i % 37 for i in range(130)], F32, BF16, 64, False),
     (16, 64, 16, [40], [7], F32, BF16, 64, True),
+    (2, 64, 16, [i % 11 for i in range(130)], [i * 13 % 37 for i in range(130)], BF16, F8, 64, False),
+    (1, 128, 64, [i % 23 for i in range(65)], [i * 13 % 70 for i in range(65)], F32, BF16, 128, True),
+    (1, 256, 128, [1, 200, 64, 65], [127, 128, 64, 63], BF16, F8, 0, False),
+    (1, 64, 32, [4, 4], [30, 31], BF16, BF16, 64, False),
+    (1, 64, 32, [3, 4], [30, 31], BF16, BF16, 64, False),
 ]
 
 
@@ -170,7 +175,7 @@ BAD_APPENDS = {  # lens, starts, a change of the page table (or none), of 3 sequ
     "length below the new rows": ([2, 1, 19], [0, 2, 3, 23], None),
     "page below zero": ([2, 1, 20], [0, 2, 3, 23], (2, 1, -1)),
     "page beyond the pool": ([2, 1, 20], [0, 2, 3, 23], (0, 0, 1 << 30)),
-    "starts fall": ([2, 1, 20], [0, 3, 2, 23], None),
+    "starts fall": ([3, 2, 21], [0, 3, 2, 23], None),
     "starts beyond the rows": ([2, 1, 21], [0, 2, 3, 24], None),
     "starts below zero": ([2, 1, 20], [-2, 2, 3, 23], None),
     "no row belongs to the first": ([2, 1, 20], [1, 2, 3, 23], None),
@@ -178,14 +183,19 @@ BAD_APPENDS = {  # lens, starts, a change of the page table (or none), of 3 sequ
 
 
 @pytest.mark.parametrize("what", BAD_APPENDS)
-def test_append_reports_what_it_cannot_use(gpu, what):
+@pytest.mark.parametrize("rows", [20, 2])  # by tiles and row by row
+def test_append_reports_what_it_cannot_use(gpu, what, rows):
     lens, starts, page = BAD_APPENDS[what]
-    c = P.Cache(3, 1, 2, 64, 16, [2, 1, 20], poison=0.5)
+    less = 20 - rows
+    lens, starts = lens[:2] + [lens[2] - less], starts[:3] + [starts[3] - less]
+    if page and page[0] == 2:
+        page = (2, 1 if rows > 16 else 0, page[2])
+    c = P.Cache(3, 1, 2, 64, 16, [2, 1, rows], poison=0.5)
     kv = handle(c, 2)
     table = c.table.copy()
     if page:
         table[page[0], page[1]] = page[2]
-    k = dev(draw(1, 23, 2, 64))
+    k = dev(draw(1, 3 + rows, 2, 64))
     kv.append(0, k, k, dev(table), dev(np.array(lens, np.int32)), dev(np.array(starts, np.int32)))
     with pytest.raises(U.UadError) as e:
         kv.synchronize()
@@ -194,7 +204,7 @@ def test_append_reports_what_it_cannot_use(gpu, what):
     # pages of no sequence are as they were
     spare = sorted(set(range(c.n_pages)) - set(c.table[c.table >= 0].tolist()))
     assert spare and bool((kv.k[0, spare] == 0.5).all()) and bool((kv.v[0, spare] == 0.5).all())
-    kv.append(0, k, k, dev(c.table), dev(c.lens), dev(np.array([0, 2, 3, 23], np.int32)))
+    kv.append(0, k, k, dev(c.table), dev(c.lens), dev(np.array([0, 2, 3, 3 + rows], np.int32)))
     kv.synchronize()
 
 

@@ -303,6 +303,10 @@ int slots(int target) { return max_slots(target); }
 int tries() { return kShareTries; }
 int fan() { return kJoinFan; }
 int most() { return kMaxSplits; }
+int tile_shift(int page_shift) { return append_tile_shift(page_shift); }
+int append_tiles_of(int from, int to, int shift) { return append_tiles(from, to, shift); }
+long long append_wgs(int rows, int seqs, int shift) { return append_grid(rows, seqs, shift); }
+int rows_fine(int from, int to, int rows) { return rows_ok(from, to, rows); }
 }
 """
 
@@ -313,6 +317,7 @@ def plan(tmp_path_factory):
     (d / "p.cpp").write_text(PLAN % CSRC)
     subprocess.run(["g++", "-O1", "-Wall", "-Werror", "-std=c++17", "-shared", "-fPIC", str(d / "p.cpp"), "-o", str(d / "p.so")], check=True)
     lib = ctypes.CDLL(str(d / "p.so"))
+    lib.append_wgs.restype = ctypes.c_longlong
     lib.share_of.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
     return lib
 
@@ -355,3 +360,22 @@ def test_plan_fills_the_workgroups_that_run_at_once(plan):
         wgs = sum(splits) * units
         assert wgs <= 256 and (wgs >= 200 or share == 4)
     assert plan_of(plan, [0], 4, 32, 256)[2] == [1]
+
+
+def test_append_tiles_hold_every_row_once_within_the_grid(plan):
+    r = np.random.default_rng(4)
+    for _ in range(400):
+        page_shift = int(r.integers(4, 9))
+        shift = plan.tile_shift(page_shift)
+        assert shift <= page_shift and 1 << shift <= 64
+        n = int(2 ** r.uniform(0, 8))
+        new = (2 ** r.uniform(0, r.choice([1, 4, 11]), n) - 1 + r.integers(0, 2)).astype(int)
+        before = r.integers(0, 300, n)
+        total = 0
+        for a, b in zip(before, before + new):
+            tiles = {p >> shift for p in range(a, b)}
+            assert plan.append_tiles_of(int(a), int(b), shift) == len(tiles)
+            total += len(tiles)
+        if new.sum():
+            assert total <= plan.append_wgs(int(new.sum()), n, shift)
+    assert [plan.rows_fine(*x) for x in ((0, 0, 0), (0, 5, 5), (2, 1, 9), (-1, 2, 9), (3, 10, 9))] == [1, 1, 0, 0, 0]
