@@ -53,10 +53,15 @@ __device__ __forceinline__ float load_pool(const void *p, size_t i) {
 }
 
 // Sine and cosine of `position` times a pair's turns: the whole turns go in 64 bits
-// (a position of 10^6 leaves 36 bits of the fraction), the rest in fp32.
+// (a position of 10^6 leaves 36 bits of the fraction), the rest in fp32 to the
+// instructions that take turns, off by at most 1.3e-7 within half a turn either way
+// (measured on 2^20 points; sincospif's 5e-8 took one prompt's append 4.6 instead of
+// 4.1 us).
 __device__ __forceinline__ void turn_of(double turns, int position, float *s, float *c) {
   const double t = turns * (double)position;
-  sincospif(2.0f * (float)(t - rint(t)), s, c);
+  const float f = (float)(t - rint(t));
+  *s = __builtin_amdgcn_sinf(f);
+  *c = __builtin_amdgcn_cosf(f);
 }
 
 // Inclusive sum over the lanes of a wave, by DPP: within rows of 16, then across them.
@@ -140,13 +145,19 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Append of many rows: one workgroup per tile (see paged.h), KV head and pool, so that
+// Append of many rows: one workgroup per tile (see paged.h), KV head, pool and up to 128
+// columns, so that
 // pages are written 16 bytes at a time: bound by memory, a row by itself would scatter
 // its values over a transposed page two bytes at a time.  K: a thread rotates 16
 // elements of a row, the pieces of 8 that are turned with each other.  V: through LDS,
 // whose 16-byte pieces are swizzled by the token's chunk, so that the lanes that read 8
 // (or 16) tokens of a column do not meet in a bank.
 // ---------------------------------------------------------------------------
+// Columns of a workgroup: 128 of 256, so that its LDS and its share of the work allow
+// eight on a CU.
+template <int HD>
+constexpr int kAppendWide = HD < 128 ? HD : 128;
+
 struct AppendTile {
   int b, first, last;  // tile's cache positions that get a row: first .. last
   int row;             // row of the first
@@ -246,22 +257,18 @@ struct Pool8 {
 template <int HD, bool F32, bool F8>
 __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvAppendArgs a) {
   constexpr int ESZ = F8 ? 1 : 2;
-  constexpr int PIECES = HD / 8;                      // of 8 elements in a row
+  constexpr int WIDE = kAppendWide<HD>;               // columns of this workgroup
+  constexpr int PIECES = WIDE / 8;                    // of 8 elements of a row
   constexpr int ROUNDS = kAppendTile * PIECES / 2 / 256;  // of 256 threads with two pieces each, at most
   constexpr int N = ROUNDS > 1 ? ROUNDS : 1;
-  __shared__ __align__(16) uint8_t lds[kAppendTile * HD * ESZ];
+  __shared__ __align__(16) uint8_t lds[kAppendTile * WIDE * ESZ];
   AppendTile t;
   if (!plan_append(a, blockIdx.x, &t)) return;
-  const int head = blockIdx.y, mask = (1 << a.d.page_shift) - 1;
-  const int page = a.table[(int64_t)t.b * a.pages_per_seq + (t.first >> a.d.page_shift)];
-  if (!page_ok(a.d, page)) {
-    if (threadIdx.x == 0) raise_status(a.status, kStatusPage);
-    return;
-  }
-  const size_t base = page_base(a.d, page, head);
+  const int head = blockIdx.y, part = blockIdx.z >> 1, mask = (1 << a.d.page_shift) - 1;
+  const int page = a.table[(int64_t)t.b * a.pages_per_seq + (t.first >> a.d.page_shift)];  // looked at when the rows are on their way
   const int tokens = t.last - t.first + 1, items = tokens * (PIECES / 2);
   const int tile_off = (t.first & mask) & ~(kAppendTile - 1);  // offset in the page of the tile's first slot
-  const bool is_v = blockIdx.z != 0;
+  const bool is_v = blockIdx.z & 1;
   const void *src = is_v ? a.v : a.k;
   const int64_t ld = is_v ? a.ldv : a.ldk;
   // an item: pieces x and y of a token; for K the ones that are turned with each other
@@ -282,15 +289,21 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvAppendArgs a) {
   for (int n = 0; n < N; ++n) {
     const int item = min((int)threadIdx.x + n * 256, items - 1), token = item / (PIECES / 2);
     int x, y;
-    pieces(item % (PIECES / 2), &x, &y);
+    pieces(part * (PIECES / 2) + item % (PIECES / 2), &x, &y);
     const int64_t at = (t.row + token) * ld + (int64_t)head * HD;
     rx[n].load(src, at + 8 * x, a.in_vec);
     ry[n].load(src, at + 8 * y, a.in_vec);
   }
+  if (!page_ok(a.d, page)) {
+    if (threadIdx.x == 0) raise_status(a.status, kStatusPage);
+    return;
+  }
+  const size_t base = page_base(a.d, page, head);
   if (!is_v) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int item = threadIdx.x + n * 256, token = item / (PIECES / 2), i = item % (PIECES / 2);
+      const int item = threadIdx.x + n * 256, token = item / (PIECES / 2);
+      const int i = part * (PIECES / 2) + item % (PIECES / 2);
       if (item >= items) break;
       float u[8], w[8];
 #pragma unroll
@@ -355,9 +368,9 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvAppendArgs a) {
   }
   __syncthreads();
   // columns in words (2 of bf16, 4 of e4m3), runs of RUN slots
-  constexpr int COLS = 4 / ESZ, WORDS = HD / COLS;
+  constexpr int COLS = 4 / ESZ, WORDS = WIDE / COLS;
   const int run0 = lead / RUN, runs = (lead + tokens - 1) / RUN - run0 + 1;
-  char *vp = (char *)a.vp + (base + tile_off) * ESZ;
+  char *vp = (char *)a.vp + (base + v_in_page(a.d, tile_off, part * WIDE)) * ESZ;
   for (int item = threadIdx.x; item < WORDS * runs; item += 256) {
     const int run = run0 + item % runs, word = item / runs, slot0 = run * RUN;
     uint32_t v[RUN];
@@ -399,7 +412,7 @@ static hipError_t launch_append_type(const KvAppendArgs &a, hipStream_t s) {
   constexpr int kMaxWgs = 1 << 23;  // work items of a grid stay below 2^32
   const int64_t tiles = append_grid(a.n_rows, a.n_seqs, append_tile_shift(a.d.page_shift));
   if ((int64_t)a.n_seqs * kAppendTileRows <= a.n_rows && tiles <= kMaxWgs && a.d.n_kv_heads <= 65535) {
-    const dim3 grid((unsigned)tiles, a.d.n_kv_heads, 2), wg(256);
+    const dim3 grid((unsigned)tiles, a.d.n_kv_heads, a.d.head_dim > 128 ? 4 : 2), wg(256);
     if (a.d.head_dim == 64) hipLaunchKernelGGL((kv_append_tile_kernel<64, F32, F8>), grid, wg, 0, s, a);
     else if (a.d.head_dim == 128) hipLaunchKernelGGL((kv_append_tile_kernel<128, F32, F8>), grid, wg, 0, s, a);
     else hipLaunchKernelGGL((kv_append_tile_kernel<256, F32, F8>), grid, wg, 0, s, a);
