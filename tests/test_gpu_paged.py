@@ -89,8 +89,9 @@ APPENDS = [
     (2, 64, 16, [i % 11 for i in range(130)], [i * 13 % 37 for i in range(130)], BF16, F8, 64, False),
     (1, 128, 64, [i % 23 for i in range(65)], [i * 13 % 70 for i in range(65)], F32, BF16, 128, True),
     (1, 256, 128, [1, 200, 64, 65], [127, 128, 64, 63], BF16, F8, 0, False),
-    (1, 64, 32, [4, 4], [30, 31], BF16, BF16, 64, False),
-    (1, 64, 32, [3, 4], [30, 31], BF16, BF16, 64, False),
+    (1, 64, 32, [8, 8], [30, 31], BF16, BF16, 64, False),
+    (1, 64, 32, [7, 8], [30, 31], BF16, BF16, 64, False),
+    (2, 64, 16, [5 + i % 17 for i in range(67)], [i * 13 % 37 for i in range(67)], BF16, F8, 64, False),
 ]
 
 
@@ -183,7 +184,7 @@ BAD_APPENDS = {  # lens, starts, a change of the page table (or none), of 3 sequ
 
 
 @pytest.mark.parametrize("what", BAD_APPENDS)
-@pytest.mark.parametrize("rows", [20, 2])  # by tiles and row by row
+@pytest.mark.parametrize("rows", [30, 2])  # by tiles and row by row
 def test_append_reports_what_it_cannot_use(gpu, what, rows):
     lens, starts, page = BAD_APPENDS[what]
     less = 20 - rows
