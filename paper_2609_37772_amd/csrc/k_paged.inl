@@ -600,23 +600,17 @@ __device__ __forceinline__ float max_row16(float v) {
   return v;
 }
 
-// A slot's values cross the XCDs' L2 caches: written through and read past them.
-__device__ __forceinline__ void put_slot(float *p, f32x4 v) {
-  union {
-    f32x4 f;
-    uint64_t u[2];
-  } x{v};
-  __hip_atomic_store((uint64_t *)p, x.u[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __hip_atomic_store((uint64_t *)p + 1, x.u[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// A slot's values cross the XCDs' L2 caches: 16-byte accesses that are written through
+// and read past them (cache policy sc1, device scope; the compiler waits for the loads).
+constexpr int kDeviceScope = 16;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t slots_of(const KvAttendArgs &a, int floats) {
+  return __builtin_amdgcn_make_buffer_rsrc(a.part, 0, a.slots * floats * 4, 0x00027000);  // raw buffer, below 2^31 bytes
 }
-__device__ __forceinline__ f32x4 get_slot(const float *p) {
-  union {
-    uint64_t u[2];
-    f32x4 f;
-  } x;
-  x.u[0] = __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  x.u[1] = __hip_atomic_load((const uint64_t *)p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return x.f;
+__device__ __forceinline__ void put_slot(__amdgpu_buffer_rsrc_t slots, unsigned i, f32x4 v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), slots, (int)(i * 4), 0, kDeviceScope);
+}
+__device__ __forceinline__ f32x4 get_slot(__amdgpu_buffer_rsrc_t slots, unsigned i) {
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(slots, (int)(i * 4), 0, kDeviceScope));
 }
 __device__ __forceinline__ uint64_t pair_of(float m, float l) {
   return (uint64_t)__float_as_uint(m) | ((uint64_t)__float_as_uint(l) << 32);
@@ -648,18 +642,20 @@ __device__ __forceinline__ bool last_to_arrive(unsigned *counter, int n, float *
 // Joins slots first, first + step, .. (n of them, at most 2 * kJoinFan): sums go to
 // put(row, column, sum of outputs, sum of weights); top [16][2] holds the joint maximum
 // and sum of each row.  The outputs are on their way while 16 lanes a row work the
-// weights out.
+// weights out; threads that the outputs leave over take a part of the slots.
 template <int HD, class Put>
 __device__ __forceinline__ void join_slots(const KvAttendArgs &a, int rows, int rows_max, int first, int step, int n,
-                                           float *weight, float *top, Put put) {
+                                           float *weight, float *top, f32x4 *shared, Put put) {
   constexpr int VEC = HD / 4, THREADS = 64 * kAttendWaves, RUN = 8;
   const int items = rows * VEC;
-  const size_t slot_floats = (size_t)rows_max * HD;
+  const int groups = min(n, max(1, THREADS / items)), mine = threadIdx.x / items;  // slots mine, mine + groups, ..
+  const int per = (n - mine + groups - 1) / groups;
+  const unsigned slot_floats = rows_max * HD;
+  const auto slots = slots_of(a, slot_floats);
   f32x4 v[RUN];
   auto fetch = [&](int item, int i0) {
-    const float *p = a.part + (size_t)first * slot_floats + (size_t)item * 4;
 #pragma unroll
-    for (int i = 0; i < RUN; ++i) v[i] = get_slot(p + (size_t)(min(i0 + i, n - 1) * step) * slot_floats);
+    for (int i = 0; i < RUN; ++i) v[i] = get_slot(slots, (first + min(mine + (i0 + i) * groups, n - 1) * step) * slot_floats + item * 4);
   };
   const int row = threadIdx.x >> 4, i = threadIdx.x & 15;
   uint64_t pair[2] = {pair_of(-INFINITY, 0.f), pair_of(-INFINITY, 0.f)};
@@ -669,7 +665,8 @@ __device__ __forceinline__ void join_slots(const KvAttendArgs &a, int rows, int 
       if (i + 16 * k < n)
         pair[k] = __hip_atomic_load(a.part_ml + (size_t)(first + (i + 16 * k) * step) * rows_max + row, __ATOMIC_RELAXED,
                                     __HIP_MEMORY_SCOPE_AGENT);
-  if ((int)threadIdx.x < items) fetch(threadIdx.x, 0);
+  const int item0 = threadIdx.x - mine * items;  // groups > 1: the only one
+  if (mine < groups) fetch(item0, 0);
   if (row < 16) {
     const float m0 = __uint_as_float((uint32_t)pair[0]), m1 = __uint_as_float((uint32_t)pair[1]);
     const float l0 = __uint_as_float((uint32_t)(pair[0] >> 32)), l1 = __uint_as_float((uint32_t)(pair[1] >> 32));
@@ -684,18 +681,31 @@ __device__ __forceinline__ void join_slots(const KvAttendArgs &a, int rows, int 
     }
   }
   __syncthreads();
-  for (int item = threadIdx.x; item < items; item += THREADS) {
+  auto sum_of = [&](int item) {
     const int r = item / VEC;
-    if (item >= THREADS) fetch(item, 0);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int i0 = 0;;) {
 #pragma unroll
-      for (int k = 0; k < RUN; ++k) o += v[k] * weight[(i0 + k) * 16 + r];
+      for (int k = 0; k < RUN; ++k)
+        if (i0 + k < per) o += v[k] * weight[(mine + (i0 + k) * groups) * 16 + r];
       i0 += RUN;
-      if (i0 >= n) break;
+      if (i0 >= per) return o;
       fetch(item, i0);
     }
-    put(r, item % VEC * 4, o, top[2 * r + 1]);
+  };
+  if (groups > 1) {  // the groups' sums meet, in order
+    if (mine < groups) shared[threadIdx.x] = sum_of(item0);
+    __syncthreads();
+    if (mine == 0) {
+      f32x4 o = shared[item0];
+      for (int g = 1; g < groups; ++g) o += shared[g * items + item0];
+      put(item0 / VEC, item0 % VEC * 4, o, top[2 * (item0 / VEC) + 1]);
+    }
+  } else {
+    for (int item = threadIdx.x; item < items; item += THREADS) {
+      if (item >= THREADS) fetch(item, 0);
+      put(item / VEC, item % VEC * 4, sum_of(item), top[2 * (item / VEC) + 1]);
+    }
   }
 }
 
@@ -937,6 +947,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
     }
   };
   const int slot = w.slot + w.split;
+  const auto slots = slots_of(a, rows_max * HD);
   if (c < rows) {
     for (int n = wave; n < NTO; n += NW) {
       f32x4 v = obuf[n * 64 + lane];
@@ -946,7 +957,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
 #pragma unroll
         for (int i = NW / 2; i < NW; ++i) v += obuf[(i * NTO + n) * 64 + lane];
       if (w.splits == 1) put_out(c, 16 * n + 4 * g, v, sum);
-      else put_slot(a.part + ((size_t)slot * rows_max + c) * HD + 16 * n + 4 * g, v);
+      else put_slot(slots, (slot * rows_max + c) * HD + 16 * n + 4 * g, v);
     }
     if (w.splits > 1 && wave == 0 && g == 0)
       __hip_atomic_store(a.part_ml + (size_t)slot * rows_max + c, pair_of(mx, sum), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -960,9 +971,9 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
     const int first = final ? w.slot : w.slot + run, step = final && w.splits > 2 * kJoinFan ? kJoinFan : 1;
     const int n = !final ? min(kJoinFan, w.splits - run) : (w.splits + step - 1) / step;
     if (!last_to_arrive(a.arrived + (final ? a.slots : 0) + first, n, word)) return;
-    join_slots<HD>(a, rows, rows_max, first, step, n, ml, top, [&](int row, int col, f32x4 v, float total) {
+    join_slots<HD>(a, rows, rows_max, first, step, n, ml, top, obuf, [&](int row, int col, f32x4 v, float total) {
       if (final) put_out(row, col, v, total);
-      else put_slot(a.part + ((size_t)first * rows_max + row) * HD + col, v);
+      else put_slot(slots, (first * rows_max + row) * HD + col, v);
     });
     if (final) return;
     if ((int)threadIdx.x < rows)
