@@ -409,6 +409,7 @@ def uad_profile_read(ctx: int) -> Dict[str, Tuple[float, int]]:
 # ----------------------------------------------------------------------------
 # Paged K/V cache
 # ----------------------------------------------------------------------------
+# Decoding calls these once a token and layer: on good arguments they look at each tensor's properties once.
 _ROW_TYPES = {torch.float32: UAD_DTYPE_F32, torch.bfloat16: UAD_DTYPE_BF16}
 
 
@@ -417,39 +418,39 @@ def _check_kv(kv, st: int, what: str):
         raise UadError(st, f"{what}: {uad_kv_last_error(kv)}")
 
 
-def _rows(t: torch.Tensor, shape: Tuple[int, ...], name: str, device: int) -> Tuple[int, int, int]:
-    """(pointer, uad dtype, elements between rows) of a device tensor of rows [n][heads][head_dim], each row dense."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != device:
-        raise ValueError(f"{name} must be a tensor on device {device}")
-    dt = _ROW_TYPES.get(t.dtype)
+def _rows(t: torch.Tensor, shape: Tuple[int, int], name: str, device: int) -> Tuple[int, int, int, int]:
+    """(pointer, uad dtype, elements between rows, rows) of a device tensor of rows [n][heads][head_dim], each dense."""
+    dt = _ROW_TYPES.get(getattr(t, "dtype", None))
     if dt is None:
-        raise ValueError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    if t.dim() != 3 or t.shape[1:] != shape:
-        raise ValueError(f"{name} must be [rows][{shape[0]}][{shape[1]}], got {tuple(t.shape)}")
-    ld, heads, inner = t.stride()
-    row = shape[0] * shape[1]
-    if t.shape[0] < 2:
-        ld = row  # the stride of a dimension of one says nothing
-    if t.numel() and (inner != 1 or (heads != shape[1] and shape[0] > 1) or ld < row):
-        raise ValueError(f"{name} must have dense rows that do not overlap, got strides {t.stride()}")
-    return t.data_ptr(), dt, max(ld, row)
+        raise ValueError(f"{name} must be a float32 or bfloat16 tensor, got {getattr(t, 'dtype', type(t))}")
+    size = t.shape
+    if size[1:] != shape or t.get_device() != device:
+        raise ValueError(f"{name} must be [rows][{shape[0]}][{shape[1]}] on device {device}, got {tuple(size)} on {t.device}")
+    n = size[0]
+    ld = shape[0] * shape[1]
+    if not t.is_contiguous():
+        row, head, inner = t.stride()
+        if n < 2:
+            row = ld  # the stride of a dimension of one says nothing
+        if inner != 1 or (head != shape[1] and shape[0] > 1) or row < ld:
+            raise ValueError(f"{name} must have dense rows that do not overlap, got strides {t.stride()}")
+        ld = row
+    return t.data_ptr(), dt, ld, n
 
 
-def _ints(t: Optional[torch.Tensor], shape: Tuple[int, ...], name: str, device: int) -> Optional[int]:
-    if t is None:
-        return None
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.shape != shape or not t.is_cuda \
-            or t.get_device() != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on device {device}")
+def _ints(t: torch.Tensor, shape: Tuple[int, ...], name: str, device: int) -> int:
+    if getattr(t, "dtype", None) is not torch.int32 or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {tuple(shape)} on device {device}")
     return t.data_ptr()
 
 
 def _table(page_table: torch.Tensor, lens: torch.Tensor, device: int) -> Tuple[int, int, int, int]:
     """(page table, pages per sequence, lens, sequences) of a call."""
-    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+    size = getattr(page_table, "shape", ())
+    if len(size) != 2:
         raise ValueError("page_table must be an int32 device tensor [n_seqs][pages_per_seq]")
-    n, wide = page_table.shape
-    return _ints(page_table, (n, wide), "page_table", device), wide, _ints(lens, (n,), "lens", device), n
+    n, wide = size
+    return _ints(page_table, size, "page_table", device), wide, _ints(lens, (n,), "lens", device), n
 
 
 def uad_kv_create(n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int,
@@ -484,15 +485,14 @@ def uad_kv_append(kv: int, layer: int, k: torch.Tensor, v: torch.Tensor, page_ta
                   row_start: Optional[torch.Tensor], positions: Optional[torch.Tensor], row_shape: Tuple[int, int],
                   device: int = 0) -> None:
     """Append rows k, v [n_rows][Hkv][hd] (rows may be slices of wider ones) to a layer's pages."""
-    pk, dk, ldk = _rows(k, row_shape, "k", device)
-    pv, dv, ldv = _rows(v, row_shape, "v", device)
-    n = k.shape[0]
-    if dk != dv or v.shape[0] != n:
+    pk, dk, ldk, n = _rows(k, row_shape, "k", device)
+    pv, dv, ldv, nv = _rows(v, row_shape, "v", device)
+    if dk != dv or nv != n:
         raise ValueError("k and v must share dtype and rows")
     pt, wide, pl, seqs = _table(page_table, lens, device)
-    ps = _ints(row_start, (seqs + 1,), "row_start", device)
-    pp = _ints(positions, (n,), "positions", device)
-    st = load_library().uad_kv_append(kv, layer, pk, pv, dk, ldk, ldv, n, ps, pl, pp, pt, wide, seqs)
+    ps = None if row_start is None else _ints(row_start, (seqs + 1,), "row_start", device)
+    pp = None if positions is None else _ints(positions, (n,), "positions", device)
+    st = (_lib or load_library()).uad_kv_append(kv, layer, pk, pv, dk, ldk, ldv, n, ps, pl, pp, pt, wide, seqs)
     if st:
         _check_kv(kv, st, "uad_kv_append")
 
@@ -502,12 +502,12 @@ def uad_kv_attend(kv: int, layer: int, q: torch.Tensor, out: torch.Tensor, page_
                   device: int = 0) -> None:
     """Attention of q [n_seqs][Hq][hd], one token per sequence, over a layer's pages into out (q's type and shape)."""
     pt, wide, pl, seqs = _table(page_table, lens, device)
-    pq, dq, ldq = _rows(q, row_shape, "q", device)
-    po, do, ldo = _rows(out, row_shape, "out", device)
-    if dq != do or q.shape[0] != seqs or out.shape[0] != seqs:
+    pq, dq, ldq, nq = _rows(q, row_shape, "q", device)
+    po, do, ldo, no = _rows(out, row_shape, "out", device)
+    if dq != do or nq != seqs or no != seqs:
         raise ValueError("q and out must share dtype and have a row per sequence")
-    pp = _ints(positions, (seqs,), "positions", device)
-    st = load_library().uad_kv_attend(kv, layer, pq, po, dq, ldq, ldo, pl, pp, pt, wide, seqs, scale)
+    pp = None if positions is None else _ints(positions, (seqs,), "positions", device)
+    st = (_lib or load_library()).uad_kv_attend(kv, layer, pq, po, dq, ldq, ldo, pl, pp, pt, wide, seqs, scale)
     if st:
         _check_kv(kv, st, "uad_kv_attend")
 

@@ -1040,13 +1040,22 @@ hipError_t launch_kv_attend(const KvAttendArgs &a, bool f32, bool f8, hipStream_
 // side by side, so V needs no LDS.  Keys from n_keys on are zeros, as with
 // prefix_pack_kernel.
 // ---------------------------------------------------------------------------
+// N (4 or 8) pool elements as bf16 bits, from an offset that is a multiple of N.
 template <bool F8, int N>
-struct PoolRun {  // N consecutive pool elements as bf16
-  __device__ static __forceinline__ void load(const void *p, size_t i, float scale, __bf16 *o) {
+__device__ __forceinline__ void load_run(const char *p, float scale, uint16_t *o) {
+  typedef uint32_t words __attribute__((ext_vector_type(N / (F8 ? 4 : 2))));
+  const words r = *(const words *)p;
 #pragma unroll
-    for (int e = 0; e < N; ++e) o[e] = (__bf16)(F8 ? load_pool<true>(p, i + e) * scale : load_pool<false>(p, i + e));
+  for (int e = 0; e < N; ++e) {
+    if constexpr (F8) {
+      const float v = __builtin_amdgcn_cvt_f32_fp8((int)(r[e / 4] >> (8 * (e % 4))), 0) * scale;
+      o[e] = __builtin_bit_cast(uint16_t, (__bf16)v);
+    } else {
+      o[e] = (uint16_t)(r[e / 2] >> (16 * (e % 2)));
+      if ((o[e] & 0x7FFFu) > 0x7F80u) o[e] |= 0x40u;  // a signalling NaN turns quiet, as in prefix_pack_kernel
+    }
   }
-};
+}
 
 template <int HD, bool F8>
 __global__ __launch_bounds__(256) void kv_prefix_kernel(KvPrefixArgs a) {
@@ -1057,41 +1066,47 @@ __global__ __launch_bounds__(256) void kv_prefix_kernel(KvPrefixArgs a) {
   const int len = usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad);
   bad |= len < a.n_keys;
   const int n_keys = min(len, a.n_keys);
-  const size_t esz = F8 ? 1 : 2;
-  const char *kp = (const char *)a.kp + src * esz, *vp = (const char *)a.vp + src * esz;
+  constexpr int ESZ = F8 ? 1 : 2;
+  const char *kp = (const char *)a.kp + src * ESZ, *vp = (const char *)a.vp + src * ESZ;
   __bf16 *kd = a.kc + blockIdx.z * a.dst_layer + (eh * a.s_alloc + (size_t)blk * 32) * HD;
   __bf16 *vd = a.vtc + blockIdx.z * a.dst_layer + vt_index(eh, blk * 32, 0, HD, a.s_alloc);
-  const int32_t *row = a.table + (int64_t)b * a.pages_per_seq;
   const int mask = (1 << a.d.page_shift) - 1;
-  for (int q = threadIdx.x; q < 32 * HD / 8; q += 256) {
-    const int key = q / (HD / 8), c = (q % (HD / 8)) * 8, s = blk * 32 + key;
-    __bf16 o[8] = {};
-    if (s < n_keys) {
-      const int page = row[s >> a.d.page_shift];
-      if (page_ok(a.d, page)) PoolRun<F8, 8>::load(kp, page_base(a.d, page, g) + k_in_page(a.d, s & mask, c), a.k_scale, o);
-      else bad = true;
+  // the block's 32 keys lie in one page, or in two of 16
+  const int32_t *row = a.table + (int64_t)b * a.pages_per_seq;
+  int page[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int s = blk * 32 + 16 * h;
+    page[h] = s < n_keys ? row[s >> a.d.page_shift] : -1;
+    if (s < n_keys && !page_ok(a.d, page[h])) {
+      bad = true;
+      page[h] = -1;
     }
-    *(bf16x8 *)(kd + key * HD + c) = bf16x8{o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]};
   }
-  for (int q = threadIdx.x; q < HD * 4; q += 256) {
-    const int c = q >> 2, ch = q & 3;
-    __bf16 o[8] = {};
+  typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+#pragma unroll
+  for (int it = 0; it < HD / 64; ++it) {
+    const int q = it * 256 + threadIdx.x;
+    const int key = q / (HD / 8), c = (q % (HD / 8)) * 8, s = blk * 32 + key, h = key >> 4;
+    uint16_t o[8] = {};
+    if (s < n_keys && page[h] >= 0) load_run<F8, 8>(kp + (page_base(a.d, page[h], g) + k_in_page(a.d, s & mask, c)) * ESZ, a.k_scale, o);
+    *(u16x8 *)(kd + key * HD + c) = u16x8{o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]};
+  }
+#pragma unroll
+  for (int it = 0; it < HD / 64; ++it) {
+    const int q = it * 256 + threadIdx.x, c = q >> 2, ch = q & 3;
+    uint16_t o[8] = {};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int s = blk * 32 + 16 * h + 4 * ch;  // four keys of one page
-      if (s < n_keys) {
-        const int page = row[s >> a.d.page_shift];
-        if (page_ok(a.d, page)) {
-          PoolRun<F8, 4>::load(vp, page_base(a.d, page, g) + v_in_page(a.d, s & mask, c), a.v_scale, o + 4 * h);
+      if (s < n_keys && page[h] >= 0) {
+        load_run<F8, 4>(vp + (page_base(a.d, page[h], g) + v_in_page(a.d, s & mask, c)) * ESZ, a.v_scale, o + 4 * h);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (s + e >= n_keys) o[4 * h + e] = (__bf16)0.f;
-        } else {
-          bad = true;
-        }
+        for (int e = 0; e < 4; ++e)
+          if (s + e >= n_keys) o[4 * h + e] = 0;
       }
     }
-    *(bf16x8 *)(vd + c * 32 + ch * 8) = bf16x8{o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]};
+    *(u16x8 *)(vd + c * 32 + ch * 8) = u16x8{o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]};
   }
   if (bad) {
     raise_status(a.status, kStatusPage);

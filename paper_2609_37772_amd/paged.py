@@ -28,6 +28,8 @@ class PagedKV:
             raise ValueError(f"pools must be bfloat16 or float8_e4m3fn, got {dtype}")
         self.device = device
         self.n_layers, self.n_heads, self.n_kv_heads, self.head_dim = n_layers, n_heads, n_kv_heads, head_dim
+        self._kv_row, self._q_row = (n_kv_heads, head_dim), (n_heads, head_dim)
+        self._scale = 1.0 / math.sqrt(head_dim)
         shapes = ((n_layers, n_pages, n_kv_heads, page_size, head_dim), (n_layers, n_pages, n_kv_heads, head_dim, page_size))
         pools = []
         for name, pool, shape in zip("kv", (k, v), shapes):
@@ -53,16 +55,14 @@ class PagedKV:
 
     def append(self, layer: int, k, v, page_table, lens, row_start=None, positions=None) -> None:
         """Append new tokens' keys (rotated) and values to a layer; see uad_kv_append."""
-        B.uad_kv_append(self.handle, layer, k, v, page_table, lens, row_start, positions,
-                        (self.n_kv_heads, self.head_dim), self.device)
+        B.uad_kv_append(self.handle, layer, k, v, page_table, lens, row_start, positions, self._kv_row, self.device)
 
     def attend(self, layer: int, q, page_table, lens, out=None, positions=None, scale: Optional[float] = None):
         """Attention of one token per sequence; see uad_kv_attend.  Allocates ``out`` when not given and returns it."""
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        B.uad_kv_attend(self.handle, layer, q, out, page_table, lens, positions,
-                        1.0 / math.sqrt(self.head_dim) if scale is None else scale,
-                        (self.n_heads, self.head_dim), self.device)
+        B.uad_kv_attend(self.handle, layer, q, out, page_table, lens, positions, self._scale if scale is None else scale,
+                        self._q_row, self.device)
         return out
 
     def set_stream(self, stream: Optional[torch.cuda.Stream]) -> None:
