@@ -872,21 +872,12 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
 #pragma unroll
       for (int n = 0; n < NTO; ++n) o[n] *= f;
     }
-    union {
-      bf16x8 v[TERMS][NT / 2];
-      __bf16 e[TERMS][4 * NT];
-    } pf;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float q = __builtin_amdgcn_exp2f(s[t][r] - m);
-        l += q;
-#pragma unroll
-        for (int i = 0; i < TERMS; ++i) {
-          pf.e[i][4 * t + r] = (__bf16)q;
-          q -= (float)pf.e[i][4 * t + r];
-        }
+        s[t][r] = __builtin_amdgcn_exp2f(s[t][r] - m);
+        l += s[t][r];
       }
     if (tail) {  // what lies behind the last key may be anything, NaN included
       constexpr int PER = F8 ? 4 : 2;  // elements of a register
@@ -900,13 +891,27 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
       }
     }
 #pragma unroll
-    for (int n = 0; n < NTO; ++n)
+    for (int u = 0; u < NT / 2; ++u) {  // 8 weights of the lane, as terms
+      union {
+        bf16x8 v;
+        __bf16 e[8];
+      } pf[TERMS];
 #pragma unroll
-      for (int u = 0; u < NT / 2; ++u) {
+      for (int e = 0; e < 8; ++e) {
+        float p = s[2 * u + e / 4][e % 4];
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i) {
+          pf[i].e[e] = (__bf16)p;
+          p -= (float)pf[i].e[e];
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NTO; ++n) {
         const bf16x8 vf = operand_of<F8>(vr[n], u);
 #pragma unroll
-        for (int i = TERMS - 1; i >= 0; --i) o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf.v[i][u], o[n], 0, 0, 0);
+        for (int i = TERMS - 1; i >= 0; --i) o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[i].v, o[n], 0, 0, 0);
       }
+    }
     if (more) load_v(tile + NW, vp);
   }
   if (bad) raise_status(a.status, kStatusPage);
