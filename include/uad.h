@@ -381,7 +381,7 @@ uad_status uad_kv_set_stream(uad_kv *kv, void *hip_stream);
 /* Append keys and values of new tokens to one layer's pages; keys are rotated on
  * the way.
  *   k, v        device [n_rows][n_kv_heads][head_dim] of dtype F32 or BF16, rows
- *               ldk / ldv elements apart (at least n_kv_heads * head_dim), aligned
+ *               ldk / ldv elements apart (n_kv_heads * head_dim .. 2^30), aligned
  *               to their type (to 16 bytes is faster)
  *   row_start   int32 [n_seqs + 1], rising from 0: rows row_start[b] ..
  *               row_start[b+1]-1 are sequence b's new tokens in order (none is
@@ -391,20 +391,22 @@ uad_status uad_kv_set_stream(uad_kv *kv, void *hip_stream);
  *               Row j of sequence b's n new rows takes cache position
  *               lens[b] - n + j.
  * Errors: UAD_E_INVALID (null pointer, bad layer, dtype or row length),
- * UAD_E_SHAPE (n_seqs beyond max_seqs, n_rows != n_seqs without row_start),
- * UAD_E_HIP. */
+ * UAD_E_SHAPE (n_seqs beyond max_seqs, n_rows != n_seqs without row_start, a page
+ * table of more than 2^30 tokens per sequence), UAD_E_HIP. */
 uad_status uad_kv_append(uad_kv *kv, int32_t layer, const void *k, const void *v, int32_t dtype, int64_t ldk,
                          int64_t ldv, int32_t n_rows, const int32_t *row_start, const int32_t *lens,
                          const int32_t *positions, const int32_t *page_table, int32_t pages_per_seq, int32_t n_seqs);
 
 /* Attention of one query token per sequence over the lens[b] tokens of its pages
  * in one layer: out = softmax(scale * q K^T) V per head, in fp32, rounded once to
- * the type of q.  A sequence of length 0 gives zeros.
+ * the type of q.  A sequence of length 0 gives zeros.  Keys behind lens[b] are as
+ * if they were not there, whatever their slots hold; a NaN in the query, or in a key
+ * or value of the sequence, makes the outputs that it enters NaN, an infinity may.
  *   q, out      device [n_seqs][n_heads][head_dim] of dtype F32 or BF16, sequences
  *               ldq / ldo elements apart, aligned to their type; out may not
  *               overlap q or the pools
  *   positions   int32 [n_seqs] rotation positions of the queries, or NULL: lens[b] - 1
- *   scale       softmax scale, finite (1/sqrt(head_dim) as a rule)
+ *   scale       softmax scale, finite, times k_scale too (1/sqrt(head_dim) as a rule)
  * Errors as uad_kv_append. */
 uad_status uad_kv_attend(uad_kv *kv, int32_t layer, const void *q, void *out, int32_t dtype, int64_t ldq, int64_t ldo,
                          const int32_t *lens, const int32_t *positions, const int32_t *page_table,

@@ -80,6 +80,36 @@ __device__ __forceinline__ int scan_wave64(int v) {
 }
 __device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
+// A workgroup's plan looks at every sequence: by each wave for itself where lanes are
+// enough, else by the whole workgroup, a run of sequences per thread.
+template <int WAVES>
+struct PlanScan {
+  const bool block;
+  const int me, per;  // this thread's sequences: me * per .. me * per + per - 1
+  int *lds;           // [WAVES] for each scan, only where the whole workgroup scans
+  __device__ __forceinline__ PlanScan(int n_seqs, int *lds_)
+      : block(n_seqs > 64), me(block ? threadIdx.x : threadIdx.x & 63), per(block ? (n_seqs + 64 * WAVES - 1) / (64 * WAVES) : 1),
+        lds(lds_) {}
+  // Inclusive sum over the threads, and the sum of all.
+  __device__ __forceinline__ int operator()(int v, int *all) {
+    v = scan_wave64(v);
+    *all = last_lane(v);
+    if (block) {
+      if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = v;
+      __syncthreads();
+      *all = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        if (w == (int)(threadIdx.x >> 6)) v += *all;
+        *all += lds[w];
+      }
+      lds += WAVES;  // the next scan's, which spares a barrier
+    }
+    return v;
+  }
+};
+constexpr int kPlanScans = 4 + kShareTries;  // of one plan at most
+
 // The sequence of a new row: how many of row_start[0 .. n_seqs] are at most r, minus
 // one.  Called by whole waves; r is the same in all lanes.
 __device__ __forceinline__ int sequence_of_row(const int32_t *row_start, int n_seqs, int r) {
@@ -166,8 +196,9 @@ struct AppendTile {
   int row;             // row of the first
 };
 
-__device__ __forceinline__ bool plan_append(const KvAppendArgs &a, int wg, AppendTile *t) {
-  const int lane = threadIdx.x & 63, per = (a.n_seqs + 63) / 64, shift = append_tile_shift(a.d.page_shift);
+__device__ __forceinline__ bool plan_append(const KvAppendArgs &a, int wg, int *lds, AppendTile *t) {
+  PlanScan<4> scan(a.n_seqs, lds);
+  const int shift = append_tile_shift(a.d.page_shift);
   bool bad = false;
   // positions [from, to) and rows of a sequence; none where they cannot be used
   auto span = [&](int b, int *from, int *to, int *row) {
@@ -179,28 +210,42 @@ __device__ __forceinline__ bool plan_append(const KvAppendArgs &a, int wg, Appen
     *to = ok ? len : 0;
     *from = ok ? len - (hi - lo) : 0;
   };
-  int mine = 0, from = 0, to = 0, row = 0;
-  for (int i = 0; i < per; ++i)
-    if (lane * per + i < a.n_seqs) {
-      span(lane * per + i, &from, &to, &row);
+  int mine = 0, from = 0, to = 0, row = 0, all;
+  for (int i = 0; i < scan.per; ++i)
+    if (scan.me * scan.per + i < a.n_seqs) {
+      span(scan.me * scan.per + i, &from, &to, &row);
       mine += append_tiles(from, to, shift);
     }
   if (bad && wg == 0) raise_status(a.status, kStatusPage);
-  const int upto = scan_wave64(mine);
-  if (wg >= last_lane(upto)) return false;
-  const int at = __builtin_ctzll(__ballot(upto > wg));
-  int start = __builtin_amdgcn_readlane(upto - mine, at), b = at * per;
-  from = __builtin_amdgcn_readlane(from, at);
-  to = __builtin_amdgcn_readlane(to, at);
-  row = __builtin_amdgcn_readlane(row, at);
-  if (per > 1)
-    for (;; ++b) {
-      if (b >= a.n_seqs) return false;  // only if the caller's arrays change while this runs
-      span(b, &from, &to, &row);
-      const int n = append_tiles(from, to, shift);
-      if (start + n > wg) break;
-      start += n;
+  const int upto = scan(mine, &all);
+  if (wg >= all) return false;
+  int start = upto - mine, b = scan.me;
+  if (scan.block) {
+    if (upto > wg && start <= wg) {  // one thread: it looks for the sequence among its own
+      for (b = scan.me * scan.per;; ++b) {
+        if (b < a.n_seqs) span(b, &from, &to, &row);
+        const int n = append_tiles(from, to, shift);
+        if (b >= a.n_seqs || start + n > wg) break;
+        start += n;
+      }
+      const int found[5] = {b, start, from, to, row};
+#pragma unroll
+      for (int i = 0; i < 5; ++i) scan.lds[i] = found[i];
     }
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(scan.lds[0]);
+    start = __builtin_amdgcn_readfirstlane(scan.lds[1]);
+    from = __builtin_amdgcn_readfirstlane(scan.lds[2]);
+    to = __builtin_amdgcn_readfirstlane(scan.lds[3]);
+    row = __builtin_amdgcn_readfirstlane(scan.lds[4]);
+    if (b >= a.n_seqs) return false;  // only if the caller's arrays change while this runs
+  } else {
+    b = __builtin_ctzll(__ballot(upto > wg));
+    start = __builtin_amdgcn_readlane(start, b);
+    from = __builtin_amdgcn_readlane(from, b);
+    to = __builtin_amdgcn_readlane(to, b);
+    row = __builtin_amdgcn_readlane(row, b);
+  }
   const int tile = (from >> shift) + wg - start;
   t->b = b;
   t->first = max(from, tile << shift);
@@ -270,8 +315,9 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvAppendArgs a) {
   constexpr int ROUNDS = kAppendTile * PIECES / 2 / 256;  // of 256 threads with two pieces each, at most
   constexpr int N = ROUNDS > 1 ? ROUNDS : 1;
   __shared__ __align__(16) uint8_t lds[kAppendTile * WIDE * ESZ];
+  __shared__ int plan[kPlanScans * 4];
   AppendTile t;
-  if (!plan_append(a, blockIdx.x, &t)) return;
+  if (!plan_append(a, blockIdx.x, plan, &t)) return;
   const int head = blockIdx.y, part = blockIdx.z >> 1, mask = (1 << a.d.page_shift) - 1;
   const int page = a.table[(int64_t)t.b * a.pages_per_seq + (t.first >> a.d.page_shift)];  // looked at when the rows are on their way
   const int tokens = t.last - t.first + 1, items = tokens * (PIECES / 2);
@@ -518,67 +564,77 @@ struct AttendWork {
   int b, unit, len, t0, t1, split, splits, slot;
 };
 
-// The plan (see paged.h), by whole waves: lane i looks after sequences i * per ..
+// The plan (see paged.h).
 template <int TILE>
-__device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, int wg, AttendWork *w) {
-  const int lane = threadIdx.x & 63, per = (a.n_seqs + 63) / 64;
+__device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, int wg, int *lds, AttendWork *w) {
+  PlanScan<kAttendWaves> scan(a.n_seqs, lds);
   bool bad = false;
   auto length = [&](int b) { return usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad); };
+  // f(length) over this thread's sequences, of which the first is kept
   int my_len = 0;
+  const int b0 = scan.me * scan.per;
+  if (b0 < a.n_seqs) my_len = length(b0);
+  auto each = [&](auto f) {
+    if (b0 < a.n_seqs) f(my_len);
+    for (int i = 1; i < scan.per; ++i)
+      if (b0 + i < a.n_seqs) f(length(b0 + i));
+  };
   int64_t n = 0;
-  for (int i = 0; i < per; ++i)
-    if (lane * per + i < a.n_seqs) {
-      my_len = length(lane * per + i);
-      n += tiles_of_length(my_len, TILE);
-    }
+  each([&](int len) { n += tiles_of_length(len, TILE); });
   if (bad && wg == 0) raise_status(a.status, kStatusPage);
   n *= units;
-  const int64_t total = ((int64_t)last_lane(scan_wave64((int)(n >> 24))) << 24) + last_lane(scan_wave64((int)(n & 0xFFFFFF)));
-  int share = first_share(total, a.target, kAttendMinTiles);
-  int mine, upto;
-  auto count = [&]() {  // workgroups of this lane's sequences, and up to them
+  int hi, lo;
+  scan((int)(n >> 22), &hi);
+  scan((int)(n & 0x3FFFFF), &lo);
+  int share = first_share(((int64_t)hi << 22) + lo, a.target, kAttendMinTiles);
+  int mine, upto, wgs;
+  auto count = [&]() {  // workgroups of this thread's sequences, and up to them
     mine = 0;
-    if (per == 1) {
-      if (lane < a.n_seqs) mine = splits_of(tiles_of_length(my_len, TILE), share) * units;
-    } else {
-      for (int i = 0; i < per; ++i)
-        if (lane * per + i < a.n_seqs) mine += splits_of(tiles_of_length(length(lane * per + i), TILE), share) * units;
-    }
-    upto = scan_wave64(mine);
-    return last_lane(upto);
+    each([&](int len) { mine += splits_of(tiles_of_length(len, TILE), share) * units; });
+    upto = scan(mine, &wgs);
   };
-  int wgs = count();
+  count();
   if ((int64_t)a.n_seqs * units < a.target)
     for (int i = 0; i < kShareTries && wgs > a.target; ++i) {
       share = next_share(share);
-      wgs = count();
+      count();
     }
   if (wg >= wgs) return false;
-  const int at = __builtin_ctzll(__ballot(upto > wg));
-  // workgroups in split units, for the slots
-  int split_mine = 0;
-  if (per == 1) {
-    split_mine = mine > units ? mine : 0;
-  } else {
-    for (int i = 0; i < per; ++i)
-      if (lane * per + i < a.n_seqs) {
-        const int s = splits_of(tiles_of_length(length(lane * per + i), TILE), share);
-        if (s > 1) split_mine += s * units;
+  int in_slots = 0, all;  // workgroups in split units, for the slots
+  each([&](int len) {
+    const int s = splits_of(tiles_of_length(len, TILE), share);
+    if (s > 1) in_slots += s * units;
+  });
+  const int slot_upto = scan(in_slots, &all);
+  int start = upto - mine, slot = slot_upto - in_slots, b, len;
+  if (scan.block) {
+    if (upto > wg && start <= wg) {  // one thread: it looks for the sequence among its own
+      len = my_len;
+      for (b = b0;;) {
+        const int s = splits_of(tiles_of_length(len, TILE), share);
+        if (start + s * units > wg) break;
+        start += s * units;
+        if (s > 1) slot += s * units;
+        if (++b >= a.n_seqs) break;
+        len = length(b);
       }
+      const int found[4] = {b, len, start, slot};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) scan.lds[i] = found[i];
+    }
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(scan.lds[0]);
+    len = __builtin_amdgcn_readfirstlane(scan.lds[1]);
+    start = __builtin_amdgcn_readfirstlane(scan.lds[2]);
+    slot = __builtin_amdgcn_readfirstlane(scan.lds[3]);
+    if (b >= a.n_seqs) return false;  // only if the lengths change while this runs
+  } else {
+    b = __builtin_ctzll(__ballot(upto > wg));
+    start = __builtin_amdgcn_readlane(start, b);
+    slot = __builtin_amdgcn_readlane(slot, b);
+    len = __builtin_amdgcn_readlane(my_len, b);
   }
-  const int split_upto = scan_wave64(split_mine);
-  int start = __builtin_amdgcn_readlane(upto - mine, at), slot = __builtin_amdgcn_readlane(split_upto - split_mine, at);
-  int b = at * per, len = __builtin_amdgcn_readlane(my_len, at);
-  int tiles, splits;
-  for (;;) {
-    if (per > 1) len = __builtin_amdgcn_readfirstlane(length(b));
-    tiles = tiles_of_length(len, TILE);
-    splits = splits_of(tiles, share);
-    if (per == 1 || start + splits * units > wg) break;
-    start += splits * units;
-    if (splits > 1) slot += splits * units;
-    if (++b >= a.n_seqs) return false;  // only if the lengths change while this runs
-  }
+  const int tiles = tiles_of_length(len, TILE), splits = splits_of(tiles, share);
   w->b = b;
   w->len = len;
   w->unit = (unsigned)(wg - start) / (unsigned)splits;
@@ -724,7 +780,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   float *ml = lds + NW * 16 * HD;                  // [NW or slots][16][2]
   float *top = ml + kAttendMl, *word = top + 32;
   static_assert(TERMS * KS * 64 * 8 * 2 <= NW * 16 * HD * 4, "the query's terms fit the waves' outputs");
-  static_assert(NW * 16 * 2 <= kAttendMl, "the waves' maxima fit the slots'");
+  static_assert(NW * 16 * 2 <= kAttendMl && kPlanScans * NW <= kAttendMl, "the waves' maxima and the plan fit the slots' weights");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
   const int runs = (a.group + 15) / 16, units = a.d.n_kv_heads * runs;
@@ -738,7 +794,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   const double turns = a.turns[p];  // 128 of them are allocated
 
   AttendWork w;
-  if (!plan_attend<TILE>(a, units, blockIdx.x, &w)) return;
+  if (!plan_attend<TILE>(a, units, blockIdx.x, (int *)ml, &w)) return;
   const int kvh = w.unit / runs, head0 = kvh * a.group + (w.unit - kvh * runs) * 16;
   const int rows = min(16, (kvh + 1) * a.group - head0);
   const int last = w.len - 1, mask = (1 << a.d.page_shift) - 1;

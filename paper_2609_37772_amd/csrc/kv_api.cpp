@@ -94,6 +94,10 @@ PagedDims dims_of(const uad_kv *kv) {
 size_t pool_esz(const uad_kv *kv) { return kv->cfg.dtype == UAD_DTYPE_F8 ? 1 : 2; }
 void *layer_of(const uad_kv *kv, void *pool, int layer) { return (char *)pool + layer * kv->layer_elems * pool_esz(kv); }
 
+// Row strides (elements) and tokens of a sequence: products with row numbers stay
+// within 64 bits, positions and the tiles behind the last one within 32.
+constexpr int64_t kMaxLd = (int64_t)1 << 30, kMaxTokens = (int64_t)1 << 30;
+
 bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
 // What append and attend check alike.
@@ -103,6 +107,8 @@ uad_status check_call(uad_kv *kv, const char *fn, int layer, int dtype, const vo
   if (dtype != UAD_DTYPE_F32 && dtype != UAD_DTYPE_BF16) return kv_fail(kv, UAD_E_INVALID, fn, "bad dtype");
   if (n_seqs < 0 || pages_per_seq < 1) return kv_fail(kv, UAD_E_INVALID, fn, "n_seqs must be >= 0, pages_per_seq >= 1");
   if (n_seqs > kv->cfg.max_seqs) return kv_fail(kv, UAD_E_SHAPE, fn, "n_seqs > max_seqs");
+  if ((int64_t)pages_per_seq * kv->cfg.page_size > kMaxTokens)
+    return kv_fail(kv, UAD_E_SHAPE, fn, "a page table of more than 2^30 tokens per sequence");
   if (n_seqs > 0 && (!a || !b || !lens || !table)) return kv_fail(kv, UAD_E_INVALID, fn, "null pointer");
   const size_t esz = dtype == UAD_DTYPE_F32 ? 4 : 2;
   if (!aligned(a, esz) || !aligned(b, esz)) return kv_fail(kv, UAD_E_INVALID, fn, "data not aligned to its type");
@@ -234,7 +240,8 @@ uad_status uad_kv_append(uad_kv *kv, int32_t layer, const void *k, const void *v
   if (st != UAD_OK) return st;
   if (n_rows < 0) return kv_fail(kv, UAD_E_INVALID, fn, "n_rows must be >= 0");
   const int64_t row = (int64_t)kv->cfg.n_kv_heads * kv->cfg.head_dim;
-  if (ldk < row || ldv < row) return kv_fail(kv, UAD_E_INVALID, fn, "ldk / ldv below n_kv_heads * head_dim");
+  if (ldk < row || ldv < row || ldk > kMaxLd || ldv > kMaxLd)
+    return kv_fail(kv, UAD_E_INVALID, fn, "ldk / ldv below n_kv_heads * head_dim or above 2^30");
   if (!row_start && n_rows != n_seqs) return kv_fail(kv, UAD_E_SHAPE, fn, "n_rows != n_seqs without row_start");
   if (none || n_seqs == 0) return UAD_OK;
   OnDevice on(kv->device);
@@ -262,8 +269,10 @@ uad_status uad_kv_attend(uad_kv *kv, int32_t layer, const void *q, void *out, in
   uad_status st = check_call(kv, fn, layer, dtype, q, out, lens, page_table, pages_per_seq, n_seqs);
   if (st != UAD_OK) return st;
   const int64_t row = (int64_t)kv->cfg.n_heads * kv->cfg.head_dim;
-  if (ldq < row || ldo < row) return kv_fail(kv, UAD_E_INVALID, fn, "ldq / ldo below n_heads * head_dim");
-  if (!std::isfinite(scale)) return kv_fail(kv, UAD_E_INVALID, fn, "scale must be finite");
+  if (ldq < row || ldo < row || ldq > kMaxLd || ldo > kMaxLd)
+    return kv_fail(kv, UAD_E_INVALID, fn, "ldq / ldo below n_heads * head_dim or above 2^30");
+  const float scale_log2 = (float)((double)scale * kv->cfg.k_scale * 1.4426950408889634);
+  if (!std::isfinite(scale_log2)) return kv_fail(kv, UAD_E_INVALID, fn, "scale must be finite, times k_scale too");
   if (n_seqs == 0) return UAD_OK;
   OnDevice on(kv->device);
   if (on.err() != hipSuccess) return kv_hip_fail(kv, on.err(), fn, "hipSetDevice");
@@ -275,7 +284,7 @@ uad_status uad_kv_attend(uad_kv *kv, int32_t layer, const void *q, void *out, in
   a.n_seqs = n_seqs; a.n_heads = kv->cfg.n_heads; a.group = kv->cfg.n_heads / kv->cfg.n_kv_heads;
   a.pages_per_seq = pages_per_seq;
   a.turns = kv->turns; a.rope_dim = kv->cfg.rope_dim; a.rope_pairs = kv->cfg.rope_pairs;
-  a.scale_log2 = (float)((double)scale * kv->cfg.k_scale * 1.4426950408889634);
+  a.scale_log2 = scale_log2;
   a.v_scale = kv->cfg.v_scale;
   a.status = kv->status;
   a.part = kv->part; a.part_ml = kv->part_ml; a.arrived = kv->arrived; a.slots = kv->slots;
@@ -294,8 +303,8 @@ uad_status uad_set_prefix_paged(uad_ctx *c, uad_kv *kv, const int32_t *lens, con
     return ctx_fail(c, UAD_E_INVALID, "batch and pages_per_seq must be >= 1, prefix_len >= 0");
   if (batch > c->cfg.max_batch) return ctx_fail(c, UAD_E_SHAPE, "batch > max_batch");
   if (prefix_len > c->cfg.max_prefix) return ctx_fail(c, UAD_E_SHAPE, "prefix_len > max_prefix");
-  if (prefix_len > (int64_t)pages_per_seq * kv->cfg.page_size)
-    return ctx_fail(c, UAD_E_SHAPE, "prefix_len beyond the page table");
+  if (prefix_len > (int64_t)pages_per_seq * kv->cfg.page_size || (int64_t)pages_per_seq * kv->cfg.page_size > kMaxTokens)
+    return ctx_fail(c, UAD_E_SHAPE, "prefix_len beyond the page table, or a table of more than 2^30 tokens per sequence");
   if (kv->device != c->device) return ctx_fail(c, UAD_E_SHAPE, "the cache is on another device");
   if (kv->cfg.n_layers != c->L || kv->cfg.n_kv_heads != c->Hkv || kv->cfg.head_dim != c->hd)
     return ctx_fail(c, UAD_E_SHAPE, "the cache has another number of layers or KV heads, or another head_dim");

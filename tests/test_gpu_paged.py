@@ -91,6 +91,8 @@ APPENDS = [
     (1, 256, 128, [1, 200, 64, 65], [127, 128, 64, 63], BF16, F8, 0, False),
     (1, 64, 32, [8, 8], [30, 31], BF16, BF16, 64, False),
     (1, 64, 32, [7, 8], [30, 31], BF16, BF16, 64, False),
+    (1, 64, 16, [9 if i % 3 else 0 for i in range(600)], [i % 40 for i in range(600)], BF16, BF16, 64, False),
+    (1, 64, 16, [17] * 70 + [0] * 200 + [400], [i % 40 for i in range(271)], BF16, F8, 64, False),
     (2, 64, 16, [5 + i % 17 for i in range(67)], [i * 13 % 37 for i in range(67)], BF16, F8, 64, False),
 ]
 
@@ -242,6 +244,9 @@ ATTENDS = [
     (5, 3, 64, 16, [0, 0, 0], BF16, F8, 64, False),
     (16, 1, 64, 16, [40] * 9, F32, BF16, 64, False),
     (1, 5, 256, 64, [20000], BF16, F8, 256, False),
+    (1, 1, 64, 16, [(i * 37) % 120 for i in range(700)], F32, BF16, 64, False),
+    (2, 1, 64, 16, [(i * 37) % 50 for i in range(1300)] + [3000], BF16, F8, 0, False),
+    (1, 2, 128, 32, [30] * 80 + [4000] + [1] * 20 + [0] * 30, BF16, BF16, 128, False),
 ]
 
 
@@ -520,6 +525,77 @@ def test_decoding_step_in_a_graph(gpu):
             assert torch.equal(lens, lens_ref)
         assert np.array_equal(bits(kv.k), bits(ref.k)) and np.array_equal(bits(kv.v), bits(ref.v))
         kv.synchronize(), ref.synchronize()
+
+
+def test_two_handles_at_once(gpu):
+    """Handles of their own on two streams share pools and run at the same time; every result is the one of a lone call."""
+    hkv, group, hd = 2, 4, 128
+    c = P.Cache(9, 2, hkv, hd, 16, [700, 90, 0, 1500], cache=BF16)
+    c.fill(4)
+    pools = dev(c.k), dev(c.v)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    table, lens = dev(c.table), dev(c.lens)
+    kvs = [U.PagedKV(2, hkv * group, hkv, hd, 16, c.n_pages, 4, rope_dim=hd, k=pools[0], v=pools[1], stream=s) for s in streams]
+    qs = [dev(draw(i, 4, hkv * group, hd)) for i in range(2)]
+    alone = [[kvs[i].attend(l, qs[i], table, lens) for l in range(2)] for i in range(2)]
+    for kv in kvs:
+        kv.synchronize()
+    for i in range(2):
+        check_attend(c, kvs[i], 1, qs[i].cpu(), alone[i][1], hd, False)
+    outs = [[torch.empty_like(qs[i]) for _ in range(40)] for i in range(2)]
+    torch.cuda.synchronize()
+    for n in range(40):
+        for i in range(2):
+            kvs[i].attend(n % 2, qs[i], table, lens, out=outs[i][n])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for n in range(40):
+            assert torch.equal(outs[i][n], alone[i][n % 2])
+
+
+def test_another_stream_and_a_closed_handle(gpu):
+    c = P.Cache(9, 1, 1, 64, 16, [300])
+    c.fill(4)
+    kv = handle(c, 4)
+    q, table, lens = dev(draw(1, 1, 4, 64)), dev(c.table), dev(c.lens)
+    want = kv.attend(0, q, table, lens)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    kv.set_stream(side)
+    with torch.cuda.stream(side):
+        out = torch.zeros_like(q)
+        kv.attend(0, q, table, lens, out=out)
+        got = out + 0  # ordered behind it on that stream
+    kv.synchronize()
+    assert torch.equal(got, want)
+    for _ in range(5):  # destroyed with work queued: waits for it
+        kv.attend(0, q, table, lens, out=out)
+    kv.close()
+    assert torch.equal(out, want)
+    with pytest.raises(U.UadError):
+        kv.attend(0, q, table, lens)
+    with pytest.raises(U.UadError):
+        kv.synchronize()
+
+
+def test_values_of_the_cache_that_are_not_finite(gpu):
+    """A NaN among a sequence's own keys and values makes its outputs NaN (an infinity may), and nobody else's."""
+    c = P.Cache(9, 1, 1, 64, 16, [100, 50, 70])
+    c.fill(4)
+    want = handle(c, 2).attend(0, dev(draw(1, 3, 2, 64)), dev(c.table), dev(c.lens))
+    for where, bad in (("k", math.nan), ("k", math.inf), ("v", math.nan)):
+        d = P.Cache(9, 1, 1, 64, 16, [100, 50, 70])
+        d.fill(4)
+        pg, off = d.slot(0, 57)
+        if where == "k":
+            d.k[0, pg, 0, off, 3] = bad
+        else:
+            d.v[0, pg, 0, :, off] = bad
+        kv = handle(d, 2)
+        got = kv.attend(0, dev(draw(1, 3, 2, 64)), dev(d.table), dev(d.lens))
+        kv.synchronize()
+        assert torch.equal(got[1:], want[1:])
+        assert bad == math.inf or bool(got[0].isnan().all())
 
 
 def test_empty_calls(gpu):

@@ -208,7 +208,7 @@ def attend(lib, h, **kw):
 @pytest.mark.parametrize("change,status", [
     (dict(layer=2), INVALID), (dict(layer=-1), INVALID), (dict(dtype=2), INVALID), (dict(dtype=-1), INVALID),
     (dict(pages=0), INVALID), (dict(n_seqs=-1), INVALID), (dict(n_seqs=5), SHAPE), (dict(lens=None), INVALID),
-    (dict(table=None), INVALID)])
+    (dict(table=None), INVALID), (dict(pages=2 ** 26 + 1), SHAPE), (dict(pages=2 ** 31 - 1), SHAPE)])
 def test_calls_refuse_alike(lib, kv, change, status):
     for call in (append, attend):
         assert call(lib, kv, **change) == status
@@ -218,13 +218,14 @@ def test_calls_refuse_alike(lib, kv, change, status):
 
 @pytest.mark.parametrize("change,status", [
     (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(ldk=127), INVALID), (dict(ldv=0), INVALID), (dict(n_rows=-1), INVALID),
-    (dict(row_start=None), SHAPE), (dict(k=X + 1), INVALID), (dict(dtype=0, v=X + 2), INVALID)])
+    (dict(ldk=2 ** 30 + 1), INVALID), (dict(ldv=2 ** 62), INVALID), (dict(row_start=None), SHAPE), (dict(k=X + 1), INVALID), (dict(dtype=0, v=X + 2), INVALID)])
 def test_append_refuses(lib, kv, change, status):
     assert append(lib, kv, **change) == status and lib.kv_stub_calls() == b""
 
 
 @pytest.mark.parametrize("change,status", [
     (dict(q=None), INVALID), (dict(out=None), INVALID), (dict(ldq=255), INVALID), (dict(ldo=-256), INVALID),
+    (dict(ldq=2 ** 30 + 1), INVALID), (dict(scale=3e38), INVALID),
     (dict(scale=float("inf")), INVALID), (dict(scale=float("nan")), INVALID), (dict(q=X + 1), INVALID), (dict(dtype=0, out=X + 2), INVALID)])
 def test_attend_refuses(lib, kv, change, status):
     assert attend(lib, kv, **change) == status and lib.kv_stub_calls() == b""
