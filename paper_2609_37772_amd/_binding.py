@@ -409,7 +409,6 @@ def uad_profile_read(ctx: int) -> Dict[str, Tuple[float, int]]:
 # ----------------------------------------------------------------------------
 # Paged K/V cache
 # ----------------------------------------------------------------------------
-# Decoding calls these once a token and layer: on good arguments they look at each tensor's properties once.
 _ROW_TYPES = {torch.float32: UAD_DTYPE_F32, torch.bfloat16: UAD_DTYPE_BF16}
 
 
@@ -418,24 +417,39 @@ def _check_kv(kv, st: int, what: str):
         raise UadError(st, f"{what}: {uad_kv_last_error(kv)}")
 
 
-def _rows(t: torch.Tensor, shape: Tuple[int, int], name: str, device: int) -> Tuple[int, int, int, int]:
-    """(pointer, uad dtype, elements between rows, rows) of a device tensor of rows [n][heads][head_dim], each dense."""
-    dt = _ROW_TYPES.get(getattr(t, "dtype", None))
-    if dt is None:
+def _row_step(t, shape: Tuple[int, int], name: str, device: int) -> int:
+    """Elements between the rows of a device tensor [n][heads][head_dim], each row dense; raises for any other."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _ROW_TYPES:
         raise ValueError(f"{name} must be a float32 or bfloat16 tensor, got {getattr(t, 'dtype', type(t))}")
-    size = t.shape
-    if size[1:] != shape or t.get_device() != device:
-        raise ValueError(f"{name} must be [rows][{shape[0]}][{shape[1]}] on device {device}, got {tuple(size)} on {t.device}")
-    n = size[0]
-    ld = shape[0] * shape[1]
-    if not t.is_contiguous():
-        row, head, inner = t.stride()
-        if n < 2:
-            row = ld  # the stride of a dimension of one says nothing
-        if inner != 1 or (head != shape[1] and shape[0] > 1) or row < ld:
-            raise ValueError(f"{name} must have dense rows that do not overlap, got strides {t.stride()}")
-        ld = row
-    return t.data_ptr(), dt, ld, n
+    if t.shape[1:] != shape or t.get_device() != device:
+        raise ValueError(f"{name} must be [rows][{shape[0]}][{shape[1]}] on device {device}, got {tuple(t.shape)} on {t.device}")
+    dense = shape[0] * shape[1]
+    if t.is_contiguous():
+        return dense
+    row, head, inner = t.stride()
+    if t.shape[0] < 2:
+        row = dense  # the stride of a dimension of one says nothing
+    if inner != 1 or (head != shape[1] and shape[0] > 1) or row < dense:
+        raise ValueError(f"{name} must have dense rows that do not overlap, got strides {t.stride()}")
+    return row
+
+
+def _row_steps(a, b, shape: Tuple[int, int], names: str, device: int) -> Tuple[int, int, int, int]:
+    """(rows, uad dtype, _row_step of a, of b) of two tensors of one type and size.  Decoding comes here once a token and
+    layer: dense ones, the usual case, are let through at the first look."""
+    try:
+        size, kind = a.shape, a.dtype
+        if a.is_contiguous() and b.is_contiguous() and b.dtype is kind and kind in _ROW_TYPES and a.get_device() == device \
+                and b.get_device() == device and size == b.shape:
+            n, heads, dim = size
+            if heads == shape[0] and dim == shape[1]:
+                return n, _ROW_TYPES[kind], heads * dim, heads * dim
+    except (AttributeError, ValueError):
+        pass
+    steps = tuple(_row_step(t, shape, n, device) for t, n in zip((a, b), names.split()))
+    if a.dtype != b.dtype or a.shape != b.shape:
+        raise ValueError(f"{names.replace(' ', ' and ')} must share dtype and rows")
+    return (a.shape[0], _ROW_TYPES[a.dtype], *steps)
 
 
 def _ints(t: torch.Tensor, shape: Tuple[int, ...], name: str, device: int) -> int:
@@ -446,10 +460,10 @@ def _ints(t: torch.Tensor, shape: Tuple[int, ...], name: str, device: int) -> in
 
 def _table(page_table: torch.Tensor, lens: torch.Tensor, device: int) -> Tuple[int, int, int, int]:
     """(page table, pages per sequence, lens, sequences) of a call."""
-    size = getattr(page_table, "shape", ())
-    if len(size) != 2:
-        raise ValueError("page_table must be an int32 device tensor [n_seqs][pages_per_seq]")
-    n, wide = size
+    try:
+        n, wide = size = page_table.shape
+    except (AttributeError, ValueError):
+        raise ValueError("page_table must be an int32 device tensor [n_seqs][pages_per_seq]") from None
     return _ints(page_table, size, "page_table", device), wide, _ints(lens, (n,), "lens", device), n
 
 
@@ -485,14 +499,12 @@ def uad_kv_append(kv: int, layer: int, k: torch.Tensor, v: torch.Tensor, page_ta
                   row_start: Optional[torch.Tensor], positions: Optional[torch.Tensor], row_shape: Tuple[int, int],
                   device: int = 0) -> None:
     """Append rows k, v [n_rows][Hkv][hd] (rows may be slices of wider ones) to a layer's pages."""
-    pk, dk, ldk, n = _rows(k, row_shape, "k", device)
-    pv, dv, ldv, nv = _rows(v, row_shape, "v", device)
-    if dk != dv or nv != n:
-        raise ValueError("k and v must share dtype and rows")
+    n, dtype, ldk, ldv = _row_steps(k, v, row_shape, "k v", device)
     pt, wide, pl, seqs = _table(page_table, lens, device)
     ps = None if row_start is None else _ints(row_start, (seqs + 1,), "row_start", device)
     pp = None if positions is None else _ints(positions, (n,), "positions", device)
-    st = (_lib or load_library()).uad_kv_append(kv, layer, pk, pv, dk, ldk, ldv, n, ps, pl, pp, pt, wide, seqs)
+    st = (_lib or load_library()).uad_kv_append(kv, layer, k.data_ptr(), v.data_ptr(), dtype, ldk, ldv, n, ps,
+                                                pl, pp, pt, wide, seqs)
     if st:
         _check_kv(kv, st, "uad_kv_append")
 
@@ -501,13 +513,13 @@ def uad_kv_attend(kv: int, layer: int, q: torch.Tensor, out: torch.Tensor, page_
                   lens: torch.Tensor, positions: Optional[torch.Tensor], scale: float, row_shape: Tuple[int, int],
                   device: int = 0) -> None:
     """Attention of q [n_seqs][Hq][hd], one token per sequence, over a layer's pages into out (q's type and shape)."""
+    n, dtype, ldq, ldo = _row_steps(q, out, row_shape, "q out", device)
     pt, wide, pl, seqs = _table(page_table, lens, device)
-    pq, dq, ldq, nq = _rows(q, row_shape, "q", device)
-    po, do, ldo, no = _rows(out, row_shape, "out", device)
-    if dq != do or nq != seqs or no != seqs:
-        raise ValueError("q and out must share dtype and have a row per sequence")
+    if n != seqs:
+        raise ValueError("q and out must have a row per sequence")
     pp = None if positions is None else _ints(positions, (seqs,), "positions", device)
-    st = (_lib or load_library()).uad_kv_attend(kv, layer, pq, po, dq, ldq, ldo, pl, pp, pt, wide, seqs, scale)
+    st = (_lib or load_library()).uad_kv_attend(kv, layer, q.data_ptr(), out.data_ptr(), dtype, ldq, ldo, pl, pp,
+                                                pt, wide, seqs, scale)
     if st:
         _check_kv(kv, st, "uad_kv_attend")
 

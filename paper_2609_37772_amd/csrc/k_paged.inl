@@ -39,19 +39,12 @@ __device__ __forceinline__ float cut_f8(float v) { return v > 448.f ? 448.f : v 
 __device__ __forceinline__ uint8_t to_f8(float v) {
   return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(cut_f8(v), 0.f, 0, false) & 0xFF);
 }
-__device__ __forceinline__ float from_f8(uint8_t b) { return __builtin_amdgcn_cvt_f32_fp8((int)b, 0); }
 
 template <bool F8>
 __device__ __forceinline__ void store_pool(void *p, size_t i, float v) {
   if constexpr (F8) ((uint8_t *)p)[i] = to_f8(v);
   else ((__bf16 *)p)[i] = (__bf16)v;
 }
-template <bool F8>
-__device__ __forceinline__ float load_pool(const void *p, size_t i) {
-  if constexpr (F8) return from_f8(((const uint8_t *)p)[i]);
-  else return __uint_as_float((uint32_t)((const uint16_t *)p)[i] << 16);
-}
-
 // Sine and cosine of `position` times a pair's turns: the whole turns go in 64 bits
 // (a position of 10^6 leaves 36 bits of the fraction), the rest in fp32 to the
 // instructions that take turns, off by at most 1.3e-7 within half a turn either way
@@ -121,7 +114,10 @@ __device__ __forceinline__ int sequence_of_row(const int32_t *row_start, int n_s
 }
 
 // ---------------------------------------------------------------------------
-// Append: one workgroup per new row.
+// Append of few rows: one workgroup per new row, a thread per pair of columns and as
+// many heads at once as there are threads.  Bound by the launch and three dependent
+// loads (length, page id, store): 2.7 us for a token of 1 x 256, 3.1 us for 64 tokens of
+// 2 x 128 in e4m3.
 // ---------------------------------------------------------------------------
 template <bool F32, bool F8>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
@@ -176,15 +172,14 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
 
 // ---------------------------------------------------------------------------
 // Append of many rows: one workgroup per tile (see paged.h), KV head, pool and up to 128
-// columns, so that
-// pages are written 16 bytes at a time: bound by memory, a row by itself would scatter
-// its values over a transposed page two bytes at a time.  K: a thread rotates 16
-// elements of a row, the pieces of 8 that are turned with each other.  V: through LDS,
-// whose 16-byte pieces are swizzled by the token's chunk, so that the lanes that read 8
-// (or 16) tokens of a column do not meet in a bank.  64 prompts of 816 rows, 1 x 256
-// bf16 (104 MB): 28.9 us, with non-temporal stores of the pages 19.3 us (5.4 TB/s; a
-// device copy of as much 22.4 us); the workgroups of a tile next to each other instead
-// of K's first and V's last: 24.7 us.
+// columns, so that pages are written 16 bytes at a time: bound by memory; a row by
+// itself would scatter its values over a transposed page two bytes at a time.  K: a
+// thread rotates 16 elements of a row, the pieces of 8 that are turned with each other.
+// V: through LDS, whose 16-byte pieces are swizzled by the token's chunk, so that the
+// lanes that read 8 (or 16) tokens of a column do not meet in a bank.  64 prompts of 816
+// rows, 1 x 256 bf16 (104 MB): 28.9 us, with non-temporal stores of the pages 19.3 us
+// (5.4 TB/s; a device copy of as much 22.4 us); the workgroups of a tile next to each
+// other instead of K's first and V's last: 24.7 us.  Row by row: 118 us.
 // ---------------------------------------------------------------------------
 // Columns of a workgroup: 128 of 256, so that its LDS and its share of the work allow
 // eight on a CU.
@@ -202,7 +197,7 @@ __device__ __forceinline__ bool plan_append(const KvAppendArgs &a, int wg, int *
   bool bad = false;
   // positions [from, to) and rows of a sequence; none where they cannot be used
   auto span = [&](int b, int *from, int *to, int *row) {
-    const int lo = a.row_start ? a.row_start[b] : b, hi = a.row_start ? a.row_start[b + 1] : b + 1;
+    const int lo = a.row_start[b], hi = a.row_start[b + 1];
     const int len = usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad);
     const bool ok = rows_ok(lo, hi, a.n_rows) && hi - lo <= len && (b > 0 || lo == 0);
     bad |= !ok;
@@ -400,7 +395,7 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvAppendArgs a) {
     }
     return;
   }
-  // V: tokens x HD in pool type, a token's 8-element piece p at place p ^ (token / RUN)
+  // V: tokens x WIDE in pool type, a token's 8-element piece p at place p ^ (token / RUN)
   constexpr int RUN = F8 ? 16 : 8;  // tokens of a 16-byte store
   const int lead = (t.first & mask) - tile_off;  // slots of the tile before the first row
   auto place = [&](int slot, int piece) { return (slot * PIECES + (piece ^ ((slot / RUN) & (PIECES - 1)))) * 8 * ESZ; };
@@ -478,7 +473,7 @@ template <bool F32, bool F8>
 static hipError_t launch_append_type(const KvAppendArgs &a, hipStream_t s) {
   constexpr int kMaxWgs = 1 << 23;  // work items of a grid stay below 2^32
   const int64_t tiles = append_grid(a.n_rows, a.n_seqs, append_tile_shift(a.d.page_shift));
-  if ((int64_t)a.n_seqs * kAppendTileRows <= a.n_rows && tiles <= kMaxWgs && a.d.n_kv_heads <= 65535) {
+  if (a.row_start && (int64_t)a.n_seqs * kAppendTileRows <= a.n_rows && tiles <= kMaxWgs && a.d.n_kv_heads <= 65535) {
     const dim3 grid((unsigned)tiles, a.d.n_kv_heads, a.d.head_dim > 128 ? 4 : 2), wg(256);
     if (a.d.head_dim == 64) hipLaunchKernelGGL((kv_append_tile_kernel<64, F32, F8>), grid, wg, 0, s, a);
     else if (a.d.head_dim == 128) hipLaunchKernelGGL((kv_append_tile_kernel<128, F32, F8>), grid, wg, 0, s, a);
@@ -524,9 +519,17 @@ hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_
 // kAttendWaves-th tile with running maxima and sums of their own and meet in LDS.  A
 // unit's splits meet in slots of the workspace: the last workgroup to arrive joins
 // them, in the order of the keys.
+//
+// One sequence of 131071 keys, 32/8 heads of 128 in bf16 (537 MB): 97 - 101 us, 5.3 -
+// 5.5 TB/s, where a kernel that only reads takes 85; 8 x 4001 keys of 16 x 64 (127 MB)
+// 29.5 - 31; 64 x 900 keys of 1 x 256 (58 MB) 20.5; 817 keys of 1 x 256 11.5 us, of
+// which the launch, the plan, the meeting in LDS and the join take about 8.  More splits
+// than workgroups run at once cost their prologues (twice as many: 109, 37 and 27 us).
 // ---------------------------------------------------------------------------
-constexpr int kAttendMinTiles = 4;  // tiles of a split, where a unit has as many
-
+// Tiles of a split, where a unit has as many.  817 keys of 1 x 256 (26 tiles): 4 tiles
+// 11.9 us, 2 tiles 12.3 (more to join), 8 tiles 14.2 (a CU takes in 26 bytes a clock of
+// these loads).
+constexpr int kAttendMinTiles = 4;
 constexpr int kAttendWaves = 8;
 // Workgroups per CU: the tiles in flight, the outputs and their operands take a wave up
 // to 256 registers at head dim 256 (two waves per SIMD) and 160 at 128; for 128, three
