@@ -104,13 +104,20 @@ struct PlanScan {
 constexpr int kPlanScans = 4 + kShareTries;  // of one plan at most
 
 // The sequence of a new row: how many of row_start[0 .. n_seqs] are at most r, minus
-// one.  Called by whole waves; r is the same in all lanes.
+// one; with more than 64, of every 64th first.  Called by whole waves; r is the same in
+// all lanes.
 __device__ __forceinline__ int sequence_of_row(const int32_t *row_start, int n_seqs, int r) {
   const int lane = threadIdx.x & 63;
-  int n = 0;
-  for (int i0 = 0; i0 <= n_seqs; i0 += 64)
-    n += __popcll(__ballot(i0 + lane <= n_seqs && row_start[min(i0 + lane, n_seqs)] <= r));
-  return n - 1;
+  int base = 0;
+  if (n_seqs >= 64) {
+    int n = 0;
+    for (int i0 = 0; i0 <= n_seqs; i0 += 64 * 64) {
+      const int i = i0 + 64 * lane;
+      n += __popcll(__ballot(i <= n_seqs && row_start[min(i, n_seqs)] <= r));
+    }
+    base = 64 * max(n - 1, 0);
+  }
+  return base + __popcll(__ballot(base + lane <= n_seqs && row_start[min(base + lane, n_seqs)] <= r)) - 1;
 }
 
 // ---------------------------------------------------------------------------
@@ -132,7 +139,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
       lo = a.row_start[b];
       hi = a.row_start[b + 1];
     }
-    bad = b < 0 || lo < 0 || hi > a.n_rows || r >= hi;
+    bad = b < 0 || !rows_ok(lo, hi, a.n_rows) || r < lo || r >= hi;
     j = r - lo;
     n_b = hi - lo;
   }

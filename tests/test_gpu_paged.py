@@ -93,6 +93,7 @@ APPENDS = [
     (1, 64, 32, [7, 8], [30, 31], BF16, BF16, 64, False),
     (1, 64, 16, [9 if i % 3 else 0 for i in range(600)], [i % 40 for i in range(600)], BF16, BF16, 64, False),
     (1, 64, 16, [17] * 70 + [0] * 200 + [400], [i % 40 for i in range(271)], BF16, F8, 64, False),
+    (1, 64, 16, [2 if i % 7 == 0 else i % 2 for i in range(4200)], [0] * 4200, BF16, BF16, 64, False),
     (2, 64, 16, [5 + i % 17 for i in range(67)], [i * 13 % 37 for i in range(67)], BF16, F8, 64, False),
 ]
 
