@@ -69,11 +69,13 @@ class uad_kv_config(ctypes.Structure):
 
 
 _lib: Optional[ctypes.CDLL] = None
+_marshal = None               # the checks of decoding's calls in C (csrc/marshal.c), and the entry points' addresses
+_append_at = _attend_at = 0
 
 
 def load_library() -> ctypes.CDLL:
     """Load libuad.so (built by ``python -m paper_2609_37772_amd.build``); raise if absent."""
-    global _lib
+    global _lib, _marshal, _append_at, _attend_at
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -112,7 +114,13 @@ def load_library() -> ctypes.CDLL:
         fn = getattr(lib, name)
         fn.argtypes = args
         fn.restype = res
-    _lib = lib
+    try:
+        from . import _marshal as marshal
+    except ImportError as e:
+        raise RuntimeError(f"{os.path.dirname(LIB_PATH)}/_marshal.so: {e}; run `python -m paper_2609_37772_amd.build`") from e
+    marshal.setup(torch.Tensor, torch.float32, torch.bfloat16, torch.int32)
+    _append_at, _attend_at = (ctypes.cast(f, ctypes.c_void_p).value for f in (lib.uad_kv_append, lib.uad_kv_attend))
+    _marshal, _lib = marshal, lib
     return lib
 
 
@@ -435,17 +443,7 @@ def _row_step(t, shape: Tuple[int, int], name: str, device: int) -> int:
 
 
 def _row_steps(a, b, shape: Tuple[int, int], names: str, device: int) -> Tuple[int, int, int, int]:
-    """(rows, uad dtype, _row_step of a, of b) of two tensors of one type and size.  Decoding comes here once a token and
-    layer: dense ones, the usual case, are let through at the first look."""
-    try:
-        size, kind = a.shape, a.dtype
-        if a.is_contiguous() and b.is_contiguous() and b.dtype is kind and kind in _ROW_TYPES and a.get_device() == device \
-                and b.get_device() == device and size == b.shape:
-            n, heads, dim = size
-            if heads == shape[0] and dim == shape[1]:
-                return n, _ROW_TYPES[kind], heads * dim, heads * dim
-    except (AttributeError, ValueError):
-        pass
+    """(rows, uad dtype, _row_step of a, of b) of two tensors of one type and size."""
     steps = tuple(_row_step(t, shape, n, device) for t, n in zip((a, b), names.split()))
     if a.dtype != b.dtype or a.shape != b.shape:
         raise ValueError(f"{names.replace(' ', ' and ')} must share dtype and rows")
@@ -499,29 +497,43 @@ def uad_kv_append(kv: int, layer: int, k: torch.Tensor, v: torch.Tensor, page_ta
                   row_start: Optional[torch.Tensor], positions: Optional[torch.Tensor], row_shape: Tuple[int, int],
                   device: int = 0) -> None:
     """Append rows k, v [n_rows][Hkv][hd] (rows may be slices of wider ones) to a layer's pages."""
+    if _marshal is None:
+        load_library()
+    st = _marshal.append(_append_at, kv, layer, k, v, page_table, lens, row_start, positions, *row_shape, device)
+    if st is None:  # not the usual case
+        st = _append_checked(kv, layer, k, v, page_table, lens, row_start, positions, row_shape, device)
+    if st:
+        _check_kv(kv, st, "uad_kv_append")
+
+
+def _append_checked(kv, layer, k, v, page_table, lens, row_start, positions, row_shape, device) -> int:
     n, dtype, ldk, ldv = _row_steps(k, v, row_shape, "k v", device)
     pt, wide, pl, seqs = _table(page_table, lens, device)
     ps = None if row_start is None else _ints(row_start, (seqs + 1,), "row_start", device)
     pp = None if positions is None else _ints(positions, (n,), "positions", device)
-    st = (_lib or load_library()).uad_kv_append(kv, layer, k.data_ptr(), v.data_ptr(), dtype, ldk, ldv, n, ps,
-                                                pl, pp, pt, wide, seqs)
-    if st:
-        _check_kv(kv, st, "uad_kv_append")
+    return load_library().uad_kv_append(kv, layer, k.data_ptr(), v.data_ptr(), dtype, ldk, ldv, n, ps, pl, pp, pt, wide, seqs)
 
 
 def uad_kv_attend(kv: int, layer: int, q: torch.Tensor, out: torch.Tensor, page_table: torch.Tensor,
                   lens: torch.Tensor, positions: Optional[torch.Tensor], scale: float, row_shape: Tuple[int, int],
                   device: int = 0) -> None:
     """Attention of q [n_seqs][Hq][hd], one token per sequence, over a layer's pages into out (q's type and shape)."""
+    if _marshal is None:
+        load_library()
+    st = _marshal.attend(_attend_at, kv, layer, q, out, page_table, lens, positions, scale, *row_shape, device)
+    if st is None:  # not the usual case
+        st = _attend_checked(kv, layer, q, out, page_table, lens, positions, scale, row_shape, device)
+    if st:
+        _check_kv(kv, st, "uad_kv_attend")
+
+
+def _attend_checked(kv, layer, q, out, page_table, lens, positions, scale, row_shape, device) -> int:
     n, dtype, ldq, ldo = _row_steps(q, out, row_shape, "q out", device)
     pt, wide, pl, seqs = _table(page_table, lens, device)
     if n != seqs:
         raise ValueError("q and out must have a row per sequence")
     pp = None if positions is None else _ints(positions, (seqs,), "positions", device)
-    st = (_lib or load_library()).uad_kv_attend(kv, layer, q.data_ptr(), out.data_ptr(), dtype, ldq, ldo, pl, pp,
-                                                pt, wide, seqs, scale)
-    if st:
-        _check_kv(kv, st, "uad_kv_attend")
+    return load_library().uad_kv_attend(kv, layer, q.data_ptr(), out.data_ptr(), dtype, ldq, ldo, pl, pp, pt, wide, seqs, scale)
 
 
 def uad_kv_synchronize(kv: int) -> None:

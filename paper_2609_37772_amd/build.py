@@ -3,7 +3,8 @@
     python -m paper_2609_37772_amd.build [--jobs N] [--debug]
 
 Compiles every translation unit under csrc/ with hipcc for gfx950 and links
-them into paper_2609_37772_amd/libuad.so.  Always recompiles (no caching), so
+them into paper_2609_37772_amd/libuad.so, and the binding's argument checks
+(csrc/marshal.c, host C) into _marshal.so.  Always recompiles (no caching), so
 a call after any source change is enough to refresh the library.
 """
 from __future__ import annotations
@@ -14,11 +15,13 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libuad.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -44,12 +47,23 @@ def _compile(src: str, extra) -> str:
     return obj
 
 
+def _compile_marshal() -> None:
+    cmd = [os.environ.get("CC", "gcc"), "-O2", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"],
+           os.path.join(CSRC, "marshal.c"), "-o", MARSHAL + ".tmp"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    os.replace(MARSHAL + ".tmp", MARSHAL)
+
+
 def build(jobs: int = 8, debug: bool = False, verbose: bool = True) -> str:
     os.makedirs(BUILD, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "*.cpp")))
     extra = ["-g"] if debug else []
     with cf.ThreadPoolExecutor(max_workers=max(1, jobs)) as ex:
+        marshal = ex.submit(_compile_marshal)
         objs = list(ex.map(lambda s: _compile(s, extra), srcs))
+        marshal.result()
     tmp = LIB + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-mcode-object-version=5", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
