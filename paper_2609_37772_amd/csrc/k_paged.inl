@@ -577,8 +577,18 @@ struct AttendWork {
 // The plan (see paged.h).
 template <int TILE>
 __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, int wg, int *lds, AttendWork *w) {
-  PlanScan<kAttendWaves> scan(a.n_seqs, lds);
   bool bad = false;
+  if (a.unsplit) {  // the page table holds too few keys for a split: a workgroup per unit
+    *w = AttendWork{};
+    w->b = (unsigned)wg / (unsigned)units;
+    w->unit = wg - w->b * units;
+    w->len = usable_length(a.lens[w->b], a.pages_per_seq, a.d.page_shift, &bad);
+    w->t1 = tiles_of_length(w->len, TILE);
+    w->splits = 1;
+    if (bad && threadIdx.x == 0) raise_status(a.status, kStatusPage);
+    return true;
+  }
+  PlanScan<kAttendWaves> scan(a.n_seqs, lds);
   auto length = [&](int b) { return usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad); };
   // f(length) over this thread's sequences, of which the first is kept
   int my_len = 0;
@@ -593,9 +603,9 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
   each([&](int len) { n += tiles_of_length(len, TILE); });
   if (bad && wg == 0) raise_status(a.status, kStatusPage);
   n *= units;
-  int hi, lo;
-  scan((int)(n >> 22), &hi);
-  scan((int)(n & 0x3FFFFF), &lo);
+  int hi = 0, lo;
+  if (!a.few_tiles) scan((int)(n >> 22), &hi);
+  scan((int)(a.few_tiles ? n : n & 0x3FFFFF), &lo);
   int share = first_share(((int64_t)hi << 22) + lo, a.target, kAttendMinTiles);
   int mine, upto, wgs;
   auto count = [&]() {  // workgroups of this thread's sequences, and up to them
@@ -1076,13 +1086,15 @@ hipError_t kv_attend_init(int head_dim) {
 }
 
 template <int HD, bool F32, bool F8>
-static hipError_t launch_attend_type(const KvAttendArgs &a, hipStream_t s) {
+static hipError_t launch_attend_type(KvAttendArgs a, hipStream_t s) {
   const int64_t units = (int64_t)a.n_seqs * a.d.n_kv_heads * ((a.group + 15) / 16);
   // the plan's workgroups: one for each unit, more where units are split, which are no
   // more than the slots, nor than the page table gives tiles
   const int64_t tiles = tiles_of_length((int)std::min<int64_t>((int64_t)a.pages_per_seq << a.d.page_shift, 0x7FFFFFFF), kTileKeys<F8>);
   const int64_t splits = splits_of((int)tiles, kAttendMinTiles);
   const int64_t grid = std::min(units * splits, units + a.slots);
+  a.unsplit = splits == 1;
+  a.few_tiles = tiles < ((int64_t)1 << 31) / units;
   hipLaunchKernelGGL((kv_attend_kernel<HD, F32, F8>), dim3((unsigned)grid), dim3(64 * kAttendWaves), attend_lds_floats<HD>() * 4,
                      s, a);
   return hipGetLastError();

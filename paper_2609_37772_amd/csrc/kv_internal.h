@@ -49,6 +49,9 @@ struct KvAttendArgs {
   int slots;
   int target;             // workgroups that run at once
   bool out_vec;           // four outputs can be stored at once
+  // set by the launcher:
+  bool unsplit;           // no sequence can have more tiles than a split takes
+  bool few_tiles;         // all tiles count in 32 bits
 };
 
 // The expert's prefix from the pages (stores as in PrefixArgs).

@@ -88,7 +88,7 @@ UAD_HD bool rows_ok(int from, int to, int n_rows) { return from >= 0 && from <= 
 constexpr int kMaxSplits = 512;   // of a unit
 constexpr int kJoinFan = 16;      // splits that one workgroup joins; above 2 * kJoinFan of them in two levels
 
-UAD_HD int tiles_of_length(int len, int tile) { return len > tile ? (int)(((int64_t)len + tile - 1) / tile) : 1; }
+UAD_HD int tiles_of_length(int len, int tile) { return len > tile ? (int)(((uint32_t)len + tile - 1) / tile) : 1; }
 
 // Tiles of a workgroup for `total` tiles on `target` workgroups that run at once.
 UAD_HD int first_share(int64_t total, int target, int min_tiles) {
@@ -106,7 +106,10 @@ UAD_HD int splits_of(int tiles, int share) {
   return s < kMaxSplits ? s : kMaxSplits;
 }
 // First tile of split s of n (and, for s + 1, the end of s).
-UAD_HD int split_begin(int tiles, int n, int s) { return (int)((int64_t)tiles * s / n); }
+UAD_HD int split_begin(int tiles, int n, int s) {
+  const int each = (int)((uint32_t)tiles / (uint32_t)n), more = tiles - each * n;
+  return each * s + (s < more ? s : more);
+}
 
 // Workgroups in units that are split: a unit of more than `share` tiles has fewer than
 // twice tiles / share, and total / share is at most `target`.
