@@ -588,48 +588,76 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
     if (bad && threadIdx.x == 0) raise_status(a.status, kStatusPage);
     return true;
   }
-  PlanScan<kAttendWaves> scan(a.n_seqs, lds);
   auto length = [&](int b) { return usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad); };
-  // f(length) over this thread's sequences, of which the first is kept
-  int my_len = 0;
-  const int b0 = scan.me * scan.per;
-  if (b0 < a.n_seqs) my_len = length(b0);
-  auto each = [&](auto f) {
-    if (b0 < a.n_seqs) f(my_len);
-    for (int i = 1; i < scan.per; ++i)
-      if (b0 + i < a.n_seqs) f(length(b0 + i));
-  };
-  int64_t n = 0;
-  each([&](int len) { n += tiles_of_length(len, TILE); });
-  if (bad && wg == 0) raise_status(a.status, kStatusPage);
-  n *= units;
-  int hi = 0, lo;
-  if (!a.few_tiles) scan((int)(n >> 22), &hi);
-  scan((int)(a.few_tiles ? n : n & 0x3FFFFF), &lo);
-  int share = first_share(((int64_t)hi << 22) + lo, a.target, kAttendMinTiles);
-  int mine, upto, wgs;
-  auto count = [&]() {  // workgroups of this thread's sequences, and up to them
-    mine = 0;
-    each([&](int len) { mine += splits_of(tiles_of_length(len, TILE), share) * units; });
-    upto = scan(mine, &wgs);
-  };
-  count();
-  if ((int64_t)a.n_seqs * units < a.target)
-    for (int i = 0; i < kShareTries && wgs > a.target; ++i) {
+  const bool spare = (int64_t)a.n_seqs * units < a.target;  // fewer units than run at once
+  int start, slot, b, tiles, splits;
+  if (a.n_seqs <= 64) {  // each wave for itself, a sequence per lane
+    const int lane = threadIdx.x & 63;
+    const bool have = lane < a.n_seqs;
+    const int len = have ? length(lane) : 0;
+    if (bad && wg == 0) raise_status(a.status, kStatusPage);
+    const int my_tiles = have ? tiles_of_length(len, TILE) : 0;
+    int64_t total;
+    if (a.few_tiles) {
+      total = last_lane(scan_wave64(my_tiles * units));
+    } else {
+      const int64_t n = (int64_t)my_tiles * units;
+      total = ((int64_t)last_lane(scan_wave64((int)(n >> 22))) << 22) + last_lane(scan_wave64((int)(n & 0x3FFFFF)));
+    }
+    int share = first_share(total, a.target, kAttendMinTiles);
+    int my_splits = have ? splits_of(my_tiles, share) : 0, upto = scan_wave64(my_splits * units);
+    for (int i = 0; spare && i < kShareTries && last_lane(upto) > a.target; ++i) {
+      share = next_share(share);
+      my_splits = have ? splits_of(my_tiles, share) : 0;
+      upto = scan_wave64(my_splits * units);
+    }
+    if (wg >= last_lane(upto)) return false;
+    const int mine = my_splits * units, in_slots = my_splits > 1 ? mine : 0, slot_upto = scan_wave64(in_slots);
+    b = __builtin_ctzll(__ballot(upto > wg));
+    start = __builtin_amdgcn_readlane(upto - mine, b);
+    slot = __builtin_amdgcn_readlane(slot_upto - in_slots, b);
+    tiles = __builtin_amdgcn_readlane(my_tiles, b);
+    splits = __builtin_amdgcn_readlane(my_splits, b);
+    w->len = __builtin_amdgcn_readlane(len, b);
+  } else {
+    PlanScan<kAttendWaves> scan(a.n_seqs, lds);
+    // f(length) over this thread's sequences, of which the first is kept
+    const int b0 = scan.me * scan.per;
+    const int my_len = b0 < a.n_seqs ? length(b0) : 0;
+    auto each = [&](auto f) {
+      if (b0 < a.n_seqs) f(my_len);
+      for (int i = 1; i < scan.per; ++i)
+        if (b0 + i < a.n_seqs) f(length(b0 + i));
+    };
+    int64_t n = 0;
+    each([&](int len) { n += tiles_of_length(len, TILE); });
+    if (bad && wg == 0) raise_status(a.status, kStatusPage);
+    n *= units;
+    int hi, lo, mine, upto, wgs, all;
+    scan((int)(n >> 22), &hi);
+    scan((int)(n & 0x3FFFFF), &lo);
+    int share = first_share(((int64_t)hi << 22) + lo, a.target, kAttendMinTiles);
+    auto count = [&]() {  // workgroups of this thread's sequences, and up to them
+      mine = 0;
+      each([&](int len) { mine += splits_of(tiles_of_length(len, TILE), share) * units; });
+      upto = scan(mine, &wgs);
+    };
+    count();
+    for (int i = 0; spare && i < kShareTries && wgs > a.target; ++i) {
       share = next_share(share);
       count();
     }
-  if (wg >= wgs) return false;
-  int in_slots = 0, all;  // workgroups in split units, for the slots
-  each([&](int len) {
-    const int s = splits_of(tiles_of_length(len, TILE), share);
-    if (s > 1) in_slots += s * units;
-  });
-  const int slot_upto = scan(in_slots, &all);
-  int start = upto - mine, slot = slot_upto - in_slots, b, len;
-  if (scan.block) {
+    if (wg >= wgs) return false;
+    int in_slots = 0;  // workgroups in split units, for the slots
+    each([&](int len) {
+      const int s = splits_of(tiles_of_length(len, TILE), share);
+      if (s > 1) in_slots += s * units;
+    });
+    const int slot_upto = scan(in_slots, &all);
+    start = upto - mine;
     if (upto > wg && start <= wg) {  // one thread: it looks for the sequence among its own
-      len = my_len;
+      int len = my_len;
+      slot = slot_upto - in_slots;
       for (b = b0;;) {
         const int s = splits_of(tiles_of_length(len, TILE), share);
         if (start + s * units > wg) break;
@@ -644,27 +672,22 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
     }
     __syncthreads();
     b = __builtin_amdgcn_readfirstlane(scan.lds[0]);
-    len = __builtin_amdgcn_readfirstlane(scan.lds[1]);
+    w->len = __builtin_amdgcn_readfirstlane(scan.lds[1]);
     start = __builtin_amdgcn_readfirstlane(scan.lds[2]);
     slot = __builtin_amdgcn_readfirstlane(scan.lds[3]);
     if (b >= a.n_seqs) return false;  // only if the lengths change while this runs
-  } else {
-    b = __builtin_ctzll(__ballot(upto > wg));
-    start = __builtin_amdgcn_readlane(start, b);
-    slot = __builtin_amdgcn_readlane(slot, b);
-    len = __builtin_amdgcn_readlane(my_len, b);
+    tiles = tiles_of_length(w->len, TILE);
+    splits = splits_of(tiles, share);
   }
-  const int tiles = tiles_of_length(len, TILE), splits = splits_of(tiles, share);
   w->b = b;
-  w->len = len;
-  w->unit = (unsigned)(wg - start) / (unsigned)splits;
+  w->splits = splits;
+  w->unit = splits == 1 ? wg - start : (unsigned)(wg - start) / (unsigned)splits;
   if (w->unit >= units) return false;  // likewise
   w->split = wg - start - w->unit * splits;
-  w->splits = splits;
   w->slot = slot + w->unit * splits;
   if (splits > 1 && w->slot + splits > a.slots) return false;  // likewise
-  w->t0 = split_begin(tiles, splits, w->split);
-  w->t1 = split_begin(tiles, splits, w->split + 1);
+  w->t0 = splits == 1 ? 0 : split_begin(tiles, splits, w->split);
+  w->t1 = splits == 1 ? tiles : split_begin(tiles, splits, w->split + 1);
   return true;
 }
 
