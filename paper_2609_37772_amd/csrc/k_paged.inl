@@ -533,10 +533,16 @@ hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_
 // which the launch, the plan, the meeting in LDS and the join take about 8.  More splits
 // than workgroups run at once cost their prologues (twice as many: 109, 37 and 27 us).
 // ---------------------------------------------------------------------------
-// Tiles of a split, where a unit has as many.  817 keys of 1 x 256 (26 tiles): 4 tiles
-// 11.9 us, 2 tiles 12.3 (more to join), 8 tiles 14.2 (a CU takes in 26 bytes a clock of
-// these loads).
+// Tiles of a split, where a unit has as many: fewer leave more to join, more keep a CU
+// reading, which takes in 26 bytes a clock of these loads (26 tiles of 1 x 256: 2 tiles
+// 12.3 us, 4 tiles 11.9, 8 tiles 14.2; 24 tiles of 2 x 128: 4 tiles 8.8, 8 tiles 10.4).
 constexpr int kAttendMinTiles = 4;
+// Tiles up to which a unit stays whole, where reading it and joining it cost the same
+// (one sequence, whole / split): head dim 256, 8 tiles 11.0 / 11.2 us, 10 tiles 12.0 /
+// 11.2; 128, 12 tiles 8.5 / 8.7, 16 tiles 9.6 / 8.8; 64, 20 tiles 7.5 / 7.8, 24 tiles
+// 8.2 / 7.8.
+template <int HD>
+constexpr int kAttendWhole = HD == 256 ? 8 : HD == 128 ? 12 : 20;
 constexpr int kAttendWaves = 8;
 // Workgroups per CU: the tiles in flight, the outputs and their operands take a wave up
 // to 256 registers at head dim 256 (two waves per SIMD) and 160 at 128; for 128, three
@@ -575,7 +581,7 @@ struct AttendWork {
 };
 
 // The plan (see paged.h).
-template <int TILE>
+template <int HD, int TILE>
 __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, int wg, int *lds, AttendWork *w) {
   bool bad = false;
   if (a.unsplit) {  // the page table holds too few keys for a split: a workgroup per unit
@@ -605,10 +611,10 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
       total = ((int64_t)last_lane(scan_wave64((int)(n >> 22))) << 22) + last_lane(scan_wave64((int)(n & 0x3FFFFF)));
     }
     int share = first_share(total, a.target, kAttendMinTiles);
-    int my_splits = have ? splits_of(my_tiles, share) : 0, upto = scan_wave64(my_splits * units);
+    int my_splits = have ? splits_of(my_tiles, share, kAttendWhole<HD>) : 0, upto = scan_wave64(my_splits * units);
     for (int i = 0; spare && i < kShareTries && last_lane(upto) > a.target; ++i) {
       share = next_share(share);
-      my_splits = have ? splits_of(my_tiles, share) : 0;
+      my_splits = have ? splits_of(my_tiles, share, kAttendWhole<HD>) : 0;
       upto = scan_wave64(my_splits * units);
     }
     if (wg >= last_lane(upto)) return false;
@@ -639,7 +645,7 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
     int share = first_share(((int64_t)hi << 22) + lo, a.target, kAttendMinTiles);
     auto count = [&]() {  // workgroups of this thread's sequences, and up to them
       mine = 0;
-      each([&](int len) { mine += splits_of(tiles_of_length(len, TILE), share) * units; });
+      each([&](int len) { mine += splits_of(tiles_of_length(len, TILE), share, kAttendWhole<HD>) * units; });
       upto = scan(mine, &wgs);
     };
     count();
@@ -650,7 +656,7 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
     if (wg >= wgs) return false;
     int in_slots = 0;  // workgroups in split units, for the slots
     each([&](int len) {
-      const int s = splits_of(tiles_of_length(len, TILE), share);
+      const int s = splits_of(tiles_of_length(len, TILE), share, kAttendWhole<HD>);
       if (s > 1) in_slots += s * units;
     });
     const int slot_upto = scan(in_slots, &all);
@@ -659,7 +665,7 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
       int len = my_len;
       slot = slot_upto - in_slots;
       for (b = b0;;) {
-        const int s = splits_of(tiles_of_length(len, TILE), share);
+        const int s = splits_of(tiles_of_length(len, TILE), share, kAttendWhole<HD>);
         if (start + s * units > wg) break;
         start += s * units;
         if (s > 1) slot += s * units;
@@ -677,7 +683,7 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
     slot = __builtin_amdgcn_readfirstlane(scan.lds[3]);
     if (b >= a.n_seqs) return false;  // only if the lengths change while this runs
     tiles = tiles_of_length(w->len, TILE);
-    splits = splits_of(tiles, share);
+    splits = splits_of(tiles, share, kAttendWhole<HD>);
   }
   w->b = b;
   w->splits = splits;
@@ -837,7 +843,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   const double turns = a.turns[p];  // 128 of them are allocated
 
   AttendWork w;
-  if (!plan_attend<TILE>(a, units, blockIdx.x, (int *)ml, &w)) return;
+  if (!plan_attend<HD, TILE>(a, units, blockIdx.x, (int *)ml, &w)) return;
   const int kvh = w.unit / runs, head0 = kvh * a.group + (w.unit - kvh * runs) * 16;
   const int rows = min(16, (kvh + 1) * a.group - head0);
   const int last = w.len - 1, mask = (1 << a.d.page_shift) - 1;
@@ -1114,7 +1120,7 @@ static hipError_t launch_attend_type(KvAttendArgs a, hipStream_t s) {
   // the plan's workgroups: one for each unit, more where units are split, which are no
   // more than the slots, nor than the page table gives tiles
   const int64_t tiles = tiles_of_length((int)std::min<int64_t>((int64_t)a.pages_per_seq << a.d.page_shift, 0x7FFFFFFF), kTileKeys<F8>);
-  const int64_t splits = splits_of((int)tiles, kAttendMinTiles);
+  const int64_t splits = splits_of((int)tiles, kAttendMinTiles, kAttendWhole<HD>);
   const int64_t grid = std::min(units * splits, units + a.slots);
   a.unsplit = splits == 1;
   a.few_tiles = tiles < ((int64_t)1 << 31) / units;

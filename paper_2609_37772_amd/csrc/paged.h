@@ -81,9 +81,10 @@ UAD_HD bool rows_ok(int from, int to, int n_rows) { return from >= 0 && from <= 
 // ---------------------------------------------------------------------------
 // The attention's work.  Unit u of sequence b is a KV head with up to 16 of its query
 // heads, read in tiles of `tile` keys; a sequence without keys counts one tile, so that
-// somebody writes its zeros.  Every unit of a sequence is cut into the same number of
-// splits of at most `share` tiles, one workgroup each.  The lengths are known on the
-// device alone, and every workgroup works the plan out for itself.
+// somebody writes its zeros.  Every unit of a sequence of more than `whole` tiles is cut
+// into the same number of splits of at most `share` tiles, one workgroup each; up to
+// `whole` the join would cost more than the shorter read gains.  The lengths are known
+// on the device alone, and every workgroup works the plan out for itself.
 // ---------------------------------------------------------------------------
 constexpr int kMaxSplits = 512;   // of a unit
 constexpr int kJoinFan = 16;      // splits that one workgroup joins; above 2 * kJoinFan of them in two levels
@@ -101,7 +102,8 @@ UAD_HD int first_share(int64_t total, int target, int min_tiles) {
 constexpr int kShareTries = 6;
 UAD_HD int next_share(int share) { return share + (share >> 4) + 1; }
 
-UAD_HD int splits_of(int tiles, int share) {
+UAD_HD int splits_of(int tiles, int share, int whole) {
+  if (tiles <= whole) return 1;
   const int s = (int)(((uint32_t)tiles + (uint32_t)share - 1) / (uint32_t)share);
   return s < kMaxSplits ? s : kMaxSplits;
 }
@@ -112,7 +114,7 @@ UAD_HD int split_begin(int tiles, int n, int s) {
 }
 
 // Workgroups in units that are split: a unit of more than `share` tiles has fewer than
-// twice tiles / share, and total / share is at most `target`.
+// twice tiles / share of them, and total / share is at most `target`.
 UAD_HD int max_slots(int target) { return 2 * target; }
 
 }  // namespace uad

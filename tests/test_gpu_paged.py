@@ -246,6 +246,10 @@ ATTENDS = [
     (16, 1, 64, 16, [40] * 9, F32, BF16, 64, False),
     (1, 5, 256, 64, [20000], BF16, F8, 256, False),
     (1, 1, 64, 16, [(i * 37) % 120 for i in range(700)], F32, BF16, 64, False),
+    (2, 6, 128, 32, [5000, 900, 64, 0, 1281], BF16, F8, 128, False),
+    (2, 4, 64, 16, [3000, 1, 700, 640, 641], F32, BF16, 64, True),
+    (1, 3, 256, 128, [256, 257, 2100, 0], F32, F8, 0, False),
+    (3, 20, 128, 16, [1500, 384, 385], BF16, BF16, 64, True),
     (2, 1, 64, 16, [(i * 37) % 50 for i in range(1300)] + [3000], BF16, F8, 0, False),
     (1, 2, 128, 32, [30] * 80 + [4000] + [1] * 20 + [0] * 30, BF16, BF16, 128, False),
 ]

@@ -298,7 +298,7 @@ extern "C" {
 int tiles_of(int len, int tile) { return tiles_of_length(len, tile); }
 int share_of(long long total, int target, int least) { return first_share(total, target, least); }
 int larger(int share) { return next_share(share); }
-int splits(int tiles, int share) { return splits_of(tiles, share); }
+int splits(int tiles, int share, int whole) { return splits_of(tiles, share, whole); }
 int begin(int tiles, int n, int s) { return split_begin(tiles, n, s); }
 int slots(int target) { return max_slots(target); }
 int tries() { return kShareTries; }
@@ -323,17 +323,17 @@ def plan(tmp_path_factory):
     return lib
 
 
-def plan_of(lib, lens, units, tile, target, least=4):
+def plan_of(lib, lens, units, tile, target, least=4, whole=4):
     tiles = [lib.tiles_of(n, tile) for n in lens]
     total = sum(tiles) * units
     share = lib.share_of(total, target, least)
-    count = lambda: sum(lib.splits(t, share) * units for t in tiles)  # noqa: E731
+    count = lambda: sum(lib.splits(t, share, whole) * units for t in tiles)  # noqa: E731
     if len(lens) * units < target:
         for _ in range(lib.tries()):
             if count() <= target:
                 break
             share = lib.larger(share)
-    return tiles, share, [lib.splits(t, share) for t in tiles]
+    return tiles, share, [lib.splits(t, share, whole) for t in tiles]
 
 
 def test_plan_covers_every_tile_within_the_slots_and_the_grid(plan):
@@ -343,16 +343,18 @@ def test_plan_covers_every_tile_within_the_slots_and_the_grid(plan):
         tile, pages, shift = int(r.choice([32, 64])), int(2 ** r.uniform(0, 14)), int(r.integers(4, 9))
         cap = min(pages << shift, 2 ** 31 - 1)
         lens = [int(x) for x in np.minimum(2 ** r.uniform(0, r.choice([3, 12, 22, 31]), n) - 1, cap)]
-        tiles, share, splits = plan_of(plan, lens, units, tile, target)
+        whole = int(r.choice([1, 4, 8, 12, 20]))
+        tiles, share, splits = plan_of(plan, lens, units, tile, target, whole=whole)
         wgs, slots = sum(splits) * units, sum(s * units for s in splits if s > 1)
         assert slots <= plan.slots(target) and max(splits) <= plan.most() and -(-max(splits) // plan.fan()) <= 2 * plan.fan()
         # the launch: as many workgroups as the lengths could need
-        most = plan.splits(plan.tiles_of(cap, tile), 4)
+        most = plan.splits(plan.tiles_of(cap, tile), 4, whole)
         assert wgs <= min(n * units * most, n * units + plan.slots(target))
         for t, s in zip(tiles, splits):
             ends = [plan.begin(t, s, i) for i in range(s + 1)]
             assert ends[0] == 0 and ends[-1] == t and all(b > a for a, b in zip(ends, ends[1:]))
-            assert s == plan.most() or max(b - a for a, b in zip(ends, ends[1:])) <= share
+            assert s == plan.most() or max(b - a for a, b in zip(ends, ends[1:])) <= max(share, whole)
+            assert t > whole or s == 1
 
 
 def test_plan_fills_the_workgroups_that_run_at_once(plan):
