@@ -93,6 +93,9 @@ APPENDS = [
     (1, 64, 32, [7, 8], [30, 31], BF16, BF16, 64, False),
     (1, 64, 16, [9 if i % 3 else 0 for i in range(600)], [i % 40 for i in range(600)], BF16, BF16, 64, False),
     (1, 64, 16, [17] * 70 + [0] * 200 + [400], [i % 40 for i in range(271)], BF16, F8, 64, False),
+    (1, 256, 64, [70, 9], [3, 60], BF16, BF16, 160, False),
+    (1, 256, 64, [70, 9], [3, 60], F32, F8, 48, True),
+    (2, 128, 32, [3, 1], [30, 31], BF16, F8, 48, False),
     (1, 64, 16, [2 if i % 7 == 0 else i % 2 for i in range(4200)], [0] * 4200, BF16, BF16, 64, False),
     (2, 64, 16, [5 + i % 17 for i in range(67)], [i * 13 % 37 for i in range(67)], BF16, F8, 64, False),
 ]
@@ -143,14 +146,15 @@ def test_append_strides_and_padding_rows(gpu, given, cache, hd, page, form):
     check_append(c, kv, 0, k, v, new, after, starts, hd, False)
 
 
-def test_append_positions(gpu):
+@pytest.mark.parametrize("second", [40, 2])  # by tiles and row by row
+def test_append_positions(gpu, second):
     """Rotation positions of the caller's, far ones and negative ones among them; base 500000."""
-    hkv, hd, page, new = 1, 128, 32, [5, 40]
+    hkv, hd, page, new = 1, 128, 32, [5, second]
     c = P.Cache(8, 1, hkv, hd, page, new)
     kv = handle(c, hkv, rope=128, theta=500000.0)
-    starts = np.array([0, 5, 45], np.int32)
-    positions = np.concatenate([[0, 1, -3, 2 ** 31 - 1, -2 ** 31], 1000003 * np.arange(40) + 7]).astype(np.int32)
-    k, v = draw(1, 45, hkv, hd), draw(2, 45, hkv, hd)
+    starts = np.array([0, 5, 5 + second], np.int32)
+    positions = np.concatenate([[0, 1, -3, 2 ** 31 - 1, -2 ** 31], 1000003 * np.arange(second) + 7]).astype(np.int32)
+    k, v = draw(1, 5 + second, hkv, hd), draw(2, 5 + second, hkv, hd)
     kv.append(0, dev(k), dev(v), dev(c.table), dev(c.lens), dev(starts), dev(positions))
     kv.synchronize()
     check_append(c, kv, 0, k, v, new, new, starts, 128, False, positions, 500000.0)
@@ -601,6 +605,53 @@ def test_values_of_the_cache_that_are_not_finite(gpu):
         kv.synchronize()
         assert torch.equal(got[1:], want[1:])
         assert bad == math.inf or bool(got[0].isnan().all())
+
+
+def test_prompt_and_prefix_in_a_graph(gpu):
+    """A new prompt into the pages and the expert's prefix from them, captured once and replayed with other rows, lengths
+    and tables; the steps between the replays are those of the same values handed over densely."""
+    shape = W.ModelShape(2, 128, 4, 2, 64, 256, 7)
+    wl = dataclasses.replace(W.get_workload("tiny"), shape=shape, batch=2, chunk=3, prefix=40)
+    side = torch.cuda.Stream()
+    ex = U.ActionExpert(shape, 2, 3, 40, stream=side)
+    ref = U.ActionExpert(shape, 2, 3, 40)
+    try:
+        ex.load_weights(W.make_weights(wl)), ref.load_weights(W.make_weights(wl))
+        c = P.Cache(3, 2, 2, 64, 16, [50, 41])
+        x0 = np.stack([W.make_noise(wl, b) for b in range(2)])
+        t, dt, mask = (dev(np.full((2, 3), f, d)) for f, d in ((0.5, np.float32), (-0.1, np.float32), (0, np.uint8)))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            kv = handle(c, 2, rope=64, stream=side)
+            table, lens, starts = dev(c.table), dev(c.lens), dev(np.array([0, 50, 91], np.int32))
+            rows = torch.zeros((2, 2, 91, 2, 64), dtype=BF16, device="cuda")
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                for l in range(2):
+                    kv.append(l, rows[0, l], rows[1, l], table, lens, starts)
+                ex.set_prefix_paged(kv, table, lens, 40)
+            for n in range(3):
+                rows.copy_(dev(draw(n, 2, 2, 91, 2, 64).to(BF16)))
+                table.copy_(dev(np.where(c.table >= 0, np.roll(np.arange(c.n_pages), n)[np.maximum(c.table, 0)], -1).astype(np.int32)))
+                graph.replay()
+                x, vel = dev(x0), torch.empty((2, 3, 7), device="cuda")
+                ex.step(x, t, dt, mask, vel)
+                ex.synchronize(), kv.synchronize()
+                d = P.Cache(3, 2, 2, 64, 16, [50, 41])
+                d.k, d.v, d.table = kv.k.cpu(), kv.v.cpu(), table.cpu().numpy()
+                dense = [np.stack([np.stack([d.tokens(l, b, 40)[j] for b in range(2)]) for l in range(2)]).astype(np.float32) for j in range(2)]
+                # what the pages hold is what was appended
+                ek, size = P.rotate(rows[0, 1, 50:90].double().cpu().numpy(), range(40), 64, False)
+                assert np.all(np.abs(dense[0][1, 1] - ek) <= P.append_bound(ek, size, 1.0, BF16))
+                ref.set_prefix_kv(dense[0], dense[1], 2, 40)
+                y, want = dev(x0), torch.empty((2, 3, 7), device="cuda")
+                torch.cuda.synchronize()
+                ref.step(y, t, dt, mask, want)
+                ref.synchronize()
+                assert torch.equal(vel, want) and torch.equal(x, y)
+    finally:
+        ex.close(), ref.close()
 
 
 def test_empty_calls(gpu):
