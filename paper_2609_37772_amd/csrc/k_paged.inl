@@ -529,20 +529,22 @@ hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_
 //
 // One sequence of 131071 keys, 32/8 heads of 128 in bf16 (537 MB): 97 - 101 us, 5.3 -
 // 5.5 TB/s, where a kernel that only reads takes 85; 8 x 4001 keys of 16 x 64 (127 MB)
-// 29.5 - 31; 64 x 900 keys of 1 x 256 (58 MB) 20.5; 817 keys of 1 x 256 11.5 us, of
-// which the launch, the plan, the meeting in LDS and the join take about 8.  More splits
-// than workgroups run at once cost their prologues (twice as many: 109, 37 and 27 us).
+// 29 - 31; 64 x 900 keys of 1 x 256 (58 MB) 20; 817 keys of 1 x 256 11.3 us, of which
+// the launch, the plan, the meeting in LDS and the join take about 7.  More splits than
+// workgroups run at once cost their prologues (twice as many: 109, 37 and 27 us).
 // ---------------------------------------------------------------------------
 // Tiles of a split, where a unit has as many: fewer leave more to join, more keep a CU
-// reading, which takes in 26 bytes a clock of these loads (26 tiles of 1 x 256: 2 tiles
-// 12.3 us, 4 tiles 11.9, 8 tiles 14.2; 24 tiles of 2 x 128: 4 tiles 8.8, 8 tiles 10.4).
+// reading, which takes in 15 to 26 bytes a clock of these loads (26 tiles of 1 x 256: 2
+// tiles 12.3 us, 4 tiles 11.9, 8 tiles 14.2; 24 tiles of 2 x 128: 4 tiles 8.8, 8 tiles
+// 10.4).
 constexpr int kAttendMinTiles = 4;
 // Tiles up to which a unit stays whole, where reading it and joining it cost the same
 // (one sequence, whole / split): head dim 256, 8 tiles 11.0 / 11.2 us, 10 tiles 12.0 /
 // 11.2; 128, 12 tiles 8.5 / 8.7, 16 tiles 9.6 / 8.8; 64, 20 tiles 7.5 / 7.8, 24 tiles
-// 8.2 / 7.8.
-template <int HD>
-constexpr int kAttendWhole = HD == 256 ? 8 : HD == 128 ? 12 : 20;
+// 8.2 / 7.8.  E4m3, whose tiles take longer to widen: 256, 6 tiles 11.7 / 11.7; 128, 8
+// tiles 8.6 / 9.3, 10 tiles 9.5 / 9.2; 64, 12 tiles 7.0 / 7.9, 16 tiles 8.1 / 8.1.
+template <int HD, bool F8>
+constexpr int kAttendWhole = (HD == 256 ? 8 : HD == 128 ? 12 : 20) * (F8 ? 3 : 4) / 4;
 constexpr int kAttendWaves = 8;
 // Workgroups per CU: the tiles in flight, the outputs and their operands take a wave up
 // to 256 registers at head dim 256 (two waves per SIMD) and 160 at 128; for 128, three
@@ -554,8 +556,10 @@ constexpr int kAttendPerCu = HD == 64 ? 2 : 1;
 template <bool F8>
 constexpr int kTileKeys = F8 ? 64 : 32;  // keys of 16-byte V^T loads by the four lane groups
 
+// 8 bf16 of a 16-byte load (u: which half of an 8-bit one); e4m3 widens exactly, its
+// scale goes into the scores' and the outputs'.
 template <bool F8>
-__device__ __forceinline__ bf16x8 operand_of(u32x4_t r, int u) {  // 8 bf16 of a 16-byte load (u: which half, 8-bit)
+__device__ __forceinline__ bf16x8 operand_of(u32x4_t r, int u) {
   union {
     bf16x8 v;
     bf16x2 p[4];
@@ -581,8 +585,9 @@ struct AttendWork {
 };
 
 // The plan (see paged.h).
-template <int HD, int TILE>
+template <int HD, bool F8>
 __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, int wg, int *lds, AttendWork *w) {
+  constexpr int TILE = kTileKeys<F8>;
   bool bad = false;
   if (a.unsplit) {  // the page table holds too few keys for a split: a workgroup per unit
     *w = AttendWork{};
@@ -611,10 +616,10 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
       total = ((int64_t)last_lane(scan_wave64((int)(n >> 22))) << 22) + last_lane(scan_wave64((int)(n & 0x3FFFFF)));
     }
     int share = first_share(total, a.target, kAttendMinTiles);
-    int my_splits = have ? splits_of(my_tiles, share, kAttendWhole<HD>) : 0, upto = scan_wave64(my_splits * units);
+    int my_splits = have ? splits_of(my_tiles, share, kAttendWhole<HD, F8>) : 0, upto = scan_wave64(my_splits * units);
     for (int i = 0; spare && i < kShareTries && last_lane(upto) > a.target; ++i) {
       share = next_share(share);
-      my_splits = have ? splits_of(my_tiles, share, kAttendWhole<HD>) : 0;
+      my_splits = have ? splits_of(my_tiles, share, kAttendWhole<HD, F8>) : 0;
       upto = scan_wave64(my_splits * units);
     }
     if (wg >= last_lane(upto)) return false;
@@ -645,7 +650,7 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
     int share = first_share(((int64_t)hi << 22) + lo, a.target, kAttendMinTiles);
     auto count = [&]() {  // workgroups of this thread's sequences, and up to them
       mine = 0;
-      each([&](int len) { mine += splits_of(tiles_of_length(len, TILE), share, kAttendWhole<HD>) * units; });
+      each([&](int len) { mine += splits_of(tiles_of_length(len, TILE), share, kAttendWhole<HD, F8>) * units; });
       upto = scan(mine, &wgs);
     };
     count();
@@ -656,7 +661,7 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
     if (wg >= wgs) return false;
     int in_slots = 0;  // workgroups in split units, for the slots
     each([&](int len) {
-      const int s = splits_of(tiles_of_length(len, TILE), share, kAttendWhole<HD>);
+      const int s = splits_of(tiles_of_length(len, TILE), share, kAttendWhole<HD, F8>);
       if (s > 1) in_slots += s * units;
     });
     const int slot_upto = scan(in_slots, &all);
@@ -665,7 +670,7 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
       int len = my_len;
       slot = slot_upto - in_slots;
       for (b = b0;;) {
-        const int s = splits_of(tiles_of_length(len, TILE), share, kAttendWhole<HD>);
+        const int s = splits_of(tiles_of_length(len, TILE), share, kAttendWhole<HD, F8>);
         if (start + s * units > wg) break;
         start += s * units;
         if (s > 1) slot += s * units;
@@ -683,7 +688,7 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
     slot = __builtin_amdgcn_readfirstlane(scan.lds[3]);
     if (b >= a.n_seqs) return false;  // only if the lengths change while this runs
     tiles = tiles_of_length(w->len, TILE);
-    splits = splits_of(tiles, share, kAttendWhole<HD>);
+    splits = splits_of(tiles, share, kAttendWhole<HD, F8>);
   }
   w->b = b;
   w->splits = splits;
@@ -843,7 +848,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   const double turns = a.turns[p];  // 128 of them are allocated
 
   AttendWork w;
-  if (!plan_attend<HD, TILE>(a, units, blockIdx.x, (int *)ml, &w)) return;
+  if (!plan_attend<HD, F8>(a, units, blockIdx.x, (int *)ml, &w)) return;
   const int kvh = w.unit / runs, head0 = kvh * a.group + (w.unit - kvh * runs) * 16;
   const int rows = min(16, (kvh + 1) * a.group - head0);
   const int last = w.len - 1, mask = (1 << a.d.page_shift) - 1;
@@ -1120,7 +1125,7 @@ static hipError_t launch_attend_type(KvAttendArgs a, hipStream_t s) {
   // the plan's workgroups: one for each unit, more where units are split, which are no
   // more than the slots, nor than the page table gives tiles
   const int64_t tiles = tiles_of_length((int)std::min<int64_t>((int64_t)a.pages_per_seq << a.d.page_shift, 0x7FFFFFFF), kTileKeys<F8>);
-  const int64_t splits = splits_of((int)tiles, kAttendMinTiles, kAttendWhole<HD>);
+  const int64_t splits = splits_of((int)tiles, kAttendMinTiles, kAttendWhole<HD, F8>);
   const int64_t grid = std::min(units * splits, units + a.slots);
   a.unsplit = splits == 1;
   a.few_tiles = tiles < ((int64_t)1 << 31) / units;
