@@ -726,13 +726,15 @@ __device__ __forceinline__ uint64_t pair_of(float m, float l) {
   return (uint64_t)__float_as_uint(m) | ((uint64_t)__float_as_uint(l) << 32);
 }
 
-// LDS of the attention: the query's bf16 terms while the keys are read, then the waves'
-// outputs; behind them the waves' maxima and sums (later the slots' weights), the joint
-// ones and a word.
+// LDS of the attention: the query's bf16 terms, the waves' outputs, their maxima and sums
+// (before that the plan, later the slots' weights), the joint ones and a word; 158 of a
+// CU's 160 KB at head dim 256 with fp32 queries.
 constexpr int kAttendMl = 2 * kJoinFan * 16;  // floats
-template <int HD>
+template <int HD, bool F32>
+constexpr int kQueryFloats = (F32 ? 3 : 2) * HD / 32 * 256;
+template <int HD, bool F32>
 constexpr int attend_lds_floats() {
-  return kAttendWaves * 16 * HD + kAttendMl + 16 * 2 + 4;
+  return kQueryFloats<HD, F32> + kAttendWaves * 16 * HD + kAttendMl + 16 * 2 + 4;
 }
 
 // The last of `n` workgroups to get here carries on; all of this workgroup's slot
@@ -830,10 +832,10 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   constexpr int ESZ = F8 ? 1 : 2;
   extern __shared__ __align__(16) float lds[];
   __bf16 *qf = (__bf16 *)lds;                      // [TERMS][KS][64][8]
-  f32x4 *obuf = (f32x4 *)lds;                      // [NW][NTO][64]
-  float *ml = lds + NW * 16 * HD;                  // [NW or slots][16][2]
+  f32x4 *obuf = (f32x4 *)(lds + kQueryFloats<HD, F32>);  // [NW][NTO][64]
+  float *ml = (float *)(obuf + NW * NTO * 64);     // [NW or slots][16][2]
   float *top = ml + kAttendMl, *word = top + 32;
-  static_assert(TERMS * KS * 64 * 8 * 2 <= NW * 16 * HD * 4, "the query's terms fit the waves' outputs");
+  static_assert(TERMS * KS * 64 * 8 * 2 == kQueryFloats<HD, F32> * 4, "the query's terms");
   static_assert(NW * 16 * 2 <= kAttendMl && kPlanScans * NW <= kAttendMl, "the waves' maxima and the plan fit the slots' weights");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
@@ -1026,28 +1028,28 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   }
   if (bad) raise_status(a.status, kStatusPage);
 
-  // The waves meet: maxima and sums, then outputs in units of the common maximum, of
-  // half the waves where no others had a tile.
+  // The waves meet: maxima, sums and outputs, each in units of its wave's maximum, of half
+  // the waves where no others had a tile. The readers weigh them, so that one barrier does;
+  // with a common unit agreed on first, in the query's place, calls took 0.1-0.3 us longer.
+  const bool all = t1 - w.t0 > NW / 2;
   l = sum_pair32(sum_pair16(l));
   if (g == 0) {
     ml[(wave * 16 + c) * 2] = m;
     ml[(wave * 16 + c) * 2 + 1] = l;
   }
-  __syncthreads();  // also: every wave is past its last read of the query
-  const bool all = t1 - w.t0 > NW / 2;
-  float mx = -INFINITY, sum = 0.f;
+  if (c < rows && (all || wave < NW / 2))
+#pragma unroll
+    for (int n = 0; n < NTO; ++n) obuf[(wave * NTO + n) * 64 + lane] = o[n];
+  __syncthreads();
+  float mx = -INFINITY, sum = 0.f, f[NW];
 #pragma unroll
   for (int i = 0; i < NW; ++i) mx = fmaxf(mx, ml[(i * 16 + c) * 2]);
 #pragma unroll
   for (int i = 0; i < NW; ++i) {
     const float li = ml[(i * 16 + c) * 2 + 1];
-    sum += li != 0.f ? li * __builtin_amdgcn_exp2f(ml[(i * 16 + c) * 2] - mx) : 0.f;
+    f[i] = li != 0.f ? __builtin_amdgcn_exp2f(ml[(i * 16 + c) * 2] - mx) : 0.f;
+    sum += li * f[i];
   }
-  const float f = l != 0.f ? __builtin_amdgcn_exp2f(m - mx) : 0.f;
-  if (c < rows && (all || wave < NW / 2))
-#pragma unroll
-    for (int n = 0; n < NTO; ++n) obuf[(wave * NTO + n) * 64 + lane] = o[n] * f;
-  __syncthreads();
   const bool vec = a.out_vec;
   auto put_out = [&](int row, int col, f32x4 v, float total) {
     const float scale = total != 0.f ? a.v_scale / total : 0.f;
@@ -1065,12 +1067,12 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   const auto slots = slots_of(a, rows_max * HD);
   if (c < rows) {
     for (int n = wave; n < NTO; n += NW) {
-      f32x4 v = obuf[n * 64 + lane];
+      f32x4 v = obuf[n * 64 + lane] * f[0];
 #pragma unroll
-      for (int i = 1; i < NW / 2; ++i) v += obuf[(i * NTO + n) * 64 + lane];
+      for (int i = 1; i < NW / 2; ++i) v += obuf[(i * NTO + n) * 64 + lane] * f[i];
       if (all)
 #pragma unroll
-        for (int i = NW / 2; i < NW; ++i) v += obuf[(i * NTO + n) * 64 + lane];
+        for (int i = NW / 2; i < NW; ++i) v += obuf[(i * NTO + n) * 64 + lane] * f[i];
       if (w.splits == 1) put_out(c, 16 * n + 4 * g, v, sum);
       else put_slot(slots, (slot * rows_max + c) * HD + 16 * n + 4 * g, v);
     }
@@ -1105,7 +1107,7 @@ int kv_attend_target(int n_cu, int head_dim) {
 template <int HD, bool F32, bool F8>
 static hipError_t attend_attr() {
   return hipFuncSetAttribute((const void *)kv_attend_kernel<HD, F32, F8>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                             attend_lds_floats<HD>() * 4);
+                             attend_lds_floats<HD, F32>() * 4);
 }
 template <int HD>
 static hipError_t attend_attrs() {
@@ -1129,8 +1131,8 @@ static hipError_t launch_attend_type(KvAttendArgs a, hipStream_t s) {
   const int64_t grid = std::min(units * splits, units + a.slots);
   a.unsplit = splits == 1;
   a.few_tiles = tiles < ((int64_t)1 << 31) / units;
-  hipLaunchKernelGGL((kv_attend_kernel<HD, F32, F8>), dim3((unsigned)grid), dim3(64 * kAttendWaves), attend_lds_floats<HD>() * 4,
-                     s, a);
+  hipLaunchKernelGGL((kv_attend_kernel<HD, F32, F8>), dim3((unsigned)grid), dim3(64 * kAttendWaves),
+                     (attend_lds_floats<HD, F32>() * 4), s, a);
   return hipGetLastError();
 }
 
