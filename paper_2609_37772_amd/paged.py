@@ -15,7 +15,8 @@ class PagedKV:
     """The paged K/V cache of a vision-language model on one GPU (see the uad_kv entry points in include/uad.h).
 
     ``k`` [n_layers][n_pages][n_kv_heads][page_size][head_dim] and ``v`` (pages transposed:
-    [n_layers][n_pages][n_kv_heads][head_dim][page_size]) are allocated when not given.
+    [n_layers][n_pages][n_kv_heads][head_dim][page_size]) are allocated when not given.  Work goes to ``stream`` (the
+    current one when not given), which tensors that a call allocates belong to.
     """
 
     def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int,
@@ -34,10 +35,13 @@ class PagedKV:
         pools = []
         for name, pool, shape in zip("kv", (k, v), shapes):
             if pool is None:
-                pool = torch.empty(shape, dtype=dtype, device=torch.device("cuda", device))
+                stream = stream or torch.cuda.current_stream(device)
+                with torch.cuda.stream(stream):
+                    pool = torch.empty(shape, dtype=dtype, device=torch.device("cuda", device))
             B._dev_ptr(pool, dtype, shape, name, device)
             pools.append(pool)
         self.k, self.v = pools
+        self._stream = stream = stream or torch.cuda.current_stream(device)
         self.handle = B.uad_kv_create(
             n_layers, n_heads, n_kv_heads, head_dim, page_size, n_pages, max_seqs, _POOL_TYPES[dtype], rope_dim,
             int(rope_pairs), rope_theta, k_scale, v_scale, self.k, self.v, device, stream)
@@ -60,13 +64,15 @@ class PagedKV:
     def attend(self, layer: int, q, page_table, lens, out=None, positions=None, scale: Optional[float] = None):
         """Attention of one token per sequence; see uad_kv_attend.  Allocates ``out`` when not given and returns it."""
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            with torch.cuda.stream(self._stream):  # memory that another stream's queued work still uses is not taken
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         B.uad_kv_attend(self.handle, layer, q, out, page_table, lens, positions, self._scale if scale is None else scale,
                         self._q_row, self.device)
         return out
 
     def set_stream(self, stream: Optional[torch.cuda.Stream]) -> None:
         B.uad_kv_set_stream(self.handle, stream)
+        self._stream = stream or torch.cuda.default_stream(self.device)
 
     def synchronize(self) -> None:
         B.uad_kv_synchronize(self.handle)

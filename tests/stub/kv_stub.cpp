@@ -1,6 +1,7 @@
 // What the paged cache's host code needs beside hip_stub.cpp: the current device, and
 // launchers that note what they were given.
 #include <cstdio>
+#include <cstring>
 #include <string>
 
 #include "../../paper_2609_37772_amd/csrc/kv_internal.h"
@@ -20,6 +21,7 @@ void kv_stub_ctx_status(uad_ctx *c, unsigned w) { *c->status = w; }
 int kv_stub_events() { return g_events; }
 int kv_stub_prefix_set(const uad_ctx *c) { return c->prefix_set ? c->prefix_len : -1; }
 hipError_t hipGetDevice(int *d) { *d = g_current; return hipSuccess; }
+hipError_t hipMemsetAsync(void *p, int v, size_t n, hipStream_t) { std::memset(p, v, n); return hipSuccess; }
 hipError_t kv_set_device(int d) { g_current = d; return hipSuccess; }
 }  // extern "C"
 

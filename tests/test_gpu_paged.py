@@ -562,6 +562,43 @@ def test_two_handles_at_once(gpu):
             assert torch.equal(outs[i][n], alone[i][n % 2])
 
 
+def test_what_a_call_allocates_is_its_streams(gpu):
+    """Freed memory that another stream's queued work may still use is not taken for pools and outputs."""
+    c = P.Cache(9, 1, 1, 64, 16, [300])
+    c.fill(4)
+    side = torch.cuda.Stream()
+    q, table, lens, k, v = dev(draw(1, 1, 4, 64)), dev(c.table), dev(c.lens), dev(c.k), dev(c.v)
+    want = handle(c, 4).attend(0, q, table, lens)
+    torch.cuda.synchronize()
+    olds = [torch.empty_like(x) for x in (q, k, v)]
+    used = {x.data_ptr() for x in olds}
+    del olds
+    kv = U.PagedKV(1, 4, 1, 64, 16, c.n_pages, 1, dtype=c.dtype, k_scale=c.scales[0], v_scale=c.scales[1], stream=side)
+    with torch.cuda.stream(side):
+        kv.k.copy_(k), kv.v.copy_(v)
+    out = kv.attend(0, q, table, lens)
+    assert not used & {out.data_ptr(), kv.k.data_ptr(), kv.v.data_ptr()}
+    kv.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_status_is_reported_once_each_time(gpu):
+    """Clearing the status does not clear what work queued right after it raises."""
+    c = P.Cache(9, 1, 1, 64, 16, [40])
+    c.fill(4)
+    side = torch.cuda.Stream()
+    kv = handle(c, 4, stream=side)
+    q, bad, lens = dev(draw(1, 1, 4, 64)), dev(np.full_like(c.table, -1)), dev(c.lens)
+    out = torch.empty_like(q)
+    torch.cuda.synchronize()
+    for _ in range(50):
+        kv.attend(0, q, bad, lens, out=out)
+        with pytest.raises(U.UadError) as e:
+            kv.synchronize()
+        assert e.value.status == 9
+    kv.synchronize()
+
+
 def test_another_stream_and_a_closed_handle(gpu):
     c = P.Cache(9, 1, 1, 64, 16, [300])
     c.fill(4)
