@@ -323,9 +323,10 @@ uad_status uad_aal(const double *release, int32_t n, double t_act, double *aal_o
  * once and hands the same array to uad_kv_append and uad_kv_attend of every
  * layer.  The device checks what it reads there: a page id outside 0..n_pages-1,
  * a length below 0, beyond the table or below the sequence's new rows, and a
- * row_start that does not rise within 0..n_rows raise UAD_E_PAGE, reported by
- * uad_kv_synchronize; such an entry touches no memory, and the results of that
- * work are invalid.  Pages may be shared between sequences for reading; two
+ * row_start that does not rise from 0 within 0..n_rows raise UAD_E_PAGE, reported
+ * by uad_kv_synchronize, whichever sequence it is and whether rows go there or
+ * not.  Nothing is written for a sequence with such a length or start, nor to a
+ * page with such an id, and the results of that work are invalid.  Pages may be shared between sequences for reading; two
  * tokens of one call that go to the same slot leave either's value there.
  *
  * Rotation.  With rope_dim > 0, elements (i, i + rope_dim/2) of a head, or
@@ -386,7 +387,8 @@ uad_status uad_kv_set_stream(uad_kv *kv, void *hip_stream);
  *   row_start   int32 [n_seqs + 1], rising from 0: rows row_start[b] ..
  *               row_start[b+1]-1 are sequence b's new tokens in order (none is
  *               fine), and rows from row_start[n_seqs] on are ignored; NULL: one
- *               row per sequence (n_rows == n_seqs)
+ *               row per sequence (n_rows == n_seqs).  With n_rows 0 nothing is
+ *               enqueued, so nothing is looked at either
  *   positions   int32 [n_rows] rotation positions, or NULL: the cache positions.
  *               Row j of sequence b's n new rows takes cache position
  *               lens[b] - n + j.

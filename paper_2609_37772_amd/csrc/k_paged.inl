@@ -132,6 +132,11 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
   int b = r, j = 0, n_b = 1;
   bool bad = false;
   if (a.row_start) {
+    // every sequence is looked at, those too in which no row lands
+    bool odd = false;
+    for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < (unsigned)a.n_seqs; i += gridDim.x * 256)
+      odd |= !sequence_ok(i, a.row_start[i], a.row_start[i + 1], a.n_rows, a.lens[i], a.pages_per_seq, a.d.page_shift);
+    if (odd) raise_status(a.status, kStatusPage);
     b = sequence_of_row(a.row_start, a.n_seqs, r);
     if (b >= a.n_seqs) return;  // a row behind the last sequence
     int lo = 0, hi = 0;
@@ -139,14 +144,14 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
       lo = a.row_start[b];
       hi = a.row_start[b + 1];
     }
-    bad = b < 0 || !rows_ok(lo, hi, a.n_rows) || r < lo || r >= hi;
+    bad = b < 0 || r < lo || r >= hi;
     j = r - lo;
     n_b = hi - lo;
+    if (!bad) bad = !sequence_ok(b, lo, hi, a.n_rows, a.lens[b], a.pages_per_seq, a.d.page_shift);
   }
   int pos = 0, page = 0;
   if (!bad) {
-    const int len = usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad);
-    pos = len - n_b + j;
+    pos = length_or_none(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad) - n_b + j;
     bad |= pos < 0;
   }
   if (!bad) {
@@ -205,8 +210,8 @@ __device__ __forceinline__ bool plan_append(const KvAppendArgs &a, int wg, int *
   // positions [from, to) and rows of a sequence; none where they cannot be used
   auto span = [&](int b, int *from, int *to, int *row) {
     const int lo = a.row_start[b], hi = a.row_start[b + 1];
-    const int len = usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad);
-    const bool ok = rows_ok(lo, hi, a.n_rows) && hi - lo <= len && (b > 0 || lo == 0);
+    const int len = a.lens[b];
+    const bool ok = sequence_ok(b, lo, hi, a.n_rows, len, a.pages_per_seq, a.d.page_shift);
     bad |= !ok;
     *row = lo;
     *to = ok ? len : 0;

@@ -48,6 +48,14 @@ UAD_HD int usable_length(int len, int pages_per_seq, int page_shift, bool *bad) 
   return len;
 }
 
+// The same, where a length that cannot be used counts as none.
+UAD_HD int length_or_none(int len, int pages_per_seq, int page_shift, bool *bad) {
+  bool cut = false;
+  const int usable = usable_length(len, pages_per_seq, page_shift, &cut);
+  *bad |= cut;
+  return cut ? 0 : usable;
+}
+
 // Elements (a, b) that rotation pair p of a head turns, p < head_dim / 2; pairs from
 // rope_dim / 2 on are left as they are.
 UAD_HD void rope_pair(int p, int rope_dim, bool neighbours, int *a, int *b) {
@@ -77,6 +85,13 @@ UAD_HD int64_t append_grid(int n_rows, int n_seqs, int shift) {
 }
 // New rows of a sequence at row_start[b] .. row_start[b + 1]: usable, or an error.
 UAD_HD bool rows_ok(int from, int to, int n_rows) { return from >= 0 && from <= to && to <= n_rows; }
+// The same of sequence b whose length with them is `len`: all of its new rows can be
+// used, or none.
+UAD_HD bool sequence_ok(int b, int from, int to, int n_rows, int len, int pages_per_seq, int page_shift) {
+  bool bad = false;
+  const int usable = usable_length(len, pages_per_seq, page_shift, &bad);
+  return !bad && rows_ok(from, to, n_rows) && to - from <= usable && (b > 0 || from == 0);
+}
 
 // ---------------------------------------------------------------------------
 // The attention's work.  Unit u of sequence b is a KV head with up to 16 of its query

@@ -1,0 +1,61 @@
+"""Lengths and starts that cannot be used, on the GPU: reported by whichever kernel an append takes, for every sequence,
+and nothing is written on their account."""
+import numpy as np
+import pytest
+
+import paper_2609_37772_amd as U
+from tests import paged_oracle as P
+from tests.test_gpu_paged import dev, draw, handle
+
+pytestmark = pytest.mark.gpu
+WIDE, PAGE = 40, 16  # a table of 640 tokens
+
+# sequences behind a first one with `most` rows: where their rows end (from there), their lengths, the rows that there
+# are, and which of them are refused
+BAD = {
+    "rows that do not exist": ([3, 5], [3, 2], 3, [1]),
+    "and a fall behind them": ([3, 5, 4], [3, 2, 0], 3, [1, 2]),
+    "falls that leave each row a sequence": ([2, 1, 2, 2, 1], [40] * 5, 2, [1, 4]),
+    "length below zero without rows": ([0, 2], [-1, 2], 2, [0]),
+    "length beyond the table without rows": ([2, 2], [2, 641], 2, [1]),
+    "length beyond the table": ([2, 4], [2, 641], 4, [1]),
+    "length beyond any table": ([2, 4], [2 ** 31 - 1, 2], 4, [0]),
+    "length below the rows": ([5, 6], [4, 1], 6, [0]),
+}
+
+
+@pytest.mark.parametrize("what", BAD)
+@pytest.mark.parametrize("most", [1, 640], ids=["row by row", "by tiles"])
+@pytest.mark.parametrize("others", [0, 70])  # sequences without rows or tokens, for more than a wave has lanes
+def test_append_reports_and_writes_nothing(gpu, what, most, others):
+    ends, lens, extra, refused = BAD[what]
+    n, rows = 1 + len(ends) + others, most + extra
+    assert (8 * n <= rows) == (most > 1)
+    starts = np.array([0, most] + [most + x for x in ends] + [most + ends[-1]] * others, np.int32)
+    lens = np.array([most, *lens] + [0] * others, np.int32)
+    c = P.Cache(3, 1, 2, 64, PAGE, [most] + [48] * len(ends) + [0] * others, wide=WIDE, poison=0.5)
+    spare = sorted(set(range(c.n_pages)) - set(c.table[c.table >= 0].tolist()))
+    table = np.where(c.table < 0, spare[0], c.table).astype(np.int32)  # every entry is a page
+    kv = handle(c, 2)
+    k = dev(draw(1, rows, 2, 64))
+    kv.append(0, k, k, dev(table), dev(lens), dev(starts))
+    with pytest.raises(U.UadError) as e:
+        kv.synchronize()
+    assert e.value.status == 9
+    kept = spare + [int(p) for b in refused for p in table[1 + b, :3]]
+    assert bool((kv.k[0, kept] == 0.5).all()) and bool((kv.v[0, kept] == 0.5).all())
+    assert bool((kv.k[0, table[0, 0]] != 0.5).any())  # the first sequence is fine
+    kv.synchronize()  # cleared
+
+
+@pytest.mark.parametrize("most", [2, 40], ids=["row by row", "by tiles"])
+def test_append_of_a_first_sequence_that_does_not_start_at_zero(gpu, most):
+    c = P.Cache(3, 1, 2, 64, PAGE, [most, 2], poison=0.5)
+    kv = handle(c, 2)
+    k = dev(draw(1, most + 2, 2, 64))
+    kv.append(0, k, k, dev(c.table), dev(c.lens), dev(np.array([1, most, most + 2], np.int32)))
+    with pytest.raises(U.UadError) as e:
+        kv.synchronize()
+    assert e.value.status == 9
+    pages = c.table[0][c.table[0] >= 0].tolist()
+    assert bool((kv.k[0, pages] == 0.5).all()) and bool((kv.v[0, pages] == 0.5).all())
