@@ -598,13 +598,13 @@ __device__ __forceinline__ bool plan_attend(const KvAttendArgs &a, int units, in
     *w = AttendWork{};
     w->b = (unsigned)wg / (unsigned)units;
     w->unit = wg - w->b * units;
-    w->len = usable_length(a.lens[w->b], a.pages_per_seq, a.d.page_shift, &bad);
+    w->len = length_or_none(a.lens[w->b], a.pages_per_seq, a.d.page_shift, &bad);
     w->t1 = tiles_of_length(w->len, TILE);
     w->splits = 1;
     if (bad && threadIdx.x == 0) raise_status(a.status, kStatusPage);
     return true;
   }
-  auto length = [&](int b) { return usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad); };
+  auto length = [&](int b) { return length_or_none(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad); };
   const bool spare = (int64_t)a.n_seqs * units < a.target;  // fewer units than run at once
   int start, slot, b, tiles, splits;
   if (a.n_seqs <= 64) {  // each wave for itself, a sequence per lane
@@ -1187,7 +1187,7 @@ __global__ __launch_bounds__(256) void kv_prefix_kernel(KvPrefixArgs a) {
   const size_t eh = (size_t)b * a.d.n_kv_heads + g;
   const size_t src = blockIdx.z * a.src_layer;
   bool bad = false;
-  const int len = usable_length(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad);
+  const int len = length_or_none(a.lens[b], a.pages_per_seq, a.d.page_shift, &bad);
   bad |= len < a.n_keys;
   const int n_keys = min(len, a.n_keys);
   constexpr int ESZ = F8 ? 1 : 2;

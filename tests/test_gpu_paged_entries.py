@@ -5,7 +5,7 @@ import pytest
 
 import paper_2609_37772_amd as U
 from tests import paged_oracle as P
-from tests.test_gpu_paged import dev, draw, handle
+from tests.test_gpu_paged import check_attend, dev, draw, handle
 
 pytestmark = pytest.mark.gpu
 WIDE, PAGE = 40, 16  # a table of 640 tokens
@@ -59,3 +59,19 @@ def test_append_of_a_first_sequence_that_does_not_start_at_zero(gpu, most):
     assert e.value.status == 9
     pages = c.table[0][c.table[0] >= 0].tolist()
     assert bool((kv.k[0, pages] == 0.5).all()) and bool((kv.v[0, pages] == 0.5).all())
+
+
+@pytest.mark.parametrize("lens,wide", [([60, 65, 40], 4), ([60, -1, 40], 4), ([60, 1281, 40], 80), ([1281] + [20] * 70, 80)])
+def test_attend_takes_a_length_that_it_cannot_use_for_none(gpu, lens, wide):
+    """Narrow tables (a workgroup per unit) and wide ones, planned by a wave's lanes and by the whole workgroup."""
+    fine = [n if 0 <= n <= 16 * wide else 0 for n in lens]
+    c = P.Cache(6, 1, 1, 64, PAGE, fine, wide=wide)
+    c.fill(2)
+    kv = handle(c, 2)
+    table = np.where(c.table < 0, 0, c.table).astype(np.int32)
+    q = draw(1, len(lens), 2, 64)
+    got = kv.attend(0, dev(q), dev(table), dev(np.array(lens, np.int32)))
+    with pytest.raises(U.UadError) as e:
+        kv.synchronize()
+    assert e.value.status == 9
+    check_attend(c, kv, 0, q, got, 0, False)  # the others' results, and zeros
