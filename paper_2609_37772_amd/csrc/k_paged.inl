@@ -733,13 +733,14 @@ __device__ __forceinline__ uint64_t pair_of(float m, float l) {
 
 // LDS of the attention: the query's bf16 terms, the waves' outputs, their maxima and sums
 // (before that the plan, later the slots' weights), the joint ones and a word; 158 of a
-// CU's 160 KB at head dim 256 with fp32 queries.
+// CU's 160 KB at head dim 256.
 constexpr int kAttendMl = 2 * kJoinFan * 16;  // floats
-template <int HD, bool F32>
-constexpr int kQueryFloats = (F32 ? 3 : 2) * HD / 32 * 256;
-template <int HD, bool F32>
+constexpr int kTerms = 3;
+template <int HD>
+constexpr int kQueryFloats = kTerms * HD / 32 * 256;
+template <int HD>
 constexpr int attend_lds_floats() {
-  return kQueryFloats<HD, F32> + kAttendWaves * 16 * HD + kAttendMl + 16 * 2 + 4;
+  return kQueryFloats<HD> + kAttendWaves * 16 * HD + kAttendMl + 16 * 2 + 4;
 }
 
 // The last of `n` workgroups to get here carries on; all of this workgroup's slot
@@ -832,15 +833,15 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   constexpr int KS = HD / 32;           // k steps of Q K^T
   constexpr int KL = F8 ? HD / 64 : KS; // 16-byte loads of a key row per lane
   constexpr int NTO = HD / 16;          // 16-column tiles of the output
-  constexpr int TERMS = F32 ? 3 : 2;
+  constexpr int TERMS = kTerms;
   constexpr int NW = kAttendWaves;
   constexpr int ESZ = F8 ? 1 : 2;
   extern __shared__ __align__(16) float lds[];
   __bf16 *qf = (__bf16 *)lds;                      // [TERMS][KS][64][8]
-  f32x4 *obuf = (f32x4 *)(lds + kQueryFloats<HD, F32>);  // [NW][NTO][64]
+  f32x4 *obuf = (f32x4 *)(lds + kQueryFloats<HD>);  // [NW][NTO][64]
   float *ml = (float *)(obuf + NW * NTO * 64);     // [NW or slots][16][2]
   float *top = ml + kAttendMl, *word = top + 32;
-  static_assert(TERMS * KS * 64 * 8 * 2 == kQueryFloats<HD, F32> * 4, "the query's terms");
+  static_assert(TERMS * KS * 64 * 8 * 2 == kQueryFloats<HD> * 4, "the query's terms");
   static_assert(NW * 16 * 2 <= kAttendMl && kPlanScans * NW <= kAttendMl, "the waves' maxima and the plan fit the slots' weights");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
@@ -1112,7 +1113,7 @@ int kv_attend_target(int n_cu, int head_dim) {
 template <int HD, bool F32, bool F8>
 static hipError_t attend_attr() {
   return hipFuncSetAttribute((const void *)kv_attend_kernel<HD, F32, F8>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                             attend_lds_floats<HD, F32>() * 4);
+                             attend_lds_floats<HD>() * 4);
 }
 template <int HD>
 static hipError_t attend_attrs() {
@@ -1137,7 +1138,7 @@ static hipError_t launch_attend_type(KvAttendArgs a, hipStream_t s) {
   a.unsplit = splits == 1;
   a.few_tiles = tiles < ((int64_t)1 << 31) / units;
   hipLaunchKernelGGL((kv_attend_kernel<HD, F32, F8>), dim3((unsigned)grid), dim3(64 * kAttendWaves),
-                     (attend_lds_floats<HD, F32>() * 4), s, a);
+                     (attend_lds_floats<HD>() * 4), s, a);
   return hipGetLastError();
 }
 
