@@ -517,9 +517,11 @@ hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_
 // Bound by reading K and V once.  A unit is a KV head of a sequence with up to 16 of
 // its query heads, the 16 columns of the matrix instruction: S^T = K Q^T and
 // O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, whose time is a tenth of the read's, so
-// that operands can be split into bf16 terms (a value = hi + lo [+ rest], each the bf16
-// of what is left): the rotated query and the weights keep 16 bits with bf16 results
-// and 24 with fp32 ones.
+// that operands can be split into bf16 terms (a value = hi + lo + rest, each the bf16
+// of what is left): the rotated query and the weights keep their 24 bits, so that a bf16
+// result too is one of fp32, rounded once.  Two terms of 16 bits for bf16 results put
+// seven times as many of them on the other side of a rounding; 817 keys of 1 x 256 took
+// 11.2 instead of 11.5 us, 48 uneven sequences of 2 x 128 in e4m3 19.8 instead of 20.9.
 //
 // A wave takes tiles of kTileKeys keys.  Row i of the t-th 16-key product is key
 // KPL * (i / 4) + 4 t + i % 4, so that lane group g ends with the scores of the
