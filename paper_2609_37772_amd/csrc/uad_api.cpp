@@ -1435,7 +1435,12 @@ uad_status uad_synchronize(uad_ctx *c) {
   e = hipMemcpy(&w, c->status, sizeof(w), hipMemcpyDeviceToHost);
   if (e != hipSuccess) return hip_fail(c, e, "uad_synchronize: status word");
   if (w == 0) return UAD_OK;
-  e = hipMemset(c->status, 0, sizeof(w));
+  // on the context's stream and waited for: a late clear would take with it what work
+  // that is queued next reports
+  const unsigned none = 0;
+  e = hipMemcpyAsync(c->status, &none, sizeof(none), hipMemcpyHostToDevice, c->stream);
+  const hipError_t done = hipStreamSynchronize(c->stream);
+  if (e == hipSuccess) e = done;
   if (e != hipSuccess) return hip_fail(c, e, "uad_synchronize: status word");
   if (w & kStatusTimeout)
     return fail(c, UAD_E_HIP, "uad_synchronize: an in-kernel wait gave up (results of that work are invalid)");
