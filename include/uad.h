@@ -311,8 +311,8 @@ uad_status uad_aal(const double *release, int32_t n, double t_act, double *aal_o
  * UAD_DTYPE_BF16 or UAD_DTYPE_F8, 16-byte aligned, with one slot per token:
  *   k  [n_layers][n_pages][n_kv_heads][page_size][head_dim]
  *   v  [n_layers][n_pages][n_kv_heads][head_dim][page_size]   (transposed pages)
- * An 8-bit pool holds x / scale (k_scale, v_scale), cut to +-448 and rounded to
- * nearest-even once; a NaN stays one.  A bf16 pool rounds to nearest-even once.
+ * An 8-bit pool holds the fp32 quotient x / scale (k_scale, v_scale), cut to +-448
+ * and rounded to nearest-even; a NaN stays one.  A bf16 pool rounds to nearest-even once.
  * Slots that no call has written may hold anything, NaN included.
  *
  * Sequences.  Calls take int32 device arrays: a page table [n_seqs][pages_per_seq]
@@ -355,7 +355,7 @@ typedef struct {
   int32_t rope_dim;   /* 0 (no rotation) or a multiple of 16 up to head_dim */
   int32_t rope_pairs; /* 0: halves (i, i + rope_dim/2); 1: neighbours */
   double rope_theta;  /* > 0 (unused with rope_dim 0) */
-  float k_scale, v_scale; /* finite and > 0; 1 with UAD_DTYPE_BF16 */
+  float k_scale, v_scale; /* > 0, finite as their reciprocals and 448 times each are; 1 with UAD_DTYPE_BF16 */
   void *k, *v;        /* the pools, device memory of the handle's device */
 } uad_kv_config;
 

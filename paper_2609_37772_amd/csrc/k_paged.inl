@@ -34,11 +34,19 @@ __device__ __forceinline__ void store_elem(void *p, int64_t i, float v) {
   if constexpr (F32) ((float *)p)[i] = v;
   else ((__bf16 *)p)[i] = (__bf16)v;
 }
-// fp32 to e4m3, cut to +-448 (the cut keeps a NaN: both comparisons fail)
-__device__ __forceinline__ float cut_f8(float v) { return v > 448.f ? 448.f : v < -448.f ? -448.f : v; }
-__device__ __forceinline__ uint8_t to_f8(float v) {
-  return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(cut_f8(v), 0.f, 0, false) & 0xFF);
+// What an 8-bit pool holds of x: x / scale, cut to +-448 (before the division, so that
+// it never meets an infinity; both comparisons keep a NaN).  The remainder makes the
+// product with the rounded reciprocal the quotient, so that a value halfway between two
+// of e4m3 stays there and goes to the even one; a zero keeps its sign.  16 uneven
+// prompts, 2 x 128: 4.9 us, by the compiler's division 5.3, by the product alone, which
+// moves such values, 4.75.
+__device__ __forceinline__ float quotient(float x, float scale, float inv) {
+  const float most = 448.f * scale;
+  x = x > most ? most : x < -most ? -most : x;
+  const float q = x * inv;
+  return fmaf(-fmaf(q, scale, -x), inv, q);
 }
+__device__ __forceinline__ uint8_t to_f8(float v) { return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(v, 0.f, 0, false) & 0xFF); }
 
 template <bool F8>
 __device__ __forceinline__ void store_pool(void *p, size_t i, float v) {
@@ -175,10 +183,10 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
     const float u = load_elem<F32>(a.v, r * a.ldv + col + 2 * p), w = load_elem<F32>(a.v, r * a.ldv + col + 2 * p + 1);
     const size_t base = page_base(a.d, page, h);
     const float kx = p < a.rope_dim / 2 ? x * c - y * s : x, ky = p < a.rope_dim / 2 ? y * c + x * s : y;
-    store_pool<F8>(a.kp, base + k_in_page(a.d, off, ea), F8 ? kx * a.k_inv : kx);
-    store_pool<F8>(a.kp, base + k_in_page(a.d, off, eb), F8 ? ky * a.k_inv : ky);
-    store_pool<F8>(a.vp, base + v_in_page(a.d, off, 2 * p), F8 ? u * a.v_inv : u);
-    store_pool<F8>(a.vp, base + v_in_page(a.d, off, 2 * p + 1), F8 ? w * a.v_inv : w);
+    store_pool<F8>(a.kp, base + k_in_page(a.d, off, ea), F8 ? quotient(kx, a.k_scale, a.k_inv) : kx);
+    store_pool<F8>(a.kp, base + k_in_page(a.d, off, eb), F8 ? quotient(ky, a.k_scale, a.k_inv) : ky);
+    store_pool<F8>(a.vp, base + v_in_page(a.d, off, 2 * p), F8 ? quotient(u, a.v_scale, a.v_inv) : u);
+    store_pool<F8>(a.vp, base + v_in_page(a.d, off, 2 * p + 1), F8 ? quotient(w, a.v_scale, a.v_inv) : w);
   }
 }
 
@@ -292,8 +300,8 @@ struct Pool8 {
 #pragma unroll
     for (int i = 0; i < (F8 ? 2 : 4); ++i) {
       if constexpr (F8) {
-        int x = __builtin_amdgcn_cvt_pk_fp8_f32(cut_f8(v[4 * i]), cut_f8(v[4 * i + 1]), 0, false);
-        w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(cut_f8(v[4 * i + 2]), cut_f8(v[4 * i + 3]), x, true);
+        int x = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
+        w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], x, true);
       } else {
         union {
           bf16x2 h;
@@ -395,8 +403,8 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvAppendArgs a) {
       if constexpr (F8)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          u[e] *= a.k_inv;
-          w[e] *= a.k_inv;
+          u[e] = quotient(u[e], a.k_scale, a.k_inv);
+          w[e] = quotient(w[e], a.k_scale, a.k_inv);
         }
       char *dst = (char *)a.kp + (base + k_in_page(a.d, (t.first & mask) + token, 0)) * ESZ;
       Pool8<F8> o;
@@ -418,8 +426,8 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvAppendArgs a) {
     float u[8], w[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      u[e] = rx[n].value(e) * (F8 ? a.v_inv : 1.f);
-      w[e] = ry[n].value(e) * (F8 ? a.v_inv : 1.f);
+      u[e] = F8 ? quotient(rx[n].value(e), a.v_scale, a.v_inv) : rx[n].value(e);
+      w[e] = F8 ? quotient(ry[n].value(e), a.v_scale, a.v_inv) : ry[n].value(e);
     }
     Pool8<F8> o;
     o.set(u);

@@ -149,6 +149,8 @@ uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_str
     return cerr(UAD_E_INVALID, "scales must be finite and > 0");
   if (!std::isfinite(1.f / m.k_scale) || !std::isfinite(1.f / m.v_scale))
     return cerr(UAD_E_INVALID, "the reciprocal of a scale overflows");
+  if (!std::isfinite(448.f * m.k_scale) || !std::isfinite(448.f * m.v_scale))
+    return cerr(UAD_E_INVALID, "448 times a scale overflows");
   if (m.dtype == UAD_DTYPE_BF16 && (m.k_scale != 1.f || m.v_scale != 1.f))
     return cerr(UAD_E_INVALID, "bf16 pools take no scale (k_scale and v_scale 1)");
   if (m.head_dim != 64 && m.head_dim != 128 && m.head_dim != 256)
@@ -255,7 +257,8 @@ uad_status uad_kv_append(uad_kv *kv, int32_t layer, const void *k, const void *v
   a.turns = kv->turns; a.rope_dim = kv->cfg.rope_dim; a.rope_pairs = kv->cfg.rope_pairs;
   const int64_t per16 = dtype == UAD_DTYPE_F32 ? 4 : 8;
   a.in_vec = aligned(k, 16) && aligned(v, 16) && ldk % per16 == 0 && ldv % per16 == 0;
-  a.k_inv = 1.f / kv->cfg.k_scale; a.v_inv = 1.f / kv->cfg.v_scale;
+  a.k_scale = kv->cfg.k_scale; a.v_scale = kv->cfg.v_scale;
+  a.k_inv = 1.f / a.k_scale; a.v_inv = 1.f / a.v_scale;
   a.status = kv->status;
   const hipError_t e = launch_kv_append(a, dtype == UAD_DTYPE_F32, kv->cfg.dtype == UAD_DTYPE_F8, kv->stream);
   return e == hipSuccess ? UAD_OK : kv_hip_fail(kv, e, fn, "launch");

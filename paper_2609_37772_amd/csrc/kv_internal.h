@@ -23,7 +23,7 @@ struct KvAppendArgs {
   bool in_vec;            // rows can be loaded 16 bytes at a time
   const double *turns;    // [rope_dim / 2] turns per position
   int rope_dim, rope_pairs;
-  float k_inv, v_inv;     // 1 / scale (8-bit pools)
+  float k_scale, v_scale, k_inv, v_inv;  // 8-bit pools hold value / scale; 1 / scale
   unsigned *status;
 };
 
