@@ -69,7 +69,7 @@ class uad_kv_config(ctypes.Structure):
 
 
 _lib: Optional[ctypes.CDLL] = None
-_marshal = None               # the checks of decoding's calls in C (csrc/marshal.c), and the entry points' addresses
+_marshal = None               # the checks of decoding's calls in C (csrc/marshal.c) where built, and the entry points' addresses
 _append_at = _attend_at = 0
 
 
@@ -116,9 +116,9 @@ def load_library() -> ctypes.CDLL:
         fn.restype = res
     try:
         from . import _marshal as marshal
-    except ImportError as e:
-        raise RuntimeError(f"{os.path.dirname(LIB_PATH)}/_marshal.so: {e}; run `python -m paper_2609_37772_amd.build`") from e
-    marshal.setup(torch.Tensor, torch.float32, torch.bfloat16, torch.int32)
+        marshal.setup(torch.Tensor, torch.float32, torch.bfloat16, torch.int32)
+    except ImportError:
+        marshal = None  # every call's checks are made here then, the same ones
     _append_at, _attend_at = (ctypes.cast(f, ctypes.c_void_p).value for f in (lib.uad_kv_append, lib.uad_kv_attend))
     _marshal, _lib = marshal, lib
     return lib
@@ -499,7 +499,9 @@ def uad_kv_append(kv: int, layer: int, k: torch.Tensor, v: torch.Tensor, page_ta
     """Append rows k, v [n_rows][Hkv][hd] (rows may be slices of wider ones) to a layer's pages."""
     if _marshal is None:
         load_library()
-    st = _marshal.append(_append_at, kv, layer, k, v, page_table, lens, row_start, positions, *row_shape, device)
+    st = None
+    if _marshal is not None:
+        st = _marshal.append(_append_at, kv, layer, k, v, page_table, lens, row_start, positions, *row_shape, device)
     if st is None:  # not the usual case
         st = _append_checked(kv, layer, k, v, page_table, lens, row_start, positions, row_shape, device)
     if st:
@@ -520,7 +522,9 @@ def uad_kv_attend(kv: int, layer: int, q: torch.Tensor, out: torch.Tensor, page_
     """Attention of q [n_seqs][Hq][hd], one token per sequence, over a layer's pages into out (q's type and shape)."""
     if _marshal is None:
         load_library()
-    st = _marshal.attend(_attend_at, kv, layer, q, out, page_table, lens, positions, scale, *row_shape, device)
+    st = None
+    if _marshal is not None:
+        st = _marshal.attend(_attend_at, kv, layer, q, out, page_table, lens, positions, scale, *row_shape, device)
     if st is None:  # not the usual case
         st = _attend_checked(kv, layer, q, out, page_table, lens, positions, scale, row_shape, device)
     if st:
