@@ -18,6 +18,7 @@ class ActionExpert:
         self.device = device
         self.max_batch, self.max_chunk, self.max_prefix = max_batch, max_chunk, max_prefix
         self.ctx = B.uad_create(shape, max_batch, max_chunk, max_prefix, device, stream)
+        self._stream = stream or torch.cuda.current_stream(device)
 
     def close(self):
         if getattr(self, "ctx", None):
@@ -37,8 +38,10 @@ class ActionExpert:
         B.uad_set_prefix_kv(self.ctx, k, v, batch, prefix_len)
 
     def set_prefix_paged(self, cache, page_table, lens, prefix_len: int) -> None:
-        """The prefix of one environment per row of ``page_table`` from a :class:`PagedKV` cache."""
+        """The prefix of one environment per row of ``page_table`` from a :class:`PagedKV` cache, on the expert's stream."""
         B.uad_set_prefix_paged(self.ctx, cache.handle, page_table, lens, prefix_len, self.device)
+        if torch.cuda.current_stream(self.device) != self._stream:  # their memory is in use there
+            page_table.record_stream(self._stream), lens.record_stream(self._stream)
 
     def step(self, x, t, dt, mask, v_out=None) -> None:
         B.uad_denoise_step(self.ctx, x, t, dt, mask, v_out)
