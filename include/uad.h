@@ -333,13 +333,17 @@ uad_status uad_aal(const double *release, int32_t n, double t_act, double *aal_o
  * neighbours (2i, 2i+1) with rope_pairs, are turned by position * w_i,
  * w_i = rope_theta^(-2i/rope_dim), i < rope_dim/2: (a, b) becomes
  * (a cos - b sin, b cos + a sin).  Angles are held in 64 bits (positions may be
- * far).  uad_kv_append turns keys, uad_kv_attend the query.
+ * far), sines and cosines of them are within 1.3e-7 (the hardware's), the rest is
+ * fp32.  uad_kv_append turns keys, uad_kv_attend the query.
  *
  * Work is enqueued on the handle's stream, allocates nothing and can be captured
  * into a HIP graph.  Work of one handle shares the handle's workspace and must
  * not overlap on the device: use a handle per stream (several handles may share
- * pools), and do not replay two graphs of one handle at once.  A handle is not
- * thread-safe.  The calling thread's current device is left as it was.
+ * pools), and do not replay two graphs of one handle at once.  What a call reads
+ * (rows, row_start, lens, positions, page table) must hold still until it has run:
+ * lengths that change under an attention can leave the workspace of its splits
+ * unfit for every later one of the handle, which must be created anew then.  A
+ * handle is not thread-safe.  The calling thread's current device is left as it was.
  * ------------------------------------------------------------------------- */
 typedef struct uad_kv uad_kv; /* opaque, owned by the library */
 
@@ -421,6 +425,11 @@ uad_status uad_kv_attend(uad_kv *kv, int32_t layer, const void *q, void *out, in
  * ordered after the work queued on the cache's stream, which goes on after it.
  *   lens        int32 device [batch]: a length below prefix_len raises UAD_E_PAGE
  *               (from both handles' synchronize), as do the ids checked there
+ * It can be captured with both handles on the captured stream.  Each replay fills
+ * the context's prefix; its length and batch are set once, by the call.  So replay
+ * before the first step outside the graph, and let no uad_set_prefix_* call with
+ * another prefix_len or batch come between the capture and a replay: later steps
+ * would take that call's sizes for the replayed keys, and no error is raised.
  * Errors: UAD_E_INVALID, UAD_E_SHAPE (batch > max_batch, prefix_len > max_prefix
  * or beyond the page table, another model or device), UAD_E_HIP (after work was
  * enqueued: no prefix is set then). */
