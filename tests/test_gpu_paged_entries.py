@@ -2,6 +2,7 @@
 and nothing is written on their account."""
 import numpy as np
 import pytest
+import torch
 
 import paper_2609_37772_amd as U
 from tests import paged_oracle as P
@@ -75,3 +76,26 @@ def test_attend_takes_a_length_that_it_cannot_use_for_none(gpu, lens, wide):
         kv.synchronize()
     assert e.value.status == 9
     check_attend(c, kv, 0, q, got, 0, False)  # the others' results, and zeros
+
+
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf")])
+def test_an_infinity_enters_its_own_outputs_only(gpu, where, bad):
+    """Of a key: all of its sequence's head; of a value: that column.  They need not be finite, the others are as ever."""
+    lens = [700, 50, 70]
+    outs = []
+    q = dev(draw(1, 3, 4, 64))
+    for value in (0.25, bad):
+        c = P.Cache(9, 1, 2, 64, PAGE, lens)
+        c.fill(4)
+        pg, off = c.slot(0, 57)
+        (c.k[0, pg, 1, off] if where == "k" else c.v[0, pg, 1, :, off])[3] = value
+        kv = handle(c, 4)
+        outs.append(kv.attend(0, q, dev(c.table), dev(c.lens)).cpu())
+        kv.synchronize()
+    want, got = outs
+    assert torch.equal(got[1:], want[1:]) and torch.equal(got[0, :2], want[0, :2])
+    if where == "v":
+        assert not bool(got[0, 2:, 3].isfinite().any())
+        got[0, 2:, 3] = want[0, 2:, 3]
+        assert torch.equal(got, want)
