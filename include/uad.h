@@ -391,7 +391,7 @@ uad_status uad_kv_set_stream(uad_kv *kv, void *hip_stream);
  *   row_start   int32 [n_seqs + 1], rising from 0: rows row_start[b] ..
  *               row_start[b+1]-1 are sequence b's new tokens in order (none is
  *               fine), and rows from row_start[n_seqs] on are ignored; NULL: one
- *               row per sequence (n_rows == n_seqs).  With n_rows 0 nothing is
+ *               row per sequence (n_rows == n_seqs).  With n_rows or n_seqs 0 nothing is
  *               enqueued, so nothing is looked at either
  *   positions   int32 [n_rows] rotation positions, or NULL: the cache positions.
  *               Row j of sequence b's n new rows takes cache position

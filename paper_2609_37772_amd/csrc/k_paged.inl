@@ -135,16 +135,10 @@ __device__ __forceinline__ int sequence_of_row(const int32_t *row_start, int n_s
 // 2 x 128 in e4m3.
 // ---------------------------------------------------------------------------
 template <bool F32, bool F8>
-__global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
-  const int r = a.row0 + blockIdx.x;
+__device__ __forceinline__ void append_row(const KvAppendArgs &a, int r) {
   int b = r, j = 0, n_b = 1;
   bool bad = false;
   if (a.row_start) {
-    // every sequence is looked at, those too in which no row lands
-    bool odd = false;
-    for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < (unsigned)a.n_seqs; i += gridDim.x * 256)
-      odd |= !sequence_ok(i, a.row_start[i], a.row_start[i + 1], a.n_rows, a.lens[i], a.pages_per_seq, a.d.page_shift);
-    if (odd) raise_status(a.status, kStatusPage);
     b = sequence_of_row(a.row_start, a.n_seqs, r);
     if (b >= a.n_seqs) return;  // a row behind the last sequence
     int lo = 0, hi = 0;
@@ -188,6 +182,24 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
     store_pool<F8>(a.vp, base + v_in_page(a.d, off, 2 * p), F8 ? quotient(u, a.v_scale, a.v_inv) : u);
     store_pool<F8>(a.vp, base + v_in_page(a.d, off, 2 * p + 1), F8 ? quotient(w, a.v_scale, a.v_inv) : w);
   }
+}
+
+template <bool F32, bool F8>
+__global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
+  const int r = a.row0 + blockIdx.x;
+  if (!a.row_start) {
+    append_row<F32, F8>(a, r);
+    return;
+  }
+  // every sequence is looked at, those too in which no row lands: loaded before the row
+  // is dealt with, looked at after it
+  unsigned i = blockIdx.x * 256 + threadIdx.x;
+  const int at = min(i, (unsigned)a.n_seqs - 1), from = a.row_start[at], to = a.row_start[at + 1], len = a.lens[at];
+  append_row<F32, F8>(a, r);
+  bool odd = i < (unsigned)a.n_seqs && !sequence_ok(at, from, to, a.n_rows, len, a.pages_per_seq, a.d.page_shift);
+  for (i += gridDim.x * 256; i < (unsigned)a.n_seqs; i += gridDim.x * 256)
+    odd |= !sequence_ok(i, a.row_start[i], a.row_start[i + 1], a.n_rows, a.lens[i], a.pages_per_seq, a.d.page_shift);
+  if (odd) raise_status(a.status, kStatusPage);
 }
 
 // ---------------------------------------------------------------------------
@@ -554,10 +566,10 @@ hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_
 // 10.4).
 constexpr int kAttendMinTiles = 4;
 // Tiles up to which a unit stays whole, where reading it and joining it cost the same
-// (one sequence, whole / split): head dim 256, 8 tiles 11.0 / 11.2 us, 10 tiles 12.0 /
-// 11.2; 128, 12 tiles 8.5 / 8.7, 16 tiles 9.6 / 8.8; 64, 20 tiles 7.5 / 7.8, 24 tiles
-// 8.2 / 7.8.  E4m3, whose tiles take longer to widen: 256, 6 tiles 11.7 / 11.7; 128, 8
-// tiles 8.6 / 9.3, 10 tiles 9.5 / 9.2; 64, 12 tiles 7.0 / 7.9, 16 tiles 8.1 / 8.1.
+// (one sequence, whole / split): head dim 256, 8 tiles 10.9 / 11.2 us, 10 tiles 11.8 /
+// 11.2; 128, 12 tiles 8.5 / 8.8, 16 tiles 9.6 / 8.9; 64, 20 tiles 7.6 / 8.0, 24 tiles
+// 8.3 / 8.0.  E4m3, whose tiles take longer to widen: 256, 6 tiles 12.2 / 12.2; 128, 8
+// tiles 8.8 / 9.6, 10 tiles 9.9 / 9.6; 64, 12 tiles 7.2 / 8.1, 16 tiles 8.4 / 8.3.
 template <int HD, bool F8>
 constexpr int kAttendWhole = (HD == 256 ? 8 : HD == 128 ? 12 : 20) * (F8 ? 3 : 4) / 4;
 constexpr int kAttendWaves = 8;
