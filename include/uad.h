@@ -373,7 +373,9 @@ typedef struct {
  * to NULL. */
 uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_stream, uad_kv **out);
 
-/* Free the handle's workspace (after synchronising its stream); the pools stay the caller's. */
+/* Free the handle's workspace (after synchronising its stream); the pools stay the
+ * caller's.  Graphs that hold work of the handle, a prefix from its pages too, must
+ * not run any more. */
 void uad_kv_destroy(uad_kv *kv);
 
 /* Message for the last non-OK status of this handle; kv == NULL: of the last

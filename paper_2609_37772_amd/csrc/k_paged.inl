@@ -131,8 +131,8 @@ __device__ __forceinline__ int sequence_of_row(const int32_t *row_start, int n_s
 // ---------------------------------------------------------------------------
 // Append of few rows: one workgroup per new row, a thread per pair of columns and as
 // many heads at once as there are threads.  Bound by the launch and three dependent
-// loads (length, page id, store): 2.7 us for a token of 1 x 256, 3.1 us for 64 tokens of
-// 2 x 128 in e4m3.
+// loads (length, page id, store): 2.0 us for a token of 1 x 256, 3.1 us for 64 tokens of
+// 2 x 128 in e4m3 (kernel time; 2.7 and 3.1 a call in a graph of them).
 // ---------------------------------------------------------------------------
 template <bool F32, bool F8>
 __device__ __forceinline__ void append_row(const KvAppendArgs &a, int r) {
@@ -554,11 +554,12 @@ hipError_t launch_kv_append(const KvAppendArgs &a, bool f32, bool f8, hipStream_
 // unit's splits meet in slots of the workspace: the last workgroup to arrive joins
 // them, in the order of the keys.
 //
-// One sequence of 131071 keys, 32/8 heads of 128 in bf16 (537 MB): 97 - 101 us, 5.3 -
+// One sequence of 131071 keys, 32/8 heads of 128 in bf16 (537 MB): 98 - 100 us, 5.4 -
 // 5.5 TB/s, where a kernel that only reads takes 85; 8 x 4001 keys of 16 x 64 (127 MB)
-// 29 - 31; 64 x 900 keys of 1 x 256 (58 MB) 20; 817 keys of 1 x 256 11.3 us, of which
+// 30; 64 x 900 keys of 1 x 256 (58 MB) 20.5; 817 keys of 1 x 256 11.5 us, of which
 // the launch, the plan, the meeting in LDS and the join take about 7.  More splits than
-// workgroups run at once cost their prologues (twice as many: 109, 37 and 27 us).
+// workgroups run at once cost their prologues (twice as many, with two terms: 109, 37
+// and 27 us).
 // ---------------------------------------------------------------------------
 // Tiles of a split, where a unit has as many: fewer leave more to join, more keep a CU
 // reading, which takes in 15 to 26 bytes a clock of these loads (26 tiles of 1 x 256: 2

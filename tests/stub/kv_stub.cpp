@@ -7,18 +7,17 @@
 #include "../../paper_2609_37772_amd/csrc/kv_internal.h"
 
 namespace {
-int g_current = 3, g_sets = 0, g_events = 0;
+int g_current = 3;
 std::string g_calls, g_text;
 hipError_t g_launch = hipSuccess;
 }  // namespace
 
 extern "C" {
-void kv_stub_reset(int fail) { g_calls.clear(); g_events = 0; g_launch = fail ? hipErrorLaunchFailure : hipSuccess; }
+void kv_stub_reset(int fail) { g_calls.clear(); g_launch = fail ? hipErrorLaunchFailure : hipSuccess; }
 const char *kv_stub_calls() { g_text = g_calls; return g_text.c_str(); }
 int kv_stub_current_device() { return g_current; }
 void kv_stub_status(uad_kv *kv, unsigned w) { *kv->status = w; }
 void kv_stub_ctx_status(uad_ctx *c, unsigned w) { *c->status = w; }
-int kv_stub_events() { return g_events; }
 int kv_stub_prefix_set(const uad_ctx *c) { return c->prefix_set ? c->prefix_len : -1; }
 hipError_t hipGetDevice(int *d) { *d = g_current; return hipSuccess; }
 hipError_t hipMemsetAsync(void *p, int v, size_t n, hipStream_t) { std::memset(p, v, n); return hipSuccess; }
