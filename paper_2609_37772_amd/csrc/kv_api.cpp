@@ -355,8 +355,10 @@ uad_status uad_kv_synchronize(uad_kv *kv) {
   if (e != hipSuccess) return kv_hip_fail(kv, e, fn, "hipStreamSynchronize");
   unsigned w = 0;
   e = hipMemcpy(&w, kv->status, sizeof(w), hipMemcpyDeviceToHost);
-  // on the stream itself: work that is queued next must not have its status cleared
+  // on the stream itself and waited for: work that is queued next, or a graph that is
+  // replayed on another stream, must not have its status cleared
   if (e == hipSuccess && w) e = hipMemsetAsync(kv->status, 0, sizeof(w), kv->stream);
+  if (e == hipSuccess && w) e = hipStreamSynchronize(kv->stream);
   if (e != hipSuccess) return kv_hip_fail(kv, e, fn, "status word");
   if (w)
     return kv_fail(kv, UAD_E_PAGE, fn, "a page id, a length or a row of the queued work could not be used (results of "

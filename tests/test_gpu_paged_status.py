@@ -28,3 +28,26 @@ def test_an_experts_status_is_reported_once_each_time(gpu):
         ex.synchronize()
     finally:
         ex.close()
+
+
+def test_a_replay_on_another_stream_is_reported_each_time(gpu):
+    """The handle's stream has nothing to do with where its graph runs."""
+    c = P.Cache(9, 1, 1, 64, 16, [40])
+    c.fill(4)
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    kv = handle(c, 4, stream=side)
+    with torch.cuda.stream(side):
+        q, lens, table = torch.ones((1, 4, 64), device="cuda"), dev(c.lens), dev(np.full_like(c.table, -1))
+        out = torch.empty_like(q)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            kv.attend(0, q, table, lens, out=out)
+    for _ in range(50):
+        with torch.cuda.stream(other):
+            graph.replay()
+        other.synchronize()
+        with pytest.raises(U.UadError) as e:
+            kv.synchronize()
+        assert e.value.status == 9
+    kv.synchronize()

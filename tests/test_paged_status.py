@@ -13,3 +13,13 @@ def test_an_experts_status_is_cleared_before_synchronize_returns(lib, ctx):  # n
     assert lib.stub_log() == b"sync copy sync "
     lib.stub_reset(-1)
     assert lib.uad_synchronize(ctx) == OK and lib.stub_log() == b"sync "
+
+
+def test_a_caches_status_is_cleared_before_synchronize_returns(lib, kv):  # noqa: F811
+    """Graphs of the handle's work may be replayed on other streams, which its own stream's clear is not ordered against."""
+    lib.stub_log.restype = ctypes.c_char_p
+    lib.stub_reset(-1)
+    lib.kv_stub_status(kv, 4)
+    assert lib.uad_kv_synchronize(kv) == PAGE and lib.stub_log() == b"sync sync "
+    lib.stub_reset(-1)
+    assert lib.uad_kv_synchronize(kv) == OK and lib.stub_log() == b"sync "
