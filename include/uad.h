@@ -312,7 +312,8 @@ uad_status uad_aal(const double *release, int32_t n, double t_act, double *aal_o
  *   k  [n_layers][n_pages][n_kv_heads][page_size][head_dim]
  *   v  [n_layers][n_pages][n_kv_heads][head_dim][page_size]   (transposed pages)
  * An 8-bit pool holds the fp32 quotient x / scale (k_scale, v_scale), cut to +-448
- * and rounded to nearest-even; a NaN stays one.  A bf16 pool rounds to nearest-even once.
+ * and rounded to nearest-even; a NaN stays one.  A bf16 pool rounds to nearest-even
+ * once.
  * Slots that no call has written may hold anything, NaN included.
  *
  * Sequences.  Calls take int32 device arrays: a page table [n_seqs][pages_per_seq]
@@ -326,8 +327,9 @@ uad_status uad_aal(const double *release, int32_t n, double t_act, double *aal_o
  * row_start that does not rise from 0 within 0..n_rows raise UAD_E_PAGE, reported
  * by uad_kv_synchronize, whichever sequence it is and whether rows go there or
  * not.  Nothing is written for a sequence with such a length or start, nor to a
- * page with such an id, and the results of that work are invalid.  Pages may be shared between sequences for reading; two
- * tokens of one call that go to the same slot leave either's value there.
+ * page with such an id, and the results of that work are invalid.  Pages may be
+ * shared between sequences for reading; two tokens of one call that go to the same
+ * slot leave either's value there.
  *
  * Rotation.  With rope_dim > 0, elements (i, i + rope_dim/2) of a head, or
  * neighbours (2i, 2i+1) with rope_pairs, are turned by position * w_i,
@@ -359,7 +361,7 @@ typedef struct {
   int32_t rope_dim;   /* 0 (no rotation) or a multiple of 16 up to head_dim */
   int32_t rope_pairs; /* 0: halves (i, i + rope_dim/2); 1: neighbours */
   double rope_theta;  /* > 0 (unused with rope_dim 0) */
-  float k_scale, v_scale; /* > 0, finite as their reciprocals and 448 times each are; 1 with UAD_DTYPE_BF16 */
+  float k_scale, v_scale; /* > 0; they, their reciprocals and 448 times each finite; 1 with UAD_DTYPE_BF16 */
   void *k, *v;        /* the pools, device memory of the handle's device */
 } uad_kv_config;
 
