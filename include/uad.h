@@ -422,6 +422,99 @@ uad_status uad_kv_attend(uad_kv *kv, int32_t layer, const void *q, void *out, in
                          const int32_t *lens, const int32_t *positions, const int32_t *page_table,
                          int32_t pages_per_seq, int32_t n_seqs, float scale);
 
+/* Scales of their own for the blocks of an 8-bit cache: pools of UAD_DTYPE_F8 that need
+ * no scale found beforehand.
+ *   k_scales, v_scales  device fp32 [n_layers][n_pages][n_kv_heads][page_size / 16], the
+ *               caller's for the life of the handle: a value is what its slot holds times
+ *               the scale of its block, 16 tokens of a page and KV head
+ * From the next call on, uad_kv_append writes them.  A block's scale is the least power of
+ * two from 2^-100 to 2^119 by which the largest finite magnitude of the block's new rows
+ * (keys after their rotation) is within 448, or what it was, if the block holds earlier
+ * tokens of the sequence and that is more.  Where it grows, the earlier tokens are rounded
+ * to the new scale, with powers of two a change only of what falls below e4m3's normal
+ * range.  Values are cut to +-448 scales and rounded to nearest-even; a NaN stays one.
+ * uad_kv_attend, uad_kv_attend_rows and uad_set_prefix_paged read them; the caller may
+ * fill pools and scales too, with any positive finite scales.  Blocks that no token is in
+ * may have any.  Unlike with one scale, rows of two sequences, or of two calls that
+ * overlap, must not go to the same block, and a page that a sequence appends to may change
+ * for others that read it as above.
+ * NULL, NULL: the handle's one scale again.  Work that is enqueued already keeps what it
+ * had.  The handle must have been created with k_scale and v_scale 1.  Errors:
+ * UAD_E_INVALID (one of them NULL, not UAD_DTYPE_F8, other k_scale or v_scale, unaligned),
+ * UAD_E_UNSUPPORTED (n_kv_heads above 65535), UAD_E_SHAPE (memory as with the pools). */
+uad_status uad_kv_set_block_scales(uad_kv *kv, float *k_scales, float *v_scales);
+
+/* Attention of the newest rows of every sequence over its pages in one layer: a prompt's,
+ * a few more of a conversation, or a token each.  Rows, row_start, lens and positions are
+ * those of the uad_kv_append that came before: row j of sequence b's n has cache position
+ * p = lens[b] - n + j, and rotation position p, or the caller's.  It sees key x, 0 <= x <
+ * lens[b], where
+ *   x <= p                                if causal is 1, and
+ *   |p - x| < window or x < n_sinks       if window > 0.
+ * out = softmax(scale * q K^T) V per head over those keys, rounded once to the type of q.
+ * Sums and softmax statistics are fp32; the matrix instructions take the rotated query and
+ * the weights in 24 bits for F32 rows and for calls of few rows, in 16 for many rows of
+ * BF16.
+ *   q, out      device [n_rows][n_heads][head_dim] of dtype F32 or BF16, rows ldq / ldo
+ *               elements apart, aligned to their type; out may not overlap q or the pools
+ *   row_start   as in uad_kv_append: rows from row_start[n_seqs] on are ignored, and their
+ *               out is left as it was; NULL: one row per sequence (n_rows == n_seqs), where
+ *               a sequence of length 0 gives zeros
+ *   window, n_sinks  0, 0: every key.  Page ids of pages that no row of the call sees
+ *               are not read (they may have been given back, see uad_kv_release)
+ * A key that a row does not see is as if it were not there, whatever its slots hold; a NaN
+ * in the row, or in a key or value that it sees, makes the outputs that it enters NaN, an
+ * infinity may.  With n_rows or n_seqs 0 nothing is enqueued.  Nothing is written for a
+ * sequence whose length or start cannot be used (without row_start: zeros).
+ * Errors as uad_kv_append, and UAD_E_INVALID (window or n_sinks below 0, n_sinks without a
+ * window, causal not 0 or 1, scale not finite), UAD_E_SHAPE (n_rows * n_heads above 2^25). */
+uad_status uad_kv_attend_rows(uad_kv *kv, int32_t layer, const void *q, void *out, int32_t dtype, int64_t ldq, int64_t ldo,
+                              int32_t n_rows, const int32_t *row_start, const int32_t *lens, const int32_t *positions,
+                              const int32_t *page_table, int32_t pages_per_seq, int32_t n_seqs, float scale,
+                              int32_t window, int32_t n_sinks, int32_t causal);
+
+/* Pages for new tokens, on the device: nothing of what the calls above read has to come
+ * from the host, and a captured decoding step takes its pages itself.  The caller owns a
+ * stack of free pages: free_pages, int32 device [n_pages], of which the first n_free[0] are
+ * page ids that no table holds.
+ *   lens        int32 device [n_seqs]: the tokens that the cache holds for each sequence
+ *   new_tokens  int32 device [n_seqs]: how many more it gets, 0 is fine; NULL: one each
+ *   lens_out    int32 device [n_seqs]: lens[b] + new_tokens[b]; may be lens
+ *   page_table  entries of pages that a sequence needs and did not yet: ceil(lens[b] /
+ *               page_size) .. ceil(lens_out[b] / page_size) - 1 of its row, taken from the top
+ *               of the stack (free_pages[n_free[0] - 1] first) in the order of sequences and
+ *               pages; no other entry is written
+ *   n_free_out  int32 device [1]: what is left; may be n_free
+ *   row_start   int32 device [n_seqs + 1] or NULL: the new rows' starts, as uad_kv_append takes
+ *   slots       int64 device [n_rows] or NULL: the slot page * page_size + offset of each new
+ *               row's token, -1 from the last one on (n_rows is not looked at without them)
+ * All sequences get what they need, or none does: lengths or counts below 0 or beyond the
+ * table, more new rows than n_rows (or than 2^31 - 1), more pages than are free, or an
+ * n_free outside 0..n_pages raise UAD_E_PAGE (from uad_kv_synchronize); lens_out and
+ * n_free_out are lens and n_free then, row_start is all 0 and slots all -1, so that an append
+ * with that row_start adds nothing.  An id outside the pool goes into the table as it is,
+ * gives the slots -1 and raises UAD_E_PAGE too.
+ * Other arguments must not overlap.  Errors: UAD_E_INVALID (null pointer, n_rows or n_seqs
+ * below 0, slots unaligned), UAD_E_SHAPE (n_seqs beyond max_seqs, a page table of more than
+ * 2^30 tokens per sequence), UAD_E_HIP. */
+uad_status uad_kv_reserve(uad_kv *kv, const int32_t *lens, const int32_t *new_tokens, int32_t *lens_out, int32_t *page_table,
+                          int32_t pages_per_seq, int32_t n_seqs, const int32_t *free_pages, const int32_t *n_free,
+                          int32_t *n_free_out, int32_t *row_start, int64_t *slots, int32_t n_rows);
+
+/* Give back the pages that no later token of their sequence sees: every entry >= 0 of a
+ * table row, but those of pages that hold a position x < lens[b] with x < n_sinks, with
+ * x > lens[b] - window, or any such x if window is 0.  They go to the top of the stack in the
+ * order of sequences and entries, their entries become -1 and n_free[0] counts them.  So
+ * window 0 gives back what a shorter lens leaves over, all of a sequence's at length 0, and
+ * a decoding step with a window keeps what the window and the sinks need.  A page that
+ * several sequences read is given back for each of them: leave such rows out.
+ * Raised as UAD_E_PAGE: a length below 0 (its sequence keeps its pages), an id beyond the
+ * pool (it stays), an n_free outside 0..n_pages or more pages than the stack takes (nothing
+ * is given back).  Errors as uad_kv_reserve, and UAD_E_INVALID (window or n_sinks below 0,
+ * n_sinks without a window). */
+uad_status uad_kv_release(uad_kv *kv, const int32_t *lens, int32_t *page_table, int32_t pages_per_seq, int32_t n_seqs,
+                          int32_t *free_pages, int32_t *n_free, int32_t window, int32_t n_sinks);
+
 /* uad_set_prefix_kv from a paged cache: environment b's prefix is the first
  * prefix_len tokens of sequence b, in every layer (values of an 8-bit pool are
  * rounded to bf16).  The cache must have the expert's n_layers, n_kv_heads and

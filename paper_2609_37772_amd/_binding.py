@@ -23,6 +23,7 @@ __all__ = [
     "UAD_RELEASE_UAER", "UAD_RELEASE_TR", "UAD_FLAG_ADARMS",
     "uad_kv_create", "uad_kv_destroy", "uad_kv_last_error", "uad_kv_set_stream", "uad_kv_append", "uad_kv_attend",
     "uad_kv_synchronize", "uad_set_prefix_paged", "UAD_DTYPE_F8",
+    "uad_kv_set_block_scales", "uad_kv_attend_rows", "uad_kv_reserve", "uad_kv_release",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libuad.so")
@@ -39,6 +40,7 @@ EXPORTED_SYMBOLS = [
     "uad_profile_enable", "uad_profile_read",
     "uad_kv_create", "uad_kv_destroy", "uad_kv_last_error", "uad_kv_set_stream", "uad_kv_append", "uad_kv_attend",
     "uad_kv_synchronize", "uad_set_prefix_paged",
+    "uad_kv_set_block_scales", "uad_kv_attend_rows", "uad_kv_reserve", "uad_kv_release",
 ]
 
 
@@ -109,6 +111,10 @@ def load_library() -> ctypes.CDLL:
         "uad_kv_attend": ([P, I32, P, P, I32, I64, I64, P, P, P, I32, I32, F32], I32),
         "uad_kv_synchronize": ([P], I32),
         "uad_set_prefix_paged": ([P, P, P, P, I32, I32, I32], I32),
+        "uad_kv_set_block_scales": ([P, P, P], I32),
+        "uad_kv_attend_rows": ([P, I32, P, P, I32, I64, I64, I32, P, P, P, P, I32, I32, F32, I32, I32, I32], I32),
+        "uad_kv_reserve": ([P, P, P, P, P, I32, I32, P, P, P, P, P, I32], I32),
+        "uad_kv_release": ([P, P, P, I32, I32, P, P, I32, I32], I32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -538,6 +544,56 @@ def _attend_checked(kv, layer, q, out, page_table, lens, positions, scale, row_s
         raise ValueError("q and out must have a row per sequence")
     pp = None if positions is None else _ints(positions, (seqs,), "positions", device)
     return load_library().uad_kv_attend(kv, layer, q.data_ptr(), out.data_ptr(), dtype, ldq, ldo, pl, pp, pt, wide, seqs, scale)
+
+
+def uad_kv_set_block_scales(kv: int, k_scales: Optional[torch.Tensor], v_scales: Optional[torch.Tensor]) -> None:
+    """Scales for the blocks of an 8-bit cache (kept by the caller), or None for both: its one scale again."""
+    k, v = (None if t is None else t.data_ptr() for t in (k_scales, v_scales))
+    _check_kv(kv, load_library().uad_kv_set_block_scales(kv, k, v), "uad_kv_set_block_scales")
+
+
+def uad_kv_attend_rows(kv: int, layer: int, q: torch.Tensor, out: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor,
+                       row_start: Optional[torch.Tensor], positions: Optional[torch.Tensor], scale: float, window: int,
+                       n_sinks: int, causal: bool, row_shape: Tuple[int, int], device: int = 0) -> None:
+    """Attention of rows q [n_rows][Hq][hd], the newest of every sequence, over a layer's pages into out."""
+    n, dtype, ldq, ldo = _row_steps(q, out, row_shape, "q out", device)
+    pt, wide, pl, seqs = _table(page_table, lens, device)
+    ps = None if row_start is None else _ints(row_start, (seqs + 1,), "row_start", device)
+    pp = None if positions is None else _ints(positions, (n,), "positions", device)
+    st = load_library().uad_kv_attend_rows(kv, layer, q.data_ptr(), out.data_ptr(), dtype, ldq, ldo, n, ps, pl, pp, pt, wide, seqs,
+                                           scale, window, n_sinks, int(causal))
+    if st:
+        _check_kv(kv, st, "uad_kv_attend_rows")
+
+
+def uad_kv_reserve(kv: int, lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
+                   new_tokens: Optional[torch.Tensor], row_start: Optional[torch.Tensor], slots: Optional[torch.Tensor],
+                   lens_out: torch.Tensor, n_free_out: torch.Tensor, n_pages: int, device: int = 0) -> None:
+    """Pages for new tokens from the free ones into the page table (new_tokens None: one for each sequence)."""
+    pt, wide, pl, seqs = _table(page_table, lens, device)
+    po, pf = _ints(lens_out, (seqs,), "lens_out", device), _ints(free_pages, (n_pages,), "free_pages", device)
+    pn, pno = _ints(n_free, (1,), "n_free", device), _ints(n_free_out, (1,), "n_free_out", device)
+    px = None if new_tokens is None else _ints(new_tokens, (seqs,), "new_tokens", device)
+    ps = None if row_start is None else _ints(row_start, (seqs + 1,), "row_start", device)
+    n, pl64 = 0, None
+    if slots is not None:
+        if not isinstance(slots, torch.Tensor) or slots.dtype is not torch.int64 or slots.dim() != 1 \
+                or slots.get_device() != device or not slots.is_contiguous():
+            raise ValueError(f"slots must be a contiguous int64 tensor [n_rows] on device {device}")
+        n, pl64 = slots.shape[0], slots.data_ptr()
+    st = load_library().uad_kv_reserve(kv, pl, px, po, pt, wide, seqs, pf, pn, pno, ps, pl64, n)
+    if st:
+        _check_kv(kv, st, "uad_kv_reserve")
+
+
+def uad_kv_release(kv: int, lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
+                   window: int, n_sinks: int, n_pages: int, device: int = 0) -> None:
+    """The pages that no later token sees go back to the free ones."""
+    pt, wide, pl, seqs = _table(page_table, lens, device)
+    pf, pn = _ints(free_pages, (n_pages,), "free_pages", device), _ints(n_free, (1,), "n_free", device)
+    st = load_library().uad_kv_release(kv, pl, pt, wide, seqs, pf, pn, window, n_sinks)
+    if st:
+        _check_kv(kv, st, "uad_kv_release")
 
 
 def uad_kv_synchronize(kv: int) -> None:

@@ -1,0 +1,567 @@
+// Attention of new rows over a paged K/V cache: a prompt's, a few more of a conversation,
+// or a single token of each sequence, with a sliding window and sinks; pools in bf16, or
+// in 8 bits with one scale or one for every block of tokens.  What a row sees is in
+// paged.h.
+#include "paged_device.h"
+
+namespace uad {
+
+// ---------------------------------------------------------------------------
+// Few rows: the attention of one token (k_paged.inl) with other columns.  A unit is a KV
+// head of a sequence with up to 16 (row, query head) pairs in the order of the rows, the
+// 16 columns of the matrix instruction; each column has its own range of keys.  A
+// sequence's tiles are those that any of its rows sees, counted without the gap that a
+// window leaves behind the sinks, and are shared out in splits like the other's.
+//
+// Masks.  A tile that every column sees whole takes no part in them.  In any other, a
+// score that its column does not see becomes -inf; what no column of the unit sees may be
+// anything (slots never written, pages given back) and is zero in V.  A value that some
+// columns see and others do not must not reach the others through 0 * NaN: values that
+// are not finite are taken out, and the columns that see them become NaN.
+// ---------------------------------------------------------------------------
+struct RowsSeq {
+  int from, n, len, units;
+  SeenTiles tiles;
+};
+struct RowsWork {
+  RowsSeq s;
+  int b, unit, t0, t1, split, splits, slot;
+};
+
+__device__ __forceinline__ int runs_of(int rows, int group) { return (int)(((int64_t)rows * group + 15) / 16); }
+
+// Sequence b; one that cannot be used has no units.
+template <int TILE>
+__device__ __forceinline__ RowsSeq rows_of(const KvRowsArgs &a, int b, bool *bad) {
+  RowsSeq s{b, 1, 0, 0, {}};
+  if (a.row_start) {
+    s.from = a.row_start[b];
+    const int to = a.row_start[b + 1], len = a.lens[b];
+    const bool ok = sequence_ok(b, s.from, to, a.n_rows, len, a.pages_per_seq, a.d.page_shift);
+    *bad |= !ok;
+    s.n = ok ? to - s.from : 0;
+    s.len = ok ? len : 0;
+  } else {
+    s.len = length_or_none(a.lens[b], a.pages_per_seq, a.d.page_shift, bad);
+  }
+  s.units = a.d.n_kv_heads * runs_of(s.n, a.group);
+  s.tiles = seen_tiles(s.len, seen_from(s.len - s.n, a.window), a.sinks, TILE);
+  return s;
+}
+
+template <int HD, bool F8>
+__device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds, RowsWork *w) {
+  constexpr int TILE = kTileKeys<F8>, WHOLE = kAttendWhole<HD, F8>;
+  bool bad = false;
+  if (a.unsplit && !a.row_start) {  // no sequence can have a split: a workgroup per unit
+    const int units = a.d.n_kv_heads * runs_of(1, a.group);
+    *w = RowsWork{};
+    w->b = (unsigned)wg / (unsigned)units;
+    w->unit = wg - w->b * units;
+    w->s = rows_of<TILE>(a, w->b, &bad);
+    w->t1 = w->s.tiles.count;
+    w->splits = 1;
+    if (bad && threadIdx.x == 0) raise_status(a.status, kStatusPage);
+    return true;
+  }
+  PlanScan<kAttendWaves> scan(a.n_seqs, lds);
+  const int b0 = scan.me * scan.per;
+  RowsSeq s0{};
+  if (b0 < a.n_seqs) s0 = rows_of<TILE>(a, b0, &bad);
+  // f over this thread's sequences, of which the first is kept
+  auto each = [&](auto f) {
+    if (b0 < a.n_seqs) f(s0);
+    for (int i = 1; i < scan.per; ++i)
+      if (b0 + i < a.n_seqs) f(rows_of<TILE>(a, b0 + i, &bad));
+  };
+  int64_t n = 0;
+  int my_units = 0, units, hi, lo, mine, upto, wgs, all;
+  each([&](const RowsSeq &s) {
+    n += (int64_t)s.units * s.tiles.count;
+    my_units += s.units;
+  });
+  if (bad && wg == 0) raise_status(a.status, kStatusPage);
+  int share = 1 << 30;
+  if (!a.unsplit) {
+    scan((int)(n >> 22), &hi);
+    scan((int)(n & 0x3FFFFF), &lo);
+    share = first_share(((int64_t)hi << 22) + lo, a.target, kAttendMinTiles);
+  }
+  scan(my_units, &units);
+  auto count = [&]() {  // workgroups of this thread's sequences, and up to them
+    mine = 0;
+    each([&](const RowsSeq &s) { mine += splits_of(s.tiles.count, share, WHOLE) * s.units; });
+    upto = scan(mine, &wgs);
+  };
+  count();
+  // with fewer units than run at once
+  for (int i = 0; units < a.target && i < kShareTries && wgs > a.target; ++i) {
+    share = next_share(share);
+    count();
+  }
+  if (wg >= wgs) return false;
+  int in_slots = 0;  // workgroups in split units, for the slots
+  each([&](const RowsSeq &s) {
+    const int k = splits_of(s.tiles.count, share, WHOLE);
+    if (k > 1) in_slots += k * s.units;
+  });
+  int slot = scan(in_slots, &all) - in_slots, start = upto - mine, b = b0;
+  if (!scan.block) {
+    b = __builtin_ctzll(__ballot(upto > wg));
+    start = __builtin_amdgcn_readlane(start, b);
+    slot = __builtin_amdgcn_readlane(slot, b);
+    w->s.from = __builtin_amdgcn_readlane(s0.from, b);
+    w->s.n = __builtin_amdgcn_readlane(s0.n, b);
+    w->s.len = __builtin_amdgcn_readlane(s0.len, b);
+    w->s.units = __builtin_amdgcn_readlane(s0.units, b);
+    w->s.tiles.first = __builtin_amdgcn_readlane(s0.tiles.first, b);
+    w->s.tiles.gap = __builtin_amdgcn_readlane(s0.tiles.gap, b);
+    w->s.tiles.count = __builtin_amdgcn_readlane(s0.tiles.count, b);
+  } else {
+    if (upto > wg && start <= wg) {  // one thread: it looks for the sequence among its own
+      RowsSeq s = s0;
+      for (;;) {
+        const int k = splits_of(s.tiles.count, share, WHOLE);
+        if (start + k * s.units > wg) break;
+        start += k * s.units;
+        if (k > 1) slot += k * s.units;
+        if (++b >= min(b0 + scan.per, a.n_seqs)) break;
+        s = rows_of<TILE>(a, b, &bad);
+      }
+      const int found[3] = {b, start, slot};
+#pragma unroll
+      for (int i = 0; i < 3; ++i) scan.lds[i] = found[i];
+    }
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(scan.lds[0]);
+    start = __builtin_amdgcn_readfirstlane(scan.lds[1]);
+    slot = __builtin_amdgcn_readfirstlane(scan.lds[2]);
+    if (b >= a.n_seqs) return false;  // only if the caller's arrays change while this runs
+    w->s = rows_of<TILE>(a, b, &bad);
+  }
+  w->b = b;
+  w->splits = splits_of(w->s.tiles.count, share, WHOLE);
+  w->unit = (unsigned)(wg - start) / (unsigned)w->splits;
+  if (w->unit >= w->s.units) return false;  // likewise
+  w->split = wg - start - w->unit * w->splits;
+  w->slot = slot + w->unit * w->splits;
+  if (w->splits > 1 && w->slot + w->splits > a.slots) return false;  // likewise
+  w->t0 = split_begin(w->s.tiles.count, w->splits, w->split);
+  w->t1 = split_begin(w->s.tiles.count, w->splits, w->split + 1);
+  return true;
+}
+
+// 16-byte pieces of V that hold a value that is not finite: those become zeros in v, and
+// ones in the bf16 operand that is returned (its other elements zero).
+template <bool F8>
+__device__ __forceinline__ bool not_finite(u32x4_t v) {
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (F8) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) any |= (v[i] >> (8 * k) & 0x7F) == 0x7F;
+    } else {
+      any |= (v[i] & 0x7F80u) == 0x7F80u || (v[i] & 0x7F800000u) == 0x7F800000u;
+    }
+  }
+  return any;
+}
+template <bool F8>
+__device__ __forceinline__ bf16x8 take_not_finite(u32x4_t &v, int u) {
+  union {
+    bf16x8 h;
+    uint16_t e[8];
+  } o;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int i = F8 ? 2 * u + e / 4 : e / 2, shift = F8 ? 8 * (e % 4) : 16 * (e % 2);
+    const uint32_t top = F8 ? 0x7Fu : 0x7F80u, whole = F8 ? 0xFFu : 0xFFFFu;
+    const bool odd = (v[i] >> shift & top) == top;
+    o.e[e] = odd ? 0x3F80u : 0u;
+    if (odd) v[i] &= ~(whole << shift);
+  }
+  return o.h;
+}
+
+template <int HD, bool F32, bool F8>
+__global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves / 4) void kv_rows_kernel(KvRowsArgs a) {
+  constexpr int TILE = kTileKeys<F8>, NT = TILE / 16, KPL = 4 * NT;
+  constexpr int KS = HD / 32;           // k steps of Q K^T
+  constexpr int KL = F8 ? HD / 64 : KS; // 16-byte loads of a key row per lane
+  constexpr int NTO = HD / 16;          // 16-column tiles of the output
+  constexpr int TERMS = kTerms;
+  constexpr int NW = kAttendWaves;
+  constexpr int ESZ = F8 ? 1 : 2;
+  extern __shared__ __align__(16) float lds[];
+  __bf16 *qf = (__bf16 *)lds;                       // [TERMS][KS][64][8]
+  f32x4 *obuf = (f32x4 *)(lds + kQueryFloats<HD>);  // [NW][NTO][64]
+  float *ml = (float *)(obuf + NW * NTO * 64);      // [NW or slots][16][2]
+  float *top = ml + kAttendMl, *word = top + 32;
+  static_assert((kPlanScans + 1) * NW + 3 <= kAttendMl, "the plan fits the slots' weights");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  constexpr int HP = HD / 2, RS = 64 * NW / HP, QN = (16 + RS - 1) / RS;
+  const int p = threadIdx.x % HP;
+  int ea, eb;
+  rope_pair(p, a.rope_dim, a.rope_pairs != 0, &ea, &eb);
+  const bool turned = p < a.rope_dim / 2;
+  const double turns = a.turns[p];  // 128 of them are allocated
+
+  RowsWork w;
+  if (!plan_rows<HD, F8>(a, blockIdx.x, (int *)ml, &w)) return;
+  const int runs = w.s.units / a.d.n_kv_heads;
+  const int kvh = w.unit / runs, m0 = (w.unit - kvh * runs) * 16, cols = min(16, w.s.n * a.group - m0);
+  const int last = w.s.len - 1, mask = (1 << a.d.page_shift) - 1;
+  const int32_t *table = a.table + (int64_t)w.b * a.pages_per_seq;
+  // column m of the unit's sequence: row m / group, query head kvh * group + m % group
+  auto row_of = [&](int m) { return (int)((unsigned)m / (unsigned)a.group); };
+  const int pos0 = w.s.len - w.s.n;  // of the sequence's first row
+  auto from_of = [&](int col) { return seen_from(pos0 + row_of(m0 + col), a.window); };
+  auto to_of = [&](int col) { return min(seen_to(pos0 + row_of(m0 + col), w.s.len, a.window, a.causal), w.s.len); };
+  const int my_col = min(c, cols - 1), lo = from_of(my_col), hi = to_of(my_col);
+  const int lo_min = from_of(0), lo_max = from_of(cols - 1), hi_min = to_of(0), hi_max = to_of(cols - 1);
+  auto tile_at = [&](int i) { return seen_tile(w.s.tiles, i) * TILE; };  // its first key
+  // keys key .. key + n - 1 that some column sees, or this lane's column does, as bits
+  auto seen_by_any = [&](int key, int n) { return run_bits(lo_min - key, hi_max - key, n) | run_bits(-key, min(a.sinks, hi_max) - key, n); };
+  auto seen_by_mine = [&](int key, int n) { return run_bits(lo - key, hi - key, n) | run_bits(-key, min(a.sinks, hi) - key, n); };
+  bool bad = false;
+
+  // Loads are waited for in the order of their issue: page ids and the query's values
+  // first, then the keys and values, which arrive while the query is rotated.
+  auto page_ids = [&](int i, int &kp, int &vp) {
+    const int k0 = tile_at(i);
+    kp = table[min(k0 + KPL * (c >> 2), last) >> a.d.page_shift];
+    vp = table[min(k0 + KPL * g, last) >> a.d.page_shift];
+  };
+  auto checked = [&](int page, int key) {  // of a run of keys; one that nobody sees is not looked at
+    if (seen_by_any(key, KPL) == 0) return 0;
+    const bool ok = page_ok(a.d, page);
+    bad |= !ok;
+    return ok ? page : 0;
+  };
+  u32x4_t kr[NT][KL], vr[NTO];
+  float ks = 1.f, vs = 1.f, next_ks = 1.f, next_vs = 1.f;  // scales of the lane group's run
+  auto load_k = [&](int i, int page, int v_page) {
+    const int k0 = tile_at(i);
+    const char *src = (const char *)a.kp + (page_base(a.d, checked(page, k0 + KPL * (c >> 2)), kvh) + (F8 ? 16 : 8) * g) * ESZ;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int off = min(k0 + KPL * (c >> 2) + 4 * t + (c & 3), last) & mask;
+#pragma unroll
+      for (int j = 0; j < KL; ++j) kr[t][j] = *(const u32x4_t *)(src + (unsigned)(off * HD * ESZ) + j * 64);
+    }
+    if constexpr (F8)
+      if (a.k_scales) {
+        const int key = k0 + KPL * g;
+        const size_t at = scale_index(a.d, checked(v_page, key), kvh, min(key, last) & mask);
+        const bool seen = seen_by_any(key, KPL) != 0;  // else the scale may be anything
+        next_ks = seen ? a.k_scales[at] : 1.f;
+        next_vs = seen ? a.v_scales[at] : 1.f;
+      }
+  };
+  auto load_v = [&](int i, int page) {
+    const int key = tile_at(i) + KPL * g, off = min(key, last & ~(KPL - 1)) & mask;
+    const char *src = (const char *)a.vp + (page_base(a.d, checked(page, key), kvh) + off + (c << a.d.page_shift)) * ESZ;
+#pragma unroll
+    for (int n = 0; n < NTO; ++n) vr[n] = *(const u32x4_t *)(src + (unsigned)((n * 16 << a.d.page_shift) * ESZ));
+  };
+
+  int tile = w.t0 + wave;
+  const int t1 = last >= 0 ? w.t1 : 0;
+  int kp = 0, vp = 0, next_kp = 0, next_vp = 0;
+  if (tile < t1) page_ids(tile, kp, vp);
+  if (tile + NW < t1) page_ids(tile + NW, next_kp, next_vp);
+  uint32_t qx[QN], qy[QN];
+  int position[QN];
+#pragma unroll
+  for (int i = 0; i < QN; ++i) {
+    const int m = m0 + min((int)threadIdx.x / HP + i * RS, cols - 1), j = row_of(m);
+    const int64_t qi = (int64_t)(w.s.from + j) * a.ldq + (int64_t)(kvh * a.group + m - j * a.group) * HD;
+    position[i] = a.positions ? a.positions[w.s.from + j] : pos0 + j;
+    qx[i] = load_raw<F32>(a.q, qi + ea);
+    qy[i] = load_raw<F32>(a.q, qi + eb);
+  }
+  if (tile < t1) {
+    load_k(tile, kp, vp);
+    load_v(tile, vp);
+  }
+
+  // the query, rotated, as bf16 terms in operand order; columns past the unit's are zero
+  {
+    auto at = [&](int e, int row) {  // operand element of column e
+      if constexpr (F8) return (((e >> 6) * 2 + ((e >> 3) & 1)) * 64 + ((e >> 4) & 3) * 16 + row) * 8 + (e & 7);
+      else return ((e >> 5) * 64 + ((e >> 3) & 3) * 16 + row) * 8 + (e & 7);
+    };
+#pragma unroll
+    for (int i = 0; i < QN; ++i) {
+      const int col = threadIdx.x / HP + i * RS;
+      if (col >= 16) break;
+      float sn = 0.f, cs = 1.f;
+      if (turned) turn_of(turns, position[i], &sn, &cs);
+      const float x = col < cols ? value_of<F32>(qx[i]) : 0.f, y = col < cols ? value_of<F32>(qy[i]) : 0.f;
+      float v0 = turned ? x * cs - y * sn : x, v1 = turned ? y * cs + x * sn : y;
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t) {
+        const __bf16 h0 = (__bf16)v0, h1 = (__bf16)v1;
+        qf[t * KS * 512 + at(ea, col)] = h0;
+        qf[t * KS * 512 + at(eb, col)] = h1;
+        v0 -= (float)h0;
+        v1 -= (float)h1;
+      }
+    }
+  }
+  __syncthreads();
+
+  f32x4 o[NTO];
+#pragma unroll
+  for (int n = 0; n < NTO; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  for (; tile < t1; tile += NW) {
+    // the query's operands are read anew for every tile: kept, they would take up to 96
+    // registers from the tiles in flight
+    asm volatile("" ::: "memory");
+    f32x4 s[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < KS; ++kb) {
+      bf16x8 qt[TERMS];
+#pragma unroll
+      for (int i = 0; i < TERMS; ++i) qt[i] = *(const bf16x8 *)(qf + ((i * KS + kb) * 64 + lane) * 8);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const bf16x8 kf = operand_of<F8>(kr[t][F8 ? kb / 2 : kb], kb & 1);
+#pragma unroll
+        for (int i = TERMS - 1; i >= 0; --i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qt[i], s[t], 0, 0, 0);
+      }
+    }
+    ks = next_ks;
+    vs = next_vs;
+    vp = next_vp;
+    const bool more = tile + NW < t1;
+    if (more) {
+      kp = next_kp;
+      if (tile + 2 * NW < t1) page_ids(tile + 2 * NW, next_kp, next_vp);
+      load_k(tile + NW, kp, vp);
+    }
+    // scores in powers of two, keys that the column does not see masked
+    const int k0 = tile_at(tile), key0 = k0 + KPL * g;
+    const bool edge = k0 + TILE > hi_min || (k0 < lo_max && k0 + TILE > a.sinks);
+    const uint32_t seen = edge ? seen_by_mine(key0, KPL) : 0xFFFFFFFFu;
+    const float to_log2 = F8 ? a.scale_log2 * ks : a.scale_log2;
+    float mt = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float v = s[t][r] * to_log2;
+        if (edge && !(seen >> (4 * t + r) & 1)) v = -INFINITY;
+        s[t][r] = v;
+        mt = fmaxf(mt, v);
+      }
+    mt = max_pair32(max_pair16(mt));
+    // the running maximum is raised when it is passed by more than 2^8 (the weights
+    // stay below that); all lanes of a query agree
+    if (__ballot(mt > m + kKvRescale || m == -INFINITY)) {
+      const float m1 = fmaxf(m, mt), f = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
+      m = m1;
+      l *= f;
+#pragma unroll
+      for (int n = 0; n < NTO; ++n) o[n] *= f;
+    }
+    const float unit = m == -INFINITY ? 0.f : m;  // nothing seen yet: every weight is 2^-inf
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[t][r] = __builtin_amdgcn_exp2f(s[t][r] - unit);
+        l += s[t][r];
+        if constexpr (F8) {  // weights that are not seen stay zero whatever the scale is
+          const float v = s[t][r] * vs;
+          s[t][r] = edge && !(seen >> (4 * t + r) & 1) ? 0.f : v;
+        }
+      }
+    bool odd = false;
+    if (edge) {
+      constexpr int PER = F8 ? 4 : 2;  // elements of a register
+      const uint32_t any = seen_by_any(key0, KPL);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t keep = 0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) keep |= (any >> (i * PER + e) & 1) ? (F8 ? 0xFFu : 0xFFFFu) << (e * 32 / PER) : 0u;
+#pragma unroll
+        for (int k = 0; k < NTO; ++k) vr[k][i] &= keep;
+      }
+#pragma unroll
+      for (int k = 0; k < NTO; ++k) odd |= not_finite<F8>(vr[k]);
+      odd = __ballot(odd) != 0;
+    }
+#pragma unroll
+    for (int u = 0; u < NT / 2; ++u) {  // 8 weights of the lane, as terms
+      if (odd) {
+        union {
+          bf16x8 v;
+          uint16_t e[8];
+        } sees;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sees.e[e] = seen >> (8 * u + e) & 1 ? 0x3F80u : 0u;
+#pragma unroll
+        for (int n = 0; n < NTO; ++n) {
+          const bf16x8 vf = take_not_finite<F8>(vr[n], u);
+          const f32x4 hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, sees.v, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[n][r] = hits[r] > 0.f ? NAN : o[n][r];
+        }
+      }
+      union {
+        bf16x8 v;
+        __bf16 e[8];
+      } pf[TERMS];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float q = s[2 * u + e / 4][e % 4];
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i) {
+          pf[i].e[e] = (__bf16)q;
+          q -= (float)pf[i].e[e];
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NTO; ++n) {
+        const bf16x8 vf = operand_of<F8>(vr[n], u);
+#pragma unroll
+        for (int i = TERMS - 1; i >= 0; --i) o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[i].v, o[n], 0, 0, 0);
+      }
+    }
+    if (more) load_v(tile + NW, vp);
+  }
+  if (bad) raise_status(a.status, kStatusPage);
+
+  // The waves meet: maxima, sums and outputs, each in units of its wave's maximum, of half
+  // the waves where no others had a tile.
+  const bool all = t1 - w.t0 > NW / 2;
+  l = sum_pair32(sum_pair16(l));
+  if (g == 0) {
+    ml[(wave * 16 + c) * 2] = m;
+    ml[(wave * 16 + c) * 2 + 1] = l;
+  }
+  if (c < cols && (all || wave < NW / 2))
+#pragma unroll
+    for (int n = 0; n < NTO; ++n) obuf[(wave * NTO + n) * 64 + lane] = o[n];
+  __syncthreads();
+  float mx = -INFINITY, sum = 0.f, f[NW];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) mx = fmaxf(mx, ml[(i * 16 + c) * 2]);
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    const float li = ml[(i * 16 + c) * 2 + 1];
+    f[i] = li != 0.f ? __builtin_amdgcn_exp2f(ml[(i * 16 + c) * 2] - mx) : 0.f;
+    sum += li * f[i];
+  }
+  const bool vec = a.out_vec;
+  auto put_out = [&](int col, int e, f32x4 v, float total) {
+    const float scale = total != 0.f ? a.v_scale / total : 0.f;
+    const int j = row_of(m0 + col);
+    const int64_t oi = (int64_t)(w.s.from + j) * a.ldo + (int64_t)(kvh * a.group + m0 + col - j * a.group) * HD + e;
+    v *= scale;
+    if (vec) {
+      if constexpr (F32) *(f32x4 *)((float *)a.out + oi) = v;
+      else *(bf16x4 *)((__bf16 *)a.out + oi) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) store_elem<F32>(a.out, oi + r, v[r]);
+    }
+  };
+  const int slot = w.slot + w.split;
+  const auto slots = slots_of(a, 16 * HD);
+  if (c < cols) {
+    for (int n = wave; n < NTO; n += NW) {
+      f32x4 v = obuf[n * 64 + lane] * f[0];
+#pragma unroll
+      for (int i = 1; i < NW / 2; ++i) v += obuf[(i * NTO + n) * 64 + lane] * f[i];
+      if (all)
+#pragma unroll
+        for (int i = NW / 2; i < NW; ++i) v += obuf[(i * NTO + n) * 64 + lane] * f[i];
+      if (w.splits == 1) put_out(c, 16 * n + 4 * g, v, sum);
+      else put_slot(slots, (slot * 16 + c) * HD + 16 * n + 4 * g, v);
+    }
+    if (w.splits > 1 && wave == 0 && g == 0)
+      __hip_atomic_store(a.part_ml + (size_t)slot * 16 + c, pair_of(mx, sum), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  if (w.splits == 1) return;
+
+  // many splits: runs of kJoinFan first, into the first slot of each
+  bool final = w.splits <= 2 * kJoinFan;
+  for (;;) {
+    const int run = w.split / kJoinFan * kJoinFan;
+    const int first = final ? w.slot : w.slot + run, step = final && w.splits > 2 * kJoinFan ? kJoinFan : 1;
+    const int n = !final ? min(kJoinFan, w.splits - run) : (w.splits + step - 1) / step;
+    if (!last_to_arrive(a.arrived + (final ? a.slots : 0) + first, n, word)) return;
+    join_slots<HD>(a, cols, 16, first, step, n, ml, top, obuf, [&](int col, int e, f32x4 v, float total) {
+      if (final) put_out(col, e, v, total);
+      else put_slot(slots, (first * 16 + col) * HD + e, v);
+    });
+    if (final) return;
+    if ((int)threadIdx.x < cols)
+      __hip_atomic_store(a.part_ml + (size_t)first * 16 + threadIdx.x,
+                         pair_of(top[2 * threadIdx.x], top[2 * threadIdx.x + 1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    final = true;
+  }
+}
+
+template <int HD, bool F32, bool F8>
+static hipError_t rows_attr() {
+  return hipFuncSetAttribute((const void *)kv_rows_kernel<HD, F32, F8>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                             attend_lds_floats<HD>() * 4);
+}
+template <int HD>
+static hipError_t rows_attrs() {
+  hipError_t e = rows_attr<HD, true, true>();
+  if (e == hipSuccess) e = rows_attr<HD, true, false>();
+  if (e == hipSuccess) e = rows_attr<HD, false, true>();
+  if (e == hipSuccess) e = rows_attr<HD, false, false>();
+  return e;
+}
+hipError_t kv_rows_init(int head_dim) {
+  return head_dim == 64 ? rows_attrs<64>() : head_dim == 128 ? rows_attrs<128>() : rows_attrs<256>();
+}
+
+template <int HD, bool F32, bool F8>
+static hipError_t launch_rows_type(KvRowsArgs a, hipStream_t s) {
+  constexpr int TILE = kTileKeys<F8>;
+  // as many workgroups as any lengths could need: a unit more for every sequence whose
+  // last has fewer columns, and a split more for each of the slots
+  const int64_t columns = (int64_t)a.n_rows * a.group;
+  const int64_t units = a.d.n_kv_heads * (a.row_start ? columns / 16 + a.n_seqs : (int64_t)a.n_seqs * ((a.group + 15) / 16));
+  int64_t most = std::min<int64_t>((int64_t)a.pages_per_seq << a.d.page_shift, 0x7FFFFFFF);
+  int64_t tiles = tiles_of_length((int)most, TILE);
+  // a window's, of up to all the rows, and the sinks', each in a tile more than they fill
+  if (a.window > 0) tiles = std::min(tiles, ((int64_t)a.window + (a.row_start ? a.n_rows : 1)) / TILE + a.sinks / TILE + 4);
+  const int64_t splits = splits_of((int)tiles, kAttendMinTiles, kAttendWhole<HD, F8>);
+  const int64_t grid = std::min(units * splits, units + a.slots);
+  a.unsplit = splits == 1;
+  hipLaunchKernelGGL((kv_rows_kernel<HD, F32, F8>), dim3((unsigned)grid), dim3(64 * kAttendWaves),
+                     (attend_lds_floats<HD>() * 4), s, a);
+  return hipGetLastError();
+}
+
+template <int HD>
+static hipError_t launch_rows_hd(const KvRowsArgs &a, bool f32, bool f8, hipStream_t s) {
+  if (f32) return f8 ? launch_rows_type<HD, true, true>(a, s) : launch_rows_type<HD, true, false>(a, s);
+  return f8 ? launch_rows_type<HD, false, true>(a, s) : launch_rows_type<HD, false, false>(a, s);
+}
+
+hipError_t launch_kv_rows(const KvRowsArgs &a, bool f32, bool f8, hipStream_t s) {
+  if (a.n_seqs < 1 || a.n_rows < 1 || a.group < 1 || a.n_heads != a.group * a.d.n_kv_heads || a.pages_per_seq < 1 ||
+      a.target < 1 || a.slots < max_slots(a.target) || a.d.page_shift < 4 || a.window < 0 || a.sinks < 0 ||
+      (!a.row_start && a.n_rows != a.n_seqs) || (!f8 && a.k_scales))
+    return hipErrorInvalidValue;
+  if (a.d.head_dim == 64) return launch_rows_hd<64>(a, f32, f8, s);
+  if (a.d.head_dim == 128) return launch_rows_hd<128>(a, f32, f8, s);
+  if (a.d.head_dim == 256) return launch_rows_hd<256>(a, f32, f8, s);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace uad

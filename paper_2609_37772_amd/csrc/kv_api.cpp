@@ -1,59 +1,17 @@
 // C ABI of the paged K/V cache: handle, argument checks, kernel arguments.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <cmath>
 #include <new>
 #include <string>
 
-#include "kv_internal.h"
+#include "kv_call.h"
 
 using namespace uad;
 
 namespace {
 
 thread_local std::string g_kv_create_err;
-
-// Every entry point leaves the calling thread's device as it found it, and lets no
-// exception (of a message's allocation, say) out into the caller's C.
-class OnDevice {
- public:
-  explicit OnDevice(int device) {
-    err_ = hipGetDevice(&was_);
-    if (err_ == hipSuccess && was_ != device) {
-      err_ = hipSetDevice(device);
-      back_ = err_ == hipSuccess;
-    }
-  }
-  ~OnDevice() {
-    if (back_) (void)hipSetDevice(was_);
-  }
-  hipError_t err() const { return err_; }
-
- private:
-  int was_ = 0;
-  bool back_ = false;
-  hipError_t err_ = hipSuccess;
-};
-
-uad_status kv_fail(uad_kv *kv, uad_status st, const char *fn, const char *what) {
-  try {
-    kv->err = std::string(fn) + ": " + what;
-  } catch (...) {
-    kv->err.clear();
-  }
-  return st;
-}
-
-uad_status kv_hip_fail(uad_kv *kv, hipError_t e, const char *fn, const char *what) {
-  (void)hipGetLastError();
-  try {
-    kv->err = std::string(fn) + ": " + what + ": " + hipGetErrorString(e);
-  } catch (...) {
-    kv->err.clear();
-  }
-  return UAD_E_HIP;
-}
 
 uad_status ctx_fail(uad_ctx *c, uad_status st, const char *what) {
   try {
@@ -62,57 +20,6 @@ uad_status ctx_fail(uad_ctx *c, uad_status st, const char *what) {
     c->err.clear();
   }
   return st;
-}
-
-// Whether `bytes` from p on are device memory of `device`, in one allocation or in
-// adjacent ones: a kernel would read and write past a shorter one.
-bool device_range(int device, const void *p, size_t bytes) {
-  const char *at = (const char *)p, *const end = at + bytes;
-  while (at < end) {
-    hipPointerAttribute_t pa{};
-    hipDeviceptr_t base = nullptr;
-    size_t size = 0;
-    if (hipPointerGetAttributes(&pa, at) != hipSuccess || pa.type != hipMemoryTypeDevice || pa.device != device ||
-        hipMemGetAddressRange(&base, &size, (hipDeviceptr_t)at) != hipSuccess || (const char *)base + size <= at) {
-      (void)hipGetLastError();
-      return false;
-    }
-    at = (const char *)base + size;
-  }
-  return true;
-}
-
-PagedDims dims_of(const uad_kv *kv) {
-  PagedDims d{};
-  d.n_pages = kv->cfg.n_pages;
-  while ((1 << d.page_shift) < kv->cfg.page_size) ++d.page_shift;
-  d.n_kv_heads = kv->cfg.n_kv_heads;
-  d.head_dim = kv->cfg.head_dim;
-  return d;
-}
-
-size_t pool_esz(const uad_kv *kv) { return kv->cfg.dtype == UAD_DTYPE_F8 ? 1 : 2; }
-void *layer_of(const uad_kv *kv, void *pool, int layer) { return (char *)pool + layer * kv->layer_elems * pool_esz(kv); }
-
-// Row strides (elements) and tokens of a sequence: products with row numbers stay
-// within 64 bits, positions and the tiles behind the last one within 32.
-constexpr int64_t kMaxLd = (int64_t)1 << 30, kMaxTokens = (int64_t)1 << 30;
-
-bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-
-// What append and attend check alike.
-uad_status check_call(uad_kv *kv, const char *fn, int layer, int dtype, const void *a, const void *b, const void *lens,
-                      const void *table, int pages_per_seq, int n_seqs) {
-  if (layer < 0 || layer >= kv->cfg.n_layers) return kv_fail(kv, UAD_E_INVALID, fn, "no such layer");
-  if (dtype != UAD_DTYPE_F32 && dtype != UAD_DTYPE_BF16) return kv_fail(kv, UAD_E_INVALID, fn, "bad dtype");
-  if (n_seqs < 0 || pages_per_seq < 1) return kv_fail(kv, UAD_E_INVALID, fn, "n_seqs must be >= 0, pages_per_seq >= 1");
-  if (n_seqs > kv->cfg.max_seqs) return kv_fail(kv, UAD_E_SHAPE, fn, "n_seqs > max_seqs");
-  if ((int64_t)pages_per_seq * kv->cfg.page_size > kMaxTokens)
-    return kv_fail(kv, UAD_E_SHAPE, fn, "a page table of more than 2^30 tokens per sequence");
-  if (n_seqs > 0 && (!a || !b || !lens || !table)) return kv_fail(kv, UAD_E_INVALID, fn, "null pointer");
-  const size_t esz = dtype == UAD_DTYPE_F32 ? 4 : 2;
-  if (!aligned(a, esz) || !aligned(b, esz)) return kv_fail(kv, UAD_E_INVALID, fn, "data not aligned to its type");
-  return UAD_OK;
 }
 
 }  // namespace
@@ -182,9 +89,10 @@ uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_str
   hipError_t e = hipDeviceGetAttribute(&kv->n_cu, hipDeviceAttributeMultiprocessorCount, device);
   if (e != hipSuccess) return cerr(UAD_E_HIP, "hipDeviceGetAttribute", e);
   const size_t o_turns = 256, n_turns = m.rope_dim / 2;
-  const size_t rows = std::min(16, m.n_heads / m.n_kv_heads);
+  const size_t rows = 16;  // of a slot; a single token's attention takes up to its group
   kv->slots = max_slots(kv_attend_target(kv->n_cu, m.head_dim));
-  const size_t o_arrived = o_turns + 128 * sizeof(double), o_ml = o_arrived + 2 * (size_t)kv->slots * sizeof(unsigned);
+  const size_t o_arrived = o_turns + 128 * sizeof(double), o_pages = o_arrived + 2 * (size_t)kv->slots * sizeof(unsigned);
+  const size_t o_ml = (o_pages + (1 + (size_t)m.max_seqs) * sizeof(unsigned) + 255) / 256 * 256;
   const size_t o_part = o_ml + kv->slots * rows * sizeof(uint64_t);
   const size_t total = o_part + kv->slots * rows * m.head_dim * sizeof(float);
   e = hipMalloc(&kv->buf, total);
@@ -194,6 +102,8 @@ uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_str
   kv->status = (unsigned *)kv->buf;
   kv->turns = (double *)((char *)kv->buf + o_turns);
   kv->arrived = (unsigned *)((char *)kv->buf + o_arrived);
+  kv->pages_arrived = (unsigned *)((char *)kv->buf + o_pages);
+  kv->page_counts = (int32_t *)kv->pages_arrived + 1;
   kv->part_ml = (uint64_t *)((char *)kv->buf + o_ml);
   kv->part = (float *)((char *)kv->buf + o_part);
   if (e == hipSuccess) e = kv_attend_init(m.head_dim);
@@ -259,6 +169,7 @@ uad_status uad_kv_append(uad_kv *kv, int32_t layer, const void *k, const void *v
   a.in_vec = aligned(k, 16) && aligned(v, 16) && ldk % per16 == 0 && ldv % per16 == 0;
   a.k_scale = kv->cfg.k_scale; a.v_scale = kv->cfg.v_scale;
   a.k_inv = 1.f / a.k_scale; a.v_inv = 1.f / a.v_scale;
+  a.k_scales = scales_of(kv, kv->k_scales, layer); a.v_scales = scales_of(kv, kv->v_scales, layer);
   a.status = kv->status;
   const hipError_t e = launch_kv_append(a, dtype == UAD_DTYPE_F32, kv->cfg.dtype == UAD_DTYPE_F8, kv->stream);
   return e == hipSuccess ? UAD_OK : kv_hip_fail(kv, e, fn, "launch");
@@ -289,6 +200,7 @@ uad_status uad_kv_attend(uad_kv *kv, int32_t layer, const void *q, void *out, in
   a.turns = kv->turns; a.rope_dim = kv->cfg.rope_dim; a.rope_pairs = kv->cfg.rope_pairs;
   a.scale_log2 = scale_log2;
   a.v_scale = kv->cfg.v_scale;
+  a.k_scales = scales_of(kv, kv->k_scales, layer); a.v_scales = scales_of(kv, kv->v_scales, layer);
   a.status = kv->status;
   a.part = kv->part; a.part_ml = kv->part_ml; a.arrived = kv->arrived; a.slots = kv->slots;
   a.target = kv_attend_target(kv->n_cu, kv->cfg.head_dim);
@@ -319,6 +231,7 @@ uad_status uad_set_prefix_paged(uad_ctx *c, uad_kv *kv, const int32_t *lens, con
   a.lens = lens; a.table = page_table; a.pages_per_seq = pages_per_seq;
   a.n_keys = prefix_len; a.s_alloc = c->s_alloc; a.dst_layer = c->kv_layer_elems; a.kc = c->kcache; a.vtc = c->vtcache;
   a.k_scale = kv->cfg.k_scale; a.v_scale = kv->cfg.v_scale;
+  a.k_scales = kv->k_scales; a.v_scales = kv->v_scales; a.scale_layer = kv->layer_elems / kv->cfg.head_dim / kScaleBlock;
   a.status = kv->status; a.ctx_status = c->status;
   // The context's queued steps read the old prefix before this, the cache's queued
   // appends come before it and later ones after it.

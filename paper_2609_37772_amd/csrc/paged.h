@@ -132,4 +132,69 @@ UAD_HD int split_begin(int tiles, int n, int s) {
 // twice tiles / share of them, and total / share is at most `target`.
 UAD_HD int max_slots(int target) { return 2 * target; }
 
+// ---------------------------------------------------------------------------
+// 8-bit pools with scales of their own: one for K and one for V of every kScaleBlock
+// tokens of a page's head, [page][KV head][page size / kScaleBlock].
+// ---------------------------------------------------------------------------
+constexpr int kScaleBlock = 16;
+
+UAD_HD size_t scale_index(const PagedDims &d, int page, int head, int off) {
+  return (((((size_t)page * d.n_kv_heads + head) << d.page_shift) + off)) / kScaleBlock;
+}
+
+// The least power of two by which magnitudes up to one of these bits (finite, no sign) lie
+// within 448 = 1.75 * 2^8, from 2^-100 (blocks of zeros) up to 2^119, whose product with
+// 448 is finite (larger values are cut): its bits.
+UAD_HD uint32_t scale_bits(uint32_t most) {
+  int e = (int)(most >> 23) - 127 - 8 + ((most & 0x7FFFFFu) > 0x600000u);
+  e = e < -100 ? -100 : e > 119 ? 119 : e;
+  return (uint32_t)(e + 127) << 23;
+}
+
+// ---------------------------------------------------------------------------
+// Attention of new rows: what a row at cache position p of a sequence of `len` tokens
+// sees, keys [lo, hi) and those before min(sinks, hi).  window 0: no window.
+// ---------------------------------------------------------------------------
+UAD_HD int seen_from(int p, int window) { return window > 0 && p >= window ? p - window + 1 : 0; }
+UAD_HD int seen_to(int p, int len, int window, bool causal) {
+  return causal ? p + 1 : window > 0 && window < len - p ? p + window : len;
+}
+
+// The tiles of `tile` keys that rows see of which the first sees from `lo`, counted
+// without the gap behind the sinks: tile i of them is tile i + (i < first ? 0 : gap).
+struct SeenTiles {
+  int first, gap, count;
+};
+UAD_HD SeenTiles seen_tiles(int len, int lo, int sinks, int tile) {
+  const int from = (int)((uint32_t)lo / (uint32_t)tile), s = sinks < lo ? sinks : lo;
+  const int t = (int)(((uint32_t)s + tile - 1) / tile);
+  SeenTiles r;
+  r.first = t < from ? t : from;
+  r.gap = from - r.first;
+  r.count = tiles_of_length(len, tile) - r.gap;
+  return r;
+}
+UAD_HD int seen_tile(const SeenTiles &s, int i) { return i < s.first ? i : i + s.gap; }
+
+// Bits from .. to-1 of a lane's run of `n` keys (n <= 32), whatever lies outside of it.
+UAD_HD uint32_t run_bits(int from, int to, int n) {
+  from = from < 0 ? 0 : from;
+  to = to > n ? n : to;
+  return to <= from ? 0u : (0xFFFFFFFFu >> (32 - (to - from))) << from;
+}
+
+// ---------------------------------------------------------------------------
+// Pages of new tokens.  Sequence b holds `len` tokens and gets n more: it needs pages
+// pages_of(len) .. pages_of(len + n) - 1 of its table row.
+// ---------------------------------------------------------------------------
+UAD_HD int pages_of(int len, int page_shift) { return (int)(((uint32_t)len + (1u << page_shift) - 1) >> page_shift); }
+UAD_HD bool growth_ok(int len, int n, int pages_per_seq, int page_shift) {
+  return len >= 0 && n >= 0 && (int64_t)len + n <= (int64_t)pages_per_seq << page_shift;
+}
+// Whether page i of a sequence of `len` tokens holds one that a later token sees.
+UAD_HD bool page_in_use(int i, int len, int window, int sinks, int page_shift) {
+  const int64_t from = (int64_t)i << page_shift, to = from + ((int64_t)1 << page_shift);
+  return from < len && (from < sinks || window == 0 || to > (int64_t)len - window + 1);
+}
+
 }  // namespace uad
