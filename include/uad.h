@@ -503,7 +503,7 @@ uad_status uad_kv_reserve(uad_kv *kv, const int32_t *lens, const int32_t *new_to
 
 /* Give back the pages that no later token of their sequence sees: every entry >= 0 of a
  * table row, but those of pages that hold a position x < lens[b] with x < n_sinks, with
- * x > lens[b] - window, or any such x if window is 0.  They go to the top of the stack in the
+ * x > lens[b] - window, or any such x if window is 0, and of a last page that is not full.  They go to the top of the stack in the
  * order of sequences and entries, their entries become -1 and n_free[0] counts them.  So
  * window 0 gives back what a shorter lens leaves over, all of a sequence's at length 0, and
  * a decoding step with a window keeps what the window and the sinks need.  A page that

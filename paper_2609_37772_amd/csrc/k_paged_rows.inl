@@ -219,12 +219,14 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   const int pos0 = w.s.len - w.s.n;  // of the sequence's first row
   auto from_of = [&](int col) { return seen_from(pos0 + row_of(m0 + col), a.window); };
   auto to_of = [&](int col) { return min(seen_to(pos0 + row_of(m0 + col), w.s.len, a.window, a.causal), w.s.len); };
-  const int my_col = min(c, cols - 1), lo = from_of(my_col), hi = to_of(my_col);
+  auto first_of = [&](int col) { return seen_first(pos0 + row_of(m0 + col), w.s.len, a.sinks, a.causal); };
+  const int my_col = min(c, cols - 1), lo = from_of(my_col), hi = to_of(my_col), first = first_of(my_col);
   const int lo_min = from_of(0), lo_max = from_of(cols - 1), hi_min = to_of(0), hi_max = to_of(cols - 1);
+  const int first_min = first_of(0), first_max = first_of(cols - 1);
   auto tile_at = [&](int i) { return seen_tile(w.s.tiles, i) * TILE; };  // its first key
   // keys key .. key + n - 1 that some column sees, or this lane's column does, as bits
-  auto seen_by_any = [&](int key, int n) { return run_bits(lo_min - key, hi_max - key, n) | run_bits(-key, min(a.sinks, hi_max) - key, n); };
-  auto seen_by_mine = [&](int key, int n) { return run_bits(lo - key, hi - key, n) | run_bits(-key, min(a.sinks, hi) - key, n); };
+  auto seen_by_any = [&](int key, int n) { return run_bits(lo_min - key, hi_max - key, n) | run_bits(-key, first_max - key, n); };
+  auto seen_by_mine = [&](int key, int n) { return run_bits(lo - key, hi - key, n) | run_bits(-key, first - key, n); };
   bool bad = false;
 
   // Loads are waited for in the order of their issue: page ids and the query's values
@@ -347,7 +349,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
     }
     // scores in powers of two, keys that the column does not see masked
     const int k0 = tile_at(tile), key0 = k0 + KPL * g;
-    const bool edge = k0 + TILE > hi_min || (k0 < lo_max && k0 + TILE > a.sinks);
+    const bool edge = (k0 < lo_max || k0 + TILE > hi_min) && k0 + TILE > first_min;
     const uint32_t seen = edge ? seen_by_mine(key0, KPL) : 0xFFFFFFFFu;
     const float to_log2 = F8 ? a.scale_log2 * ks : a.scale_log2;
     float mt = -INFINITY;
@@ -496,16 +498,16 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   bool final = w.splits <= 2 * kJoinFan;
   for (;;) {
     const int run = w.split / kJoinFan * kJoinFan;
-    const int first = final ? w.slot : w.slot + run, step = final && w.splits > 2 * kJoinFan ? kJoinFan : 1;
+    const int from = final ? w.slot : w.slot + run, step = final && w.splits > 2 * kJoinFan ? kJoinFan : 1;
     const int n = !final ? min(kJoinFan, w.splits - run) : (w.splits + step - 1) / step;
-    if (!last_to_arrive(a.arrived + (final ? a.slots : 0) + first, n, word)) return;
-    join_slots<HD>(a, cols, 16, first, step, n, ml, top, obuf, [&](int col, int e, f32x4 v, float total) {
+    if (!last_to_arrive(a.arrived + (final ? a.slots : 0) + from, n, word)) return;
+    join_slots<HD>(a, cols, 16, from, step, n, ml, top, obuf, [&](int col, int e, f32x4 v, float total) {
       if (final) put_out(col, e, v, total);
-      else put_slot(slots, (first * 16 + col) * HD + e, v);
+      else put_slot(slots, (from * 16 + col) * HD + e, v);
     });
     if (final) return;
     if ((int)threadIdx.x < cols)
-      __hip_atomic_store(a.part_ml + (size_t)first * 16 + threadIdx.x,
+      __hip_atomic_store(a.part_ml + (size_t)from * 16 + threadIdx.x,
                          pair_of(top[2 * threadIdx.x], top[2 * threadIdx.x + 1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     final = true;
   }

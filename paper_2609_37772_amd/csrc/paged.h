@@ -153,11 +153,16 @@ UAD_HD uint32_t scale_bits(uint32_t most) {
 
 // ---------------------------------------------------------------------------
 // Attention of new rows: what a row at cache position p of a sequence of `len` tokens
-// sees, keys [lo, hi) and those before min(sinks, hi).  window 0: no window.
+// sees, keys [lo, hi) and those before `first`.  window 0: no window.
 // ---------------------------------------------------------------------------
 UAD_HD int seen_from(int p, int window) { return window > 0 && p >= window ? p - window + 1 : 0; }
 UAD_HD int seen_to(int p, int len, int window, bool causal) {
   return causal ? p + 1 : window > 0 && window < len - p ? p + window : len;
+}
+
+UAD_HD int seen_first(int p, int len, int sinks, bool causal) {
+  const int most = causal ? p + 1 : len;
+  return sinks < most ? sinks : most;
 }
 
 // The tiles of `tile` keys that rows see of which the first sees from `lo`, counted
@@ -191,7 +196,8 @@ UAD_HD int pages_of(int len, int page_shift) { return (int)(((uint32_t)len + (1u
 UAD_HD bool growth_ok(int len, int n, int pages_per_seq, int page_shift) {
   return len >= 0 && n >= 0 && (int64_t)len + n <= (int64_t)pages_per_seq << page_shift;
 }
-// Whether page i of a sequence of `len` tokens holds one that a later token sees.
+// Whether page i of a sequence of `len` tokens holds one that a later token sees, or is the
+// one, not full, that the next token goes to.
 UAD_HD bool page_in_use(int i, int len, int window, int sinks, int page_shift) {
   const int64_t from = (int64_t)i << page_shift, to = from + ((int64_t)1 << page_shift);
   return from < len && (from < sinks || window == 0 || to > (int64_t)len - window + 1);
