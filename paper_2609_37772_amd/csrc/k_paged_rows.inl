@@ -2,7 +2,7 @@
 // or a single token of each sequence, with a sliding window and sinks; pools in bf16, or
 // in 8 bits with one scale or one for every block of tokens.  What a row sees is in
 // paged.h.
-#include "paged_device.h"
+#include "paged_rows.h"
 
 namespace uad {
 
@@ -19,35 +19,10 @@ namespace uad {
 // columns see and others do not must not reach the others through 0 * NaN: values that
 // are not finite are taken out, and the columns that see them become NaN.
 // ---------------------------------------------------------------------------
-struct RowsSeq {
-  int from, n, len, units;
-  SeenTiles tiles;
-};
 struct RowsWork {
   RowsSeq s;
   int b, unit, t0, t1, split, splits, slot;
 };
-
-__device__ __forceinline__ int runs_of(int rows, int group) { return (int)(((int64_t)rows * group + 15) / 16); }
-
-// Sequence b; one that cannot be used has no units.
-template <int TILE>
-__device__ __forceinline__ RowsSeq rows_of(const KvRowsArgs &a, int b, bool *bad) {
-  RowsSeq s{b, 1, 0, 0, {}};
-  if (a.row_start) {
-    s.from = a.row_start[b];
-    const int to = a.row_start[b + 1], len = a.lens[b];
-    const bool ok = sequence_ok(b, s.from, to, a.n_rows, len, a.pages_per_seq, a.d.page_shift);
-    *bad |= !ok;
-    s.n = ok ? to - s.from : 0;
-    s.len = ok ? len : 0;
-  } else {
-    s.len = length_or_none(a.lens[b], a.pages_per_seq, a.d.page_shift, bad);
-  }
-  s.units = a.d.n_kv_heads * runs_of(s.n, a.group);
-  s.tiles = seen_tiles(s.len, seen_from(s.len - s.n, a.window), a.sinks, TILE);
-  return s;
-}
 
 template <int HD, bool F8>
 __device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds, RowsWork *w) {
@@ -149,39 +124,6 @@ __device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds,
   w->t0 = split_begin(w->s.tiles.count, w->splits, w->split);
   w->t1 = split_begin(w->s.tiles.count, w->splits, w->split + 1);
   return true;
-}
-
-// 16-byte pieces of V that hold a value that is not finite: those become zeros in v, and
-// ones in the bf16 operand that is returned (its other elements zero).
-template <bool F8>
-__device__ __forceinline__ bool not_finite(u32x4_t v) {
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (F8) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) any |= (v[i] >> (8 * k) & 0x7F) == 0x7F;
-    } else {
-      any |= (v[i] & 0x7F80u) == 0x7F80u || (v[i] & 0x7F800000u) == 0x7F800000u;
-    }
-  }
-  return any;
-}
-template <bool F8>
-__device__ __forceinline__ bf16x8 take_not_finite(u32x4_t &v, int u) {
-  union {
-    bf16x8 h;
-    uint16_t e[8];
-  } o;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int i = F8 ? 2 * u + e / 4 : e / 2, shift = F8 ? 8 * (e % 4) : 16 * (e % 2);
-    const uint32_t top = F8 ? 0x7Fu : 0x7F80u, whole = F8 ? 0xFFu : 0xFFFFu;
-    const bool odd = (v[i] >> shift & top) == top;
-    o.e[e] = odd ? 0x3F80u : 0u;
-    if (odd) v[i] &= ~(whole << shift);
-  }
-  return o.h;
 }
 
 template <int HD, bool F32, bool F8>
@@ -527,7 +469,8 @@ static hipError_t rows_attrs() {
   return e;
 }
 hipError_t kv_rows_init(int head_dim) {
-  return head_dim == 64 ? rows_attrs<64>() : head_dim == 128 ? rows_attrs<128>() : rows_attrs<256>();
+  const hipError_t e = head_dim == 64 ? rows_attrs<64>() : head_dim == 128 ? rows_attrs<128>() : rows_attrs<256>();
+  return e == hipSuccess ? kv_prompt_init(head_dim) : e;
 }
 
 template <int HD, bool F32, bool F8>
@@ -555,11 +498,20 @@ static hipError_t launch_rows_hd(const KvRowsArgs &a, bool f32, bool f8, hipStre
   return f8 ? launch_rows_type<HD, false, true>(a, s) : launch_rows_type<HD, false, false>(a, s);
 }
 
+// Which kernel: 0: that of few rows; else the waves that share a column of that of many.
+static int prompt_key_waves(const KvRowsArgs &a) {
+  const int64_t columns = (int64_t)a.n_rows * a.group;
+  if (!a.row_start || columns < 64 * (int64_t)a.n_seqs) return 0;
+  return columns / 128 * a.d.n_kv_heads < 256 ? 2 : 1;
+}
+
 hipError_t launch_kv_rows(const KvRowsArgs &a, bool f32, bool f8, hipStream_t s) {
   if (a.n_seqs < 1 || a.n_rows < 1 || a.group < 1 || a.n_heads != a.group * a.d.n_kv_heads || a.pages_per_seq < 1 ||
       a.target < 1 || a.slots < max_slots(a.target) || a.d.page_shift < 4 || a.window < 0 || a.sinks < 0 ||
       (!a.row_start && a.n_rows != a.n_seqs) || (!f8 && a.k_scales))
     return hipErrorInvalidValue;
+  const int key_waves = prompt_key_waves(a);
+  if (key_waves) return launch_kv_prompt(a, key_waves, f32, f8, s);
   if (a.d.head_dim == 64) return launch_rows_hd<64>(a, f32, f8, s);
   if (a.d.head_dim == 128) return launch_rows_hd<128>(a, f32, f8, s);
   if (a.d.head_dim == 256) return launch_rows_hd<256>(a, f32, f8, s);

@@ -117,6 +117,8 @@ hipError_t launch_kv_prefix(const KvPrefixArgs &a, int batch, int n_layers, bool
 // of append and attend (which go there by themselves).
 hipError_t kv_rows_init(int head_dim);
 hipError_t launch_kv_rows(const KvRowsArgs &a, bool f32, bool f8, hipStream_t s);
+hipError_t kv_prompt_init(int head_dim);
+hipError_t launch_kv_prompt(const KvRowsArgs &a, int key_waves, bool f32, bool f8, hipStream_t s);
 hipError_t launch_kv_append_blocks(const KvAppendArgs &a, bool f32, hipStream_t s);
 hipError_t launch_kv_reserve(const KvReserveArgs &a, hipStream_t s);
 hipError_t launch_kv_release(const KvReleaseArgs &a, hipStream_t s);
