@@ -129,7 +129,8 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
   };
   int next_ids = tiles.count > 0 ? page_ids(0) : 0;
 
-  // The query: rotated in fp32, through LDS into operands.
+  // The query: rotated and scaled in fp32, so that scores are in powers of two, through LDS
+  // into operands.
   bf16x8 qf[TERMS][KS];
   {
     float *q32 = (float *)lds_bytes;  // [COLS][HD], 16-byte piece p of column i at p ^ (i % 8)
@@ -158,8 +159,8 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
         if (turned) turn_of(turns, position[i], &sn, &cs);
         const float u = col < cols ? value_of<F32>(x[i]) : 0.f, v = col < cols ? value_of<F32>(y[i]) : 0.f;
         if (col < COLS) {
-          q32[at(col, ea)] = turned ? u * cs - v * sn : u;
-          q32[at(col, eb)] = turned ? v * cs + u * sn : v;
+          q32[at(col, ea)] = (turned ? u * cs - v * sn : u) * a.scale_log2;
+          q32[at(col, eb)] = (turned ? v * cs + u * sn : v) * a.scale_log2;
         }
       }
     }
@@ -225,12 +226,25 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
     }
   };
 
+  // the 16 bytes of K that are operand ks of part `part` of a tile (and the next one in 8 bits)
+  const int k_row = 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
+  auto k_piece = [&](const uint8_t *buf, int part, int ks) {
+    return *(const u32x4_t *)(buf + (32 * part + k_row) * (KP * 16) + (((F8 ? ks & ~1 : 2 * ks) + h) ^ k_bits(k_row)) * 16);
+  };
+  // the 16 bytes of V^T that are operand u of part `part` of a tile for columns 32 n .. (both
+  // operands of it in 8 bits)
+  auto v_piece = [&](const uint8_t *buf, int n, int part, int u) {
+    const int d = 32 * n + c;
+    return *(const u32x4_t *)(buf + KBYTES + d * (VP * 16) + ((F8 ? 2 * part + h : 4 * part + 2 * h + u) ^ v_bits(d)) * 16);
+  };
+
   f32x16 o[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[n][r] = 0.f;
   float m = -INFINITY, l = 0.f;
+  uint32_t nans[NT / 2] = {};  // 16 bits for each of o
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds_bytes;
   int ids = checked(next_ids, 0);
   load_tile(0, ids, lds0);
@@ -239,7 +253,7 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
   for (int i = 0; i < tiles.count; ++i) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();  // this tile is there, and everyone is done with the other buffer
-    const uint8_t *buf = lds_bytes + (i & 1) * BUF;
+    uint8_t *buf = lds_bytes + (i & 1) * BUF;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       ks_[s] = next_ks[s];
@@ -251,41 +265,95 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
       load_scales(i + 1, ids);
       if (i + 2 < tiles.count) next_ids = page_ids(i + 2);
     }
-    // scores
-    f32x16 sc[NS];
+    const int k0 = tile_at(i);
+    const bool edge = (k0 < lo_max || k0 + TILE > hi_min) && k0 + TILE > first_min;
+    uint32_t seen[NS];  // of this lane's scores
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
+    for (int s = 0; s < NS; ++s) seen[s] = edge ? seen_by_mine(k0 + 32 * (KW == 1 ? s : kw) + 16 * h, 16) : 0xFFFFu;
+    if (edge) {
+      // What no column sees may be anything, and becomes zero: a thread looks at the pieces
+      // of V^T that it loaded.  What only some see must not reach the others as 0 * NaN.
+      u32x4_t *mine = (u32x4_t *)(buf + KBYTES + threadIdx.x * 16);
+      const uint32_t any = seen_by_any(k0 + v_key, RUN);
+      u32x4_t keep = {0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < RUN; ++e) keep[e * ESZ / 4] |= (any >> e & 1) ? (F8 ? 0xFFu : 0xFFFFu) << (e * ESZ % 4 * 8) : 0u;
+      bool odd = false;
+#pragma unroll
+      for (int n = 0; n < V_PASSES; ++n) {
+        const u32x4_t v = mine[n * 256] & keep;
+        odd |= not_finite<F8>(v);
+        mine[n * 256] = v;
+      }
+      if (__syncthreads_or(odd)) {  // columns that see such a value become NaN at the end, and it a zero
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            union {
+              bf16x8 v;
+              uint16_t e[8];
+            } sees;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sees.e[e] = seen[s] >> (8 * u + e) & 1 ? 0x3F80u : 0u;
+#pragma unroll 1  // rare: registers count for more
+            for (int n = 0; n < NT; ++n) {
+              u32x4_t raw = v_piece(buf, n, KW == 1 ? s : kw, u);
+              f32x16 hits;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) hits[r] = 0.f;
+              hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(take_not_finite<F8>(raw, F8 ? u : 0), sees.v, hits, 0, 0, 0);
+              uint32_t bits = 0;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) bits |= hits[r] > 0.f ? 1u << r : 0u;
+#pragma unroll
+              for (int k = 0; k < NT / 2; ++k) nans[k] |= n / 2 == k ? bits << (n % 2 * 16) : 0u;
+            }
+          }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < V_PASSES; ++n) {
+          u32x4_t v = mine[n * 256];
+#pragma unroll
+          for (int u = 0; u < (F8 ? 2 : 1); ++u) (void)take_not_finite<F8>(v, u);
+          mine[n * 256] = v;
+        }
+        __syncthreads();
+      }
+    }
+    // scores, in powers of two
+    f32x16 sc[NS];
+    u32x4_t raw[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int r = 0; r < 16; ++r) sc[s][r] = 0.f;
-      const int key = 32 * (KW == 1 ? s : kw) + 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
-      const uint8_t *row = buf + key * (KP * 16);
-      u32x4_t raw;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        if (!F8 || ks % 2 == 0) raw = *(const u32x4_t *)(row + (((F8 ? ks & ~1 : 2 * ks) + h) ^ k_bits(key)) * 16);
-        const bf16x8 kf = operand_of<F8>(raw, ks & 1);
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        if (!F8 || ks % 2 == 0) raw[s] = k_piece(buf, KW == 1 ? s : kw, ks);
+        const bf16x8 kf = operand_of<F8>(raw[s], ks & 1);
 #pragma unroll
         for (int t = TERMS - 1; t >= 0; --t) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[t][ks], sc[s], 0, 0, 0);
       }
+    if constexpr (F8)
+      if (a.k_scales) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) sc[s] *= ks_[s];
+      }
+    if (edge) {
+      asm volatile("");  // a branch: the other tiles are spared three instructions a score
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[s][r] = seen[s] >> r & 1 ? sc[s][r] : -INFINITY;
     }
-    // in powers of two, keys that the column does not see masked
-    const int k0 = tile_at(i);
-    const bool edge = (k0 < lo_max || k0 + TILE > hi_min) && k0 + TILE > first_min;
-    uint32_t seen[NS];
     float mt = -INFINITY;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const float to_log2 = F8 ? a.scale_log2 * ks_[s] : a.scale_log2;
-      seen[s] = 0xFFFFu;
-      if (edge) seen[s] = seen_by_mine(k0 + 32 * (KW == 1 ? s : kw) + 16 * h, 16);
+    for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float v = sc[s][r] * to_log2;
-        if (edge && !(seen[s] >> r & 1)) v = -INFINITY;
-        sc[s][r] = v;
-        mt = fmaxf(mt, v);
-      }
-    }
+      for (int r = 0; r < 16; ++r) mt = fmaxf(mt, sc[s][r]);
     mt = max_pair32(mt);
     if (__ballot(mt > m + kKvRescale || m == -INFINITY)) {
       const float m1 = fmaxf(m, mt), f = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
@@ -295,72 +363,47 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
       for (int n = 0; n < NT; ++n) o[n] *= f;
     }
     const float base = m == -INFINITY ? 0.f : m;  // nothing seen yet: every weight is 2^-inf
-    bf16x8 pf[TERMS][2 * NS];
+    // weights and outputs, 8 keys a lane at a time
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float p = __builtin_amdgcn_exp2f(sc[s][r] - base);
-        l += p;
-        if constexpr (F8) {  // weights that are not seen stay zero whatever the scale is
-          p *= vs_[s];
-          if (edge && !(seen[s] >> r & 1)) p = 0.f;
-        }
+      for (int u = 0; u < 2; ++u) {
+        bf16x8 pf[TERMS];
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-          pf[t][2 * s + r / 8][r % 8] = (__bf16)p;
-          p -= (float)pf[t][2 * s + r / 8][r % 8];
-        }
-      }
-    // outputs
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int d = 32 * n + c;
-      const uint8_t *row = buf + KBYTES + d * (VP * 16);
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        const int part = KW == 1 ? s : kw;
-        u32x4_t raw;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          if (!F8 || u == 0) raw = *(const u32x4_t *)(row + ((F8 ? 2 * part + h : 4 * part + 2 * h + u) ^ v_bits(d)) * 16);
-          if (edge) {  // what nobody sees may be anything; what some do not see must not reach them
-            const int key = k0 + 32 * part + 16 * h + (F8 ? 0 : 8 * u);
-            const uint32_t any = seen_by_any(key, RUN);
-            constexpr int PER = 4 / ESZ;
-            if (!F8 || u == 0)
-#pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                uint32_t keep = 0;
-#pragma unroll
-                for (int e = 0; e < PER; ++e) keep |= (any >> (w * PER + e) & 1) ? (F8 ? 0xFFu : 0xFFFFu) << (e * 32 / PER) : 0u;
-                raw[w] &= keep;
-              }
-            if (__ballot(not_finite<F8>(raw))) {
-              const bf16x8 odd = take_not_finite<F8>(raw, F8 ? u : 0);
-              union {
-                bf16x8 v;
-                uint16_t e[8];
-              } sees;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) sees.e[e] = seen[s] >> (8 * u + e) & 1 ? 0x3F80u : 0u;
-              f32x16 hits;
-#pragma unroll
-              for (int r = 0; r < 16; ++r) hits[r] = 0.f;
-              hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd, sees.v, hits, 0, 0, 0);
-#pragma unroll
-              for (int r = 0; r < 16; ++r) o[n][r] = hits[r] > 0.f ? NAN : o[n][r];
-            }
+        for (int e = 0; e < 8; ++e) {
+          float p = __builtin_amdgcn_exp2f(sc[s][8 * u + e] - base);
+          sum[e & 1] += p;
+          if constexpr (F8) {  // weights that are not seen stay zero whatever the scale is
+            p *= vs_[s];
+            if (edge) p = seen[s] >> (8 * u + e) & 1 ? p : 0.f;
           }
-          const bf16x8 vf = operand_of<F8>(raw, F8 ? u : 0);
 #pragma unroll
-          for (int t = TERMS - 1; t >= 0; --t) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t][2 * s + u], o[n], 0, 0, 0);
+          for (int t = 0; t < TERMS; ++t) {
+            pf[t][e] = (__bf16)p;
+            p -= (float)pf[t][e];
+          }
+        }
+        l += sum[0] + sum[1];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const bf16x8 vf = operand_of<F8>(v_piece(buf, n, KW == 1 ? s : kw, u), F8 ? u : 0);
+#pragma unroll
+          for (int t = TERMS - 1; t >= 0; --t) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t], o[n], 0, 0, 0);
         }
       }
-    }
   }
   if (bad) raise_status(a.status, kStatusPage);
   l = sum_pair32(l);
+  uint32_t any_nan = 0;
+#pragma unroll
+  for (int k = 0; k < NT / 2; ++k) any_nan |= nans[k];
+  if (__ballot(any_nan != 0)) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[n][r] = nans[n / 2] >> (n % 2 * 16 + r) & 1 ? NAN : o[n][r];
+  }
 
   // two waves with the same columns meet in LDS, the second's values in units of its maximum
   if constexpr (KW == 2) {
