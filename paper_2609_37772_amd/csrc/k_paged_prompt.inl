@@ -5,37 +5,67 @@ namespace uad {
 
 // ---------------------------------------------------------------------------
 // Many rows: bound by the matrix instructions.  A unit is a KV head of a sequence with up
-// to 128 (row, query head) pairs, 32 columns to each of four waves (or 64, where two waves
-// share 32 columns and take half of every tile's keys each: for calls with too few units
-// to fill the chip).  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16: row i of
-// the 32-key product is key 16 (i / 4 % 2) + 4 (i / 8) + i % 4, so that a half wave ends
-// with the scores of 16 consecutive keys, which are its operand of the P V product as they
-// stand.  Tiles of 64 keys go from memory to LDS past the registers, the next one while
-// this one is worked on; a 16-byte piece p of a row lies at piece p ^ (a few bits of the row),
-// so that the rows that a read takes at once do not meet in a bank.  The query is held in
-// registers, rotated in fp32 on the way.
+// to 128 (row, query head) pairs, its columns; each of its waves takes 32 of them (or 16,
+// where 32 columns' outputs and query would leave a SIMD one wave).  For calls with too few
+// units to fill the chip a unit has 64 columns, and two waves share theirs and take half of
+// every tile's keys each.
+//
+// S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16 (16x16x32): rows of K enter in
+// an order in which each group of lanes ends with the scores of 16 (8) consecutive keys,
+// which are its operand of the P V product as they stand.  Tiles of 64 keys go from memory
+// to LDS past the registers, the next one while this one is worked on; a 16-byte piece p
+// of a row lies at piece p ^ (a few bits of the row), so that rows that are read at once do
+// not meet in a bank.  The query is held in registers, rotated and scaled in fp32 on the way.
 //
 // Precision: the query and the weights enter as bf16 terms, two (16 bits) for bf16 rows and
 // three for fp32 rows; keys and values as stored.  One term would halve the time and add
 // as much error again as the output's one rounding to bf16 has, twice over: once for the
 // query, whose error the scores take in, and once for the weights.
+//
+// Masks as in the kernel of few rows: what no column sees is zero in V, and values that are
+// not finite where some columns do not see them are taken out of LDS and noted for those
+// that do.
 // ---------------------------------------------------------------------------
 constexpr int kPromptTile = 64;
 
-// LDS: two buffers of a tile's K and V^T; before that the query in fp32, after it, where two
-// waves share columns, one's outputs, maxima and sums.
-template <int HD, bool F8, int KW>
-constexpr int prompt_lds_bytes() {
-  constexpr int buffers = 2 * 2 * kPromptTile * HD * (F8 ? 1 : 2), query = 128 / KW * HD * 4;
-  constexpr int meeting = KW == 2 ? 64 * HD * 4 + 2 * 2 * 64 * 4 : 0;
-  constexpr int most = buffers > query ? buffers : query;
-  return most > meeting ? most : meeting;
-}
-// Waves per SIMD: outputs and query take 32 columns x head dim x (4 + 2 TERMS) bytes.
+// Columns of a wave: outputs and query take it columns x head dim x (4 + 2 terms) bytes,
+// and two waves are to share a SIMD's 512 registers.
 template <int HD, bool F32>
-constexpr int kPromptPerSimd = HD == 256 || (HD == 128 && F32) ? 1 : 2;
+constexpr int kPromptCols = HD == 256 || (HD == 128 && F32) ? 16 : 32;
+template <int HD, bool F32>
+constexpr int kPromptThreads = 64 * 128 / kPromptCols<HD, F32>;
+
+// LDS: two buffers of a tile's K and V^T; before that the query in fp32 (in the first buffer
+// and where two waves share columns, which are calls that wait for latency, no further, so
+// that the first tile can be on its way to the second), after it, where waves share
+// columns, one's outputs, maxima and sums.
+template <int HD, bool F8, int KW>
+struct PromptLds {
+  static constexpr int buffer = 2 * kPromptTile * HD * (F8 ? 1 : 2), query = 128 / KW * HD * 4;
+  static constexpr int second = KW == 2 && query > buffer ? query : buffer;  // where the second buffer lies
+  static constexpr int meeting = KW == 2 ? 64 * HD * 4 + 4 * 2 * 64 * 4 : 0;
+  static constexpr int tiles = second + buffer, most = tiles > query ? tiles : query;
+  static constexpr int bytes = most > meeting ? most : meeting;
+};
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+
+// The matrix instruction of a wave with C columns: rows x C results, lane (c, g) has those
+// of column c and rows 4 g + 4 GROUPS k + r at 4 k + r.
+template <int C>
+struct Product;
+template <>
+struct Product<32> {
+  typedef f32x16 acc;
+  static constexpr int values = 16;
+  static __device__ __forceinline__ acc of(bf16x8 a, bf16x8 b, acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Product<16> {
+  typedef f32x4 acc;
+  static constexpr int values = 4;
+  static __device__ __forceinline__ acc of(bf16x8 a, bf16x8 b, acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
 
 // 16 bytes per lane from memory to LDS at `to` + 16 * lane.  The compiler would wait for
 // each before the next read of LDS: the kernel waits itself, once per tile.
@@ -44,18 +74,32 @@ __device__ __forceinline__ void load_to_lds(const void *from, uint32_t to) {
   asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
                : "=&s"(kept) : "s"(to), "v"(from) : "memory");
 }
+// The same from an address that is one for the wave and an offset below 2^31.
+__device__ __forceinline__ void load_to_lds(const void *base, uint32_t offset, uint32_t to) {
+  uint32_t kept;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+               : "=&s"(kept) : "s"(to), "v"(offset), "s"(base) : "memory");
+}
 
 template <int HD, bool F32, bool F8, int KW>
-__global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kernel(KvRowsArgs a) {
+__global__ __launch_bounds__((kPromptThreads<HD, F32>), 2) void kv_prompt_kernel(KvRowsArgs a) {
+  using Lds = PromptLds<HD, F8, KW>;
+  constexpr int C = kPromptCols<HD, F32>, THREADS = kPromptThreads<HD, F32>, NW = THREADS / 64;
+  using Mul = Product<C>;
+  typedef typename Mul::acc acc;
+  constexpr int VAL = Mul::values, GROUPS = 64 / C;   // results a lane; groups of lanes
   constexpr int TILE = kPromptTile, COLS = 128 / KW, NS = 2 / KW;  // NS: 32-key parts of a tile that a wave takes
-  constexpr int KS = HD / 16, NT = HD / 32, TERMS = F32 ? 3 : 2, ESZ = F8 ? 1 : 2;
-  constexpr int KP = HD * ESZ / 16, VP = TILE * ESZ / 16;          // 16-byte pieces of a row of K, of V^T
-  constexpr int KBYTES = TILE * HD * ESZ, BUF = 2 * KBYTES;
-  constexpr int RUN = 16 / ESZ;                                    // keys of a piece of V^T
+  constexpr int RUN = 32 / GROUPS;                    // consecutive keys of a part that a lane has
+  constexpr int MK = 32 / C;                          // products of a part: 32 keys in rows of C
+  constexpr int K = 8 * GROUPS, KS = HD / K;          // depth of a product, steps of Q K^T
+  constexpr int NT = HD / C;                          // output tiles
+  constexpr int TERMS = F32 ? 3 : 2, ESZ = F8 ? 1 : 2;
+  constexpr int KP = HD * ESZ / 16, VP = TILE * ESZ / 16;  // 16-byte pieces of a row of K, of V^T
+  constexpr int KBYTES = TILE * HD * ESZ, PIECE = 16 / ESZ;  // keys of a piece of V^T
   extern __shared__ __align__(16) uint8_t lds_bytes[];
-  __shared__ int plan[4 * 4];
+  __shared__ int plan[4 * NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane & 31, h = lane >> 5;
+  const int c = lane % C, g = lane / C;
   const int cw = wave / KW, kw = wave % KW;
 
   // the unit: sequences' units side by side, a sequence's last rows first (where rows are
@@ -64,7 +108,7 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
   RowsSeq sq;
   int b, unit;
   {
-    PlanScan<4> scan(a.n_seqs, plan);
+    PlanScan<NW> scan(a.n_seqs, plan);
     const int b0 = scan.me * scan.per;
     bool bad = false;
     auto units_of = [&](int i) {
@@ -109,7 +153,7 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
   auto from_at = [&](int p) { return seen_from(p, a.window); };
   auto to_at = [&](int p) { return min(seen_to(p, sq.len, a.window, a.causal), sq.len); };
   auto first_at = [&](int p) { return seen_first(p, sq.len, a.sinks, a.causal); };
-  const int p_min = pos0 + row_of(m0), p_max = pos0 + row_of(m0 + cols - 1), p_mine = pos0 + row_of(m0 + min(32 * cw + c, cols - 1));
+  const int p_min = pos0 + row_of(m0), p_max = pos0 + row_of(m0 + cols - 1), p_mine = pos0 + row_of(m0 + min(C * cw + c, cols - 1));
   const int lo = from_at(p_mine), hi = to_at(p_mine), first = first_at(p_mine);
   const int lo_min = from_at(p_min), lo_max = from_at(p_max), hi_min = to_at(p_min), hi_max = to_at(p_max);
   const int first_min = first_at(p_min), first_max = first_at(p_max);
@@ -122,90 +166,52 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
   // Page ids of a tile's four runs of 16 keys, in lanes 0 .. 3 (and every four more).
   auto page_ids = [&](int i) { return table[min(tile_at(i) + 16 * (lane & 3), last) >> a.d.page_shift]; };
   auto checked = [&](int id, int i) {
-    if (seen_by_any(tile_at(i) + 16 * (lane & 3), 16) == 0) return 0;  // not looked at
+    const int k0 = tile_at(i);
+    const bool whole = k0 >= lo_min && k0 + TILE <= hi_max;
+    if (!whole && seen_by_any(k0 + 16 * (lane & 3), 16) == 0) return 0;  // not looked at
     const bool ok = page_ok(a.d, id);
     bad |= !ok;
     return ok ? id : 0;
   };
-  int next_ids = tiles.count > 0 ? page_ids(0) : 0;
 
-  // The query: rotated and scaled in fp32, so that scores are in powers of two, through LDS
-  // into operands.
-  bf16x8 qf[TERMS][KS];
-  {
-    float *q32 = (float *)lds_bytes;  // [COLS][HD], 16-byte piece p of column i at p ^ (i % 8)
-    constexpr int HP = HD / 2, AT_ONCE = 256 / HP, BATCH = 8;
-    const int p = threadIdx.x % HP;
-    int ea, eb;
-    rope_pair(p, a.rope_dim, a.rope_pairs != 0, &ea, &eb);
-    const bool turned = p < a.rope_dim / 2;
-    const double turns = a.turns[p];  // 128 of them are allocated
-    auto at = [&](int col, int e) { return col * HD + (((e >> 2) ^ (col & 7)) << 2) + (e & 3); };
-    for (int i0 = threadIdx.x / HP; i0 < COLS; i0 += AT_ONCE * BATCH) {
-      uint32_t x[BATCH], y[BATCH];
-      int position[BATCH];
-#pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        const int m = m0 + min(i0 + i * AT_ONCE, cols - 1), j = row_of(m);
-        const int64_t qi = (int64_t)(sq.from + j) * a.ldq + (int64_t)(kvh * group + m - j * group) * HD;
-        position[i] = a.positions ? a.positions[sq.from + j] : pos0 + j;
-        x[i] = load_raw<F32>(a.q, qi + ea);
-        y[i] = load_raw<F32>(a.q, qi + eb);
-      }
-#pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        const int col = i0 + i * AT_ONCE;
-        float sn = 0.f, cs = 1.f;
-        if (turned) turn_of(turns, position[i], &sn, &cs);
-        const float u = col < cols ? value_of<F32>(x[i]) : 0.f, v = col < cols ? value_of<F32>(y[i]) : 0.f;
-        if (col < COLS) {
-          q32[at(col, ea)] = (turned ? u * cs - v * sn : u) * a.scale_log2;
-          q32[at(col, eb)] = (turned ? v * cs + u * sn : v) * a.scale_log2;
-        }
-      }
-    }
-    __syncthreads();
-    const int col = 32 * cw + c;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int d0 = F8 ? (ks >> 1) * 32 + 16 * h + 8 * (ks & 1) : 16 * ks + 8 * h;
-      const f32x4 v[2] = {*(const f32x4 *)(q32 + at(col, d0)), *(const f32x4 *)(q32 + at(col, d0 + 4))};
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float x = v[e / 4][e % 4];
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-          qf[t][ks][e] = (__bf16)x;
-          x -= (float)qf[t][ks][e];
-        }
-      }
-    }
-    __syncthreads();
-  }
-
-  // Loads of a tile into buffer `to`.  K: thread t of pass n takes piece 256 n + t, of a row
-  // whose 16-key run is one for the wave; V^T: a column each, the same keys in every pass.
-  constexpr int K_PASSES = TILE * KP / 256, V_PASSES = HD * VP / 256, V_ROWS = 256 / VP;
-  auto k_bits = [&](int key) { return KP == 4 ? (key >> 1 & 1) | (key >> 4 & 1) << 1 : (key & 3) | (key >> 4 & 1) << 2; };
+  // Loads of a tile into the buffer at `to`.  K: thread t of pass n takes piece n * THREADS + t,
+  // of a row whose run of 16 is one for the wave; V^T: the same keys of other columns in every
+  // pass.
+  constexpr int K_PASSES = TILE * KP / THREADS, V_PASSES = HD * VP / THREADS, V_ROWS = THREADS / VP;
+  static_assert(K_PASSES > 0 && V_PASSES > 0 && V_ROWS % 8 == 0, "every thread has a piece in every pass");
+  auto k_bits = [&](int key) {  // of the 8 rows that are read at once
+    const int far = key >> (C == 32 ? 4 : 3) & 1;
+    return KP == 4 ? (key >> 1 & 1) | far << 1 : (key & 3) | far << 2;
+  };
   auto v_bits = [&](int d) { return VP == 4 ? d >> 1 & 3 : d & 7; };
-  const int v_row = threadIdx.x / VP, v_key = ((threadIdx.x % VP) ^ v_bits(v_row)) * RUN;
+  const int v_row = threadIdx.x / VP, v_key = ((threadIdx.x % VP) ^ v_bits(v_row)) * PIECE;
+  const uint32_t v_offset = (((uint32_t)v_row << a.d.page_shift) + (v_key & 15)) * ESZ;
   auto load_tile = [&](int i, int ids, uint32_t to) {
     const int k0 = tile_at(i);
+    int page[4];
+    size_t at[4];  // a run's page and KV head, in elements
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      page[r] = __builtin_amdgcn_readlane(ids, r);
+      at[r] = page_base(a.d, page[r], kvh);
+    }
 #pragma unroll
     for (int n = 0; n < K_PASSES; ++n) {
-      const int piece = n * 256 + threadIdx.x, row = piece / KP, p = piece % KP;
-      const int page = __builtin_amdgcn_readlane(ids, (n * 256 + wave * 64) / KP / 16);
-      const size_t at = page_base(a.d, page, kvh) + k_in_page(a.d, (k0 + row) & mask, 0);
-      load_to_lds((const char *)a.kp + at * ESZ + (p ^ k_bits(row)) * 16, to + n * 4096 + wave * 1024);
+      const int piece = n * THREADS + threadIdx.x, row = piece / KP, p = piece % KP;
+      const int r = (n * THREADS + wave * 64) / KP / 16;  // one for the wave
+      const size_t base = r == 0 ? at[0] : r == 1 ? at[1] : r == 2 ? at[2] : at[3];
+      load_to_lds((const char *)a.kp + (base + k_in_page(a.d, (k0 + 16 * r) & mask, 0)) * ESZ,
+                  (uint32_t)((row & 15) * HD * ESZ + (p ^ k_bits(row)) * 16), to + (n * THREADS + wave * 64) * 16);
     }
-    const int run16 = v_key >> 4;
-    const int id0 = __builtin_amdgcn_readlane(ids, 0), id1 = __builtin_amdgcn_readlane(ids, 1);
-    const int id2 = __builtin_amdgcn_readlane(ids, 2), id3 = __builtin_amdgcn_readlane(ids, 3);
-    const int page = run16 == 0 ? id0 : run16 == 1 ? id1 : run16 == 2 ? id2 : id3;
-    const char *src = (const char *)a.vp + (page_base(a.d, page, kvh) + v_in_page(a.d, (k0 + v_key) & mask, v_row)) * ESZ;
+    size_t v_at[4];  // and the run's first slot
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v_at[r] = at[r] + ((k0 + 16 * r) & mask);
+    const int r = v_key >> 4;
+    const size_t base = r == 0 ? v_at[0] : r == 1 ? v_at[1] : r == 2 ? v_at[2] : v_at[3];
+    const char *src = (const char *)a.vp + base * ESZ + v_offset;
 #pragma unroll
     for (int n = 0; n < V_PASSES; ++n)
-      load_to_lds(src + ((size_t)(n * V_ROWS) << a.d.page_shift) * ESZ, to + KBYTES + n * 4096 + wave * 1024);
+      load_to_lds(src + ((size_t)(n * V_ROWS) << a.d.page_shift) * ESZ, to + KBYTES + (n * THREADS + wave * 64) * 16);
   };
   // scales of the blocks that this lane's scores and weights lie in
   float ks_[NS], vs_[NS], next_ks[NS], next_vs[NS];
@@ -215,45 +221,151 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
       next_ks[s] = next_vs[s] = 1.f;
       if constexpr (F8)
         if (a.k_scales) {
-          const int part = KW == 1 ? s : kw, key = tile_at(i) + 32 * part + 16 * h;
+          const int part = KW == 1 ? s : kw, key = tile_at(i) + 32 * part + RUN * g;
           const int lower = __builtin_amdgcn_readlane(ids, 2 * part), upper = __builtin_amdgcn_readlane(ids, 2 * part + 1);
-          const size_t at = scale_index(a.d, h ? upper : lower, kvh, key & mask);
-          if (seen_by_any(key, 16) != 0) {  // else it may be anything
+          const size_t at = scale_index(a.d, RUN * g >= 16 ? upper : lower, kvh, key & mask);
+          if (seen_by_any(key & ~15, 16) != 0) {  // else it may be anything
             next_ks[s] = a.k_scales[at];
             next_vs[s] = a.v_scales[at];
           }
         }
     }
   };
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds_bytes;
+  // tile i's buffer: where two waves share columns the first tile takes the second one
+  constexpr int FLIP = KW == 2 ? 1 : 0;
+  auto buffer_of = [&](int i) { return ((i + FLIP) & 1) * Lds::second; };
 
-  // the 16 bytes of K that are operand ks of part `part` of a tile (and the next one in 8 bits)
-  const int k_row = 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
-  auto k_piece = [&](const uint8_t *buf, int part, int ks) {
-    return *(const u32x4_t *)(buf + (32 * part + k_row) * (KP * 16) + (((F8 ? ks & ~1 : 2 * ks) + h) ^ k_bits(k_row)) * 16);
+  int next_ids = tiles.count > 0 ? page_ids(0) : 0, ids = 0;
+  // The query: rotated and scaled in fp32, so that scores are in powers of two, through LDS
+  // into operands.  A thread takes the same 16 elements, two pieces of 8 that are turned
+  // with each other, of consecutive columns, whose rows are mostly one, and so is the turn.
+  bf16x8 qf[TERMS][KS];
+  {
+    float *q32 = (float *)lds_bytes;  // [COLS][HD], 16-byte piece p of column i at p ^ (i % 8)
+    constexpr int ITEMS = HD / 16, N = COLS * ITEMS / THREADS;  // of a column; columns of a thread
+    const int i = threadIdx.x % ITEMS, col0 = threadIdx.x / ITEMS * N, half = a.rope_dim / 16;
+    const bool apart = !a.rope_pairs && i < half;
+    const int x = apart ? i : 2 * i, y = apart ? i + half : 2 * i + 1;
+    const int64_t per16 = F32 ? 4 : 8;
+    const bool vec = ((uintptr_t)a.q & 15) == 0 && a.ldq % per16 == 0;
+    Raw8<F32> rx[N], ry[N];
+    int row[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int m = m0 + min(col0 + n, cols - 1);
+      row[n] = row_of(m);
+      const int64_t at = (int64_t)(sq.from + row[n]) * a.ldq + (int64_t)(kvh * group + m - row[n] * group) * HD;
+      rx[n].load(a.q, at + 8 * x, vec);
+      ry[n].load(a.q, at + 8 * y, vec);
+    }
+    if (KW == 2 && tiles.count > 0) {
+      ids = checked(next_ids, 0);
+      load_tile(0, ids, lds0 + buffer_of(0));
+      load_scales(0, ids);
+      if (tiles.count > 1) next_ids = page_ids(1);
+    }
+    auto put = [&](int col, int piece, const float *v) {  // 8 elements
+      f32x4 *at = (f32x4 *)(q32 + col * HD);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) at[(2 * piece + k) ^ (col & 7)] = f32x4{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]} * a.scale_log2;
+    };
+    float sn[8], cs[8];
+    int turned = -1;  // the row whose turn they are
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float u[8], w[8];
+      const bool real = col0 + n < cols;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        u[e] = real ? rx[n].value(e) : 0.f;
+        w[e] = real ? ry[n].value(e) : 0.f;
+      }
+      if (i < half) {
+        if (row[n] != turned) {
+          turned = row[n];
+          const int position = a.positions ? a.positions[sq.from + turned] : pos0 + turned;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) turn_of(a.turns[8 * i + e], position, &sn[e], &cs[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (a.rope_pairs) {  // elements 16 i + 2 e and the next
+            float &p = e < 4 ? u[2 * e] : w[2 * e - 8], &q = e < 4 ? u[2 * e + 1] : w[2 * e - 7];
+            const float p0 = p, q0 = q;
+            p = p0 * cs[e] - q0 * sn[e];
+            q = q0 * cs[e] + p0 * sn[e];
+          } else {
+            const float p0 = u[e], q0 = w[e];
+            u[e] = p0 * cs[e] - q0 * sn[e];
+            w[e] = q0 * cs[e] + p0 * sn[e];
+          }
+        }
+      }
+      put(col0 + n, x, u);
+      put(col0 + n, y, w);
+    }
+    __syncthreads();
+    const int col = C * cw + c;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      // the 8 dims of this lane: a 16-byte piece of a row of K, or half of one of 8 bits
+      const int d0 = F8 ? (ks >> 1) * 2 * K + 16 * g + 8 * (ks & 1) : K * ks + 8 * g;
+      f32x4 v[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) v[k] = ((const f32x4 *)(q32 + col * HD))[(d0 / 4 + k) ^ (col & 7)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float z = v[e / 4][e % 4];
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+          qf[t][ks][e] = (__bf16)z;
+          z -= (float)qf[t][ks][e];
+        }
+      }
+    }
+    __syncthreads();
+  }
+
+  // the 16 bytes of K that are operand ks of product k of part `part` (and the next one in 8 bits)
+  auto k_piece = [&](const uint8_t *buf, int part, int k, int ks) {
+    // row c of the product is the key whose score ends with lanes (, c / 4 % GROUPS) as number 4 k + c % 4, or 4 (c / 8) + c % 4
+    const int key = 32 * part + RUN * (c / 4 % GROUPS) + 4 * (C == 32 ? c >> 3 : k) + (c & 3);
+    return *(const u32x4_t *)(buf + key * (KP * 16) + (((F8 ? (ks >> 1) : ks) * GROUPS + g) ^ k_bits(key)) * 16);
   };
-  // the 16 bytes of V^T that are operand u of part `part` of a tile for columns 32 n .. (both
-  // operands of it in 8 bits)
-  auto v_piece = [&](const uint8_t *buf, int n, int part, int u) {
-    const int d = 32 * n + c;
-    return *(const u32x4_t *)(buf + KBYTES + d * (VP * 16) + ((F8 ? 2 * part + h : 4 * part + 2 * h + u) ^ v_bits(d)) * 16);
+  // operand u of part `part` of V^T for output tile n: keys 32 part + RUN g + 8 u ..
+  auto v_operand = [&](const uint8_t *buf, int n, int part, int u) {
+    const int d = C * n + c, key = 32 * part + RUN * g + 8 * u;
+    const uint8_t *at = buf + KBYTES + d * (VP * 16) + ((key / PIECE) ^ v_bits(d)) * 16;
+    u32x4_t r;
+    if constexpr (F8) {
+      typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+      const u32x2_t w = *(const u32x2_t *)(at + key % PIECE);
+      r[0] = w[0];
+      r[1] = w[1];
+    } else {
+      r = *(const u32x4_t *)at;
+    }
+    return operand_of<F8>(r, 0);
   };
 
-  f32x16 o[NT];
+  acc o[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[n][r] = 0.f;
+    for (int r = 0; r < VAL; ++r) o[n][r] = 0.f;
   float m = -INFINITY, l = 0.f;
-  uint32_t nans[NT / 2] = {};  // 16 bits for each of o
-  const uint32_t lds0 = (uint32_t)(uintptr_t)lds_bytes;
-  int ids = checked(next_ids, 0);
-  load_tile(0, ids, lds0);
-  load_scales(0, ids);
-  if (tiles.count > 1) next_ids = page_ids(1);
+  uint32_t nans[(NT * VAL + 31) / 32] = {};  // a bit for each value of o
+  if (KW == 1 && tiles.count > 0) {
+    ids = checked(next_ids, 0);
+    load_tile(0, ids, lds0 + buffer_of(0));
+    load_scales(0, ids);
+    if (tiles.count > 1) next_ids = page_ids(1);
+  }
   for (int i = 0; i < tiles.count; ++i) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();  // this tile is there, and everyone is done with the other buffer
-    uint8_t *buf = lds_bytes + (i & 1) * BUF;
+    uint8_t *buf = lds_bytes + buffer_of(i);
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       ks_[s] = next_ks[s];
@@ -261,7 +373,7 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
     }
     if (i + 1 < tiles.count) {
       ids = checked(next_ids, i + 1);
-      load_tile(i + 1, ids, lds0 + ((i + 1) & 1) * BUF);
+      load_tile(i + 1, ids, lds0 + buffer_of(i + 1));
       load_scales(i + 1, ids);
       if (i + 2 < tiles.count) next_ids = page_ids(i + 2);
     }
@@ -269,27 +381,27 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
     const bool edge = (k0 < lo_max || k0 + TILE > hi_min) && k0 + TILE > first_min;
     uint32_t seen[NS];  // of this lane's scores
 #pragma unroll
-    for (int s = 0; s < NS; ++s) seen[s] = edge ? seen_by_mine(k0 + 32 * (KW == 1 ? s : kw) + 16 * h, 16) : 0xFFFFu;
+    for (int s = 0; s < NS; ++s) seen[s] = edge ? seen_by_mine(k0 + 32 * (KW == 1 ? s : kw) + RUN * g, RUN) : 0xFFFFu;
     if (edge) {
       // What no column sees may be anything, and becomes zero: a thread looks at the pieces
       // of V^T that it loaded.  What only some see must not reach the others as 0 * NaN.
       u32x4_t *mine = (u32x4_t *)(buf + KBYTES + threadIdx.x * 16);
-      const uint32_t any = seen_by_any(k0 + v_key, RUN);
+      const uint32_t any = seen_by_any(k0 + v_key, PIECE);
       u32x4_t keep = {0, 0, 0, 0};
 #pragma unroll
-      for (int e = 0; e < RUN; ++e) keep[e * ESZ / 4] |= (any >> e & 1) ? (F8 ? 0xFFu : 0xFFFFu) << (e * ESZ % 4 * 8) : 0u;
+      for (int e = 0; e < PIECE; ++e) keep[e * ESZ / 4] |= (any >> e & 1) ? (F8 ? 0xFFu : 0xFFFFu) << (e * ESZ % 4 * 8) : 0u;
       bool odd = false;
 #pragma unroll
       for (int n = 0; n < V_PASSES; ++n) {
-        const u32x4_t v = mine[n * 256] & keep;
+        const u32x4_t v = mine[n * THREADS] & keep;
         odd |= not_finite<F8>(v);
-        mine[n * 256] = v;
+        mine[n * THREADS] = v;
       }
       if (__syncthreads_or(odd)) {  // columns that see such a value become NaN at the end, and it a zero
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
+          for (int u = 0; u < RUN / 8; ++u) {
             union {
               bf16x8 v;
               uint16_t e[8];
@@ -298,63 +410,75 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
             for (int e = 0; e < 8; ++e) sees.e[e] = seen[s] >> (8 * u + e) & 1 ? 0x3F80u : 0u;
 #pragma unroll 1  // rare: registers count for more
             for (int n = 0; n < NT; ++n) {
-              u32x4_t raw = v_piece(buf, n, KW == 1 ? s : kw, u);
-              f32x16 hits;
+              union {
+                bf16x8 v;
+                u32x4_t w;
+              } vf{v_operand(buf, n, KW == 1 ? s : kw, u)};
+              acc hits;
 #pragma unroll
-              for (int r = 0; r < 16; ++r) hits[r] = 0.f;
-              hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(take_not_finite<F8>(raw, F8 ? u : 0), sees.v, hits, 0, 0, 0);
+              for (int r = 0; r < VAL; ++r) hits[r] = 0.f;
+              hits = Mul::of(take_not_finite<false>(vf.w, 0), sees.v, hits);
               uint32_t bits = 0;
 #pragma unroll
-              for (int r = 0; r < 16; ++r) bits |= hits[r] > 0.f ? 1u << r : 0u;
+              for (int r = 0; r < VAL; ++r) bits |= hits[r] > 0.f ? 1u << r : 0u;
 #pragma unroll
-              for (int k = 0; k < NT / 2; ++k) nans[k] |= n / 2 == k ? bits << (n % 2 * 16) : 0u;
+              for (int k = 0; k < (NT * VAL + 31) / 32; ++k) nans[k] |= n * VAL / 32 == k ? bits << (n * VAL % 32) : 0u;
             }
           }
         __syncthreads();
 #pragma unroll
         for (int n = 0; n < V_PASSES; ++n) {
-          u32x4_t v = mine[n * 256];
+          u32x4_t v = mine[n * THREADS];
 #pragma unroll
           for (int u = 0; u < (F8 ? 2 : 1); ++u) (void)take_not_finite<F8>(v, u);
-          mine[n * 256] = v;
+          mine[n * THREADS] = v;
         }
         __syncthreads();
       }
     }
     // scores, in powers of two
-    f32x16 sc[NS];
-    u32x4_t raw[NS];
+    acc sc[NS][MK];
+    u32x4_t raw[NS][MK];
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[s][r] = 0.f;
+      for (int k = 0; k < MK; ++k)
+#pragma unroll
+        for (int r = 0; r < VAL; ++r) sc[s][k][r] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        if (!F8 || ks % 2 == 0) raw[s] = k_piece(buf, KW == 1 ? s : kw, ks);
-        const bf16x8 kf = operand_of<F8>(raw[s], ks & 1);
+      for (int s = 0; s < NS; ++s)
 #pragma unroll
-        for (int t = TERMS - 1; t >= 0; --t) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[t][ks], sc[s], 0, 0, 0);
-      }
+        for (int k = 0; k < MK; ++k) {
+          if (!F8 || ks % 2 == 0) raw[s][k] = k_piece(buf, KW == 1 ? s : kw, k, ks);
+          const bf16x8 kf = operand_of<F8>(raw[s][k], ks & 1);
+#pragma unroll
+          for (int t = TERMS - 1; t >= 0; --t) sc[s][k] = Mul::of(kf, qf[t][ks], sc[s][k]);
+        }
     if constexpr (F8)
       if (a.k_scales) {
 #pragma unroll
-        for (int s = 0; s < NS; ++s) sc[s] *= ks_[s];
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+          for (int k = 0; k < MK; ++k) sc[s][k] *= ks_[s];
       }
     if (edge) {
       asm volatile("");  // a branch: the other tiles are spared three instructions a score
 #pragma unroll
       for (int s = 0; s < NS; ++s)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sc[s][r] = seen[s] >> r & 1 ? sc[s][r] : -INFINITY;
+        for (int e = 0; e < RUN; ++e) sc[s][e / VAL][e % VAL] = seen[s] >> e & 1 ? sc[s][e / VAL][e % VAL] : -INFINITY;
     }
     float mt = -INFINITY;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mt = fmaxf(mt, sc[s][r]);
+      for (int e = 0; e < RUN; ++e) mt = fmaxf(mt, sc[s][e / VAL][e % VAL]);
+    if constexpr (C == 16) mt = max_pair16(mt);
     mt = max_pair32(mt);
+    // the running maximum is raised when it is passed by more than 2^8 (the weights
+    // stay below that); all lanes of a column agree
     if (__ballot(mt > m + kKvRescale || m == -INFINITY)) {
       const float m1 = fmaxf(m, mt), f = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
       m = m1;
@@ -367,12 +491,12 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < RUN / 8; ++u) {
         bf16x8 pf[TERMS];
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float p = __builtin_amdgcn_exp2f(sc[s][8 * u + e] - base);
+          float p = __builtin_amdgcn_exp2f(sc[s][(8 * u + e) / VAL][(8 * u + e) % VAL] - base);
           sum[e & 1] += p;
           if constexpr (F8) {  // weights that are not seen stay zero whatever the scale is
             p *= vs_[s];
@@ -387,34 +511,37 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
         l += sum[0] + sum[1];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const bf16x8 vf = operand_of<F8>(v_piece(buf, n, KW == 1 ? s : kw, u), F8 ? u : 0);
+          const bf16x8 vf = v_operand(buf, n, KW == 1 ? s : kw, u);
 #pragma unroll
-          for (int t = TERMS - 1; t >= 0; --t) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t], o[n], 0, 0, 0);
+          for (int t = TERMS - 1; t >= 0; --t) o[n] = Mul::of(vf, pf[t], o[n]);
         }
       }
   }
   if (bad) raise_status(a.status, kStatusPage);
+  if constexpr (C == 16) l = sum_pair16(l);
   l = sum_pair32(l);
   uint32_t any_nan = 0;
 #pragma unroll
-  for (int k = 0; k < NT / 2; ++k) any_nan |= nans[k];
+  for (int k = 0; k < (NT * VAL + 31) / 32; ++k) any_nan |= nans[k];
   if (__ballot(any_nan != 0)) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[n][r] = nans[n / 2] >> (n % 2 * 16 + r) & 1 ? NAN : o[n][r];
+      for (int r = 0; r < VAL; ++r) o[n][r] = nans[n * VAL / 32] >> (n * VAL % 32 + r) & 1 ? NAN : o[n][r];
   }
 
   // two waves with the same columns meet in LDS, the second's values in units of its maximum
+  constexpr int QUADS = VAL / 4;
   if constexpr (KW == 2) {
     __syncthreads();
-    f32x4 *part = (f32x4 *)lds_bytes + cw * (NT * 4 * 64);
+    f32x4 *part = (f32x4 *)lds_bytes + cw * (NT * QUADS * 64);
     float *ml = (float *)(lds_bytes + 64 * HD * 4) + cw * 128;
     if (kw == 1) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) part[(n * 4 + k) * 64 + lane] = f32x4{o[n][4 * k], o[n][4 * k + 1], o[n][4 * k + 2], o[n][4 * k + 3]};
+        for (int k = 0; k < QUADS; ++k)
+          part[(n * QUADS + k) * 64 + lane] = f32x4{o[n][4 * k], o[n][4 * k + 1], o[n][4 * k + 2], o[n][4 * k + 3]};
       ml[lane] = m;
       ml[64 + lane] = l;
     }
@@ -426,22 +553,22 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const f32x4 v = part[(n * 4 + k) * 64 + lane];
+      for (int k = 0; k < QUADS; ++k) {
+        const f32x4 v = part[(n * QUADS + k) * 64 + lane];
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[n][4 * k + r] = o[n][4 * k + r] * f0 + v[r] * f1;
       }
   }
-  const int col = 32 * cw + c;
+  const int col = C * cw + c;
   if (col >= cols) return;
   const float scale = l != 0.f ? a.v_scale / l : 0.f;
   const int j = row_of(m0 + col);
-  const int64_t oi = (int64_t)(sq.from + j) * a.ldo + (int64_t)(kvh * group + m0 + col - j * group) * HD + 4 * h;
+  const int64_t oi = (int64_t)(sq.from + j) * a.ldo + (int64_t)(kvh * group + m0 + col - j * group) * HD + 4 * g;
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int64_t at = oi + 32 * n + 8 * k;
+    for (int k = 0; k < QUADS; ++k) {
+      const int64_t at = oi + C * n + 4 * GROUPS * k;
       const f32x4 v = f32x4{o[n][4 * k], o[n][4 * k + 1], o[n][4 * k + 2], o[n][4 * k + 3]} * scale;
       if (a.out_vec) {
         if constexpr (F32) *(f32x4 *)((float *)a.out + at) = v;
@@ -456,7 +583,7 @@ __global__ __launch_bounds__(256, (kPromptPerSimd<HD, F32>)) void kv_prompt_kern
 template <int HD, bool F32, bool F8, int KW>
 static hipError_t prompt_attr() {
   return hipFuncSetAttribute((const void *)kv_prompt_kernel<HD, F32, F8, KW>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                             prompt_lds_bytes<HD, F8, KW>());
+                             (PromptLds<HD, F8, KW>::bytes));
 }
 template <int HD, bool F32, bool F8>
 static hipError_t prompt_attrs() {
@@ -479,7 +606,7 @@ template <int HD, bool F32, bool F8, int KW>
 static hipError_t launch_prompt_type(const KvRowsArgs &a, hipStream_t s) {
   // as many workgroups as any starts could need
   const int64_t grid = a.d.n_kv_heads * ((int64_t)a.n_rows * a.group / (128 / KW) + a.n_seqs);
-  hipLaunchKernelGGL((kv_prompt_kernel<HD, F32, F8, KW>), dim3((unsigned)grid), dim3(256), (prompt_lds_bytes<HD, F8, KW>()), s, a);
+  hipLaunchKernelGGL((kv_prompt_kernel<HD, F32, F8, KW>), dim3((unsigned)grid), dim3(kPromptThreads<HD, F32>), ((PromptLds<HD, F8, KW>::bytes)), s, a);
   return hipGetLastError();
 }
 template <int HD, int KW>
