@@ -224,123 +224,234 @@ hipError_t launch_kv_append_blocks(const KvAppendArgs &a, bool f32, hipStream_t 
 }
 
 // ---------------------------------------------------------------------------
-// Pages of new tokens.  Every workgroup works out the sums over all sequences for itself
-// (a run of them per thread, see PlanScan) and fills its share of the table's entries and
-// of the slots; the last to be done writes lengths and the free pages' number, which may
-// be where the others read them.
+// Pages of new tokens.  Every workgroup works out the sums over all sequences for itself,
+// into LDS (up to kSumEntries of them; with more sequences an entry stands for a run), and
+// fills its share of the table's entries and of the slots, eight rows a thread.  Lengths
+// and the free pages' number may be written where the others read them: then by the last
+// workgroup to be done.  64 sequences with a token each: 3.3 us, four dependent loads and
+// four scans; 1024 prompts, 530 000 rows: see there.
 // ---------------------------------------------------------------------------
-// The run of sequences (a thread's of the scan) that item i falls to, of sums up to and
-// with each: the first above i.
-__device__ __forceinline__ int run_of(const int *upto, int n, int i) {
+constexpr int kSumEntries = 2048, kSumsPerThread = kSumEntries / 256;
+
+// Sums of two values over the threads, each within 31 bits in all.
+struct SumScan {
+  int *lds;  // [8] for each scan
+  // Sums of the threads before this one, and of all.
+  __device__ __forceinline__ void operator()(int x, int y, int *x_before, int *x_all, int *y_before, int *y_all) {
+    const int x_upto = scan_wave64(x), y_upto = scan_wave64(y), wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 63) {
+      lds[wave] = x_upto;
+      lds[4 + wave] = y_upto;
+    }
+    __syncthreads();
+    *x_before = x_upto - x;
+    *y_before = y_upto - y;
+    *x_all = *y_all = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      *x_before += w < wave ? lds[w] : 0;
+      *y_before += w < wave ? lds[4 + w] : 0;
+      *x_all += lds[w];
+      *y_all += lds[4 + w];
+    }
+    lds += 8;
+  }
+};
+// The first entry whose sum is above i.
+__device__ __forceinline__ int entry_of(const int *upto, int n, int i) {
   int lo = 0;
-  for (int step = n / 2; step > 0; step /= 2)
-    if (upto[lo + step - 1] <= i) lo += step;
+  for (int step = kSumEntries / 2; step > 0; step /= 2)
+    if (lo + step <= n && upto[lo + step - 1] <= i) lo += step;
   return lo;
 }
 
+// Slots of runs of RUN rows; `begin` and `next` walk the sequences from an entry on.
+template <int RUN, class Begin, class Next>
+__device__ __forceinline__ void fill_slots(const KvReserveArgs &a, int me, int everyone, int total_rows, int n_free, int entries,
+                                           const int *rows_upto, Begin begin, Next next, bool *odd) {
+  const bool wide = RUN > 1 && ((uintptr_t)a.slots & 15) == 0;
+  for (int64_t r0 = (int64_t)me * RUN; r0 < a.n_rows; r0 += (int64_t)everyone * RUN) {
+    int64_t slot[RUN];
+    int id[RUN], off[RUN];
+#pragma unroll
+    for (int k = 0; k < RUN; ++k) slot[k] = -1;
+    if (r0 < total_rows) {
+      auto s = begin(entry_of(rows_upto, entries - 1, (int)r0));
+#pragma unroll
+      for (int k = 0; k < RUN; ++k) {
+        const int r = min((int)r0 + k, total_rows - 1);
+        while (s.b < a.n_seqs - 1 && r >= s.row + s.n) next(&s);  // the last at the latest
+        const int p = s.len + r - s.row, i = (p >> a.page_shift) - pages_of(s.len, a.page_shift);
+        off[k] = p & ((1 << a.page_shift) - 1);
+        // below 0: the page that the sequence's last token is in
+        const int32_t *at = i < 0 ? a.table + (int64_t)s.b * a.pages_per_seq + (p >> a.page_shift) : a.free_pages + (n_free - 1 - (s.page + i));
+        id[k] = *at;
+      }
+#pragma unroll
+      for (int k = 0; k < RUN; ++k) {
+        const bool fine = id[k] >= 0 && id[k] < a.n_pages;
+        *odd |= !fine;
+        if (fine && r0 + k < total_rows) slot[k] = ((int64_t)id[k] << a.page_shift) + off[k];
+      }
+    }
+    if (wide && r0 + RUN <= a.n_rows) {
+      typedef int64_t i64x2_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int k = 0; k + 1 < RUN; k += 2) *(i64x2_t *)(a.slots + r0 + k) = i64x2_t{slot[k], slot[k + 1]};
+    } else {
+#pragma unroll
+      for (int k = 0; k < RUN; ++k)
+        if (r0 + k < a.n_rows) a.slots[r0 + k] = slot[k];
+    }
+  }
+}
+
 __global__ __launch_bounds__(256) void kv_reserve_kernel(KvReserveArgs a) {
-  __shared__ int plan[6 * 4], rows_upto[256], pages_upto[256], word[1];
-  PlanScan<4> scan(a.n_seqs, plan);
-  const int threads = scan.block ? 256 : 64, b0 = scan.me * scan.per;
+  __shared__ int scans[2 * 8], rows_upto[kSumEntries], pages_upto[kSumEntries], lens[kSumEntries], word[1];
+  SumScan scan{scans};
+  const int per = (a.n_seqs + kSumEntries - 1) / kSumEntries, entries = (a.n_seqs + per - 1) / per;  // sequences of an entry
+  const int mine = (entries + 255) / 256, e0 = threadIdx.x * mine;                                  // entries of a thread
   auto tokens = [&](int b) { return a.new_tokens ? a.new_tokens[b] : 1; };
+  auto pages = [&](int len, int n) { return pages_of(len + n, a.page_shift) - pages_of(len, a.page_shift); };
+  const int n_free = *a.n_free;
   bool bad = false;
   int64_t rows = 0;
-  for (int b = b0; b < min(b0 + scan.per, a.n_seqs); ++b) {
-    const int len = a.lens[b], n = tokens(b);
-    if (growth_ok(len, n, a.pages_per_seq, a.page_shift)) rows += n;
-    else bad = true;
+  int row_sum[kSumsPerThread], page_sum[kSumsPerThread], need = 0;  // up to and with each entry; checked before they count
+  auto count = [&](int len, int n) {
+    if (growth_ok(len, n, a.pages_per_seq, a.page_shift)) {
+      rows += n;
+      need += pages(len, n);
+    } else {
+      bad = true;
+    }
+  };
+  if (per == 1) {
+    int len[kSumsPerThread], n[kSumsPerThread];  // all on their way at once
+#pragma unroll
+    for (int k = 0; k < kSumsPerThread; ++k) {
+      const int b = min(e0 + min(k, mine - 1), a.n_seqs - 1);
+      len[k] = a.lens[b];
+      n[k] = tokens(b);
+    }
+#pragma unroll
+    for (int k = 0; k < kSumsPerThread; ++k) {
+      if (k < mine && e0 + k < a.n_seqs) {
+        lens[e0 + k] = len[k];
+        count(len[k], n[k]);
+      }
+      row_sum[k] = (int)rows;
+      page_sum[k] = need;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kSumsPerThread; ++k) {
+      if (k < mine)
+        for (int b = (e0 + k) * per; b < min((e0 + k + 1) * per, a.n_seqs); ++b) count(a.lens[b], tokens(b));
+      row_sum[k] = (int)rows;
+      page_sum[k] = need;
+    }
   }
-  int hi, lo;
-  scan((int)(rows >> 22), &hi);
-  scan((int)(rows & 0x3FFFFF), &lo);
+  int hi, lo, none[2];
+  scan((int)(rows >> 22), (int)(rows & 0x3FFFFF), &none[0], &hi, &none[1], &lo);
   const int64_t all_rows = ((int64_t)hi << 22) + lo;
-  bad |= all_rows > 0x7FFFFFFF || (a.slots && all_rows > a.n_rows);
+  bad |= all_rows > 0x7FFFFFFF || (a.slots && all_rows > a.n_rows) || n_free < 0 || n_free > a.n_pages;
   bad = __syncthreads_or(bad);
   // sums fit from here on; a page that is needed gets a row at least
-  int need = 0, total_rows = 0, total = 0, my_rows = bad ? 0 : (int)rows;
-  for (int b = b0; !bad && b < min(b0 + scan.per, a.n_seqs); ++b) {
-    const int len = a.lens[b];
-    need += pages_of(len + tokens(b), a.page_shift) - pages_of(len, a.page_shift);
-  }
-  const int rows_to = scan(my_rows, &total_rows), pages_to = scan(need, &total);
-  const int n_free = *a.n_free;
-  bad |= n_free < 0 || n_free > a.n_pages || total > n_free;
-  if (threadIdx.x < (unsigned)threads) {
-    rows_upto[threadIdx.x] = rows_to;
-    pages_upto[threadIdx.x] = pages_to;
-  }
+  int rows_before, total_rows, pages_before, total;
+  scan(bad ? 0 : (int)rows, bad ? 0 : need, &rows_before, &total_rows, &pages_before, &total);
+  bad |= total > n_free;
+#pragma unroll
+  for (int k = 0; k < kSumsPerThread; ++k)
+    if (k < mine && e0 + k < entries) {
+      rows_upto[e0 + k] = rows_before + row_sum[k];
+      pages_upto[e0 + k] = pages_before + page_sum[k];
+    }
   __syncthreads();
-  const int me = blockIdx.x * 256 + threadIdx.x, everyone = gridDim.x * 256;
+  // Nothing that may be written in place is read from here on, but for lengths with more
+  // sequences than entries: that this workgroup has got here can be told at once.
+  const bool early = per == 1 && gridDim.x > 1;
+  unsigned arrived = 0;
+  if (early && threadIdx.x == 0) arrived = __hip_atomic_fetch_add(a.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // the first workgroups fill the slots, the others the table, or each does both
+  const bool apart = a.slot_wgs < (int)gridDim.x, slots = a.slots && (int)blockIdx.x < a.slot_wgs, table = !apart || (int)blockIdx.x >= a.slot_wgs;
+  const int me = blockIdx.x * 256 + threadIdx.x, slot_threads = a.slot_wgs * 256;
+  const int table_me = apart ? me - slot_threads : me, table_threads = apart ? (int)gridDim.x * 256 - slot_threads : slot_threads;
   if (bad) {
     if (me == 0) raise_status(a.status, kStatusPage);
-    if (a.row_start)
-      for (int b = me; b <= a.n_seqs; b += everyone) a.row_start[b] = 0;
-    if (a.slots)
-      for (int64_t r = me; r < a.n_rows; r += everyone) a.slots[r] = -1;
+    if (a.row_start && blockIdx.x == 0)
+      for (int b = threadIdx.x; b <= a.n_seqs; b += 256) a.row_start[b] = 0;
+    if (slots)
+      for (int64_t r = me; r < a.n_rows; r += slot_threads) a.slots[r] = -1;
   } else {
     bool odd = false;
-    auto page = [&](int i) {  // the i-th that is taken
-      return a.free_pages[n_free - 1 - i];
+    // sequences from entry e on: what comes before sequence b, and its length and new rows
+    struct At {
+      int e, b, row, page, len, n;
     };
-    // the sequence of row or page i: its first row or page, and its tokens before
-    auto walk = [&](const int *upto, int i, bool by_rows, int *first) {
-      const int run = run_of(upto, threads, i);
-      int b = run * scan.per, at = run ? upto[run - 1] : 0;
-      for (; b < a.n_seqs - 1; ++b) {  // the last at the latest
-        const int len = a.lens[b], n = tokens(b);
-        const int k = by_rows ? n : pages_of(len + n, a.page_shift) - pages_of(len, a.page_shift);
-        if (i < at + k) break;
-        at += k;
+    auto enter = [&](At *s) {
+      if (per == 1) {
+        s->len = lens[s->b];
+        s->n = rows_upto[s->b] - s->row;
+      } else {
+        s->len = a.lens[s->b];
+        s->n = tokens(s->b);
       }
-      *first = at;
-      return b;
     };
-    for (int i = me; i < total; i += everyone) {
-      int first;
-      const int b = walk(pages_upto, i, false, &first), id = page(i);
-      a.table[(int64_t)b * a.pages_per_seq + pages_of(a.lens[b], a.page_shift) + i - first] = id;
+    auto begin = [&](int e) {
+      At s{e, e * per, e ? rows_upto[e - 1] : 0, e ? pages_upto[e - 1] : 0, 0, 0};
+      enter(&s);
+      return s;
+    };
+    auto next = [&](At *s) {
+      s->row += s->n;
+      s->page += pages(s->len, s->n);
+      ++s->b;
+      enter(s);
+    };
+    for (int i = table_me; table && i < total; i += table_threads) {
+      At s = begin(entry_of(pages_upto, entries - 1, i));
+      while (s.b < a.n_seqs - 1 && i >= s.page + pages(s.len, s.n)) next(&s);  // the last at the latest
+      const int id = a.free_pages[n_free - 1 - i];
+      a.table[(int64_t)s.b * a.pages_per_seq + pages_of(s.len, a.page_shift) + i - s.page] = id;
       odd |= id < 0 || id >= a.n_pages;
     }
-    if (a.slots)
-      for (int64_t r = me; r < a.n_rows; r += everyone) {
-        int64_t slot = -1;
-        if (r < total_rows) {
-          int first, first_page = 0;
-          const int b = walk(rows_upto, (int)r, true, &first), len = a.lens[b], p = len + (int)r - first;
-          const int i = (p >> a.page_shift) - pages_of(len, a.page_shift);
-          int id;
-          if (i < 0) {  // the page that the sequence's last token is in
-            id = a.table[(int64_t)b * a.pages_per_seq + (p >> a.page_shift)];
-          } else {
-            const int run = b / scan.per;
-            first_page = run ? pages_upto[run - 1] : 0;
-            for (int x = run * scan.per; x < b; ++x)
-              first_page += pages_of(a.lens[x] + tokens(x), a.page_shift) - pages_of(a.lens[x], a.page_shift);
-            id = page(first_page + i);
-          }
-          const bool fine = id >= 0 && id < a.n_pages;
-          odd |= !fine;
-          if (fine) slot = ((int64_t)id << a.page_shift) + (p & ((1 << a.page_shift) - 1));
-        }
-        a.slots[r] = slot;
-      }
+    if (slots && a.n_rows <= slot_threads) {
+      fill_slots<1>(a, me, slot_threads, total_rows, n_free, entries, rows_upto, begin, next, &odd);
+    } else if (slots) {
+      fill_slots<8>(a, me, slot_threads, total_rows, n_free, entries, rows_upto, begin, next, &odd);
+    }
     if (odd) raise_status(a.status, kStatusPage);
   }
-  if (gridDim.x > 1 && !last_to_arrive(a.arrived, gridDim.x, (float *)word)) return;
-  __syncthreads();
-  if (scan.block || threadIdx.x < 64) {
-    int at = rows_to - my_rows;
-    for (int b = b0; b < min(b0 + scan.per, a.n_seqs); ++b) {
-      const int len = a.lens[b], n = bad ? 0 : tokens(b);
-      if (a.row_start && !bad) a.row_start[b] = at;
+  // row_start and, where it lies apart, lens_out are the first workgroup's
+  const bool in_place = a.lens_out == a.lens;
+  auto finish = [&](bool starts, bool lengths) {
+    int at = rows_before;
+    for (int b = e0 * per; b < min((e0 + mine) * per, a.n_seqs); ++b) {
+      const int len = per == 1 ? lens[b] : a.lens[b], n = bad ? 0 : per == 1 ? rows_upto[b] - at : tokens(b);
+      if (starts) a.row_start[b] = at;
       at += n;
-      a.lens_out[b] = len + n;
+      if (lengths) a.lens_out[b] = len + n;
     }
+  };
+  const bool starts = a.row_start && !bad;
+  if (blockIdx.x == 0) {
+    if (starts || !in_place) finish(starts, !in_place);
+    if (starts && threadIdx.x == 0) a.row_start[a.n_seqs] = total_rows;
   }
-  if (threadIdx.x == 0) {
-    if (a.row_start && !bad) a.row_start[a.n_seqs] = total_rows;
-    *a.n_free_out = bad ? n_free : n_free - total;
+  if (early) {
+    if (threadIdx.x == 0) {
+      word[0] = arrived == gridDim.x - 1;
+      if (word[0]) __hip_atomic_store(a.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!word[0]) return;
+  } else if (gridDim.x > 1) {
+    if (!last_to_arrive(a.arrived, gridDim.x, (float *)word)) return;
+  } else {
+    __syncthreads();
   }
+  if (in_place && !bad) finish(false, true);
+  if (threadIdx.x == 0) *a.n_free_out = bad ? n_free : n_free - total;
 }
 
 // Pages that no later token sees: counted by a wave per sequence, then moved to the free
@@ -354,14 +465,22 @@ __device__ __forceinline__ bool gone(const KvReleaseArgs &a, int len, int i, int
 __global__ __launch_bounds__(256) void kv_count_gone_kernel(KvReleaseArgs a) {
   const int lane = threadIdx.x & 63;
   bool odd = false;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.n_free_was = *a.n_free;  // which the other kernel reads and writes
   for (int b = blockIdx.x * 4 + (threadIdx.x >> 6); b < a.n_seqs; b += gridDim.x * 4) {
     const int len = a.lens[b];
     const int32_t *row = a.table + (int64_t)b * a.pages_per_seq;
+    constexpr int AHEAD = 4;
     int n = 0;
     odd |= len < 0;
-    for (int i0 = 0; len >= 0 && i0 < a.pages_per_seq; i0 += 64) {
-      const int i = i0 + lane;
-      n += __popcll(__ballot(i < a.pages_per_seq && gone(a, len, i, row[min(i, a.pages_per_seq - 1)], &odd)));
+    for (int i0 = 0; len >= 0 && i0 < a.pages_per_seq; i0 += 64 * AHEAD) {
+      int id[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) id[k] = row[min(i0 + 64 * k + lane, a.pages_per_seq - 1)];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const int i = i0 + 64 * k + lane;
+        n += __popcll(__ballot(i < a.pages_per_seq && gone(a, len, i, id[k], &odd)));
+      }
     }
     if (lane == 0) a.counts[b] = n;
   }
@@ -369,58 +488,75 @@ __global__ __launch_bounds__(256) void kv_count_gone_kernel(KvReleaseArgs a) {
 }
 
 __global__ __launch_bounds__(256) void kv_release_kernel(KvReleaseArgs a) {
-  __shared__ int plan[2 * 4], upto[256], word[1];
-  PlanScan<4> scan(a.n_seqs, plan);
-  const int b0 = scan.me * scan.per;
-  int mine = 0, total;  // pages: at most as many as the pool has, else nothing is done
-  int64_t all = 0;
-  for (int b = b0; b < min(b0 + scan.per, a.n_seqs); ++b) all += a.counts[b];
-  const int n_free = *a.n_free;
-  mine = all > a.n_pages ? a.n_pages : (int)all;
-  bool bad = n_free < 0 || n_free > a.n_pages || all > a.n_pages;
-  // up to 256 runs of up to 2^31 pages: in units of 2^10 first
-  int big;
-  scan(mine >> 10, &big);
-  bad |= big > (a.n_pages >> 10) + 1;
-  bad = __syncthreads_or(bad);
-  const int to = scan(bad ? 0 : mine, &total);
+  __shared__ int scans[2 * 8], upto[kSumEntries];
+  SumScan scan{scans};
+  const int per = (a.n_seqs + kSumEntries - 1) / kSumEntries, entries = (a.n_seqs + per - 1) / per;
+  const int mine = (entries + 255) / 256, e0 = threadIdx.x * mine;
+  const int n_free = *a.n_free_was;
+  int64_t pages = 0;  // at most as many as the pool has, else nothing is done
+  int sums[kSumsPerThread], first[kSumsPerThread];
+#pragma unroll
+  for (int k = 0; k < kSumsPerThread; ++k) first[k] = a.counts[min((e0 + min(k, mine - 1)) * per, a.n_seqs - 1)];
+#pragma unroll
+  for (int k = 0; k < kSumsPerThread; ++k) {
+    if (k < mine && (e0 + k) * per < a.n_seqs) {
+      pages += first[k];
+      for (int b = (e0 + k) * per + 1; b < min((e0 + k + 1) * per, a.n_seqs); ++b) pages += a.counts[b];
+    }
+    sums[k] = (int)pages;
+  }
+  int big, before, total, none[3];
+  const bool many = pages > a.n_pages;
+  scan(many ? 1 << 22 : (int)(pages >> 10), 0, &none[0], &big, &none[1], &none[2]);  // in units of 2^10, so that they fit
+  bool bad = __syncthreads_or(many) || big > (a.n_pages >> 10) + 1 || n_free < 0 || n_free > a.n_pages;
+  scan(bad ? 0 : (int)pages, 0, &before, &total, &none[0], &none[1]);
   bad |= (int64_t)n_free + total > a.n_pages;
-  if (scan.block || threadIdx.x < 64) upto[scan.me] = to;
+#pragma unroll
+  for (int k = 0; k < kSumsPerThread; ++k)
+    if (k < mine && e0 + k < entries) upto[e0 + k] = before + sums[k];
   __syncthreads();
   if (!bad) {
     const int lane = threadIdx.x & 63;
     for (int b = blockIdx.x * 4 + (threadIdx.x >> 6); b < a.n_seqs; b += gridDim.x * 4) {
       if (a.counts[b] == 0) continue;
-      const int len = a.lens[b], run = b / scan.per;
-      int at = n_free + (run ? upto[run - 1] : 0);
-      for (int x = run * scan.per; x < b; ++x) at += a.counts[x];
+      const int len = a.lens[b], e = b / per;
+      int at = n_free + (e ? upto[e - 1] : 0);
+      for (int x = e * per; x < b; ++x) at += a.counts[x];
       int32_t *row = a.table + (int64_t)b * a.pages_per_seq;
-      for (int i0 = 0; i0 < a.pages_per_seq; i0 += 64) {
-        const int i = i0 + lane, id = row[min(i, a.pages_per_seq - 1)];
-        bool odd = false;
-        const bool go = i < a.pages_per_seq && gone(a, len, i, id, &odd);
-        const uint64_t goes = __ballot(go);
-        if (go) {
-          const int to_i = at + __popcll(goes & ((1ull << lane) - 1));
-          if (to_i < a.n_pages) a.free_pages[to_i] = id;  // always, unless the caller's arrays change while this runs
-          row[i] = -1;
+      constexpr int AHEAD = 4;
+      for (int i0 = 0; i0 < a.pages_per_seq; i0 += 64 * AHEAD) {
+        int id[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) id[k] = row[min(i0 + 64 * k + lane, a.pages_per_seq - 1)];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+          const int i = i0 + 64 * k + lane;
+          bool odd = false;
+          const bool go = i < a.pages_per_seq && gone(a, len, i, id[k], &odd);
+          const uint64_t goes = __ballot(go);
+          if (go) {
+            const int to = at + __popcll(goes & ((1ull << lane) - 1));
+            if (to < a.n_pages) a.free_pages[to] = id[k];  // always, unless the caller's arrays change while this runs
+            row[i] = -1;
+          }
+          at += __popcll(goes);
         }
-        at += __popcll(goes);
       }
     }
   } else if (blockIdx.x == 0 && threadIdx.x == 0) {
     raise_status(a.status, kStatusPage);
   }
-  if (gridDim.x > 1 && !last_to_arrive(a.arrived, gridDim.x, (float *)word)) return;
-  if (threadIdx.x == 0 && !bad) *a.n_free = n_free + total;
+  if (blockIdx.x == 0 && threadIdx.x == 0 && !bad) *a.n_free = n_free + total;
 }
 
 hipError_t launch_kv_reserve(const KvReserveArgs &a, hipStream_t s) {
   if (a.n_seqs < 1 || a.pages_per_seq < 1 || a.page_shift < 4 || a.n_pages < 1 || a.n_rows < 0) return hipErrorInvalidValue;
-  // a workgroup for every 2048 slots, up to two a CU
+  // a workgroup for every 2048 slots, up to two a CU, and from four of them on others for
+  // the table
+  KvReserveArgs p = a;
   const int64_t items = std::max<int64_t>(a.slots ? a.n_rows : 0, (int64_t)a.n_seqs * 8);
-  const unsigned grid = (unsigned)std::min<int64_t>((items + 2047) / 2048, 512);
-  hipLaunchKernelGGL(kv_reserve_kernel, dim3(grid), dim3(256), 0, s, a);
+  p.slot_wgs = (int)std::min<int64_t>((items + 2047) / 2048, 512);
+  hipLaunchKernelGGL(kv_reserve_kernel, dim3(p.slot_wgs < 4 ? p.slot_wgs : p.slot_wgs + std::min(p.slot_wgs / 2, 128)), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -92,7 +92,7 @@ uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_str
   const size_t rows = 16;  // of a slot; a single token's attention takes up to its group
   kv->slots = max_slots(kv_attend_target(kv->n_cu, m.head_dim));
   const size_t o_arrived = o_turns + 128 * sizeof(double), o_pages = o_arrived + 2 * (size_t)kv->slots * sizeof(unsigned);
-  const size_t o_ml = (o_pages + (1 + (size_t)m.max_seqs) * sizeof(unsigned) + 255) / 256 * 256;
+  const size_t o_ml = (o_pages + (2 + (size_t)m.max_seqs) * sizeof(unsigned) + 255) / 256 * 256;
   const size_t o_part = o_ml + kv->slots * rows * sizeof(uint64_t);
   const size_t total = o_part + kv->slots * rows * m.head_dim * sizeof(float);
   e = hipMalloc(&kv->buf, total);

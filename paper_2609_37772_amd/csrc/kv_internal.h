@@ -78,6 +78,7 @@ struct KvReserveArgs {
   int n_rows;
   int n_pages, page_shift;
   unsigned *status, *arrived;        // arrived: zero between launches
+  int slot_wgs;                      // set by the launcher: workgroups that fill slots
 };
 struct KvReleaseArgs {
   const int32_t *lens;
@@ -86,8 +87,8 @@ struct KvReleaseArgs {
   int32_t *free_pages, *n_free;
   int window, sinks;
   int n_pages, page_shift;
-  int32_t *counts;                   // [n_seqs] workspace
-  unsigned *status, *arrived;
+  int32_t *counts, *n_free_was;      // [n_seqs], [1]: workspace
+  unsigned *status;
 };
 
 // The expert's prefix from the pages (stores as in PrefixArgs).
@@ -141,6 +142,6 @@ struct uad_kv {
   unsigned *arrived = nullptr;
   int slots = 0;
   unsigned *pages_arrived = nullptr;  // of the page tables' calls
-  int32_t *page_counts = nullptr;     // [max_seqs], likewise
+  int32_t *page_counts = nullptr;     // [1 + max_seqs], likewise
   hipEvent_t ev = nullptr;  // orders the cache's stream and an expert's
 };

@@ -138,8 +138,8 @@ uad_status uad_kv_release(uad_kv *kv, const int32_t *lens, int32_t *page_table, 
   a.free_pages = free_pages; a.n_free = n_free;
   a.window = std::min(window, kMaxSeen); a.sinks = std::min(n_sinks, kMaxSeen);
   a.n_pages = kv->cfg.n_pages; a.page_shift = dims_of(kv).page_shift;
-  a.counts = kv->page_counts;
-  a.status = kv->status; a.arrived = kv->pages_arrived;
+  a.n_free_was = kv->page_counts; a.counts = kv->page_counts + 1;
+  a.status = kv->status;
   const hipError_t e = launch_kv_release(a, kv->stream);
   return e == hipSuccess ? UAD_OK : kv_hip_fail(kv, e, fn, "launch");
 }
