@@ -72,12 +72,12 @@ class uad_kv_config(ctypes.Structure):
 
 _lib: Optional[ctypes.CDLL] = None
 _marshal = None               # the checks of decoding's calls in C (csrc/marshal.c) where built, and the entry points' addresses
-_append_at = _attend_at = 0
+_append_at = _attend_at = _rows_at = _reserve_at = _release_at = 0
 
 
 def load_library() -> ctypes.CDLL:
     """Load libuad.so (built by ``python -m paper_2609_37772_amd.build``); raise if absent."""
-    global _lib, _marshal, _append_at, _attend_at
+    global _lib, _marshal, _append_at, _attend_at, _rows_at, _reserve_at, _release_at
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -122,10 +122,12 @@ def load_library() -> ctypes.CDLL:
         fn.restype = res
     try:
         from . import _marshal as marshal
-        marshal.setup(torch.Tensor, torch.float32, torch.bfloat16, torch.int32)
+        marshal.setup(torch.Tensor, torch.float32, torch.bfloat16, torch.int32, torch.int64)
     except ImportError:
         marshal = None  # every call's checks are made here then, the same ones
-    _append_at, _attend_at = (ctypes.cast(f, ctypes.c_void_p).value for f in (lib.uad_kv_append, lib.uad_kv_attend))
+    _append_at, _attend_at, _rows_at, _reserve_at, _release_at = (
+        ctypes.cast(f, ctypes.c_void_p).value
+        for f in (lib.uad_kv_append, lib.uad_kv_attend, lib.uad_kv_attend_rows, lib.uad_kv_reserve, lib.uad_kv_release))
     _marshal, _lib = marshal, lib
     return lib
 
@@ -556,20 +558,44 @@ def uad_kv_attend_rows(kv: int, layer: int, q: torch.Tensor, out: torch.Tensor, 
                        row_start: Optional[torch.Tensor], positions: Optional[torch.Tensor], scale: float, window: int,
                        n_sinks: int, causal: bool, row_shape: Tuple[int, int], device: int = 0) -> None:
     """Attention of rows q [n_rows][Hq][hd], the newest of every sequence, over a layer's pages into out."""
+    if _marshal is None:
+        load_library()
+    st = None
+    if _marshal is not None:
+        st = _marshal.rows(_rows_at, kv, layer, q, out, page_table, lens, row_start, positions, scale, window, n_sinks, causal,
+                           *row_shape, device)
+    if st is None:  # not the usual case
+        st = _rows_checked(kv, layer, q, out, page_table, lens, row_start, positions, scale, window, n_sinks, causal, row_shape, device)
+    if st:
+        _check_kv(kv, st, "uad_kv_attend_rows")
+
+
+def _rows_checked(kv, layer, q, out, page_table, lens, row_start, positions, scale, window, n_sinks, causal, row_shape, device) -> int:
     n, dtype, ldq, ldo = _row_steps(q, out, row_shape, "q out", device)
     pt, wide, pl, seqs = _table(page_table, lens, device)
     ps = None if row_start is None else _ints(row_start, (seqs + 1,), "row_start", device)
     pp = None if positions is None else _ints(positions, (n,), "positions", device)
-    st = load_library().uad_kv_attend_rows(kv, layer, q.data_ptr(), out.data_ptr(), dtype, ldq, ldo, n, ps, pl, pp, pt, wide, seqs,
-                                           scale, window, n_sinks, int(causal))
-    if st:
-        _check_kv(kv, st, "uad_kv_attend_rows")
+    return load_library().uad_kv_attend_rows(kv, layer, q.data_ptr(), out.data_ptr(), dtype, ldq, ldo, n, ps, pl, pp, pt, wide, seqs,
+                                             scale, window, n_sinks, int(causal))
 
 
 def uad_kv_reserve(kv: int, lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
                    new_tokens: Optional[torch.Tensor], row_start: Optional[torch.Tensor], slots: Optional[torch.Tensor],
                    lens_out: torch.Tensor, n_free_out: torch.Tensor, n_pages: int, device: int = 0) -> None:
     """Pages for new tokens from the free ones into the page table (new_tokens None: one for each sequence)."""
+    if _marshal is None:
+        load_library()
+    st = None
+    if _marshal is not None:
+        st = _marshal.reserve(_reserve_at, kv, lens, page_table, free_pages, n_free, new_tokens, row_start, slots, lens_out, n_free_out,
+                              n_pages, device)
+    if st is None:  # not the usual case
+        st = _reserve_checked(kv, lens, page_table, free_pages, n_free, new_tokens, row_start, slots, lens_out, n_free_out, n_pages, device)
+    if st:
+        _check_kv(kv, st, "uad_kv_reserve")
+
+
+def _reserve_checked(kv, lens, page_table, free_pages, n_free, new_tokens, row_start, slots, lens_out, n_free_out, n_pages, device) -> int:
     pt, wide, pl, seqs = _table(page_table, lens, device)
     po, pf = _ints(lens_out, (seqs,), "lens_out", device), _ints(free_pages, (n_pages,), "free_pages", device)
     pn, pno = _ints(n_free, (1,), "n_free", device), _ints(n_free_out, (1,), "n_free_out", device)
@@ -581,19 +607,27 @@ def uad_kv_reserve(kv: int, lens: torch.Tensor, page_table: torch.Tensor, free_p
                 or slots.get_device() != device or not slots.is_contiguous():
             raise ValueError(f"slots must be a contiguous int64 tensor [n_rows] on device {device}")
         n, pl64 = slots.shape[0], slots.data_ptr()
-    st = load_library().uad_kv_reserve(kv, pl, px, po, pt, wide, seqs, pf, pn, pno, ps, pl64, n)
-    if st:
-        _check_kv(kv, st, "uad_kv_reserve")
+    return load_library().uad_kv_reserve(kv, pl, px, po, pt, wide, seqs, pf, pn, pno, ps, pl64, n)
 
 
 def uad_kv_release(kv: int, lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
                    window: int, n_sinks: int, n_pages: int, device: int = 0) -> None:
     """The pages that no later token sees go back to the free ones."""
-    pt, wide, pl, seqs = _table(page_table, lens, device)
-    pf, pn = _ints(free_pages, (n_pages,), "free_pages", device), _ints(n_free, (1,), "n_free", device)
-    st = load_library().uad_kv_release(kv, pl, pt, wide, seqs, pf, pn, window, n_sinks)
+    if _marshal is None:
+        load_library()
+    st = None
+    if _marshal is not None:
+        st = _marshal.release(_release_at, kv, lens, page_table, free_pages, n_free, window, n_sinks, n_pages, device)
+    if st is None:  # not the usual case
+        st = _release_checked(kv, lens, page_table, free_pages, n_free, window, n_sinks, n_pages, device)
     if st:
         _check_kv(kv, st, "uad_kv_release")
+
+
+def _release_checked(kv, lens, page_table, free_pages, n_free, window, n_sinks, n_pages, device) -> int:
+    pt, wide, pl, seqs = _table(page_table, lens, device)
+    pf, pn = _ints(free_pages, (n_pages,), "free_pages", device), _ints(n_free, (1,), "n_free", device)
+    return load_library().uad_kv_release(kv, pl, pt, wide, seqs, pf, pn, window, n_sinks)
 
 
 def uad_kv_synchronize(kv: int) -> None:

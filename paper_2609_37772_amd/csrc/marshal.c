@@ -8,7 +8,7 @@
 #include <Python.h>
 #include <stdint.h>
 
-static PyObject *tensor_type, *f32, *bf16, *i32;
+static PyObject *tensor_type, *f32, *bf16, *i32, *i64;
 static PyObject *s_dtype, *s_shape, *s_is_contiguous, *s_get_device, *s_data_ptr;
 
 typedef struct {
@@ -51,6 +51,14 @@ static int look_ints(PyObject *t, int64_t n, long device, void **data) {
   if (!look(t, 1, device, &x) || x.kind != i32 || x.size[0] != n) return 0;
   *data = x.data;
   return 1;
+}
+
+/* A whole number of 32 bits. */
+static int look_int(PyObject *o, int32_t *v) {
+  if (!PyLong_CheckExact(o)) return 0;
+  const long x = PyLong_AsLong(o);
+  *v = (int32_t)x;
+  return x >= INT32_MIN && x <= INT32_MAX && !PyErr_Occurred();
 }
 
 /* What both calls look at alike: two tensors of rows, page table, lengths, positions. */
@@ -125,15 +133,97 @@ static PyObject *attend(PyObject *self, PyObject *const *x, Py_ssize_t n) {
   return PyLong_FromLong(st);
 }
 
-/* setup(torch.Tensor, torch.float32, torch.bfloat16, torch.int32): kept for good */
+typedef int32_t (*rows_fn)(void *, int32_t, const void *, void *, int32_t, int64_t, int64_t, int32_t, const void *, const void *,
+                           const void *, const void *, int32_t, int32_t, float, int32_t, int32_t, int32_t);
+typedef int32_t (*reserve_fn)(void *, const void *, const void *, void *, void *, int32_t, int32_t, const void *, const void *,
+                              void *, void *, void *, int32_t);
+typedef int32_t (*release_fn)(void *, const void *, void *, int32_t, int32_t, void *, void *, int32_t, int32_t);
+
+/* rows(uad_kv_attend_rows, kv, layer, q, out, page_table, lens, row_start, positions, scale, window, sinks, causal, heads,
+ * dim, device) */
+static PyObject *rows(PyObject *self, PyObject *const *x, Py_ssize_t n) {
+  Call c;
+  void *row_start;
+  int32_t st, window, sinks;
+  (void)self;
+  if (n != 16 || !look_call(x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[8], x[13], x[14], x[15], &c) ||
+      !look_ints(x[7], c.table.size[0] + 1, c.device, &row_start) || !PyFloat_Check(x[9]) || !look_int(x[10], &window) ||
+      !look_int(x[11], &sinks) || !PyBool_Check(x[12]))
+    return long_way();
+  const float scale = (float)PyFloat_AS_DOUBLE(x[9]);
+  const int64_t row = (int64_t)c.heads * c.dim;
+  const int32_t causal = x[12] == Py_True;
+  Py_BEGIN_ALLOW_THREADS
+  st = ((rows_fn)c.fn)(c.kv, (int32_t)c.layer, c.a.data, c.b.data, c.dtype, row, row, (int32_t)c.a.size[0], row_start, c.lens,
+                       c.positions, c.table.data, (int32_t)c.table.size[1], (int32_t)c.table.size[0], scale, window, sinks, causal);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+/* What both page table calls look at alike. */
+typedef struct {
+  void *fn, *kv, *lens, *free_pages, *n_free;
+  Tensor table;
+  long device;
+} Pages;
+
+static int look_pages(PyObject *fn, PyObject *kv, PyObject *lens, PyObject *table, PyObject *free_pages, PyObject *n_free,
+                      PyObject *n_pages, PyObject *device, Pages *p) {
+  int32_t pages;
+  if (!PyLong_Check(fn) || !PyLong_Check(kv) || !PyLong_Check(device) || !look_int(n_pages, &pages)) return 0;
+  p->fn = PyLong_AsVoidPtr(fn);
+  p->kv = PyLong_AsVoidPtr(kv);
+  p->device = PyLong_AsLong(device);
+  if (PyErr_Occurred() || !p->fn || !p->kv || !look(table, 2, p->device, &p->table) || p->table.kind != i32) return 0;
+  return lens != Py_None && free_pages != Py_None && n_free != Py_None && look_ints(lens, p->table.size[0], p->device, &p->lens) &&
+         look_ints(free_pages, pages, p->device, &p->free_pages) && look_ints(n_free, 1, p->device, &p->n_free);
+}
+
+/* reserve(uad_kv_reserve, kv, lens, page_table, free_pages, n_free, new_tokens, row_start, slots, lens_out, n_free_out,
+ * n_pages, device) */
+static PyObject *reserve(PyObject *self, PyObject *const *x, Py_ssize_t n) {
+  Pages p;
+  Tensor slots = {NULL, {0, 0, 0}, NULL};
+  void *new_tokens, *row_start, *lens_out, *n_free_out;
+  int32_t st;
+  (void)self;
+  if (n != 13 || !look_pages(x[0], x[1], x[2], x[3], x[4], x[5], x[11], x[12], &p) || x[9] == Py_None || x[10] == Py_None)
+    return long_way();
+  const int64_t seqs = p.table.size[0];
+  if (!look_ints(x[6], seqs, p.device, &new_tokens) || !look_ints(x[7], seqs + 1, p.device, &row_start) ||
+      !look_ints(x[9], seqs, p.device, &lens_out) || !look_ints(x[10], 1, p.device, &n_free_out) ||
+      (x[8] != Py_None && (!look(x[8], 1, p.device, &slots) || slots.kind != i64)))
+    return long_way();
+  Py_BEGIN_ALLOW_THREADS
+  st = ((reserve_fn)p.fn)(p.kv, p.lens, new_tokens, lens_out, p.table.data, (int32_t)p.table.size[1], (int32_t)seqs, p.free_pages,
+                          p.n_free, n_free_out, row_start, slots.data, (int32_t)slots.size[0]);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+/* release(uad_kv_release, kv, lens, page_table, free_pages, n_free, window, sinks, n_pages, device) */
+static PyObject *release(PyObject *self, PyObject *const *x, Py_ssize_t n) {
+  Pages p;
+  int32_t st, window, sinks;
+  (void)self;
+  if (n != 10 || !look_pages(x[0], x[1], x[2], x[3], x[4], x[5], x[8], x[9], &p) || !look_int(x[6], &window) || !look_int(x[7], &sinks))
+    return long_way();
+  Py_BEGIN_ALLOW_THREADS
+  st = ((release_fn)p.fn)(p.kv, p.lens, p.table.data, (int32_t)p.table.size[1], (int32_t)p.table.size[0], p.free_pages, p.n_free, window,
+                          sinks);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+/* setup(torch.Tensor, torch.float32, torch.bfloat16, torch.int32, torch.int64): kept for good */
 static PyObject *setup(PyObject *self, PyObject *const *x, Py_ssize_t n) {
   (void)self;
-  if (n != 4) {
-    PyErr_SetString(PyExc_TypeError, "setup(Tensor, float32, bfloat16, int32)");
+  if (n != 5) {
+    PyErr_SetString(PyExc_TypeError, "setup(Tensor, float32, bfloat16, int32, int64)");
     return NULL;
   }
-  PyObject **keep[4] = {&tensor_type, &f32, &bf16, &i32};
-  for (int i = 0; i < 4; ++i) {
+  PyObject **keep[5] = {&tensor_type, &f32, &bf16, &i32, &i64};
+  for (int i = 0; i < 5; ++i) {
     Py_INCREF(x[i]);
     Py_XSETREF(*keep[i], x[i]);
   }
@@ -142,6 +232,9 @@ static PyObject *setup(PyObject *self, PyObject *const *x, Py_ssize_t n) {
 
 static PyMethodDef methods[] = {{"append", (PyCFunction)(void (*)(void))append, METH_FASTCALL, NULL},
                                 {"attend", (PyCFunction)(void (*)(void))attend, METH_FASTCALL, NULL},
+                                {"rows", (PyCFunction)(void (*)(void))rows, METH_FASTCALL, NULL},
+                                {"reserve", (PyCFunction)(void (*)(void))reserve, METH_FASTCALL, NULL},
+                                {"release", (PyCFunction)(void (*)(void))release, METH_FASTCALL, NULL},
                                 {"setup", (PyCFunction)(void (*)(void))setup, METH_FASTCALL, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};

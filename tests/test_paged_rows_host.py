@@ -334,10 +334,58 @@ def test_the_binding_hands_over_what_it_is_given(calls):
                          a["n_free"].data_ptr(), 5, 1)
 
 
+USUAL = [(B.uad_kv_attend_rows, rows_call()), (B.uad_kv_attend_rows, rows_call(row_start=None, q=rows_call()["q"][:3], out=rows_call()["q"][:3])),
+         (B.uad_kv_attend_rows, rows_call(positions=ints(5), causal=False)), (B.uad_kv_reserve, reserve_call()),
+         (B.uad_kv_reserve, reserve_call(new_tokens=None, row_start=None, slots=None)), (B.uad_kv_release, release_call())]
+
+
+@pytest.mark.parametrize("call,args", USUAL)
+def test_the_checks_in_c_hand_over_what_those_in_python_do(calls, monkeypatch, call, args):
+    name = {B.uad_kv_attend_rows: "rows", B.uad_kv_reserve: "reserve", B.uad_kv_release: "release"}[call]
+    used = []
+    fast = getattr(B._marshal, name)
+    monkeypatch.setattr(B._marshal, name, lambda *a: used.append(fast(*a)) or used[-1])
+    call(**args)
+    assert used == [0] and len(calls) == 1  # in C
+    monkeypatch.setattr(B, "_marshal", None)
+    call(**args)
+    assert len(calls) == 2 and calls[0] == calls[1]
+
+
+def test_the_checks_in_c_leave_odd_arguments_to_those_in_python(calls):
+    B.uad_kv_attend_rows(**rows_call(scale=1))
+    B.uad_kv_attend_rows(**rows_call(causal=1))
+    B.uad_kv_attend_rows(**rows_call(kv=None))
+    B.uad_kv_release(**release_call(kv=None))
+    assert len(calls) == 4 and calls[1][-1] == 1 and calls[2][1] is None
+    for f, n in ((B._marshal.rows, 16), (B._marshal.reserve, 13), (B._marshal.release, 10)):
+        for bad in ((), (1,), (None,) * n, (1, "x") + (None,) * (n - 2)):
+            assert f(*bad) is None
+    a = release_call()
+    order = [a[k] for k in ("kv", "lens", "page_table", "free_pages", "n_free", "window", "n_sinks", "n_pages", "device")]
+    for i, odd in ((5, 2 ** 31), (5, 1.0), (6, None), (7, 8), (8, 0)):
+        args = list(order)
+        args[i] = odd
+        assert B._marshal.release(B._release_at, *args) is None
+    assert len(calls) == 4
+
+
+def test_the_checks_in_c_keep_no_reference(calls):
+    import sys
+    a, b = rows_call(), reserve_call()
+    tensors = [t for x in (a, b) for t in x.values() if isinstance(t, torch.Tensor)]
+    before = [sys.getrefcount(t) for t in tensors]
+    for _ in range(500):
+        B.uad_kv_attend_rows(**a)
+        B.uad_kv_reserve(**b)
+        calls.clear()
+    assert all(abs(x - sys.getrefcount(t)) < 20 for x, t in zip(before, tensors))
+
+
 X5 = torch.zeros((5, HQ, HD))
 
 
-@pytest.mark.parametrize("call,change", [(B.uad_kv_attend_rows, rows_call(**c)) for c in (
+REFUSED = ([(B.uad_kv_attend_rows, rows_call(**c)) for c in (
     dict(q=X5), dict(out=X5), dict(q=X5.half(), out=X5.half()), dict(q=X5[:, :2], out=X5[:, :2]), dict(q=X5[:4].bfloat16()), dict(q=None), dict(lens=None),
     dict(lens=ints(2)), dict(page_table=ints(3)), dict(row_start=ints(3)), dict(row_start=torch.zeros(4)), dict(positions=ints(3)), dict(device=0))]
     + [(B.uad_kv_reserve, reserve_call(**c)) for c in (
@@ -345,7 +393,13 @@ X5 = torch.zeros((5, HQ, HD))
         dict(lens_out=ints(3).long()), dict(slots=ints(6)), dict(slots=torch.zeros((2, 3), dtype=torch.int64)), dict(row_start=ints(3)), dict(device=0),
         dict(slots=torch.zeros(12, dtype=torch.int64)[::2]), dict(page_table=ints(7, 3).t()))]
     + [(B.uad_kv_release, release_call(**c)) for c in (dict(lens=ints(2)), dict(free_pages=ints(10)), dict(n_free=None), dict(page_table=ints(3, 7).long()))])
-def test_the_binding_refuses_before_the_library(calls, call, change):
+
+
+@pytest.mark.parametrize("in_c", [True, False])
+@pytest.mark.parametrize("call,change", REFUSED)
+def test_the_binding_refuses_before_the_library(calls, monkeypatch, call, change, in_c):
+    if not in_c:
+        monkeypatch.setattr(B, "_marshal", None)
     with pytest.raises(ValueError):
         call(**change)
     assert not calls
