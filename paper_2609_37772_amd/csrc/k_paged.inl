@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvAppendArgs a) {
   __shared__ __align__(16) uint8_t lds[kAppendTile * WIDE * ESZ];
   __shared__ int plan[kPlanScans * 4];
   AppendTile t;
-  if (!plan_append(a, blockIdx.x, plan, &t)) return;
+  if (!plan_append<4>(a, blockIdx.x, plan, &t)) return;
   const int head = blockIdx.y, part = blockIdx.z >> 1, mask = (1 << a.d.page_shift) - 1;
   const int page = a.table[(int64_t)t.b * a.pages_per_seq + (t.first >> a.d.page_shift)];  // looked at when the rows are on their way
   const int tokens = t.last - t.first + 1, items = tokens * (PIECES / 2);

@@ -5,10 +5,10 @@
 namespace uad {
 
 // ---------------------------------------------------------------------------
-// Append with scales for blocks: a wave per block of 16 tokens, KV head and pool, so that
-// who finds a block's largest magnitude also writes it; as many waves to a workgroup as
-// blocks in a tile of up to 64 cache positions (see paged.h), or one for the token of a
-// sequence.  Rows are loaded once and kept in registers.  Scales are powers of two: values
+// Append with scales for blocks: a wave (two at head dim 256, whose registers four on a
+// SIMD would not hold) per block of 16 tokens, KV head and pool, so that who finds a block's
+// largest magnitude also writes it; a workgroup for the blocks of a tile of up to 64 cache
+// positions (see paged.h), or for the token of a sequence.  Rows are loaded once and kept in registers.  Scales are powers of two: values
 // are divided exactly, and what a block holds already, rounded anew where its scale must
 // grow, changes only where it falls below e4m3's normal range.  V goes to its transposed
 // page through LDS, 16 bytes a column.
@@ -34,33 +34,45 @@ __device__ __forceinline__ u32x4_t first_bytes(u32x4_t a, u32x4_t b, int n) {
   return a;
 }
 
-template <int HD, bool F32, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void kv_append_blocks_kernel(KvAppendArgs a) {
-  constexpr int PIECES = HD / 8, ITEMS = kScaleBlock * PIECES / 2;  // of 8 elements of a row; pairs of a block
-  constexpr int N = ITEMS / 64;                                     // of a lane
-  __shared__ __align__(16) uint8_t lds[WAVES * kScaleBlock * HD];
-  __shared__ int plan[kPlanScans * 4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// 4 x 4 bytes: byte i of each of four words.
+__device__ __forceinline__ void transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t *o) {
+  const uint32_t ab = __builtin_amdgcn_perm(b, a, 0x05010400u), cd = __builtin_amdgcn_perm(d, c, 0x05010400u);  // a0 b0 a1 b1
+  const uint32_t ef = __builtin_amdgcn_perm(b, a, 0x07030602u), gh = __builtin_amdgcn_perm(d, c, 0x07030602u);  // a2 b2 a3 b3
+  o[0] = __builtin_amdgcn_perm(cd, ab, 0x05040100u);
+  o[1] = __builtin_amdgcn_perm(cd, ab, 0x07060302u);
+  o[2] = __builtin_amdgcn_perm(gh, ef, 0x05040100u);
+  o[3] = __builtin_amdgcn_perm(gh, ef, 0x07060302u);
+}
+
+template <int HD, bool F32, int BLOCKS, int PARTS>
+__global__ __launch_bounds__(64 * BLOCKS * PARTS) void kv_append_blocks_kernel(KvAppendArgs a) {
+  constexpr int WAVES = BLOCKS * PARTS, PIECES = HD / 8;  // of 8 elements of a row
+  constexpr int PAIRS = PIECES / 2 / PARTS;               // of them, of a wave and token
+  constexpr int N = kScaleBlock * PAIRS / 64;             // of a lane
+  __shared__ __align__(16) uint8_t lds[BLOCKS * kScaleBlock * HD];
+  __shared__ int plan[(kPlanScans + 1) * WAVES];
+  __shared__ float most_of[2 * WAVES];
+  const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) / PARTS, part = (threadIdx.x >> 6) % PARTS;
   const int head = blockIdx.y, shift = a.d.page_shift, mask = (1 << shift) - 1;
   const bool is_v = blockIdx.z != 0;
+  const int wg = a.row0 + blockIdx.x;
   AppendTile t;
-  if constexpr (WAVES == 1) {
+  if constexpr (BLOCKS == 1) {
     bool bad = false;
-    t.b = t.row = a.row0 + blockIdx.x;
+    t.b = t.row = wg;
     t.first = t.last = length_or_none(a.lens[t.b], a.pages_per_seq, shift, &bad) - 1;
     if (t.first < 0) {  // no room for a new token, or none that can be used
       if (threadIdx.x == 0) raise_status(a.status, kStatusPage);
       return;
     }
   } else {
-    if (!plan_append(a, a.row0 + blockIdx.x, plan, &t)) return;
+    if (!plan_append<WAVES>(a, wg, plan, &t)) return;
   }
   // this wave's block of the tile, and its tokens first .. last that get rows
-  const int block = (t.first & ~(kScaleBlock - 1)) + kScaleBlock * wave;
-  const int first = max(t.first, block), last = min(t.last, block + kScaleBlock - 1), tokens = last - first + 1;
-  if (tokens <= 0) return;  // no barrier follows
-  const int page = a.table[(int64_t)t.b * a.pages_per_seq + (block >> shift)];  // looked at when the rows are on their way
-  const int held = first - block, items = tokens * (PIECES / 2);                // tokens that the block has already
+  const int block0 = t.first & ~(kScaleBlock - 1), block = block0 + kScaleBlock * wave;
+  const int first = max(t.first, block), last = min(t.last, block + kScaleBlock - 1), tokens = max(last - first + 1, 0);
+  const int page = a.table[(int64_t)t.b * a.pages_per_seq + (t.first >> shift)];  // looked at when the rows are on their way
+  const int held = first - block, items = tokens * PAIRS;  // tokens that the block has already
   const void *src = is_v ? a.v : a.k;
   const int64_t ld = is_v ? a.ldv : a.ldk;
   const int row0 = t.row + first - t.first;
@@ -71,73 +83,126 @@ __global__ __launch_bounds__(64 * WAVES) void kv_append_blocks_kernel(KvAppendAr
     *x = apart ? i : 2 * i;
     *y = apart ? i + half : 2 * i + 1;
   };
+  // an item: a lane's pair of pieces, of a token for each round (behind the last one: of it)
+  static_assert(64 % PAIRS == 0, "the same pieces in every round");
+  const int mine = part * PAIRS + lane % PAIRS;
+  auto token_of = [&](int n) { return min((lane + n * 64) / PAIRS, tokens - 1); };
+  int px, py;
+  pieces(mine, &px, &py);
+  uint64_t step[8] = {};
+  if (!is_v && mine < half) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) step[e] = a.steps[8 * mine + e];
+  }
   Raw8<F32> rx[N], ry[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     if (n * 64 >= items) break;
-    const int item = min(lane + n * 64, items - 1);
-    int x, y;
-    pieces(item % (PIECES / 2), &x, &y);
-    const int64_t at = (int64_t)(row0 + item / (PIECES / 2)) * ld + (int64_t)head * HD;
-    rx[n].load(src, at + 8 * x, a.in_vec);
-    ry[n].load(src, at + 8 * y, a.in_vec);
+    const int64_t at = (int64_t)(row0 + token_of(n)) * ld + (int64_t)head * HD;
+    rx[n].load(src, at + 8 * px, a.in_vec);
+    ry[n].load(src, at + 8 * py, a.in_vec);
   }
-  if (!page_ok(a.d, page)) {
+  if (!page_ok(a.d, page)) {  // the whole tile's
     if (lane == 0) raise_status(a.status, kStatusPage);
     return;
   }
-  const size_t scale_at = scale_index(a.d, page, head, block & mask);
-  float *scales = is_v ? a.v_scales : a.k_scales;
-  const float was = held ? scales[scale_at] : 0.f;
+  float *scales = (is_v ? a.v_scales : a.k_scales) + scale_index(a.d, page, head, block0 & mask) + wave;
+  const float was = tokens && held ? *scales : 0.f;
   float u[N][8], w[N][8], most = 0.f;
+  uint32_t turn[8] = {};  // of the lane's pairs at the last item's token
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     if (n * 64 >= items) break;
-    const int item = min(lane + n * 64, items - 1), i = item % (PIECES / 2);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       u[n][e] = rx[n].value(e);
       w[n][e] = ry[n].value(e);
     }
-    if (!is_v && i < half) {
-      const int token = item / (PIECES / 2), position = a.positions ? a.positions[row0 + token] : first + token;
+    if (!is_v && mine < half) {
+      const int position = a.positions ? a.positions[row0 + token_of(n)] : first + token_of(n);
+      float s[8], c[8];
+      // the next round's token is as many further, up to the last one
+      if (n == 0 || a.positions || lane + n * 64 >= items) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float s, c;
-        turn_of(a.turns[8 * i + e], position, &s, &c);
-        if (a.rope_pairs) {  // elements 16 i + 2 e and the next
+        for (int e = 0; e < 8; ++e) turn[e] = turned(step[e], position);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) turn[e] += (uint32_t)(step[e] * (64 / PAIRS) >> 32);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sine_of(turn[e], &s[e], &c[e]);
+      if (a.rope_pairs) {  // elements 16 i + 2 e and the next
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
           float &p = e < 4 ? u[n][2 * e] : w[n][2 * e - 8], &q = e < 4 ? u[n][2 * e + 1] : w[n][2 * e - 7];
           const float p0 = p, q0 = q;
-          p = p0 * c - q0 * s;
-          q = q0 * c + p0 * s;
-        } else {
+          p = p0 * c[e] - q0 * s[e];
+          q = q0 * c[e] + p0 * s[e];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
           const float p0 = u[n][e], q0 = w[n][e];
-          u[n][e] = p0 * c - q0 * s;
-          w[n][e] = q0 * c + p0 * s;
+          u[n][e] = p0 * c[e] - q0 * s[e];
+          w[n][e] = q0 * c[e] + p0 * s[e];
         }
       }
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {  // the largest finite magnitude
-      const float x = fabsf(u[n][e]), y = fabsf(w[n][e]);
-      most = fmaxf(most, fmaxf(x < INFINITY ? x : 0.f, y < INFINITY ? y : 0.f));
-    }
+    for (int e = 0; e < 8; ++e) most = fmaxf(most, fmaxf(fabsf(u[n][e]), fabsf(w[n][e])));  // which passes a NaN over
   }
-  most = max_pair32(max_pair16(max_row16(most)));
+  auto over_block = [&](float m, int k) {
+    m = max_pair32(max_pair16(max_row16(m)));
+    if constexpr (PARTS > 1) {  // the waves of a block
+      if (lane == 0) most_of[k * WAVES + (threadIdx.x >> 6)] = m;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) m = fmaxf(m, most_of[k * WAVES + wave * PARTS + i]);
+    }
+    return m;
+  };
+  most = over_block(most, 0);
+  const float most_any = most;
+  bool infinite = __builtin_amdgcn_readfirstlane(__float_as_int(most)) == 0x7F800000;
+  if constexpr (PARTS > 1) {  // in any block: all waves take part
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) infinite |= most_of[i] == INFINITY;
+  }
+  if (infinite) {  // of the finite ones
+    most = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if (n * 64 >= items) break;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = fabsf(u[n][e]), y = fabsf(w[n][e]);
+        most = fmaxf(most, fmaxf(x < INFINITY ? x : 0.f, y < INFINITY ? y : 0.f));
+      }
+    }
+    most = over_block(most, 1);
+  }
   float scale = __uint_as_float(scale_bits(__float_as_uint(most)));
   if (held) scale = fmaxf(scale, was);
   const bool grows = held && scale > was;
   const float ratio = grows ? was / scale : 1.f, inv = 1.f / scale;
-  if (lane == 0 && (!held || grows)) scales[scale_at] = scale;
+  if (lane == 0 && part == 0 && tokens && (!held || grows)) *scales = scale;
   const size_t base = page_base(a.d, page, head);
+  // nothing to cut and a power of two: the quotients are products, exactly
+  const bool plain = __builtin_amdgcn_readfirstlane(most_any <= 448.f * scale && (__float_as_uint(scale) & 0x7FFFFFu) == 0) != 0;
   auto quantised = [&](float *x) {
+    if (plain) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = quotient(x[e], scale, inv);
+      for (int e = 0; e < 8; ++e) x[e] *= inv;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = quotient(x[e], scale, inv);
+    }
   };
   if (!is_v) {
+    if (!tokens) return;
     uint8_t *dst = (uint8_t *)a.kp + base + k_in_page(a.d, block & mask, 0);  // the block's rows lie side by side
     if (grows)
-      for (int i = lane; i < held * (HD / 16); i += 64) {
+      for (int i = part * 64 + lane; i < held * (HD / 16); i += 64 * PARTS) {
         u32x4_t *p = (u32x4_t *)dst + i;
         *p = rescaled16(*p, ratio);
       }
@@ -145,68 +210,81 @@ __global__ __launch_bounds__(64 * WAVES) void kv_append_blocks_kernel(KvAppendAr
     for (int n = 0; n < N; ++n) {
       const int item = lane + n * 64;
       if (item >= items) break;
-      int x, y;
-      pieces(item % (PIECES / 2), &x, &y);
       quantised(u[n]);
       quantised(w[n]);
-      uint8_t *to = dst + (held + item / (PIECES / 2)) * HD;
+      uint8_t *to = dst + (held + token_of(n)) * HD;
       Pool8<true> o;
       o.set(u[n]);
-      o.put_page(to + 8 * x);
+      o.put_page(to + 8 * px);
       o.set(w[n]);
-      o.put_page(to + 8 * y);
+      o.put_page(to + 8 * py);
     }
     return;
   }
-  // V: the block's tokens in LDS, a token's 8-byte piece p at place p ^ token, then four
-  // columns a lane
-  uint8_t *mine = lds + wave * kScaleBlock * HD;
+  // V: the tile's tokens in LDS, a token's 8-byte piece p at place p ^ token, then a block of
+  // four columns a thread, the tile's blocks of a column next to each other
+  __shared__ int held_of[BLOCKS], tokens_of[BLOCKS];
+  __shared__ float ratio_of[BLOCKS];
   auto place = [&](int token, int piece) { return (token * PIECES + (piece ^ (token & (PIECES - 1)))) * 8; };
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const int item = lane + n * 64, token = item / (PIECES / 2), i = item % (PIECES / 2);
+    const int item = lane + n * 64, token = kScaleBlock * wave + held + token_of(n);
     if (item >= items) break;
     quantised(u[n]);
     quantised(w[n]);
     Pool8<true> o;
     o.set(u[n]);
-    o.put(mine + place(held + token, 2 * i));
+    o.put(lds + place(token, 2 * mine));
     o.set(w[n]);
-    o.put(mine + place(held + token, 2 * i + 1));
+    o.put(lds + place(token, 2 * mine + 1));
   }
-  __builtin_amdgcn_wave_barrier();
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // a wave's own LDS: nobody else is waited for
-  uint8_t *vp = (uint8_t *)a.vp + base + v_in_page(a.d, block & mask, 0);
-  if (lane >= HD / 4) return;
-  uint32_t v[kScaleBlock];
+  if (lane == 0 && part == 0) {
+    held_of[wave] = held;
+    tokens_of[wave] = tokens;
+    ratio_of[wave] = ratio;
+  }
+  __syncthreads();
+  const int blocks = (t.last - block0) / kScaleBlock + 1;
+  uint8_t *vp = (uint8_t *)a.vp + base + v_in_page(a.d, block0 & mask, 0);
+  for (int item = threadIdx.x; item < HD / 4 * blocks; item += 64 * WAVES) {
+    const int blk = item % blocks, word = item / blocks;
+    const int old_tokens = held_of[blk], new_tokens = tokens_of[blk];
+    const float by = ratio_of[blk];
+    uint32_t v[kScaleBlock];
 #pragma unroll
-  for (int e = 0; e < kScaleBlock; ++e) v[e] = *(const uint32_t *)(mine + place(e, lane / 2) + (lane & 1) * 4);
+    for (int e = 0; e < kScaleBlock; ++e) v[e] = *(const uint32_t *)(lds + place(kScaleBlock * blk + e, word / 2) + (word & 1) * 4);
+    u32x4_t cols[4];
 #pragma unroll
-  for (int col = 0; col < 4; ++col) {
-    u32x4_t o;
+    for (int k = 0; k < 4; ++k) {
+      uint32_t x[4];
+      transpose4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3], x);
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      o[k] = (v[4 * k] >> (8 * col) & 0xFF) | (v[4 * k + 1] >> (8 * col) & 0xFF) << 8 | (v[4 * k + 2] >> (8 * col) & 0xFF) << 16 |
-             (v[4 * k + 3] >> (8 * col) & 0xFF) << 24;
-    u32x4_t *dst = (u32x4_t *)(vp + ((size_t)(4 * lane + col) << shift));
-    if (tokens < kScaleBlock) {  // what is held, and what lies behind the last token
-      const u32x4_t old = *dst;
-      o = first_bytes(grows ? rescaled16(old, ratio) : old, first_bytes(o, old, held + tokens), held);
+      for (int col = 0; col < 4; ++col) cols[col][k] = x[col];
     }
-    __builtin_nontemporal_store(o, dst);
+#pragma unroll
+    for (int col = 0; col < 4; ++col) {
+      u32x4_t o = cols[col];
+      u32x4_t *dst = (u32x4_t *)(vp + ((size_t)(4 * word + col) << shift) + kScaleBlock * blk);
+      if (new_tokens < kScaleBlock) {  // what is held, and what lies behind the last token
+        const u32x4_t old = *dst;
+        o = first_bytes(by != 1.f ? rescaled16(old, by) : old, first_bytes(o, old, old_tokens + new_tokens), old_tokens);
+      }
+      __builtin_nontemporal_store(o, dst);
+    }
   }
 }
 
 template <int HD, bool F32>
 static hipError_t launch_append_blocks_type(const KvAppendArgs &a, hipStream_t s) {
-  constexpr int64_t kMaxWgs = 1 << 22;  // work items of a grid stay below 2^32
+  constexpr int64_t kMaxWgs = 1 << 21;  // work items of a grid stay below 2^32
   const int64_t tiles = a.row_start ? append_grid(a.n_rows, a.n_seqs, append_tile_shift(a.d.page_shift)) : a.n_rows;
   for (int64_t r = 0; r < tiles; r += kMaxWgs) {
     KvAppendArgs p = a;
     p.row0 = (int)r;
     const dim3 grid((unsigned)std::min(tiles - r, kMaxWgs), a.d.n_kv_heads, 2);
-    if (!a.row_start) hipLaunchKernelGGL((kv_append_blocks_kernel<HD, F32, 1>), grid, dim3(64), 0, s, p);
-    else hipLaunchKernelGGL((kv_append_blocks_kernel<HD, F32, kAppendTile / kScaleBlock>), grid, dim3(kAppendTile / kScaleBlock * 64), 0, s, p);
+    constexpr int BLOCKS = kAppendTile / kScaleBlock, PARTS = HD > 128 ? 2 : 1;
+    if (!a.row_start) hipLaunchKernelGGL((kv_append_blocks_kernel<HD, F32, 1, 1>), grid, dim3(64), 0, s, p);
+    else hipLaunchKernelGGL((kv_append_blocks_kernel<HD, F32, BLOCKS, PARTS>), grid, dim3(BLOCKS * PARTS * 64), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

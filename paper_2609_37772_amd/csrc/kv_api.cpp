@@ -91,7 +91,7 @@ uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_str
   const size_t o_turns = 256, n_turns = m.rope_dim / 2;
   const size_t rows = 16;  // of a slot; a single token's attention takes up to its group
   kv->slots = max_slots(kv_attend_target(kv->n_cu, m.head_dim));
-  const size_t o_arrived = o_turns + 128 * sizeof(double), o_pages = o_arrived + 2 * (size_t)kv->slots * sizeof(unsigned);
+  const size_t o_steps = o_turns + 128 * sizeof(double), o_arrived = o_steps + 128 * sizeof(uint64_t), o_pages = o_arrived + 2 * (size_t)kv->slots * sizeof(unsigned);
   const size_t o_ml = (o_pages + (2 + (size_t)m.max_seqs) * sizeof(unsigned) + 255) / 256 * 256;
   const size_t o_part = o_ml + kv->slots * rows * sizeof(uint64_t);
   const size_t total = o_part + kv->slots * rows * m.head_dim * sizeof(float);
@@ -101,6 +101,7 @@ uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_str
   if (e == hipSuccess) e = hipEventCreateWithFlags(&kv->ev, hipEventDisableTiming);
   kv->status = (unsigned *)kv->buf;
   kv->turns = (double *)((char *)kv->buf + o_turns);
+  kv->steps = (uint64_t *)((char *)kv->buf + o_steps);
   kv->arrived = (unsigned *)((char *)kv->buf + o_arrived);
   kv->pages_arrived = (unsigned *)((char *)kv->buf + o_pages);
   kv->page_counts = (int32_t *)kv->pages_arrived + 1;
@@ -110,9 +111,13 @@ uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_str
   if (n_turns) {
     // turns (angle / 2 pi) per position of pair i: theta^(-2i/rope_dim) / 2 pi
     double turns[128];
-    for (size_t i = 0; i < n_turns; ++i)
+    uint64_t steps[128];
+    for (size_t i = 0; i < n_turns; ++i) {
       turns[i] = std::pow(m.rope_theta, -2.0 * (double)i / (double)m.rope_dim) / (2.0 * M_PI);
+      steps[i] = steps_of(turns[i]);
+    }
     if (e == hipSuccess) e = hipMemcpy(kv->turns, turns, n_turns * sizeof(double), hipMemcpyHostToDevice);
+    if (e == hipSuccess) e = hipMemcpy(kv->steps, steps, n_turns * sizeof(uint64_t), hipMemcpyHostToDevice);
   }
   // the null-stream memset may still run when another stream's work begins
   if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
@@ -164,7 +169,7 @@ uad_status uad_kv_append(uad_kv *kv, int32_t layer, const void *k, const void *v
   a.kp = layer_of(kv, kv->cfg.k, layer); a.vp = layer_of(kv, kv->cfg.v, layer);
   a.row_start = row_start; a.lens = lens; a.positions = positions; a.table = page_table;
   a.n_rows = n_rows; a.n_seqs = n_seqs; a.pages_per_seq = pages_per_seq;
-  a.turns = kv->turns; a.rope_dim = kv->cfg.rope_dim; a.rope_pairs = kv->cfg.rope_pairs;
+  a.turns = kv->turns; a.steps = kv->steps; a.rope_dim = kv->cfg.rope_dim; a.rope_pairs = kv->cfg.rope_pairs;
   const int64_t per16 = dtype == UAD_DTYPE_F32 ? 4 : 8;
   a.in_vec = aligned(k, 16) && aligned(v, 16) && ldk % per16 == 0 && ldv % per16 == 0;
   a.k_scale = kv->cfg.k_scale; a.v_scale = kv->cfg.v_scale;

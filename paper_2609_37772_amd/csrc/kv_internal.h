@@ -22,6 +22,7 @@ struct KvAppendArgs {
   int row0;               // first row of this launch
   bool in_vec;            // rows can be loaded 16 bytes at a time
   const double *turns;    // [rope_dim / 2] turns per position
+  const uint64_t *steps;  // the same in units of 2^-64 turns, whole turns left out
   int rope_dim, rope_pairs;
   float k_scale, v_scale, k_inv, v_inv;  // 8-bit pools hold value / scale; 1 / scale
   float *k_scales, *v_scales;  // the layer's, of every block of tokens (see paged.h), or null
@@ -137,6 +138,7 @@ struct uad_kv {
   void *buf = nullptr;     // status word, turns, workspace
   unsigned *status = nullptr;
   double *turns = nullptr;
+  uint64_t *steps = nullptr;
   float *part = nullptr;
   uint64_t *part_ml = nullptr;
   unsigned *arrived = nullptr;

@@ -68,6 +68,14 @@ UAD_HD void rope_pair(int p, int rope_dim, bool neighbours, int *a, int *b) {
   }
 }
 
+// Turns per position in units of 2^-64, whole turns left out (53 bits of it matter; more
+// than 2^53 turns, which no position makes sense with, count as none).
+inline uint64_t steps_of(double turns) {
+  const double whole = turns < 9007199254740992.0 ? (double)(int64_t)turns : turns;
+  const double high = (turns - whole) * 4294967296.0, low = high - (double)(uint32_t)high;
+  return ((uint64_t)(uint32_t)high << 32) + (uint64_t)(low * 4294967296.0);
+}
+
 // ---------------------------------------------------------------------------
 // Appends of many rows go by tiles: runs of up to kAppendTile cache positions that start
 // at a multiple of their size and lie in one page.

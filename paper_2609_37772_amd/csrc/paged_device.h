@@ -67,6 +67,19 @@ __device__ __forceinline__ void turn_of(double turns, int position, float *s, fl
   *c = __builtin_amdgcn_cosf(f);
 }
 
+// The same in whole numbers, for those who turn much: a turn is 2^64 steps, of which a
+// product with the position keeps the rest (`steps`), and 2^32 of `turned`, off by one at
+// most.  On a CU's vector unit about 80 clocks a wave, where the doubles take 130.
+__device__ __forceinline__ uint32_t turned(uint64_t steps, int position) {
+  const uint32_t lo = (uint32_t)steps, hi = (uint32_t)(steps >> 32), p = (uint32_t)position;
+  return __umulhi(p, lo) + p * hi - (position < 0 ? lo : 0u);
+}
+__device__ __forceinline__ void sine_of(uint32_t turned, float *s, float *c) {
+  const float f = (float)(int)turned * 0x1p-32f;
+  *s = __builtin_amdgcn_sinf(f);
+  *c = __builtin_amdgcn_cosf(f);
+}
+
 // Inclusive sum over the lanes of a wave, by DPP: within rows of 16, then across them.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int dpp_i(int v) {
@@ -140,8 +153,9 @@ struct AppendTile {
   int row;             // row of the first
 };
 
+template <int WAVES>
 __device__ __forceinline__ bool plan_append(const KvAppendArgs &a, int wg, int *lds, AppendTile *t) {
-  PlanScan<4> scan(a.n_seqs, lds);
+  PlanScan<WAVES> scan(a.n_seqs, lds);
   const int shift = append_tile_shift(a.d.page_shift);
   bool bad = false;
   // positions [from, to) and rows of a sequence; none where they cannot be used

@@ -26,6 +26,7 @@ int tile_of(int first, int gap, int i) { SeenTiles s{first, gap, 0}; return seen
 unsigned run(int from, int to, int n) { return run_bits(from, to, n); }
 int pages(int len, int shift) { return pages_of(len, shift); }
 int grows(int len, int n, int pages, int shift) { return growth_ok(len, n, pages, shift); }
+unsigned long long steps(double turns) { return steps_of(turns); }
 int used(int i, int len, int w, int s, int shift) { return page_in_use(i, len, w, s, shift); }
 }
 """
@@ -41,6 +42,15 @@ def idx(tmp_path_factory):
     lib.bits_of_scale.restype = lib.run.restype = ctypes.c_uint
     lib.bits_of_scale.argtypes = [ctypes.c_uint]
     return lib
+
+
+def test_turns_in_whole_numbers(idx):
+    idx.steps.restype, idx.steps.argtypes = ctypes.c_ulonglong, [ctypes.c_double]
+    r = np.random.default_rng(5)
+    from fractions import Fraction
+    for x in [0.0, 0.15915494309189535, 1 - 2.0 ** -53, 1.0, 2.0 ** -70, 1234567.75, 2.0 ** 53, 1e300] + list(10.0 ** r.uniform(-9, 3, 200)):
+        want = int((Fraction(float(x)) % 1) * 2 ** 64)
+        assert abs(idx.steps(x) - want) <= 1, x
 
 
 def test_every_block_has_its_scale(idx):
