@@ -126,7 +126,8 @@ __device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds,
   return true;
 }
 
-template <int HD, bool F32, bool F8>
+// SINGLE: a row for every sequence, so that all columns of a unit see the same keys.
+template <int HD, bool F32, bool F8, bool SINGLE>
 __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves / 4) void kv_rows_kernel(KvRowsArgs a) {
   constexpr int TILE = kTileKeys<F8>, NT = TILE / 16, KPL = 4 * NT;
   constexpr int KS = HD / 32;           // k steps of Q K^T
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   const int last = w.s.len - 1, mask = (1 << a.d.page_shift) - 1;
   const int32_t *table = a.table + (int64_t)w.b * a.pages_per_seq;
   // column m of the unit's sequence: row m / group, query head kvh * group + m % group
-  auto row_of = [&](int m) { return (int)((unsigned)m / (unsigned)a.group); };
+  auto row_of = [&](int m) { return SINGLE ? 0 : (int)((unsigned)m / (unsigned)a.group); };
   const int pos0 = w.s.len - w.s.n;  // of the sequence's first row
   auto from_of = [&](int col) { return seen_from(pos0 + row_of(m0 + col), a.window); };
   auto to_of = [&](int col) { return min(seen_to(pos0 + row_of(m0 + col), w.s.len, a.window, a.causal), w.s.len); };
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
     // scores in powers of two, keys that the column does not see masked
     const int k0 = tile_at(tile), key0 = k0 + KPL * g;
     const bool edge = (k0 < lo_max || k0 + TILE > hi_min) && k0 + TILE > first_min;
-    const uint32_t seen = edge ? seen_by_mine(key0, KPL) : 0xFFFFFFFFu;
+    const uint32_t seen = !edge ? 0xFFFFFFFFu : SINGLE ? seen_by_any(key0, KPL) : seen_by_mine(key0, KPL);
     const float to_log2 = F8 ? a.scale_log2 * ks : a.scale_log2;
     float mt = -INFINITY;
 #pragma unroll
@@ -338,13 +339,15 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
 #pragma unroll
         for (int k = 0; k < NTO; ++k) vr[k][i] &= keep;
       }
+      if constexpr (!SINGLE) {
 #pragma unroll
-      for (int k = 0; k < NTO; ++k) odd |= not_finite<F8>(vr[k]);
-      odd = __ballot(odd) != 0;
+        for (int k = 0; k < NTO; ++k) odd |= not_finite<F8>(vr[k]);
+        odd = __ballot(odd) != 0;
+      }
     }
 #pragma unroll
     for (int u = 0; u < NT / 2; ++u) {  // 8 weights of the lane, as terms
-      if (odd) {
+      if (!SINGLE && odd) {
         union {
           bf16x8 v;
           uint16_t e[8];
@@ -457,8 +460,10 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
 
 template <int HD, bool F32, bool F8>
 static hipError_t rows_attr() {
-  return hipFuncSetAttribute((const void *)kv_rows_kernel<HD, F32, F8>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                             attend_lds_floats<HD>() * 4);
+  hipError_t e = hipSuccess;
+  for (const void *f : {(const void *)kv_rows_kernel<HD, F32, F8, false>, (const void *)kv_rows_kernel<HD, F32, F8, true>})
+    if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, attend_lds_floats<HD>() * 4);
+  return e;
 }
 template <int HD>
 static hipError_t rows_attrs() {
@@ -487,8 +492,10 @@ static hipError_t launch_rows_type(KvRowsArgs a, hipStream_t s) {
   const int64_t splits = splits_of((int)tiles, kAttendMinTiles, kAttendWhole<HD, F8>);
   const int64_t grid = std::min(units * splits, units + a.slots);
   a.unsplit = splits == 1;
-  hipLaunchKernelGGL((kv_rows_kernel<HD, F32, F8>), dim3((unsigned)grid), dim3(64 * kAttendWaves),
-                     (attend_lds_floats<HD>() * 4), s, a);
+  const dim3 wgs((unsigned)grid), wg(64 * kAttendWaves);
+  constexpr int lds = attend_lds_floats<HD>() * 4;
+  if (a.row_start) hipLaunchKernelGGL((kv_rows_kernel<HD, F32, F8, false>), wgs, wg, lds, s, a);
+  else hipLaunchKernelGGL((kv_rows_kernel<HD, F32, F8, true>), wgs, wg, lds, s, a);
   return hipGetLastError();
 }
 
