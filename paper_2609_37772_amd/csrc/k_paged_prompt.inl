@@ -29,11 +29,13 @@ namespace uad {
 constexpr int kPromptTile = 64;
 
 // Columns of a wave: outputs and query take it columns x head dim x (4 + 2 terms) bytes,
-// and two waves are to share a SIMD's 512 registers.
-template <int HD, bool F32>
-constexpr int kPromptCols = HD == 256 || (HD == 128 && F32) ? 16 : 32;
-template <int HD, bool F32>
-constexpr int kPromptThreads = 64 * 128 / kPromptCols<HD, F32>;
+// and two waves are to share a SIMD's 512 registers.  Where workgroups are too few for
+// that, 16 columns give each of them twice the waves: at head dim 128 a tenth faster than
+// 32; at 64 a tile of 8 bits has fewer pieces than twice the threads.
+template <int HD, bool F32, int KW>
+constexpr int kPromptCols = (KW == 2 && HD == 128) || HD == 256 || (HD == 128 && F32) ? 16 : 32;
+template <int HD, bool F32, int KW>
+constexpr int kPromptThreads = 64 * 128 / kPromptCols<HD, F32, KW>;
 
 // LDS: two buffers of a tile's K and V^T; before that the query in fp32 (in the first buffer
 // and where two waves share columns, which are calls that wait for latency, no further, so
@@ -67,24 +69,34 @@ struct Product<16> {
   static __device__ __forceinline__ acc of(bf16x8 a, bf16x8 b, acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 
-// 16 bytes per lane from memory to LDS at `to` + 16 * lane.  The compiler would wait for
-// each before the next read of LDS: the kernel waits itself, once per tile.
-__device__ __forceinline__ void load_to_lds(const void *from, uint32_t to) {
-  uint32_t kept;  // m0 is the compiler's
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
-               : "=&s"(kept) : "s"(to), "v"(from) : "memory");
+// 16 bytes per lane from memory to LDS at `to` + 16 * lane, by the lanes of `mask` (all or
+// none: a branch would part the instructions that these loads are to lie between).  The
+// compiler would wait for each before the next read of LDS: the kernel waits itself, once
+// per tile.  No reads of LDS are held back by it either: they are on the other side of a
+// barrier, or of the other buffer.
+__device__ __forceinline__ void load_to_lds(const void *from, uint32_t to, uint64_t mask) {
+  uint32_t kept;  // m0 and exec are the compiler's
+  uint64_t lanes;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b64 %1, exec\n\ts_mov_b32 m0, %2\n\ts_mov_b64 exec, %4\n\ts_nop 0\n\t"
+               "global_load_lds_dwordx4 %3, off\n\ts_mov_b64 exec, %1\n\ts_mov_b32 m0, %0"
+               : "=&s"(kept), "=&s"(lanes) : "s"(to), "v"(from), "s"(mask));
 }
 // The same from an address that is one for the wave and an offset below 2^31.
-__device__ __forceinline__ void load_to_lds(const void *base, uint32_t offset, uint32_t to) {
+__device__ __forceinline__ void load_to_lds(const void *base, uint32_t offset, uint32_t to, uint64_t mask) {
   uint32_t kept;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
-               : "=&s"(kept) : "s"(to), "v"(offset), "s"(base) : "memory");
+  uint64_t lanes;
+  const uint64_t at = (uint64_t)base;
+  base = (const void *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32 |
+                        (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at));
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b64 %1, exec\n\ts_mov_b32 m0, %2\n\ts_mov_b64 exec, %5\n\ts_nop 0\n\t"
+               "global_load_lds_dwordx4 %3, %4\n\ts_mov_b64 exec, %1\n\ts_mov_b32 m0, %0"
+               : "=&s"(kept), "=&s"(lanes) : "s"(to), "v"(offset), "s"(base), "s"(mask));
 }
 
 template <int HD, bool F32, bool F8, int KW>
-__global__ __launch_bounds__((kPromptThreads<HD, F32>), 2) void kv_prompt_kernel(KvRowsArgs a) {
+__global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), 2) void kv_prompt_kernel(KvRowsArgs a) {
   using Lds = PromptLds<HD, F8, KW>;
-  constexpr int C = kPromptCols<HD, F32>, THREADS = kPromptThreads<HD, F32>, NW = THREADS / 64;
+  constexpr int C = kPromptCols<HD, F32, KW>, THREADS = kPromptThreads<HD, F32, KW>, NW = THREADS / 64;
   using Mul = Product<C>;
   typedef typename Mul::acc acc;
   constexpr int VAL = Mul::values, GROUPS = 64 / C;   // results a lane; groups of lanes
@@ -186,32 +198,28 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32>), 2) void kv_prompt_kernel
   auto v_bits = [&](int d) { return VP == 4 ? d >> 1 & 3 : d & 7; };
   const int v_row = threadIdx.x / VP, v_key = ((threadIdx.x % VP) ^ v_bits(v_row)) * PIECE;
   const uint32_t v_offset = (((uint32_t)v_row << a.d.page_shift) + (v_key & 15)) * ESZ;
-  auto load_tile = [&](int i, int ids, uint32_t to) {
-    const int k0 = tile_at(i);
-    int page[4];
-    size_t at[4];  // a run's page and KV head, in elements
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      page[r] = __builtin_amdgcn_readlane(ids, r);
-      at[r] = page_base(a.d, page[r], kvh);
-    }
-#pragma unroll
-    for (int n = 0; n < K_PASSES; ++n) {
-      const int piece = n * THREADS + threadIdx.x, row = piece / KP, p = piece % KP;
-      const int r = (n * THREADS + wave * 64) / KP / 16;  // one for the wave
-      const size_t base = r == 0 ? at[0] : r == 1 ? at[1] : r == 2 ? at[2] : at[3];
-      load_to_lds((const char *)a.kp + (base + k_in_page(a.d, (k0 + 16 * r) & mask, 0)) * ESZ,
-                  (uint32_t)((row & 15) * HD * ESZ + (p ^ k_bits(row)) * 16), to + (n * THREADS + wave * 64) * 16);
-    }
-    size_t v_at[4];  // and the run's first slot
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v_at[r] = at[r] + ((k0 + 16 * r) & mask);
-    const int r = v_key >> 4;
-    const size_t base = r == 0 ? v_at[0] : r == 1 ? v_at[1] : r == 2 ? v_at[2] : v_at[3];
-    const char *src = (const char *)a.vp + base * ESZ + v_offset;
-#pragma unroll
-    for (int n = 0; n < V_PASSES; ++n)
-      load_to_lds(src + ((size_t)(n * V_ROWS) << a.d.page_shift) * ESZ, to + KBYTES + (n * THREADS + wave * 64) * 16);
+  // The loads of a tile are shared out over the products of the one before: issued all at
+  // once they held a wave up for 1000 to 1800 of the 5000 to 9000 clocks of a tile.
+  int next_k0 = 0, next_pages = 0;  // pages in lanes 0 .. 3
+  const char *next_v = nullptr;     // this thread's first piece of V^T
+  uint32_t next_to = 0;
+  uint64_t next_mask = 0;
+  auto plan_tile = [&](int i, int ids, uint32_t to, int real) __attribute__((always_inline)) {
+    next_k0 = __builtin_amdgcn_readfirstlane(tile_at(i));
+    next_pages = ids;
+    const int r = v_key >> 4, page = __shfl(ids, r);
+    next_v = (const char *)a.vp + (page_base(a.d, page, kvh) + ((next_k0 + 16 * r) & mask)) * ESZ + v_offset;
+    next_to = __builtin_amdgcn_readfirstlane(to);
+    next_mask = (uint64_t)(int64_t)__builtin_amdgcn_readfirstlane(real >> 31);
+  };
+  auto load_k = [&](int n) __attribute__((always_inline)) {
+    const int row = (n * THREADS + (int)threadIdx.x) / KP, p = (n * THREADS + (int)threadIdx.x) % KP;
+    const int r = (n * THREADS + wave * 64) / KP / 16;  // one for the wave
+    load_to_lds((const char *)a.kp + (page_base(a.d, __builtin_amdgcn_readlane(next_pages, r), kvh) + k_in_page(a.d, (next_k0 + 16 * r) & mask, 0)) * ESZ,
+                (uint32_t)((row & 15) * HD * ESZ + (p ^ k_bits(row)) * 16), next_to + (n * THREADS + wave * 64) * 16, next_mask);
+  };
+  auto load_v = [&](int n) __attribute__((always_inline)) {
+    load_to_lds(next_v + ((size_t)(n * V_ROWS) << a.d.page_shift) * ESZ, next_to + KBYTES + (n * THREADS + wave * 64) * 16, next_mask);
   };
   // scales of the blocks that this lane's scores and weights lie in
   float ks_[NS], vs_[NS], next_ks[NS], next_vs[NS];
@@ -237,6 +245,13 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32>), 2) void kv_prompt_kernel
   auto buffer_of = [&](int i) { return ((i + FLIP) & 1) * Lds::second; };
 
   int next_ids = tiles.count > 0 ? page_ids(0) : 0, ids = 0;
+  auto first_tile = [&]() __attribute__((always_inline)) {
+    plan_tile(0, ids, lds0 + buffer_of(0), -1);
+#pragma unroll
+    for (int n = 0; n < K_PASSES; ++n) load_k(n);
+#pragma unroll
+    for (int n = 0; n < V_PASSES; ++n) load_v(n);
+  };
   // The query: rotated and scaled in fp32, so that scores are in powers of two, through LDS
   // into operands.  A thread takes the same 16 elements, two pieces of 8 that are turned
   // with each other, of consecutive columns, whose rows are mostly one, and so is the turn.
@@ -261,7 +276,7 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32>), 2) void kv_prompt_kernel
     }
     if (KW == 2 && tiles.count > 0) {
       ids = checked(next_ids, 0);
-      load_tile(0, ids, lds0 + buffer_of(0));
+      first_tile();
       load_scales(0, ids);
       if (tiles.count > 1) next_ids = page_ids(1);
     }
@@ -358,7 +373,7 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32>), 2) void kv_prompt_kernel
   uint32_t nans[(NT * VAL + 31) / 32] = {};  // a bit for each value of o
   if (KW == 1 && tiles.count > 0) {
     ids = checked(next_ids, 0);
-    load_tile(0, ids, lds0 + buffer_of(0));
+    first_tile();
     load_scales(0, ids);
     if (tiles.count > 1) next_ids = page_ids(1);
   }
@@ -373,10 +388,10 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32>), 2) void kv_prompt_kernel
     }
     if (i + 1 < tiles.count) {
       ids = checked(next_ids, i + 1);
-      load_tile(i + 1, ids, lds0 + buffer_of(i + 1));
       load_scales(i + 1, ids);
       if (i + 2 < tiles.count) next_ids = page_ids(i + 2);
     }
+    plan_tile(min(i + 1, tiles.count - 1), ids, lds0 + buffer_of(i + 1), i + 1 - tiles.count);
     const int k0 = tile_at(i);
     const bool edge = (k0 < lo_max || k0 + TILE > hi_min) && k0 + TILE > first_min;
     uint32_t seen[NS];  // of this lane's scores
@@ -445,8 +460,10 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32>), 2) void kv_prompt_kernel
       for (int k = 0; k < MK; ++k)
 #pragma unroll
         for (int r = 0; r < VAL; ++r) sc[s][k][r] = 0.f;
+    static_assert(KS % K_PASSES == 0 && NT % V_PASSES == 0, "loads between the products");
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+    for (int ks = 0; ks < KS; ++ks) {
+      if (ks % (KS / K_PASSES) == 0) load_k(ks / (KS / K_PASSES));
 #pragma unroll
       for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -456,6 +473,7 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32>), 2) void kv_prompt_kernel
 #pragma unroll
           for (int t = TERMS - 1; t >= 0; --t) sc[s][k] = Mul::of(kf, qf[t][ks], sc[s][k]);
         }
+    }
     if constexpr (F8)
       if (a.k_scales) {
 #pragma unroll
@@ -511,6 +529,7 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32>), 2) void kv_prompt_kernel
         l += sum[0] + sum[1];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+          if (s == 0 && u == 0 && n % (NT / V_PASSES) == 0) load_v(n / (NT / V_PASSES));
           const bf16x8 vf = v_operand(buf, n, KW == 1 ? s : kw, u);
 #pragma unroll
           for (int t = TERMS - 1; t >= 0; --t) o[n] = Mul::of(vf, pf[t], o[n]);
@@ -606,7 +625,7 @@ template <int HD, bool F32, bool F8, int KW>
 static hipError_t launch_prompt_type(const KvRowsArgs &a, hipStream_t s) {
   // as many workgroups as any starts could need
   const int64_t grid = a.d.n_kv_heads * ((int64_t)a.n_rows * a.group / (128 / KW) + a.n_seqs);
-  hipLaunchKernelGGL((kv_prompt_kernel<HD, F32, F8, KW>), dim3((unsigned)grid), dim3(kPromptThreads<HD, F32>), ((PromptLds<HD, F8, KW>::bytes)), s, a);
+  hipLaunchKernelGGL((kv_prompt_kernel<HD, F32, F8, KW>), dim3((unsigned)grid), dim3(kPromptThreads<HD, F32, KW>), ((PromptLds<HD, F8, KW>::bytes)), s, a);
   return hipGetLastError();
 }
 template <int HD, int KW>
