@@ -21,7 +21,7 @@ namespace uad {
 // ---------------------------------------------------------------------------
 struct RowsWork {
   RowsSeq s;
-  int b, unit, t0, t1, split, splits, slot;
+  int b, unit, split, splits, slot;
 };
 
 template <int HD, bool F8>
@@ -34,7 +34,6 @@ __device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds,
     w->b = (unsigned)wg / (unsigned)units;
     w->unit = wg - w->b * units;
     w->s = rows_of<TILE>(a, w->b, &bad);
-    w->t1 = w->s.tiles.count;
     w->splits = 1;
     if (bad && threadIdx.x == 0) raise_status(a.status, kStatusPage);
     return true;
@@ -121,8 +120,6 @@ __device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds,
   w->split = wg - start - w->unit * w->splits;
   w->slot = slot + w->unit * w->splits;
   if (w->splits > 1 && w->slot + w->splits > a.slots) return false;  // likewise
-  w->t0 = split_begin(w->s.tiles.count, w->splits, w->split);
-  w->t1 = split_begin(w->s.tiles.count, w->splits, w->split + 1);
   return true;
 }
 
@@ -166,7 +163,9 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   const int my_col = min(c, cols - 1), lo = from_of(my_col), hi = to_of(my_col), first = first_of(my_col);
   const int lo_min = from_of(0), lo_max = from_of(cols - 1), hi_min = to_of(0), hi_max = to_of(cols - 1);
   const int first_min = first_of(0), first_max = first_of(cols - 1);
-  auto tile_at = [&](int i) { return seen_tile(w.s.tiles, i) * TILE; };  // its first key
+  // a unit parts the tiles that its own columns see among the splits that its sequence's have
+  const SeenTiles tiles = SINGLE ? w.s.tiles : seen_tiles(max(hi_max, first_max), lo_min, a.sinks, TILE);
+  auto tile_at = [&](int i) { return seen_tile(tiles, i) * TILE; };  // its first key
   // keys key .. key + n - 1 that some column sees, or this lane's column does, as bits
   auto seen_by_any = [&](int key, int n) { return run_bits(lo_min - key, hi_max - key, n) | run_bits(-key, first_max - key, n); };
   auto seen_by_mine = [&](int key, int n) { return run_bits(lo - key, hi - key, n) | run_bits(-key, first - key, n); };
@@ -212,8 +211,9 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
     for (int n = 0; n < NTO; ++n) vr[n] = *(const u32x4_t *)(src + (unsigned)((n * 16 << a.d.page_shift) * ESZ));
   };
 
-  int tile = w.t0 + wave;
-  const int t1 = last >= 0 ? w.t1 : 0;
+  const int t0 = split_begin(tiles.count, w.splits, w.split);
+  int tile = t0 + wave;
+  const int t1 = last >= 0 ? split_begin(tiles.count, w.splits, w.split + 1) : 0;
   int kp = 0, vp = 0, next_kp = 0, next_vp = 0;
   if (tile < t1) page_ids(tile, kp, vp);
   if (tile + NW < t1) page_ids(tile + NW, next_kp, next_vp);
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
 
   // The waves meet: maxima, sums and outputs, each in units of its wave's maximum, of half
   // the waves where no others had a tile.
-  const bool all = t1 - w.t0 > NW / 2;
+  const bool all = t1 - t0 > NW / 2;
   l = sum_pair32(sum_pair16(l));
   if (g == 0) {
     ml[(wave * 16 + c) * 2] = m;
@@ -506,10 +506,24 @@ static hipError_t launch_rows_hd(const KvRowsArgs &a, bool f32, bool f8, hipStre
 }
 
 // Which kernel: 0: that of few rows; else the waves that share a column of that of many.
-static int prompt_key_waves(const KvRowsArgs &a) {
+// The kernel of few rows reads a KV head's cache for every 16 columns and parts a long
+// history, that of many reads it for 64 or 128 and does not: the one loses from a size of
+// the query on, whatever the lengths (of 8 bits half is read, and that of many has to widen
+// it).  us, few rows / many (two waves a column), causal, short and long histories:
+//   query elements  head dim 256             128                       64                        128, 8 bits
+//   0.2 M to 0.4 M  -                        22.0 / 29.3, 64.8 / 90.2  15.4 / 19.7, 20.7 / 25.0  12.4 / 22.9, 30.5 / 116
+//   0.5 M           38.1 / 40.9, 97.1 / 130  8.7 / 10.8,  62.3 / 54.6  21.9 / 23.6, 63.9 / 72.0  10.0 / 11.5, 45.6 / 65.0
+//   0.8 M to 1 M    36.8 / 28.0, 172 / 132   28.0 / 19.4, 119 / 90     44.8 / 25.4, 118 / 72     35.2 / 36.5, 81 / 117
+//   2 M             25.6 / 13.4, 140 / 44.8  57.3 / 19.9, 248 / 91     25.0 / 9.4,  80.9 / 33.3  47.4 / 23.4, 156 / 118
+// With fewer than 16 columns a sequence its units would be mostly empty.  Two waves share a
+// column where units of 128 columns would be too few to fill the chip (128 units at head dim
+// 128: 53 us, with one wave 73) or half empty (25.4 and 30.4 at 64 columns a sequence); from
+// 256 full ones on one wave takes 71 us for 97 at head dim 256, at 128 and 512 units 200 for
+// 214, of 8 bits 228 for 362.
+static int prompt_key_waves(const KvRowsArgs &a, bool f8) {
   const int64_t columns = (int64_t)a.n_rows * a.group;
-  if (!a.row_start || columns < 64 * (int64_t)a.n_seqs) return 0;
-  return columns / 128 * a.d.n_kv_heads < 256 ? 2 : 1;
+  if (!a.row_start || columns < 16 * (int64_t)a.n_seqs || columns * a.d.n_kv_heads * a.d.head_dim < (f8 ? 1200000 : 600000)) return 0;
+  return columns < 128 * (int64_t)a.n_seqs || columns / 128 * a.d.n_kv_heads < 256 ? 2 : 1;
 }
 
 hipError_t launch_kv_rows(const KvRowsArgs &a, bool f32, bool f8, hipStream_t s) {
@@ -517,7 +531,7 @@ hipError_t launch_kv_rows(const KvRowsArgs &a, bool f32, bool f8, hipStream_t s)
       a.target < 1 || a.slots < max_slots(a.target) || a.d.page_shift < 4 || a.window < 0 || a.sinks < 0 ||
       (!a.row_start && a.n_rows != a.n_seqs) || (!f8 && a.k_scales))
     return hipErrorInvalidValue;
-  const int key_waves = prompt_key_waves(a);
+  const int key_waves = prompt_key_waves(a, f8);
   if (key_waves) return launch_kv_prompt(a, key_waves, f32, f8, s);
   if (a.d.head_dim == 64) return launch_rows_hd<64>(a, f32, f8, s);
   if (a.d.head_dim == 128) return launch_rows_hd<128>(a, f32, f8, s);
