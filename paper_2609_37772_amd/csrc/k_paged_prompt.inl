@@ -27,6 +27,10 @@ namespace uad {
 // that do.
 // ---------------------------------------------------------------------------
 constexpr int kPromptTile = 64;
+// Tiles of a split at least, and those up to which a unit stays whole: a split costs the query
+// anew and a join, which take as long as 3 tiles.  102 units of 13 tiles at head dim 256:
+// 36.0 us whole, 31.5 us in two; 16 units of 63: 130 whole, 43 split.
+constexpr int kPromptMinTiles = 3, kPromptWhole = 6;
 
 // Columns of a wave: outputs and query take it columns x head dim x (4 + 2 terms) bytes,
 // and two waves are to share a SIMD's 512 registers.  Where workgroups are too few for
@@ -36,6 +40,10 @@ template <int HD, bool F32, int KW>
 constexpr int kPromptCols = (KW == 2 && HD == 128) || HD == 256 || (HD == 128 && F32) ? 16 : 32;
 template <int HD, bool F32, int KW>
 constexpr int kPromptThreads = 64 * 128 / kPromptCols<HD, F32, KW>;
+// Waves of a SIMD: where LDS has room for two workgroups of 8 waves a CU, the registers are
+// to be 128 at most (8 sequences of 64 rows on 2000 tokens: 54 us, with 129 registers 82).
+template <int HD, bool F32, int KW>
+constexpr int kPromptPerSimd = HD == 128 && !F32 && KW == 2 ? 4 : 2;
 
 // LDS: two buffers of a tile's K and V^T; before that the query in fp32 (in the first buffer
 // and where two waves share columns, which are calls that wait for latency, no further, so
@@ -94,7 +102,7 @@ __device__ __forceinline__ void load_to_lds(const void *base, uint32_t offset, u
 }
 
 template <int HD, bool F32, bool F8, int KW>
-__global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), 2) void kv_prompt_kernel(KvRowsArgs a) {
+__global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), (kPromptPerSimd<HD, F32, KW>)) void kv_prompt_kernel(KvRowsArgs a) {
   using Lds = PromptLds<HD, F8, KW>;
   constexpr int C = kPromptCols<HD, F32, KW>, THREADS = kPromptThreads<HD, F32, KW>, NW = THREADS / 64;
   using Mul = Product<C>;
@@ -109,7 +117,7 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), 2) void kv_prompt_ke
   constexpr int KP = HD * ESZ / 16, VP = TILE * ESZ / 16;  // 16-byte pieces of a row of K, of V^T
   constexpr int KBYTES = TILE * HD * ESZ, PIECE = 16 / ESZ;  // keys of a piece of V^T
   extern __shared__ __align__(16) uint8_t lds_bytes[];
-  __shared__ int plan[4 * NW];
+  __shared__ int plan[(kPlanScans + 2) * NW + 3];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane % C, g = lane / C;
   const int cw = wave / KW, kw = wave % KW;
@@ -117,50 +125,15 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), 2) void kv_prompt_ke
   // the unit: sequences' units side by side, a sequence's last rows first (where rows are
   // causal they see the most), its KV heads next to each other
   const int group = a.group;
-  RowsSeq sq;
-  int b, unit;
-  {
-    PlanScan<NW> scan(a.n_seqs, plan);
-    const int b0 = scan.me * scan.per;
-    bool bad = false;
-    auto units_of = [&](int i) {
-      const RowsSeq s = rows_of<TILE>(a, i, &bad);
-      return a.d.n_kv_heads * (int)(((int64_t)s.n * group + COLS - 1) / COLS);
-    };
-    int mine = 0, all;
-    for (int i = 0; i < scan.per; ++i)
-      if (b0 + i < a.n_seqs) mine += units_of(b0 + i);
-    if (bad && blockIdx.x == 0) raise_status(a.status, kStatusPage);
-    const int upto = scan(mine, &all), wg = blockIdx.x;
-    if (wg >= all) return;
-    int start = upto - mine;
-    if (!scan.block) {
-      b = __builtin_ctzll(__ballot(upto > wg));
-      start = __builtin_amdgcn_readlane(start, b);
-    } else {
-      if (upto > wg && start <= wg) {
-        int i = b0;
-        for (; i < min(b0 + scan.per, a.n_seqs) - 1; ++i) {
-          const int k = units_of(i);
-          if (start + k > wg) break;
-          start += k;
-        }
-        scan.lds[0] = i;
-        scan.lds[1] = start;
-      }
-      __syncthreads();
-      b = __builtin_amdgcn_readfirstlane(scan.lds[0]);
-      start = __builtin_amdgcn_readfirstlane(scan.lds[1]);
-    }
-    sq = rows_of<TILE>(a, b, &bad);
-    unit = wg - start;
-  }
-  const int runs = (int)(((int64_t)sq.n * group + COLS - 1) / COLS);
-  const int run = runs - 1 - unit / a.d.n_kv_heads, kvh = unit % a.d.n_kv_heads;
-  if (run < 0) return;  // only if the caller's arrays change while this runs
+  constexpr bool SPLITS = KW == 2;
+  RowsWork w;
+  if (!plan_rows<TILE, COLS, kPromptWhole, kPromptMinTiles, NW, true>(a, blockIdx.x, plan, &w)) return;
+  const RowsSeq sq = w.s;
+  const int runs = sq.units / a.d.n_kv_heads;
+  const int run = runs - 1 - w.unit / a.d.n_kv_heads, kvh = w.unit % a.d.n_kv_heads;
   const int m0 = run * COLS, cols = min(COLS, sq.n * group - m0);
   const int last = sq.len - 1, mask = (1 << a.d.page_shift) - 1, pos0 = sq.len - sq.n;
-  const int32_t *table = a.table + (int64_t)b * a.pages_per_seq;
+  const int32_t *table = a.table + (int64_t)w.b * a.pages_per_seq;
   auto row_of = [&](int m) { return (int)((unsigned)m / (unsigned)group); };
   auto from_at = [&](int p) { return seen_from(p, a.window); };
   auto to_at = [&](int p) { return min(seen_to(p, sq.len, a.window, a.causal), sq.len); };
@@ -170,7 +143,10 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), 2) void kv_prompt_ke
   const int lo_min = from_at(p_min), lo_max = from_at(p_max), hi_min = to_at(p_min), hi_max = to_at(p_max);
   const int first_min = first_at(p_min), first_max = first_at(p_max);
   const SeenTiles tiles = seen_tiles(max(hi_max, first_max), lo_min, a.sinks, TILE);
-  auto tile_at = [&](int i) { return seen_tile(tiles, i) * TILE; };
+  if (SPLITS && !w.of_unit(tiles.count)) return;
+  const int t0 = SPLITS ? split_begin(tiles.count, w.splits, w.split) : 0;
+  const int n_tiles = SPLITS ? split_begin(tiles.count, w.splits, w.split + 1) - t0 : tiles.count;
+  auto tile_at = [&](int i) { return seen_tile(tiles, t0 + i) * TILE; };
   auto seen_by_any = [&](int key, int n) { return run_bits(lo_min - key, hi_max - key, n) | run_bits(-key, first_max - key, n); };
   auto seen_by_mine = [&](int key, int n) { return run_bits(lo - key, hi - key, n) | run_bits(-key, first - key, n); };
   bool bad = false;
@@ -244,7 +220,7 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), 2) void kv_prompt_ke
   constexpr int FLIP = KW == 2 ? 1 : 0;
   auto buffer_of = [&](int i) { return ((i + FLIP) & 1) * Lds::second; };
 
-  int next_ids = tiles.count > 0 ? page_ids(0) : 0, ids = 0;
+  int next_ids = n_tiles > 0 ? page_ids(0) : 0, ids = 0;
   auto first_tile = [&]() __attribute__((always_inline)) {
     plan_tile(0, ids, lds0 + buffer_of(0), -1);
 #pragma unroll
@@ -274,11 +250,11 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), 2) void kv_prompt_ke
       rx[n].load(a.q, at + 8 * x, vec);
       ry[n].load(a.q, at + 8 * y, vec);
     }
-    if (KW == 2 && tiles.count > 0) {
+    if (KW == 2 && n_tiles > 0) {
       ids = checked(next_ids, 0);
       first_tile();
       load_scales(0, ids);
-      if (tiles.count > 1) next_ids = page_ids(1);
+      if (n_tiles > 1) next_ids = page_ids(1);
     }
     auto put = [&](int col, int piece, const float *v) {  // 8 elements
       f32x4 *at = (f32x4 *)(q32 + col * HD);
@@ -371,13 +347,13 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), 2) void kv_prompt_ke
     for (int r = 0; r < VAL; ++r) o[n][r] = 0.f;
   float m = -INFINITY, l = 0.f;
   uint32_t nans[(NT * VAL + 31) / 32] = {};  // a bit for each value of o
-  if (KW == 1 && tiles.count > 0) {
+  if (KW == 1 && n_tiles > 0) {
     ids = checked(next_ids, 0);
     first_tile();
     load_scales(0, ids);
-    if (tiles.count > 1) next_ids = page_ids(1);
+    if (n_tiles > 1) next_ids = page_ids(1);
   }
-  for (int i = 0; i < tiles.count; ++i) {
+  for (int i = 0; i < n_tiles; ++i) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();  // this tile is there, and everyone is done with the other buffer
     uint8_t *buf = lds_bytes + buffer_of(i);
@@ -386,12 +362,12 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), 2) void kv_prompt_ke
       ks_[s] = next_ks[s];
       vs_[s] = next_vs[s];
     }
-    if (i + 1 < tiles.count) {
+    if (i + 1 < n_tiles) {
       ids = checked(next_ids, i + 1);
       load_scales(i + 1, ids);
-      if (i + 2 < tiles.count) next_ids = page_ids(i + 2);
+      if (i + 2 < n_tiles) next_ids = page_ids(i + 2);
     }
-    plan_tile(min(i + 1, tiles.count - 1), ids, lds0 + buffer_of(i + 1), i + 1 - tiles.count);
+    plan_tile(min(i + 1, n_tiles - 1), ids, lds0 + buffer_of(i + 1), i + 1 - n_tiles);
     const int k0 = tile_at(i);
     const bool edge = (k0 < lo_max || k0 + TILE > hi_min) && k0 + TILE > first_min;
     uint32_t seen[NS];  // of this lane's scores
@@ -565,38 +541,80 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), 2) void kv_prompt_ke
       ml[64 + lane] = l;
     }
     __syncthreads();
-    if (kw == 1) return;
-    const float m1 = ml[lane], l1 = ml[64 + lane], mx = fmaxf(m, m1);
-    const float f0 = l != 0.f ? __builtin_amdgcn_exp2f(m - mx) : 0.f, f1 = l1 != 0.f ? __builtin_amdgcn_exp2f(m1 - mx) : 0.f;
-    l = l * f0 + l1 * f1;
+    if (kw == 0) {
+      const float m1 = ml[lane], l1 = ml[64 + lane], mx = fmaxf(m, m1);
+      const float f0 = l != 0.f ? __builtin_amdgcn_exp2f(m - mx) : 0.f, f1 = l1 != 0.f ? __builtin_amdgcn_exp2f(m1 - mx) : 0.f;
+      l = l * f0 + l1 * f1;
+      m = mx;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < QUADS; ++k) {
+          const f32x4 v = part[(n * QUADS + k) * 64 + lane];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[n][4 * k + r] = o[n][4 * k + r] * f0 + v[r] * f1;
+        }
+    }
+  }
+  const int col = C * cw + c, j = row_of(m0 + min(col, cols - 1));
+  const int64_t oi = (int64_t)(sq.from + j) * a.ldo + (int64_t)(kvh * group + m0 + col - j * group) * HD + 4 * g;
+  auto put_out = [&](int n, int k, f32x4 v) {
+    const int64_t at = oi + C * n + 4 * GROUPS * k;
+    if (a.out_vec) {
+      if constexpr (F32) *(f32x4 *)((float *)a.out + at) = v;
+      else *(bf16x4 *)((__bf16 *)a.out + at) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) store_elem<F32>(a.out, at + r, v[r]);
+    }
+  };
+  if (!SPLITS || w.splits == 1) {
+    if (kw == 1 || col >= cols) return;
+    const float scale = l != 0.f ? a.v_scale / l : 0.f;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int k = 0; k < QUADS; ++k) {
-        const f32x4 v = part[(n * QUADS + k) * 64 + lane];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) o[n][4 * k + r] = o[n][4 * k + r] * f0 + v[r] * f1;
-      }
+      for (int k = 0; k < QUADS; ++k)
+        put_out(n, k, f32x4{o[n][4 * k], o[n][4 * k + 1], o[n][4 * k + 2], o[n][4 * k + 3]} * scale);
+    return;
   }
-  const int col = C * cw + c;
-  if (col >= cols) return;
-  const float scale = l != 0.f ? a.v_scale / l : 0.f;
-  const int j = row_of(m0 + col);
-  const int64_t oi = (int64_t)(sq.from + j) * a.ldo + (int64_t)(kvh * group + m0 + col - j * group) * HD + 4 * g;
+  if constexpr (SPLITS) {
+    // a slot: a wave's outputs as it holds them, and a maximum and a sum a column
+    const auto slots = slots_of(a, COLS * HD);
+    auto at = [&](int slot, int n, int k) { return (unsigned)((slot * (COLS / C) + cw) * (NT * QUADS) + n * QUADS + k) * 256 + 4 * lane; };
+    const int mine = w.slot + w.split;
+    if (kw == 0 && col < cols) {
 #pragma unroll
-  for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int k = 0; k < QUADS; ++k) {
-      const int64_t at = oi + C * n + 4 * GROUPS * k;
-      const f32x4 v = f32x4{o[n][4 * k], o[n][4 * k + 1], o[n][4 * k + 2], o[n][4 * k + 3]} * scale;
-      if (a.out_vec) {
-        if constexpr (F32) *(f32x4 *)((float *)a.out + at) = v;
-        else *(bf16x4 *)((__bf16 *)a.out + at) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-      } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) store_elem<F32>(a.out, at + r, v[r]);
-      }
+        for (int k = 0; k < QUADS; ++k) put_slot(slots, at(mine, n, k), f32x4{o[n][4 * k], o[n][4 * k + 1], o[n][4 * k + 2], o[n][4 * k + 3]});
+      if (g == 0) __hip_atomic_store(a.part_ml + (size_t)mine * COLS + col, pair_of(m, l), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    if (!last_to_arrive(a.arrived + w.slot, w.splits, (float *)plan)) return;
+    // the last to arrive joins the splits in their order; two waves with the same columns
+    // take half of the outputs each
+    if (col >= cols) return;
+    constexpr int HALF = NT * QUADS / 2;
+    f32x4 sum[HALF];
+    float total = 0.f, top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < HALF; ++n) sum[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < w.splits; ++s) {
+      const uint64_t pair = __hip_atomic_load(a.part_ml + (size_t)(w.slot + s) * COLS + col, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      f32x4 v[HALF];
+#pragma unroll
+      for (int n = 0; n < HALF; ++n) v[n] = get_slot(slots, at(w.slot + s, 0, kw * HALF + n));
+      const float ms = __uint_as_float((uint32_t)pair), ls = __uint_as_float((uint32_t)(pair >> 32)), mx = fmaxf(top, ms);
+      const float f0 = total != 0.f ? __builtin_amdgcn_exp2f(top - mx) : 0.f, f1 = ls != 0.f ? __builtin_amdgcn_exp2f(ms - mx) : 0.f;
+      total = total * f0 + ls * f1;
+      top = mx;
+#pragma unroll
+      for (int n = 0; n < HALF; ++n) sum[n] = sum[n] * f0 + v[n] * f1;
+    }
+    const float scale = total != 0.f ? a.v_scale / total : 0.f;
+#pragma unroll
+    for (int n = 0; n < HALF; ++n) put_out((kw * HALF + n) / QUADS, (kw * HALF + n) % QUADS, sum[n] * scale);
+  }
 }
 
 template <int HD, bool F32, bool F8, int KW>
@@ -622,9 +640,19 @@ hipError_t kv_prompt_init(int head_dim) {
 }
 
 template <int HD, bool F32, bool F8, int KW>
-static hipError_t launch_prompt_type(const KvRowsArgs &a, hipStream_t s) {
-  // as many workgroups as any starts could need
-  const int64_t grid = a.d.n_kv_heads * ((int64_t)a.n_rows * a.group / (128 / KW) + a.n_seqs);
+static hipError_t launch_prompt_type(KvRowsArgs a, hipStream_t s) {
+  // as many workgroups as any starts could need: a unit more for every sequence, and a split
+  // more for each of the slots, where one round does not take all
+  const int64_t units = a.d.n_kv_heads * ((int64_t)a.n_rows * a.group / (128 / KW) + a.n_seqs);
+  int64_t splits = 1;
+  if (KW == 2) {
+    const int64_t most = std::min<int64_t>((int64_t)a.pages_per_seq << a.d.page_shift, 0x7FFFFFFF);
+    int64_t tiles = tiles_of_length((int)most, kPromptTile);
+    if (a.window > 0) tiles = std::min(tiles, ((int64_t)a.window + a.n_rows) / kPromptTile + a.sinks / kPromptTile + 4);
+    splits = splits_of((int)tiles, kPromptMinTiles, kPromptWhole);
+  }
+  a.unsplit = splits == 1;
+  const int64_t grid = std::min(units * splits, units <= a.target ? a.target : units + a.slots);
   hipLaunchKernelGGL((kv_prompt_kernel<HD, F32, F8, KW>), dim3((unsigned)grid), dim3(kPromptThreads<HD, F32, KW>), ((PromptLds<HD, F8, KW>::bytes)), s, a);
   return hipGetLastError();
 }

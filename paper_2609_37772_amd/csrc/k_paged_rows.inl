@@ -19,110 +19,6 @@ namespace uad {
 // columns see and others do not must not reach the others through 0 * NaN: values that
 // are not finite are taken out, and the columns that see them become NaN.
 // ---------------------------------------------------------------------------
-struct RowsWork {
-  RowsSeq s;
-  int b, unit, split, splits, slot;
-};
-
-template <int HD, bool F8>
-__device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds, RowsWork *w) {
-  constexpr int TILE = kTileKeys<F8>, WHOLE = kAttendWhole<HD, F8>;
-  bool bad = false;
-  if (a.unsplit && !a.row_start) {  // no sequence can have a split: a workgroup per unit
-    const int units = a.d.n_kv_heads * runs_of(1, a.group);
-    *w = RowsWork{};
-    w->b = (unsigned)wg / (unsigned)units;
-    w->unit = wg - w->b * units;
-    w->s = rows_of<TILE>(a, w->b, &bad);
-    w->splits = 1;
-    if (bad && threadIdx.x == 0) raise_status(a.status, kStatusPage);
-    return true;
-  }
-  PlanScan<kAttendWaves> scan(a.n_seqs, lds);
-  const int b0 = scan.me * scan.per;
-  RowsSeq s0{};
-  if (b0 < a.n_seqs) s0 = rows_of<TILE>(a, b0, &bad);
-  // f over this thread's sequences, of which the first is kept
-  auto each = [&](auto f) {
-    if (b0 < a.n_seqs) f(s0);
-    for (int i = 1; i < scan.per; ++i)
-      if (b0 + i < a.n_seqs) f(rows_of<TILE>(a, b0 + i, &bad));
-  };
-  int64_t n = 0;
-  int my_units = 0, units, hi, lo, mine, upto, wgs, all;
-  each([&](const RowsSeq &s) {
-    n += (int64_t)s.units * s.tiles.count;
-    my_units += s.units;
-  });
-  if (bad && wg == 0) raise_status(a.status, kStatusPage);
-  int share = 1 << 30;
-  if (!a.unsplit) {
-    scan((int)(n >> 22), &hi);
-    scan((int)(n & 0x3FFFFF), &lo);
-    share = first_share(((int64_t)hi << 22) + lo, a.target, kAttendMinTiles);
-  }
-  scan(my_units, &units);
-  auto count = [&]() {  // workgroups of this thread's sequences, and up to them
-    mine = 0;
-    each([&](const RowsSeq &s) { mine += splits_of(s.tiles.count, share, WHOLE) * s.units; });
-    upto = scan(mine, &wgs);
-  };
-  count();
-  // with fewer units than run at once
-  for (int i = 0; units < a.target && i < kShareTries && wgs > a.target; ++i) {
-    share = next_share(share);
-    count();
-  }
-  if (wg >= wgs) return false;
-  int in_slots = 0;  // workgroups in split units, for the slots
-  each([&](const RowsSeq &s) {
-    const int k = splits_of(s.tiles.count, share, WHOLE);
-    if (k > 1) in_slots += k * s.units;
-  });
-  int slot = scan(in_slots, &all) - in_slots, start = upto - mine, b = b0;
-  if (!scan.block) {
-    b = __builtin_ctzll(__ballot(upto > wg));
-    start = __builtin_amdgcn_readlane(start, b);
-    slot = __builtin_amdgcn_readlane(slot, b);
-    w->s.from = __builtin_amdgcn_readlane(s0.from, b);
-    w->s.n = __builtin_amdgcn_readlane(s0.n, b);
-    w->s.len = __builtin_amdgcn_readlane(s0.len, b);
-    w->s.units = __builtin_amdgcn_readlane(s0.units, b);
-    w->s.tiles.first = __builtin_amdgcn_readlane(s0.tiles.first, b);
-    w->s.tiles.gap = __builtin_amdgcn_readlane(s0.tiles.gap, b);
-    w->s.tiles.count = __builtin_amdgcn_readlane(s0.tiles.count, b);
-  } else {
-    if (upto > wg && start <= wg) {  // one thread: it looks for the sequence among its own
-      RowsSeq s = s0;
-      for (;;) {
-        const int k = splits_of(s.tiles.count, share, WHOLE);
-        if (start + k * s.units > wg) break;
-        start += k * s.units;
-        if (k > 1) slot += k * s.units;
-        if (++b >= min(b0 + scan.per, a.n_seqs)) break;
-        s = rows_of<TILE>(a, b, &bad);
-      }
-      const int found[3] = {b, start, slot};
-#pragma unroll
-      for (int i = 0; i < 3; ++i) scan.lds[i] = found[i];
-    }
-    __syncthreads();
-    b = __builtin_amdgcn_readfirstlane(scan.lds[0]);
-    start = __builtin_amdgcn_readfirstlane(scan.lds[1]);
-    slot = __builtin_amdgcn_readfirstlane(scan.lds[2]);
-    if (b >= a.n_seqs) return false;  // only if the caller's arrays change while this runs
-    w->s = rows_of<TILE>(a, b, &bad);
-  }
-  w->b = b;
-  w->splits = splits_of(w->s.tiles.count, share, WHOLE);
-  w->unit = (unsigned)(wg - start) / (unsigned)w->splits;
-  if (w->unit >= w->s.units) return false;  // likewise
-  w->split = wg - start - w->unit * w->splits;
-  w->slot = slot + w->unit * w->splits;
-  if (w->splits > 1 && w->slot + w->splits > a.slots) return false;  // likewise
-  return true;
-}
-
 // SINGLE: a row for every sequence, so that all columns of a unit see the same keys.
 template <int HD, bool F32, bool F8, bool SINGLE>
 __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves / 4) void kv_rows_kernel(KvRowsArgs a) {
@@ -149,7 +45,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   const double turns = a.turns[p];  // 128 of them are allocated
 
   RowsWork w;
-  if (!plan_rows<HD, F8>(a, blockIdx.x, (int *)ml, &w)) return;
+  if (!plan_rows<TILE, 16, kAttendWhole<HD, F8>, kAttendMinTiles, NW, false>(a, blockIdx.x, (int *)ml, &w)) return;
   const int runs = w.s.units / a.d.n_kv_heads;
   const int kvh = w.unit / runs, m0 = (w.unit - kvh * runs) * 16, cols = min(16, w.s.n * a.group - m0);
   const int last = w.s.len - 1, mask = (1 << a.d.page_shift) - 1;
@@ -163,8 +59,8 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   const int my_col = min(c, cols - 1), lo = from_of(my_col), hi = to_of(my_col), first = first_of(my_col);
   const int lo_min = from_of(0), lo_max = from_of(cols - 1), hi_min = to_of(0), hi_max = to_of(cols - 1);
   const int first_min = first_of(0), first_max = first_of(cols - 1);
-  // a unit parts the tiles that its own columns see among the splits that its sequence's have
   const SeenTiles tiles = SINGLE ? w.s.tiles : seen_tiles(max(hi_max, first_max), lo_min, a.sinks, TILE);
+  if (!SINGLE && !w.of_unit(tiles.count)) return;
   auto tile_at = [&](int i) { return seen_tile(tiles, i) * TILE; };  // its first key
   // keys key .. key + n - 1 that some column sees, or this lane's column does, as bits
   auto seen_by_any = [&](int key, int n) { return run_bits(lo_min - key, hi_max - key, n) | run_bits(-key, first_max - key, n); };
@@ -506,23 +402,22 @@ static hipError_t launch_rows_hd(const KvRowsArgs &a, bool f32, bool f8, hipStre
 }
 
 // Which kernel: 0: that of few rows; else the waves that share a column of that of many.
-// The kernel of few rows reads a KV head's cache for every 16 columns and parts a long
-// history, that of many reads it for 64 or 128 and does not: the one loses from a size of
-// the query on, whatever the lengths (of 8 bits half is read, and that of many has to widen
-// it).  us, few rows / many (two waves a column), causal, short and long histories:
+// The kernel of few rows reads a KV head's cache for every 16 columns, that of many for 64
+// or 128, with more to do before and after: the one loses from a size of the query on,
+// whatever the lengths.  us, few rows / many (two waves a column), causal, short and long
+// histories:
 //   query elements  head dim 256             128                       64                        128, 8 bits
-//   0.2 M to 0.4 M  -                        22.0 / 29.3, 64.8 / 90.2  15.4 / 19.7, 20.7 / 25.0  12.4 / 22.9, 30.5 / 116
-//   0.5 M           38.1 / 40.9, 97.1 / 130  8.7 / 10.8,  62.3 / 54.6  21.9 / 23.6, 63.9 / 72.0  10.0 / 11.5, 45.6 / 65.0
-//   0.8 M to 1 M    36.8 / 28.0, 172 / 132   28.0 / 19.4, 119 / 90     44.8 / 25.4, 118 / 72     35.2 / 36.5, 81 / 117
-//   2 M             25.6 / 13.4, 140 / 44.8  57.3 / 19.9, 248 / 91     25.0 / 9.4,  80.9 / 33.3  47.4 / 23.4, 156 / 118
+//   65 T to 130 T   20.7 / 20.9, 40.8 / 33   11.9 / 15.3, 23.4 / 24.8  12.6 / 14.4, 24.7 / 23.1  18.2 / 26.1
+//   260 T           14.9 / 15.9, 40.5 / 27   16.1 / 15.6, 40.7 / 28.2  6.6 / 8.2,   21.0 / 23.6  12.7 / 16.5, 30.3 / 29.6
+//   520 T           38.6 / 25.2, 97.9 / 43   8.8 / 11.7,  62.5 / 25.6  22.0 / 17.6, 62.9 / 34.0  10.3 / 12.3, 45.4 / 27.7
+//   1000 T          37.3 / 22.9, 173 / 50    42.6 / 23.4, 126 / 57     45.0 / 24.5, 118 / 54     35.5 / 26.0, 79 / 67
 // With fewer than 16 columns a sequence its units would be mostly empty.  Two waves share a
-// column where units of 128 columns would be too few to fill the chip (128 units at head dim
-// 128: 53 us, with one wave 73) or half empty (25.4 and 30.4 at 64 columns a sequence); from
-// 256 full ones on one wave takes 71 us for 97 at head dim 256, at 128 and 512 units 200 for
-// 214, of 8 bits 228 for 362.
-static int prompt_key_waves(const KvRowsArgs &a, bool f8) {
+// column where units of 128 columns would be too few to fill the chip or half empty (25 and
+// 30 us at 64 columns a sequence); from 256 full ones on one wave takes 69 us for 100 at head
+// dim 256, at 128 and 512 units 198 for 214, of 8 bits 225 for 268.
+static int prompt_key_waves(const KvRowsArgs &a) {
   const int64_t columns = (int64_t)a.n_rows * a.group;
-  if (!a.row_start || columns < 16 * (int64_t)a.n_seqs || columns * a.d.n_kv_heads * a.d.head_dim < (f8 ? 1200000 : 600000)) return 0;
+  if (!a.row_start || columns < 16 * (int64_t)a.n_seqs || columns * a.d.n_kv_heads * a.d.head_dim < 250000) return 0;
   return columns < 128 * (int64_t)a.n_seqs || columns / 128 * a.d.n_kv_heads < 256 ? 2 : 1;
 }
 
@@ -531,7 +426,7 @@ hipError_t launch_kv_rows(const KvRowsArgs &a, bool f32, bool f8, hipStream_t s)
       a.target < 1 || a.slots < max_slots(a.target) || a.d.page_shift < 4 || a.window < 0 || a.sinks < 0 ||
       (!a.row_start && a.n_rows != a.n_seqs) || (!f8 && a.k_scales))
     return hipErrorInvalidValue;
-  const int key_waves = prompt_key_waves(a, f8);
+  const int key_waves = prompt_key_waves(a);
   if (key_waves) return launch_kv_prompt(a, key_waves, f32, f8, s);
   if (a.d.head_dim == 64) return launch_rows_hd<64>(a, f32, f8, s);
   if (a.d.head_dim == 128) return launch_rows_hd<128>(a, f32, f8, s);

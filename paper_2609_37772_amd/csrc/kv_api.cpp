@@ -89,7 +89,7 @@ uad_status uad_kv_create(const uad_kv_config *cfg, int32_t device, void *hip_str
   hipError_t e = hipDeviceGetAttribute(&kv->n_cu, hipDeviceAttributeMultiprocessorCount, device);
   if (e != hipSuccess) return cerr(UAD_E_HIP, "hipDeviceGetAttribute", e);
   const size_t o_turns = 256, n_turns = m.rope_dim / 2;
-  const size_t rows = 16;  // of a slot; a single token's attention takes up to its group
+  const size_t rows = 64;  // of a slot: attention takes up to its group, 16 or 64
   kv->slots = max_slots(kv_attend_target(kv->n_cu, m.head_dim));
   const size_t o_steps = o_turns + 128 * sizeof(double), o_arrived = o_steps + 128 * sizeof(uint64_t), o_pages = o_arrived + 2 * (size_t)kv->slots * sizeof(unsigned);
   const size_t o_ml = (o_pages + (2 + (size_t)m.max_seqs) * sizeof(unsigned) + 255) / 256 * 256;

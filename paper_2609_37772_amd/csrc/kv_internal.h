@@ -43,8 +43,8 @@ struct KvAttendArgs {
   float v_scale;
   const float *k_scales, *v_scales;  // the layer's, of every block of tokens, or null (then the above are 1)
   unsigned *status;
-  // joins of units that several workgroups share: a slot for each, of up to 16 rows
-  // (min(16, group) for a single token) of unnormalised outputs [rows][head_dim] and a
+  // joins of units that several workgroups share: a slot for each, of up to 64 rows
+  // (min(16, group) for a single token, 16 for a few) of unnormalised outputs [rows][head_dim] and a
   // (max, sum) pair per row, and two arrival counters (zero between launches: the last
   // to arrive clears them)
   float *part;

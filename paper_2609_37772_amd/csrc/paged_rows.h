@@ -13,10 +13,11 @@ struct RowsSeq {
   SeenTiles tiles;
 };
 
-__device__ __forceinline__ int runs_of(int rows, int group) { return (int)(((int64_t)rows * group + 15) / 16); }
+template <int COLS>
+__device__ __forceinline__ int runs_of(int rows, int group) { return (int)(((int64_t)rows * group + COLS - 1) / COLS); }
 
 // Sequence b; one that cannot be used has no units.
-template <int TILE>
+template <int TILE, int COLS>
 __device__ __forceinline__ RowsSeq rows_of(const KvRowsArgs &a, int b, bool *bad) {
   RowsSeq s{b, 1, 0, 0, {}};
   if (a.row_start) {
@@ -29,9 +30,129 @@ __device__ __forceinline__ RowsSeq rows_of(const KvRowsArgs &a, int b, bool *bad
   } else {
     s.len = length_or_none(a.lens[b], a.pages_per_seq, a.d.page_shift, bad);
   }
-  s.units = a.d.n_kv_heads * runs_of(s.n, a.group);
+  s.units = a.d.n_kv_heads * runs_of<COLS>(s.n, a.group);
   s.tiles = seen_tiles(s.len, seen_from(s.len - s.n, a.window), a.sinks, TILE);
   return s;
+}
+
+// What workgroup `wg` does: split `split` of `splits` of a unit of up to COLS columns, whose
+// slots begin at `slot`; false if it has nothing to do.  A sequence's units have as many
+// splits as its tiles ask for (of MIN tiles at least, where it has more than WHOLE), and
+// share out the tiles that they see themselves.  ONE_ROUND: with fewer units than workgroups
+// that run at once, no splits either that would make them more.
+struct RowsWork {
+  RowsSeq s;
+  int b, unit, split, splits, slot;
+  // Of a unit that sees `tiles` tiles; a split that is not needed is not done.
+  __device__ __forceinline__ bool of_unit(int tiles) {
+    const int each = (int)(((unsigned)s.tiles.count + splits - 1) / (unsigned)splits);
+    splits = max(1, min(splits, (int)(((unsigned)tiles + each - 1) / (unsigned)each)));
+    return split < splits;
+  }
+};
+
+template <int TILE, int COLS, int WHOLE, int MIN, int NW, bool ONE_ROUND>
+__device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds, RowsWork *w) {
+  bool bad = false;
+  if (a.unsplit && !a.row_start) {  // no sequence can have a split: a workgroup per unit
+    const int units = a.d.n_kv_heads * runs_of<COLS>(1, a.group);
+    *w = RowsWork{};
+    w->b = (unsigned)wg / (unsigned)units;
+    w->unit = wg - w->b * units;
+    w->s = rows_of<TILE, COLS>(a, w->b, &bad);
+    w->splits = 1;
+    if (bad && threadIdx.x == 0) raise_status(a.status, kStatusPage);
+    return true;
+  }
+  PlanScan<NW> scan(a.n_seqs, lds);
+  const int b0 = scan.me * scan.per;
+  RowsSeq s0{};
+  if (b0 < a.n_seqs) s0 = rows_of<TILE, COLS>(a, b0, &bad);
+  // f over this thread's sequences, of which the first is kept
+  auto each = [&](auto f) {
+    if (b0 < a.n_seqs) f(s0);
+    for (int i = 1; i < scan.per; ++i)
+      if (b0 + i < a.n_seqs) f(rows_of<TILE, COLS>(a, b0 + i, &bad));
+  };
+  int64_t n = 0;
+  int my_units = 0, units, hi, lo, mine, upto, wgs, all;
+  each([&](const RowsSeq &s) {
+    n += (int64_t)s.units * s.tiles.count;
+    my_units += s.units;
+  });
+  if (bad && wg == 0) raise_status(a.status, kStatusPage);
+  int share = 1 << 30;
+  if (!a.unsplit) {
+    scan((int)(n >> 22), &hi);
+    scan((int)(n & 0x3FFFFF), &lo);
+    share = first_share(((int64_t)hi << 22) + lo, a.target, MIN);
+  }
+  scan(my_units, &units);
+  // ONE_ROUND: a remainder of less than half a share is not worth a join
+  auto whole = [&]() { return ONE_ROUND ? max(WHOLE, share + (share >> 1)) : WHOLE; };
+  auto count = [&]() {  // workgroups of this thread's sequences, and up to them
+    mine = 0;
+    each([&](const RowsSeq &s) { mine += splits_of(s.tiles.count, share, whole()) * s.units; });
+    upto = scan(mine, &wgs);
+  };
+  count();
+  // with fewer units than run at once
+  for (int i = 0; units < a.target && i < kShareTries && wgs > a.target; ++i) {
+    share = next_share(share);
+    count();
+  }
+  if (ONE_ROUND && units < a.target && wgs > a.target) {
+    share = 1 << 30;
+    count();
+  }
+  if (wg >= wgs) return false;
+  int in_slots = 0;  // workgroups in split units, for the slots
+  each([&](const RowsSeq &s) {
+    const int k = splits_of(s.tiles.count, share, whole());
+    if (k > 1) in_slots += k * s.units;
+  });
+  int slot = scan(in_slots, &all) - in_slots, start = upto - mine, b = b0;
+  if (!scan.block) {
+    b = __builtin_ctzll(__ballot(upto > wg));
+    start = __builtin_amdgcn_readlane(start, b);
+    slot = __builtin_amdgcn_readlane(slot, b);
+    w->s.from = __builtin_amdgcn_readlane(s0.from, b);
+    w->s.n = __builtin_amdgcn_readlane(s0.n, b);
+    w->s.len = __builtin_amdgcn_readlane(s0.len, b);
+    w->s.units = __builtin_amdgcn_readlane(s0.units, b);
+    w->s.tiles.first = __builtin_amdgcn_readlane(s0.tiles.first, b);
+    w->s.tiles.gap = __builtin_amdgcn_readlane(s0.tiles.gap, b);
+    w->s.tiles.count = __builtin_amdgcn_readlane(s0.tiles.count, b);
+  } else {
+    if (upto > wg && start <= wg) {  // one thread: it looks for the sequence among its own
+      RowsSeq s = s0;
+      for (;;) {
+        const int k = splits_of(s.tiles.count, share, whole());
+        if (start + k * s.units > wg) break;
+        start += k * s.units;
+        if (k > 1) slot += k * s.units;
+        if (++b >= min(b0 + scan.per, a.n_seqs)) break;
+        s = rows_of<TILE, COLS>(a, b, &bad);
+      }
+      const int found[3] = {b, start, slot};
+#pragma unroll
+      for (int i = 0; i < 3; ++i) scan.lds[i] = found[i];
+    }
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(scan.lds[0]);
+    start = __builtin_amdgcn_readfirstlane(scan.lds[1]);
+    slot = __builtin_amdgcn_readfirstlane(scan.lds[2]);
+    if (b >= a.n_seqs) return false;  // only if the caller's arrays change while this runs
+    w->s = rows_of<TILE, COLS>(a, b, &bad);
+  }
+  w->b = b;
+  w->splits = splits_of(w->s.tiles.count, share, whole());
+  w->unit = (unsigned)(wg - start) / (unsigned)w->splits;
+  if (w->unit >= w->s.units) return false;  // likewise
+  w->split = wg - start - w->unit * w->splits;
+  w->slot = slot + w->unit * w->splits;
+  if (w->splits > 1 && w->slot + w->splits > a.slots) return false;  // likewise
+  return true;
 }
 
 // 16-byte pieces of V that hold a value that is not finite: those become zeros in v, and
