@@ -22,6 +22,12 @@ namespace uad {
 // as much error again as the output's one rounding to bf16 has, twice over: once for the
 // query, whose error the scores take in, and once for the weights.
 //
+// Measured: one causal prompt of 8191 rows, 32/8 heads of 128: 917 us, with two terms 1.2
+// PFLOP/s of the 1.3 to 1.4 that a library's large products reach; 816 rows that all see
+// each other, 8/1 heads of 256: 31.5 us, of which plan, query and join are 11; 16 prompts
+// of up to 1024 rows in 8 bits, 12/2 heads of 128: 68 us, not much more than the one unit
+// with the most tiles takes.
+//
 // Masks as in the kernel of few rows: what no column sees is zero in V, and values that are
 // not finite where some columns do not see them are taken out of LDS and noted for those
 // that do.

@@ -67,9 +67,9 @@ __device__ __forceinline__ void turn_of(double turns, int position, float *s, fl
   *c = __builtin_amdgcn_cosf(f);
 }
 
-// The same in whole numbers, for those who turn much: a turn is 2^64 steps, of which a
-// product with the position keeps the rest (`steps`), and 2^32 of `turned`, off by one at
-// most.  On a CU's vector unit about 80 clocks a wave, where the doubles take 130.
+// The same in whole numbers, without 64-bit floats, for those who turn much: a turn is 2^64
+// steps, of which a product with the position keeps the rest (`steps`), and 2^32 of
+// `turned`, off by one at most.
 __device__ __forceinline__ uint32_t turned(uint64_t steps, int position) {
   const uint32_t lo = (uint32_t)steps, hi = (uint32_t)(steps >> 32), p = (uint32_t)position;
   return __umulhi(p, lo) + p * hi - (position < 0 ? lo : 0u);
