@@ -346,7 +346,7 @@ struct SumScan {
 // The first entry whose sum is above i.
 __device__ __forceinline__ int entry_of(const int *upto, int n, int i) {
   int lo = 0;
-  for (int step = kSumEntries / 2; step > 0; step /= 2)
+  for (int step = n > 0 ? 1 << (31 - __builtin_clz(n)) : 0; step > 0; step /= 2)
     if (lo + step <= n && upto[lo + step - 1] <= i) lo += step;
   return lo;
 }
