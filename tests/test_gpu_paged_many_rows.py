@@ -38,6 +38,13 @@ MANY = [
     (16, 16, 256, 64, [129, 1], [129, 300], BF16, F8, 256, False, 0, 0, False),
     (16, 16, 256, 16, [130], [131], F32, F8, 256, False, 20, 3, True),
     (16, 16, 256, 32, [130], [140], F32, BF16, 256, False, 0, 0, True),
+    # sequences beyond a thread each, heads beyond a unit's columns
+    (2, 16, 64, 16, [1 + i % 2 for i in range(1100)], [1 + i % 2 + i * 7 % 50 for i in range(1100)], BF16, BF16, 64, False, 0, 0, True),
+    (2, 16, 128, 16, [i % 4 for i in range(700)], [i % 4 + (900 if i == 650 else i % 9) for i in range(700)], BF16, "blocks", 128, False, 20, 3, True),
+    (1, 16, 256, 16, [2 + i % 2 for i in range(600)], [3 + i % 30 for i in range(600)], F32, BF16, 64, True, 0, 0, False),
+    (4, 16, 64, 16, [8 + i % 3 for i in range(70)], [10 + i * 11 % 130 for i in range(70)], BF16, "blocks", 64, False, 0, 0, True),
+    (1, 200, 128, 16, [31], [500], BF16, BF16, 128, False, 0, 0, True),
+    (2, 150, 64, 32, [17, 2], [300, 1000], F32, F8, 64, False, 100, 7, True),
 ]
 
 
