@@ -418,17 +418,20 @@ static hipError_t launch_rows_hd(const KvRowsArgs &a, bool f32, bool f8, hipStre
 // whatever the lengths.  us, few rows / many (two waves a column), causal, short and long
 // histories:
 //   query elements  head dim 256             128                       64                        128, 8 bits
-//   65 T to 130 T   20.7 / 20.9, 40.8 / 33   11.9 / 15.3, 23.4 / 24.8  12.6 / 14.4, 24.7 / 23.1  18.2 / 26.1
-//   260 T           14.9 / 15.9, 40.5 / 27   16.1 / 15.6, 40.7 / 28.2  6.6 / 8.2,   21.0 / 23.6  12.7 / 16.5, 30.3 / 29.6
-//   520 T           38.6 / 25.2, 97.9 / 43   8.8 / 11.7,  62.5 / 25.6  22.0 / 17.6, 62.9 / 34.0  10.3 / 12.3, 45.4 / 27.7
-//   1000 T          37.3 / 22.9, 173 / 50    42.6 / 23.4, 126 / 57     45.0 / 24.5, 118 / 54     35.5 / 26.0, 79 / 67
+//   65k to 130k     20.7 / 20.9, 40.8 / 33   11.9 / 15.3, 23.4 / 24.8  12.6 / 14.4, 24.7 / 23.1  18.2 / 26.1
+//   260k            14.9 / 15.9, 40.5 / 27   16.1 / 15.6, 40.7 / 28.2  6.6 / 8.2,   21.0 / 23.6  12.7 / 16.5, 30.3 / 29.6
+//   520k            38.6 / 25.2, 97.9 / 43   8.8 / 11.7,  62.5 / 25.6  22.0 / 17.6, 62.9 / 34.0  10.3 / 12.3, 45.4 / 27.7
+//   1000k           37.3 / 22.9, 173 / 50    42.6 / 23.4, 126 / 57     45.0 / 24.5, 118 / 54     35.5 / 26.0, 79 / 67
+// At head dim 256, where the kernel of few rows spills, 130k elements are enough; 33k, 16 rows
+// of 8 heads on 4000 tokens, take 28.0 us for 32.4.
 // With fewer than 16 columns a sequence its units would be mostly empty.  Two waves share a
 // column where units of 128 columns would be too few to fill the chip or half empty (25 and
 // 30 us at 64 columns a sequence); from 256 full ones on one wave takes 69 us for 100 at head
 // dim 256, at 128 and 512 units 198 for 214, of 8 bits 225 for 268.
 static int prompt_key_waves(const KvRowsArgs &a) {
   const int64_t columns = (int64_t)a.n_rows * a.group;
-  if (!a.row_start || columns < 16 * (int64_t)a.n_seqs || columns * a.d.n_kv_heads * a.d.head_dim < 250000) return 0;
+  const int64_t few = a.d.head_dim == 256 ? 130000 : 250000;
+  if (!a.row_start || columns < 16 * (int64_t)a.n_seqs || columns * a.d.n_kv_heads * a.d.head_dim < few) return 0;
   return columns < 128 * (int64_t)a.n_seqs || columns / 128 * a.d.n_kv_heads < 256 ? 2 : 1;
 }
 
