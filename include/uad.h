@@ -451,10 +451,8 @@ uad_status uad_kv_set_block_scales(uad_kv *kv, float *k_scales, float *v_scales)
  * lens[b], where
  *   x <= p                                if causal is 1, and
  *   |p - x| < window or x < n_sinks       if window > 0.
- * out = softmax(scale * q K^T) V per head over those keys, rounded once to the type of q.
- * Sums and softmax statistics are fp32; the matrix instructions take the rotated query and
- * the weights in 24 bits for F32 rows and for calls of few rows, in 16 for many rows of
- * BF16.
+ * out = softmax(scale * q K^T) V per head over those keys, in fp32, rounded once to the type
+ * of q.
  *   q, out      device [n_rows][n_heads][head_dim] of dtype F32 or BF16, rows ldq / ldo
  *               elements apart, aligned to their type; out may not overlap q or the pools
  *   row_start   as in uad_kv_append: rows from row_start[n_seqs] on are ignored, and their

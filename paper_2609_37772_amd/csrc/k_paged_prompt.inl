@@ -17,16 +17,14 @@ namespace uad {
 // of a row lies at piece p ^ (a few bits of the row), so that rows that are read at once do
 // not meet in a bank.  The query is held in registers, rotated and scaled in fp32 on the way.
 //
-// Precision: the query and the weights enter as bf16 terms, two (16 bits) for bf16 rows and
-// three for fp32 rows; keys and values as stored.  One term would halve the time and add
-// as much error again as the output's one rounding to bf16 has, twice over: once for the
-// query, whose error the scores take in, and once for the weights.
+// Precision: the query and the weights enter as three bf16 terms (24 bits, all of an fp32
+// value), as in the kernel of few rows: a row is held in no fewer bits for others that its
+// call has.  Keys and values as stored.
 //
-// Measured: one causal prompt of 8191 rows, 32/8 heads of 128: 917 us, with two terms 1.2
+// Measured: one causal prompt of 8191 rows, 32/8 heads of 128: 1357 us, with three terms 1.2
 // PFLOP/s of the 1.3 to 1.4 that a library's large products reach; 816 rows that all see
-// each other, 8/1 heads of 256: 31.5 us, of which plan, query and join are 11; 16 prompts
-// of up to 1024 rows in 8 bits, 12/2 heads of 128: 68 us, not much more than the one unit
-// with the most tiles takes.
+// each other, 8/1 heads of 256: 35 us; 16 prompts of up to 1024 rows in 8 bits, 12/2 heads of
+// 128: 92 us, not much more than the one unit with the most tiles takes.
 //
 // Masks as in the kernel of few rows: what no column sees is zero in V, and values that are
 // not finite where some columns do not see them are taken out of LDS and noted for those
@@ -39,17 +37,17 @@ constexpr int kPromptTile = 64;
 constexpr int kPromptMinTiles = 3, kPromptWhole = 6;
 
 // Columns of a wave: outputs and query take it columns x head dim x (4 + 2 terms) bytes,
-// and two waves are to share a SIMD's 512 registers.  Where workgroups are too few for
-// that, 16 columns give each of them twice the waves: at head dim 128 a tenth faster than
-// 32; at 64 a tile of 8 bits has fewer pieces than twice the threads.
-template <int HD, bool F32, int KW>
-constexpr int kPromptCols = (KW == 2 && HD == 128) || HD == 256 || (HD == 128 && F32) ? 16 : 32;
-template <int HD, bool F32, int KW>
-constexpr int kPromptThreads = 64 * 128 / kPromptCols<HD, F32, KW>;
-// Waves of a SIMD: where LDS has room for two workgroups of 8 waves a CU, the registers are
-// to be 128 at most (8 sequences of 64 rows on 2000 tokens: 54 us, with 129 registers 82).
-template <int HD, bool F32, int KW>
-constexpr int kPromptPerSimd = HD == 128 && !F32 && KW == 2 ? 4 : 2;
+// and two waves are to share a SIMD's 512 registers.  At head dim 128 32 columns leave 18 of
+// the query's registers (28 with 8-bit pools) to be read again from memory for every tile, and
+// are faster all the same than 16, which read each operand from LDS for half as many columns:
+// a prompt of 8191 rows 1357 us for 1433, the fleet of 16 in 8 bits 92 for 99.  Where
+// workgroups are too few to fill the chip, 16 columns give each of them twice the waves: 8
+// sequences of 64 rows in 8 bits 73 us for 81; at 64 a tile of 8 bits has fewer pieces than
+// twice the threads.
+template <int HD, int KW>
+constexpr int kPromptCols = (KW == 2 && HD == 128) || HD == 256 ? 16 : 32;
+template <int HD, int KW>
+constexpr int kPromptThreads = 64 * 128 / kPromptCols<HD, KW>;
 
 // LDS: two buffers of a tile's K and V^T; before that the query in fp32 (in the first buffer
 // and where two waves share columns, which are calls that wait for latency, no further, so
@@ -108,9 +106,9 @@ __device__ __forceinline__ void load_to_lds(const void *base, uint32_t offset, u
 }
 
 template <int HD, bool F32, bool F8, int KW>
-__global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), (kPromptPerSimd<HD, F32, KW>)) void kv_prompt_kernel(KvRowsArgs a) {
+__global__ __launch_bounds__((kPromptThreads<HD, KW>), 2) void kv_prompt_kernel(KvRowsArgs a) {
   using Lds = PromptLds<HD, F8, KW>;
-  constexpr int C = kPromptCols<HD, F32, KW>, THREADS = kPromptThreads<HD, F32, KW>, NW = THREADS / 64;
+  constexpr int C = kPromptCols<HD, KW>, THREADS = kPromptThreads<HD, KW>, NW = THREADS / 64;
   using Mul = Product<C>;
   typedef typename Mul::acc acc;
   constexpr int VAL = Mul::values, GROUPS = 64 / C;   // results a lane; groups of lanes
@@ -119,7 +117,7 @@ __global__ __launch_bounds__((kPromptThreads<HD, F32, KW>), (kPromptPerSimd<HD, 
   constexpr int MK = 32 / C;                          // products of a part: 32 keys in rows of C
   constexpr int K = 8 * GROUPS, KS = HD / K;          // depth of a product, steps of Q K^T
   constexpr int NT = HD / C;                          // output tiles
-  constexpr int TERMS = F32 ? 3 : 2, ESZ = F8 ? 1 : 2;
+  constexpr int TERMS = kTerms, ESZ = F8 ? 1 : 2;
   constexpr int KP = HD * ESZ / 16, VP = TILE * ESZ / 16;  // 16-byte pieces of a row of K, of V^T
   constexpr int KBYTES = TILE * HD * ESZ, PIECE = 16 / ESZ;  // keys of a piece of V^T
   extern __shared__ __align__(16) uint8_t lds_bytes[];
@@ -659,7 +657,7 @@ static hipError_t launch_prompt_type(KvRowsArgs a, hipStream_t s) {
   }
   a.unsplit = splits == 1;
   const int64_t grid = std::min(units * splits, units <= a.target ? a.target : units + a.slots);
-  hipLaunchKernelGGL((kv_prompt_kernel<HD, F32, F8, KW>), dim3((unsigned)grid), dim3(kPromptThreads<HD, F32, KW>), ((PromptLds<HD, F8, KW>::bytes)), s, a);
+  hipLaunchKernelGGL((kv_prompt_kernel<HD, F32, F8, KW>), dim3((unsigned)grid), dim3(kPromptThreads<HD, KW>), ((PromptLds<HD, F8, KW>::bytes)), s, a);
   return hipGetLastError();
 }
 template <int HD, int KW>
