@@ -34,7 +34,8 @@ constexpr int kPromptTile = 64;
 // Tiles of a split at least, and those up to which a unit stays whole: a split costs the query
 // anew and a join, which take as long as 3 tiles.  102 units of 13 tiles at head dim 256:
 // 36.0 us whole, 31.5 us in two; 16 units of 63: 130 whole, 43 split.
-constexpr int kPromptMinTiles = 3, kPromptWhole = 6;
+template <int KW>
+__host__ __device__ constexpr RowsKind many_rows() { return {kPromptTile, 128 / KW, 6, 3, true}; }
 
 // Columns of a wave: outputs and query take it columns x head dim x (4 + 2 terms) bytes,
 // and two waves are to share a SIMD's 512 registers.  At head dim 128 32 columns leave 18 of
@@ -131,7 +132,7 @@ __global__ __launch_bounds__((kPromptThreads<HD, KW>), 2) void kv_prompt_kernel(
   const int group = a.group;
   constexpr bool SPLITS = KW == 2;
   RowsWork w;
-  if (!plan_rows<TILE, COLS, kPromptWhole, kPromptMinTiles, NW, true>(a, blockIdx.x, plan, &w)) return;
+  if (!plan_rows<NW>(many_rows<KW>(), a, blockIdx.x, plan, &w)) return;
   const RowsSeq sq = w.s;
   const int runs = sq.units / a.d.n_kv_heads;
   const int run = runs - 1 - w.unit / a.d.n_kv_heads, kvh = w.unit % a.d.n_kv_heads;
@@ -645,19 +646,12 @@ hipError_t kv_prompt_init(int head_dim) {
 
 template <int HD, bool F32, bool F8, int KW>
 static hipError_t launch_prompt_type(KvRowsArgs a, hipStream_t s) {
-  // as many workgroups as any starts could need: a unit more for every sequence, and a split
-  // more for each of the slots, where one round does not take all
-  const int64_t units = a.d.n_kv_heads * ((int64_t)a.n_rows * a.group / (128 / KW) + a.n_seqs);
-  int64_t splits = 1;
-  if (KW == 2) {
-    const int64_t most = std::min<int64_t>((int64_t)a.pages_per_seq << a.d.page_shift, 0x7FFFFFFF);
-    int64_t tiles = tiles_of_length((int)most, kPromptTile);
-    if (a.window > 0) tiles = std::min(tiles, ((int64_t)a.window + a.n_rows) / kPromptTile + a.sinks / kPromptTile + 4);
-    splits = splits_of((int)tiles, kPromptMinTiles, kPromptWhole);
-  }
-  a.unsplit = splits == 1;
-  const int64_t grid = std::min(units * splits, units <= a.target ? a.target : units + a.slots);
-  hipLaunchKernelGGL((kv_prompt_kernel<HD, F32, F8, KW>), dim3((unsigned)grid), dim3(kPromptThreads<HD, KW>), ((PromptLds<HD, F8, KW>::bytes)), s, a);
+  constexpr RowsKind kind = many_rows<KW>();
+  // units of 128 columns are not split
+  const int64_t tokens = KW == 2 ? (int64_t)a.pages_per_seq << a.d.page_shift : kind.tile;
+  const RowsGrid grid = rows_grid(kind, a.n_rows, a.n_seqs, true, a.d.n_kv_heads, a.group, tokens, a.window, a.sinks, a.target, a.slots);
+  a.unsplit = grid.unsplit;
+  hipLaunchKernelGGL((kv_prompt_kernel<HD, F32, F8, KW>), dim3((unsigned)grid.wgs), dim3(kPromptThreads<HD, KW>), ((PromptLds<HD, F8, KW>::bytes)), s, a);
   return hipGetLastError();
 }
 template <int HD, int KW>

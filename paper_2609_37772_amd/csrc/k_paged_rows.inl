@@ -30,6 +30,9 @@ namespace uad {
 // each on 20000 tokens of 5 sequences with a window of 1000 10.1.
 // ---------------------------------------------------------------------------
 
+template <int HD, bool F8>
+__host__ __device__ constexpr RowsKind few_rows() { return {kTileKeys<F8>, 16, kAttendWhole<HD, F8>, kAttendMinTiles, false}; }
+
 // SINGLE: a row for every sequence, so that all columns of a unit see the same keys.
 template <int HD, bool F32, bool F8, bool SINGLE>
 __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves / 4) void kv_rows_kernel(KvRowsArgs a) {
@@ -56,7 +59,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, kAttendPerCu<HD> * kAttendWaves 
   const double turns = a.turns[p];  // 128 of them are allocated
 
   RowsWork w;
-  if (!plan_rows<TILE, 16, kAttendWhole<HD, F8>, kAttendMinTiles, NW, false>(a, blockIdx.x, (int *)ml, &w)) return;
+  if (!plan_rows<NW>(few_rows<HD, F8>(), a, blockIdx.x, (int *)ml, &w)) return;
   const int runs = w.s.units / a.d.n_kv_heads;
   const int kvh = w.unit / runs, m0 = (w.unit - kvh * runs) * 16, cols = min(16, w.s.n * a.group - m0);
   const int last = w.s.len - 1, mask = (1 << a.d.page_shift) - 1;
@@ -387,19 +390,10 @@ hipError_t kv_rows_init(int head_dim) {
 
 template <int HD, bool F32, bool F8>
 static hipError_t launch_rows_type(KvRowsArgs a, hipStream_t s) {
-  constexpr int TILE = kTileKeys<F8>;
-  // as many workgroups as any lengths could need: a unit more for every sequence whose
-  // last has fewer columns, and a split more for each of the slots
-  const int64_t columns = (int64_t)a.n_rows * a.group;
-  const int64_t units = a.d.n_kv_heads * (a.row_start ? columns / 16 + a.n_seqs : (int64_t)a.n_seqs * ((a.group + 15) / 16));
-  int64_t most = std::min<int64_t>((int64_t)a.pages_per_seq << a.d.page_shift, 0x7FFFFFFF);
-  int64_t tiles = tiles_of_length((int)most, TILE);
-  // a window's, of up to all the rows, and the sinks', each in a tile more than they fill
-  if (a.window > 0) tiles = std::min(tiles, ((int64_t)a.window + (a.row_start ? a.n_rows : 1)) / TILE + a.sinks / TILE + 4);
-  const int64_t splits = splits_of((int)tiles, kAttendMinTiles, kAttendWhole<HD, F8>);
-  const int64_t grid = std::min(units * splits, units + a.slots);
-  a.unsplit = splits == 1;
-  const dim3 wgs((unsigned)grid), wg(64 * kAttendWaves);
+  const RowsGrid grid = rows_grid(few_rows<HD, F8>(), a.n_rows, a.n_seqs, a.row_start != nullptr, a.d.n_kv_heads, a.group,
+                                  (int64_t)a.pages_per_seq << a.d.page_shift, a.window, a.sinks, a.target, a.slots);
+  a.unsplit = grid.unsplit;
+  const dim3 wgs((unsigned)grid.wgs), wg(64 * kAttendWaves);
   constexpr int lds = attend_lds_floats<HD>() * 4;
   if (a.row_start) hipLaunchKernelGGL((kv_rows_kernel<HD, F32, F8, false>), wgs, wg, lds, s, a);
   else hipLaunchKernelGGL((kv_rows_kernel<HD, F32, F8, true>), wgs, wg, lds, s, a);

@@ -141,6 +141,58 @@ UAD_HD int split_begin(int tiles, int n, int s) {
 UAD_HD int max_slots(int target) { return 2 * target; }
 
 // ---------------------------------------------------------------------------
+// The same for new rows.  A sequence's rows are units of up to `cols` (row, query head) pairs
+// of a KV head, its tiles those that any of its rows sees.  The launch knows bounds of the
+// units and tiles only, the plan on the device what they are: what both decide by is here, so
+// that no workgroup that a plan counts on is left out of a launch.
+// ---------------------------------------------------------------------------
+// What differs between the kernels (constants there: from functions, as a variable's would be
+// loaded, for 0.4 to 0.9 us a call).
+struct RowsKind {
+  int tile, cols, whole, min_tiles;
+  bool one_round;  // with idle workgroups, no splits that all of them together could not take
+};
+constexpr int kUncut = 1 << 30;  // a share that no unit is more than
+
+UAD_HD int runs_of(int rows, int group, int cols) { return (int)(((int64_t)rows * group + cols - 1) / cols); }
+// Whether some of the workgroups that run at once would have no unit.
+UAD_HD bool leaves_idle(int64_t units, int target) { return units < target; }
+// Splits of a sequence's units; one_round: a remainder of less than half a share is not worth
+// a join.
+UAD_HD int rows_splits(const RowsKind &k, int tiles, int share) {
+  const int rest = share + (share >> 1);
+  return splits_of(tiles, share, k.one_round && rest > k.whole ? rest : k.whole);
+}
+// The plan's share of `units` units, from `share` on, the first or that of a launch without
+// splits; count(share) gives the workgroups.
+template <class Count>
+UAD_HD int rows_share(const RowsKind &k, int share, int units, int target, Count count) {
+  for (int i = 0;; ++i) {
+    if (count(share) <= target || !leaves_idle(units, target)) return share;
+    if (i < kShareTries) share = next_share(share);
+    else if (k.one_round && share < kUncut) share = kUncut;
+    else return share;
+  }
+}
+// Workgroups to launch: a unit more for every sequence, whose last may have fewer columns, and
+// a split more for each of the slots.
+struct RowsGrid {
+  int64_t wgs;
+  bool unsplit;  // no sequence can have a split
+};
+UAD_HD RowsGrid rows_grid(const RowsKind &k, int n_rows, int n_seqs, bool starts, int n_kv_heads, int group, int64_t max_tokens,
+                          int window, int sinks, int target, int slots) {
+  const int64_t units = n_kv_heads * (starts ? (int64_t)n_rows * group / k.cols + n_seqs : (int64_t)n_seqs * runs_of(1, group, k.cols));
+  int64_t tiles = tiles_of_length((int)(max_tokens < 0x7FFFFFFF ? max_tokens : 0x7FFFFFFF), k.tile);
+  // a window's, of up to all the rows, and the sinks', each in a tile more than they fill
+  const int64_t seen = ((int64_t)window + (starts ? n_rows : 1)) / k.tile + sinks / k.tile + 4;
+  if (window > 0 && seen < tiles) tiles = seen;
+  const int64_t splits = splits_of((int)tiles, k.min_tiles, k.whole);
+  const int64_t most = k.one_round && leaves_idle(units, target) ? target : units + slots;
+  return {units * splits < most ? units * splits : most, splits == 1};
+}
+
+// ---------------------------------------------------------------------------
 // 8-bit pools with scales of their own: one for K and one for V of every kScaleBlock
 // tokens of a page's head, [page][KV head][page size / kScaleBlock].
 // ---------------------------------------------------------------------------

@@ -13,12 +13,8 @@ struct RowsSeq {
   SeenTiles tiles;
 };
 
-template <int COLS>
-__device__ __forceinline__ int runs_of(int rows, int group) { return (int)(((int64_t)rows * group + COLS - 1) / COLS); }
-
 // Sequence b; one that cannot be used has no units.
-template <int TILE, int COLS>
-__device__ __forceinline__ RowsSeq rows_of(const KvRowsArgs &a, int b, bool *bad) {
+__device__ __forceinline__ RowsSeq rows_of(RowsKind k, const KvRowsArgs &a, int b, bool *bad) {
   RowsSeq s{b, 1, 0, 0, {}};
   if (a.row_start) {
     s.from = a.row_start[b];
@@ -30,17 +26,15 @@ __device__ __forceinline__ RowsSeq rows_of(const KvRowsArgs &a, int b, bool *bad
   } else {
     s.len = length_or_none(a.lens[b], a.pages_per_seq, a.d.page_shift, bad);
   }
-  s.units = a.d.n_kv_heads * runs_of<COLS>(s.n, a.group);
-  s.tiles = seen_tiles(s.len, seen_from(s.len - s.n, a.window), a.sinks, TILE);
+  s.units = a.d.n_kv_heads * runs_of(s.n, a.group, k.cols);
+  s.tiles = seen_tiles(s.len, seen_from(s.len - s.n, a.window), a.sinks, k.tile);
   return s;
 }
 
-// What workgroup `wg` does: split `split` of `splits` of a unit of up to COLS columns, whose
-// slots begin at `slot`; false if it has nothing to do.  A sequence's units have as many
-// splits as its tiles ask for (of MIN tiles at least, where it has more than WHOLE), and
-// share out the tiles that they see themselves.  ONE_ROUND: with fewer units than workgroups
-// that run at once, no splits either that would make them more, and the longest sequences'
-// come first.
+// What workgroup `wg` does: split `split` of `splits` of a unit, whose slots begin at `slot`;
+// false if it has nothing to do.  A sequence's units have as many splits as its tiles ask for
+// (see rows_share), and share out the tiles that they see themselves.  one_round: the longest
+// sequences' come first.
 struct RowsWork {
   RowsSeq s;
   int b, unit, split, splits, slot;
@@ -52,15 +46,15 @@ struct RowsWork {
   }
 };
 
-template <int TILE, int COLS, int WHOLE, int MIN, int NW, bool ONE_ROUND>
-__device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds, RowsWork *w) {
+template <int NW>
+__device__ __forceinline__ bool plan_rows(RowsKind k, const KvRowsArgs &a, int wg, int *lds, RowsWork *w) {
   bool bad = false;
   if (a.unsplit && !a.row_start) {  // no sequence can have a split: a workgroup per unit
-    const int units = a.d.n_kv_heads * runs_of<COLS>(1, a.group);
+    const int units = a.d.n_kv_heads * runs_of(1, a.group, k.cols);
     *w = RowsWork{};
     w->b = (unsigned)wg / (unsigned)units;
     w->unit = wg - w->b * units;
-    w->s = rows_of<TILE, COLS>(a, w->b, &bad);
+    w->s = rows_of(k, a, w->b, &bad);
     w->splits = 1;
     if (bad && threadIdx.x == 0) raise_status(a.status, kStatusPage);
     return true;
@@ -68,13 +62,12 @@ __device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds,
   PlanScan<NW> scan(a.n_seqs, lds);
   const int b0 = scan.me * scan.per;
   RowsSeq s0{};
-  if (b0 < a.n_seqs) s0 = rows_of<TILE, COLS>(a, b0, &bad);
+  if (b0 < a.n_seqs) s0 = rows_of(k, a, b0, &bad);
   int seq = b0;  // whose s0 is
-  if (ONE_ROUND && !scan.block && __ballot(b0 < a.n_seqs && s0.tiles.count != __builtin_amdgcn_readfirstlane(s0.tiles.count))) {
+  if (k.one_round && !scan.block && __ballot(b0 < a.n_seqs && s0.tiles.count != __builtin_amdgcn_readfirstlane(s0.tiles.count))) {
     // the longest first, so that none of theirs is left for the end (16 sequences of up to
     // 1024 rows: 82.6 -> 69.2 us; where all are alike it would cost up to 5 of 100)
-    static_assert(!ONE_ROUND || TILE >= 64, "a key below 2^31");
-    const int key = s0.tiles.count << 6 | (63 - scan.me);
+    const int key = s0.tiles.count << 6 | (63 - scan.me);  // below 2^31: such tiles have 64 keys
     int rank = 0;
     for (int j = 0; j < a.n_seqs; ++j) rank += __builtin_amdgcn_readlane(key, j) > key;
     seq = __builtin_amdgcn_ds_permute(4 * (scan.me < a.n_seqs ? rank : scan.me), scan.me);
@@ -84,7 +77,7 @@ __device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds,
   auto each = [&](auto f) {
     if (b0 < a.n_seqs) f(s0);
     for (int i = 1; i < scan.per; ++i)
-      if (b0 + i < a.n_seqs) f(rows_of<TILE, COLS>(a, b0 + i, &bad));
+      if (b0 + i < a.n_seqs) f(rows_of(k, a, b0 + i, &bad));
   };
   int64_t n = 0;
   int my_units = 0, units, hi, lo, mine, upto, wgs, all;
@@ -93,35 +86,25 @@ __device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds,
     my_units += s.units;
   });
   if (bad && wg == 0) raise_status(a.status, kStatusPage);
-  int share = 1 << 30;
+  auto count = [&](int share) {  // workgroups of this thread's sequences, up to them, and all
+    mine = 0;
+    each([&](const RowsSeq &s) { mine += rows_splits(k, s.tiles.count, share) * s.units; });
+    upto = scan(mine, &wgs);
+    return wgs;
+  };
+  int share = kUncut;
   if (!a.unsplit) {
     scan((int)(n >> 22), &hi);
     scan((int)(n & 0x3FFFFF), &lo);
-    share = first_share(((int64_t)hi << 22) + lo, a.target, MIN);
+    share = first_share(((int64_t)hi << 22) + lo, a.target, k.min_tiles);
   }
   scan(my_units, &units);
-  // ONE_ROUND: a remainder of less than half a share is not worth a join
-  auto whole = [&]() { return ONE_ROUND ? max(WHOLE, share + (share >> 1)) : WHOLE; };
-  auto count = [&]() {  // workgroups of this thread's sequences, and up to them
-    mine = 0;
-    each([&](const RowsSeq &s) { mine += splits_of(s.tiles.count, share, whole()) * s.units; });
-    upto = scan(mine, &wgs);
-  };
-  count();
-  // with fewer units than run at once
-  for (int i = 0; units < a.target && i < kShareTries && wgs > a.target; ++i) {
-    share = next_share(share);
-    count();
-  }
-  if (ONE_ROUND && units < a.target && wgs > a.target) {
-    share = 1 << 30;
-    count();
-  }
+  share = rows_share(k, share, units, a.target, count);
   if (wg >= wgs) return false;
   int in_slots = 0;  // workgroups in split units, for the slots
   each([&](const RowsSeq &s) {
-    const int k = splits_of(s.tiles.count, share, whole());
-    if (k > 1) in_slots += k * s.units;
+    const int splits = rows_splits(k, s.tiles.count, share);
+    if (splits > 1) in_slots += splits * s.units;
   });
   int slot = scan(in_slots, &all) - in_slots, start = upto - mine, b = b0;
   if (!scan.block) {
@@ -140,12 +123,12 @@ __device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds,
     if (upto > wg && start <= wg) {  // one thread: it looks for the sequence among its own
       RowsSeq s = s0;
       for (;;) {
-        const int k = splits_of(s.tiles.count, share, whole());
-        if (start + k * s.units > wg) break;
-        start += k * s.units;
-        if (k > 1) slot += k * s.units;
+        const int splits = rows_splits(k, s.tiles.count, share);
+        if (start + splits * s.units > wg) break;
+        start += splits * s.units;
+        if (splits > 1) slot += splits * s.units;
         if (++b >= min(b0 + scan.per, a.n_seqs)) break;
-        s = rows_of<TILE, COLS>(a, b, &bad);
+        s = rows_of(k, a, b, &bad);
       }
       const int found[3] = {b, start, slot};
 #pragma unroll
@@ -157,9 +140,9 @@ __device__ __forceinline__ bool plan_rows(const KvRowsArgs &a, int wg, int *lds,
     slot = __builtin_amdgcn_readfirstlane(scan.lds[2]);
     if (b >= a.n_seqs) return false;  // only if the caller's arrays change while this runs
     w->b = b;
-    w->s = rows_of<TILE, COLS>(a, b, &bad);
+    w->s = rows_of(k, a, b, &bad);
   }
-  w->splits = splits_of(w->s.tiles.count, share, whole());
+  w->splits = rows_splits(k, w->s.tiles.count, share);
   w->unit = (unsigned)(wg - start) / (unsigned)w->splits;
   if (w->unit >= w->s.units) return false;  // likewise
   w->split = wg - start - w->unit * w->splits;

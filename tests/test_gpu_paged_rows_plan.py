@@ -1,0 +1,45 @@
+"""Attention of many new rows with as many units as workgroups run at once, some sequences long and others short: every row
+is written, and the handle's later split calls are right too; against the definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from tests import rows_oracle as R
+from tests.test_gpu_paged import BF16, F32, dev, draw
+from tests.test_gpu_paged_rows import check, handle, made, starts_of
+
+pytestmark = pytest.mark.gpu
+
+MIXES = [
+    # hkv, group, hd, new rows, lengths, given
+    (8, 4, 128, [10, 483], [3000, 483], BF16),
+    (8, 4, 128, [10, 481], [3000, 481], F32),
+    (8, 4, 128, [241, 241], [10000, 241], BF16),
+    (1, 8, 256, [1, 2033], [4000, 2033], BF16),
+    (8, 4, 64, [10, 995], [3000, 995], BF16),
+    (4, 4, 128, [385, 609], [19200, 609], BF16),
+    (8, 4, 128, [65, 65, 65, 257], [6000, 65, 65, 257], F32),
+]
+
+
+def call(kv, c, q, new):
+    out = torch.full_like(q, float("nan"))
+    kv.attend_rows(0, q, dev(c.table), dev(c.lens), dev(starts_of(new)), out=out)
+    return out
+
+
+@pytest.mark.parametrize("i", range(len(MIXES)))
+def test_as_many_units_as_run_at_once(gpu, i):
+    hkv, group, hd, new, lens, given = MIXES[i]
+    c = made(40 + i, hkv, hd, 64, lens, BF16)
+    kv = handle(c, hkv * group, rope=hd)
+    q = (1.5 * draw(i, sum(new), hkv * group, hd)).to(given)
+    got = call(kv, c, dev(q), new)
+    # split calls of other numbers of rows afterwards, on the same handle
+    others = [[64] + [0] * (len(new) - 1), [min(n, 20) for n in new], [1] * len(new)]
+    later = [call(kv, c, dev(q[:sum(n)]), n) for n in others]
+    kv.synchronize()
+    for out, n in zip([got, *later], [new, *others]):
+        want = R.attend_rows(c, 0, q[:sum(n)].double().numpy(), n, hd, False, 1 / math.sqrt(hd))
+        check(out.double().cpu().numpy(), want, hd, given, n)
