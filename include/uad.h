@@ -463,7 +463,8 @@ uad_status uad_kv_set_block_scales(uad_kv *kv, float *k_scales, float *v_scales)
  * A key that a row does not see is as if it were not there, whatever its slots hold; a NaN
  * in the row, or in a key or value that it sees, makes the outputs that it enters NaN, an
  * infinity may.  With n_rows or n_seqs 0 nothing is enqueued.  Nothing is written for a
- * sequence whose length or start cannot be used (without row_start: zeros).
+ * sequence whose length or start cannot be used (without row_start: zeros), and where starts
+ * fall perhaps not for all rows of others.
  * Errors as uad_kv_append, and UAD_E_INVALID (window or n_sinks below 0, n_sinks without a
  * window, causal not 0 or 1, scale not finite), UAD_E_SHAPE (n_rows * n_heads above 2^25). */
 uad_status uad_kv_attend_rows(uad_kv *kv, int32_t layer, const void *q, void *out, int32_t dtype, int64_t ldq, int64_t ldo,

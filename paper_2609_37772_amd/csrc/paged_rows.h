@@ -14,11 +14,12 @@ struct RowsSeq {
 };
 
 // Sequence b; one that cannot be used has no units.
-__device__ __forceinline__ RowsSeq rows_of(RowsKind k, const KvRowsArgs &a, int b, bool *bad) {
+__device__ __forceinline__ RowsSeq rows_of(RowsKind k, const KvRowsArgs &a, int b, bool *bad, bool *falls) {
   RowsSeq s{b, 1, 0, 0, {}};
   if (a.row_start) {
     s.from = a.row_start[b];
     const int to = a.row_start[b + 1], len = a.lens[b];
+    *falls |= s.from > to;
     const bool ok = sequence_ok(b, s.from, to, a.n_rows, len, a.pages_per_seq, a.d.page_shift);
     *bad |= !ok;
     s.n = ok ? to - s.from : 0;
@@ -48,13 +49,13 @@ struct RowsWork {
 
 template <int NW>
 __device__ __forceinline__ bool plan_rows(RowsKind k, const KvRowsArgs &a, int wg, int *lds, RowsWork *w) {
-  bool bad = false;
+  bool bad = false, falls = false;
   if (a.unsplit && !a.row_start) {  // no sequence can have a split: a workgroup per unit
     const int units = a.d.n_kv_heads * runs_of(1, a.group, k.cols);
     *w = RowsWork{};
     w->b = (unsigned)wg / (unsigned)units;
     w->unit = wg - w->b * units;
-    w->s = rows_of(k, a, w->b, &bad);
+    w->s = rows_of(k, a, w->b, &bad, &falls);
     w->splits = 1;
     if (bad && threadIdx.x == 0) raise_status(a.status, kStatusPage);
     return true;
@@ -62,7 +63,7 @@ __device__ __forceinline__ bool plan_rows(RowsKind k, const KvRowsArgs &a, int w
   PlanScan<NW> scan(a.n_seqs, lds);
   const int b0 = scan.me * scan.per;
   RowsSeq s0{};
-  if (b0 < a.n_seqs) s0 = rows_of(k, a, b0, &bad);
+  if (b0 < a.n_seqs) s0 = rows_of(k, a, b0, &bad, &falls);
   int seq = b0;  // whose s0 is
   if (k.one_round && !scan.block && __ballot(b0 < a.n_seqs && s0.tiles.count != __builtin_amdgcn_readfirstlane(s0.tiles.count))) {
     // the longest first, so that none of theirs is left for the end (16 sequences of up to
@@ -77,7 +78,7 @@ __device__ __forceinline__ bool plan_rows(RowsKind k, const KvRowsArgs &a, int w
   auto each = [&](auto f) {
     if (b0 < a.n_seqs) f(s0);
     for (int i = 1; i < scan.per; ++i)
-      if (b0 + i < a.n_seqs) f(rows_of(k, a, b0 + i, &bad));
+      if (b0 + i < a.n_seqs) f(rows_of(k, a, b0 + i, &bad, &falls));
   };
   int64_t n = 0;
   int my_units = 0, units, hi, lo, mine, upto, wgs, all;
@@ -92,8 +93,11 @@ __device__ __forceinline__ bool plan_rows(RowsKind k, const KvRowsArgs &a, int w
     upto = scan(mine, &wgs);
     return wgs;
   };
+  // Sequences whose starts fall share rows with others, which may be more than the launch is
+  // for: units stay whole then, so that none is begun without an end.
+  const bool any_falls = a.row_start && (scan.block ? __syncthreads_or(falls) != 0 : __ballot(falls) != 0);
   int share = kUncut;
-  if (!a.unsplit) {
+  if (!a.unsplit && !any_falls) {
     scan((int)(n >> 22), &hi);
     scan((int)(n & 0x3FFFFF), &lo);
     share = first_share(((int64_t)hi << 22) + lo, a.target, k.min_tiles);
@@ -128,7 +132,7 @@ __device__ __forceinline__ bool plan_rows(RowsKind k, const KvRowsArgs &a, int w
         start += splits * s.units;
         if (splits > 1) slot += splits * s.units;
         if (++b >= min(b0 + scan.per, a.n_seqs)) break;
-        s = rows_of(k, a, b, &bad);
+        s = rows_of(k, a, b, &bad, &falls);
       }
       const int found[3] = {b, start, slot};
 #pragma unroll
@@ -138,13 +142,14 @@ __device__ __forceinline__ bool plan_rows(RowsKind k, const KvRowsArgs &a, int w
     b = __builtin_amdgcn_readfirstlane(scan.lds[0]);
     start = __builtin_amdgcn_readfirstlane(scan.lds[1]);
     slot = __builtin_amdgcn_readfirstlane(scan.lds[2]);
-    if (b >= a.n_seqs) return false;  // only if the caller's arrays change while this runs
+    // only if the caller's arrays change while this runs, or starts fall so often that sums overflow
+    if ((unsigned)b >= (unsigned)a.n_seqs) return false;
     w->b = b;
-    w->s = rows_of(k, a, b, &bad);
+    w->s = rows_of(k, a, b, &bad, &falls);
   }
   w->splits = rows_splits(k, w->s.tiles.count, share);
   w->unit = (unsigned)(wg - start) / (unsigned)w->splits;
-  if (w->unit >= w->s.units) return false;  // likewise
+  if ((unsigned)w->unit >= (unsigned)w->s.units) return false;  // likewise
   w->split = wg - start - w->unit * w->splits;
   w->slot = slot + w->unit * w->splits;
   if (w->splits > 1 && w->slot + w->splits > a.slots) return false;  // likewise

@@ -19,10 +19,12 @@ static void plan(const RowsKind &k, bool cut, int n_rows, int n_seqs, const int 
   const RowsGrid grid = rows_grid(k, n_rows, n_seqs, true, hkv, group, cut ? (int64_t)pages << shift : k.tile, window, sinks, target, max_slots(target));
   int64_t tiles = 0;
   int units = 0, wgs = 0, slots = 0;
+  bool falls = false;
   std::vector<SeenTiles> seen;
   std::vector<int> of;
   for (int b = 0; b < n_seqs; ++b) {
     const bool ok = sequence_ok(b, starts[b], starts[b + 1], n_rows, lens[b], pages, shift);
+    falls |= starts[b] > starts[b + 1];
     const int n = ok ? starts[b + 1] - starts[b] : 0, len = ok ? lens[b] : 0;
     of.push_back(hkv * runs_of(n, group, k.cols));
     seen.push_back(seen_tiles(len, seen_from(len - n, window), sinks, k.tile));
@@ -34,7 +36,7 @@ static void plan(const RowsKind &k, bool cut, int n_rows, int n_seqs, const int 
     for (int b = 0; b < n_seqs; ++b) wgs += rows_splits(k, seen[b].count, share) * of[b];
     return wgs;
   };
-  const int share = rows_share(k, grid.unsplit ? kUncut : first_share(tiles, target, k.min_tiles), units, target, count);
+  const int share = rows_share(k, grid.unsplit || falls ? kUncut : first_share(tiles, target, k.min_tiles), units, target, count);
   for (int b = 0; b < n_seqs; ++b) {
     const int s = rows_splits(k, seen[b].count, share);
     if (s > 1) slots += s * of[b];
@@ -112,6 +114,16 @@ def plan(lib, kind, new, lens, hkv, group, target, starts=None, n_rows=None, win
 def test_as_many_units_as_run_at_once(lib, new, lens, hkv, group, target):
     units, wgs, slots, grid = plan(lib, MANY[0], new, lens, hkv, group, target)
     assert units == target and wgs <= grid and slots <= 2 * target
+
+
+@pytest.mark.parametrize("kind", FEW + MANY)
+@pytest.mark.parametrize("n_seqs,rows", [(5, 200), (5, 483), (90, 100), (3, 90)])
+def test_starts_that_fall_leave_units_whole(lib, kind, n_seqs, rows):
+    """Starts 0, n, 0, n, ..: usable sequences have more rows in all than the call, and the launch is for the call's.  No unit
+    has splits then, so none is begun whose others are missing."""
+    starts, lens = [rows * (b % 2) for b in range(n_seqs + 1)], [10000] + [rows] * (n_seqs - 1)
+    units, wgs, slots, _ = plan(lib, kind, None, lens, 8, 4, 256, starts=starts, n_rows=rows)
+    assert slots == 0 and wgs == units == 8 * ((n_seqs + 1) // 2) * -(-rows * 4 // kind[0][1])
 
 
 @pytest.mark.parametrize("kind", FEW + MANY)
