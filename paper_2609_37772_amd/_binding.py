@@ -8,6 +8,7 @@ missing or fails to load, every call raises.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Dict, Optional, Tuple
 
@@ -433,6 +434,17 @@ def _check_kv(kv, st: int, what: str):
         raise UadError(st, f"{what}: {uad_kv_last_error(kv)}")
 
 
+def _i32(value, name: str) -> int:
+    """A whole number of 32 bits, as the C interface takes; raises for any other (ctypes would cut it to 32 bits)."""
+    try:
+        n = operator.index(value)
+    except TypeError:
+        raise ValueError(f"{name} must be a whole number, got {value!r}") from None
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name} must be a number of 32 bits, got {n}")
+    return n
+
+
 def _row_step(t, shape: Tuple[int, int], name: str, device: int) -> int:
     """Elements between the rows of a device tensor [n][heads][head_dim], each row dense; raises for any other."""
     if not isinstance(t, torch.Tensor) or t.dtype not in _ROW_TYPES:
@@ -470,7 +482,7 @@ def _table(page_table: torch.Tensor, lens: torch.Tensor, device: int) -> Tuple[i
         n, wide = size = page_table.shape
     except (AttributeError, ValueError):
         raise ValueError("page_table must be an int32 device tensor [n_seqs][pages_per_seq]") from None
-    return _ints(page_table, size, "page_table", device), wide, _ints(lens, (n,), "lens", device), n
+    return _ints(page_table, size, "page_table", device), _i32(wide, "pages_per_seq"), _ints(lens, (n,), "lens", device), _i32(n, "n_seqs")
 
 
 def uad_kv_create(n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int,
@@ -478,8 +490,10 @@ def uad_kv_create(n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, p
                   v_scale: float, k: torch.Tensor, v: torch.Tensor, device: int = 0,
                   stream: Optional[torch.cuda.Stream] = None) -> int:
     """Create a paged-cache handle over the pools ``k`` and ``v`` (kept by the caller); returns it."""
-    cfg = uad_kv_config(n_layers, n_heads, n_kv_heads, head_dim, page_size, n_pages, max_seqs, dtype, rope_dim,
-                        rope_pairs, float(rope_theta), float(k_scale), float(v_scale), k.data_ptr(), v.data_ptr())
+    sizes = dict(n_layers=n_layers, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, page_size=page_size, n_pages=n_pages,
+                 max_seqs=max_seqs, dtype=dtype, rope_dim=rope_dim, rope_pairs=rope_pairs)
+    cfg = uad_kv_config(*(_i32(value, name) for name, value in sizes.items()), float(rope_theta), float(k_scale), float(v_scale),
+                        k.data_ptr(), v.data_ptr())
     if stream is None:
         stream = torch.cuda.current_stream(device)
     out = ctypes.c_void_p()
@@ -521,7 +535,8 @@ def _append_checked(kv, layer, k, v, page_table, lens, row_start, positions, row
     pt, wide, pl, seqs = _table(page_table, lens, device)
     ps = None if row_start is None else _ints(row_start, (seqs + 1,), "row_start", device)
     pp = None if positions is None else _ints(positions, (n,), "positions", device)
-    return load_library().uad_kv_append(kv, layer, k.data_ptr(), v.data_ptr(), dtype, ldk, ldv, n, ps, pl, pp, pt, wide, seqs)
+    return load_library().uad_kv_append(kv, _i32(layer, "layer"), k.data_ptr(), v.data_ptr(), dtype, ldk, ldv, n, ps, pl, pp, pt, wide,
+                                        seqs)
 
 
 def uad_kv_attend(kv: int, layer: int, q: torch.Tensor, out: torch.Tensor, page_table: torch.Tensor,
@@ -545,7 +560,8 @@ def _attend_checked(kv, layer, q, out, page_table, lens, positions, scale, row_s
     if n != seqs:
         raise ValueError("q and out must have a row per sequence")
     pp = None if positions is None else _ints(positions, (seqs,), "positions", device)
-    return load_library().uad_kv_attend(kv, layer, q.data_ptr(), out.data_ptr(), dtype, ldq, ldo, pl, pp, pt, wide, seqs, scale)
+    return load_library().uad_kv_attend(kv, _i32(layer, "layer"), q.data_ptr(), out.data_ptr(), dtype, ldq, ldo, pl, pp, pt, wide, seqs,
+                                        scale)
 
 
 def uad_kv_set_block_scales(kv: int, k_scales: Optional[torch.Tensor], v_scales: Optional[torch.Tensor]) -> None:
@@ -575,8 +591,8 @@ def _rows_checked(kv, layer, q, out, page_table, lens, row_start, positions, sca
     pt, wide, pl, seqs = _table(page_table, lens, device)
     ps = None if row_start is None else _ints(row_start, (seqs + 1,), "row_start", device)
     pp = None if positions is None else _ints(positions, (n,), "positions", device)
-    return load_library().uad_kv_attend_rows(kv, layer, q.data_ptr(), out.data_ptr(), dtype, ldq, ldo, n, ps, pl, pp, pt, wide, seqs,
-                                             scale, window, n_sinks, int(causal))
+    return load_library().uad_kv_attend_rows(kv, _i32(layer, "layer"), q.data_ptr(), out.data_ptr(), dtype, ldq, ldo, n, ps, pl, pp, pt,
+                                             wide, seqs, scale, _i32(window, "window"), _i32(n_sinks, "n_sinks"), int(causal))
 
 
 def uad_kv_reserve(kv: int, lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
@@ -606,7 +622,7 @@ def _reserve_checked(kv, lens, page_table, free_pages, n_free, new_tokens, row_s
         if not isinstance(slots, torch.Tensor) or slots.dtype is not torch.int64 or slots.dim() != 1 \
                 or slots.get_device() != device or not slots.is_contiguous():
             raise ValueError(f"slots must be a contiguous int64 tensor [n_rows] on device {device}")
-        n, pl64 = slots.shape[0], slots.data_ptr()
+        n, pl64 = _i32(slots.shape[0], "the length of slots"), slots.data_ptr()
     return load_library().uad_kv_reserve(kv, pl, px, po, pt, wide, seqs, pf, pn, pno, ps, pl64, n)
 
 
@@ -627,7 +643,7 @@ def uad_kv_release(kv: int, lens: torch.Tensor, page_table: torch.Tensor, free_p
 def _release_checked(kv, lens, page_table, free_pages, n_free, window, n_sinks, n_pages, device) -> int:
     pt, wide, pl, seqs = _table(page_table, lens, device)
     pf, pn = _ints(free_pages, (n_pages,), "free_pages", device), _ints(n_free, (1,), "n_free", device)
-    return load_library().uad_kv_release(kv, pl, pt, wide, seqs, pf, pn, window, n_sinks)
+    return load_library().uad_kv_release(kv, pl, pt, wide, seqs, pf, pn, _i32(window, "window"), _i32(n_sinks, "n_sinks"))
 
 
 def uad_kv_synchronize(kv: int) -> None:
@@ -638,4 +654,4 @@ def uad_set_prefix_paged(ctx: int, kv: int, page_table: torch.Tensor, lens: torc
                          device: int = 0) -> None:
     """The first prefix_len tokens of each sequence of a paged cache become the expert's prefix K/V."""
     pt, wide, pl, seqs = _table(page_table, lens, device)
-    _check(ctx, load_library().uad_set_prefix_paged(ctx, kv, pl, pt, wide, seqs, prefix_len), "uad_set_prefix_paged")
+    _check(ctx, load_library().uad_set_prefix_paged(ctx, kv, pl, pt, wide, seqs, _i32(prefix_len, "prefix_len")), "uad_set_prefix_paged")
