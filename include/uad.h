@@ -493,6 +493,7 @@ uad_status uad_kv_attend_rows(uad_kv *kv, int32_t layer, const void *q, void *ou
  * n_free_out are lens and n_free then, row_start is all 0 and slots all -1, so that an append
  * with that row_start adds nothing.  An id outside the pool goes into the table as it is,
  * gives the slots -1 and raises UAD_E_PAGE too.
+ * With n_seqs 0 nothing is enqueued and no output is written, n_free_out and slots neither.
  * Other arguments must not overlap.  Errors: UAD_E_INVALID (null pointer, n_rows or n_seqs
  * below 0, slots unaligned), UAD_E_SHAPE (n_seqs beyond max_seqs, a page table of more than
  * 2^30 tokens per sequence), UAD_E_HIP. */
@@ -502,8 +503,9 @@ uad_status uad_kv_reserve(uad_kv *kv, const int32_t *lens, const int32_t *new_to
 
 /* Give back the pages that no later token of their sequence sees: every entry >= 0 of a
  * table row, but those of pages that hold a position x < lens[b] with x < n_sinks, with
- * x > lens[b] - window, or any such x if window is 0, and of a last page that is not full.  They go to the top of the stack in the
- * order of sequences and entries, their entries become -1 and n_free[0] counts them.  So
+ * x > lens[b] - window, or any such x if window is 0, and of a last page that is not full.
+ * They go to the top of the stack in the order of sequences and entries, their entries become
+ * -1 and n_free[0] counts them; with n_seqs 0 nothing is enqueued.  So
  * window 0 gives back what a shorter lens leaves over, all of a sequence's at length 0, and
  * a decoding step with a window keeps what the window and the sinks need.  A page that
  * several sequences read is given back for each of them: leave such rows out.
