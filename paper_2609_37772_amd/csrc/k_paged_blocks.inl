@@ -195,14 +195,15 @@ __global__ __launch_bounds__(64 * BLOCKS * PARTS) void kv_append_blocks_kernel(K
   if (lane == 0 && part == 0 && tokens && (!held || grows)) *scales = scale;
   const size_t base = page_base(a.d, page, head);
   // nothing to cut and a power of two: the quotients are products, exactly
-  const bool plain = __builtin_amdgcn_readfirstlane(most_any <= 448.f * scale && (__float_as_uint(scale) & 0x7FFFFFu) == 0) != 0;
+  const bool plain = __builtin_amdgcn_readfirstlane(most_any <= 448.f * scale && most_any < INFINITY && (__float_as_uint(scale) & 0x7FFFFFu) == 0) != 0;
   auto quantised = [&](float *x) {
     if (plain) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] *= inv;
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = quotient(x[e], scale, inv);
+      for (int e = 0; e < 8; ++e)  // infinities apart: of a scale that the caller has set, 448 times it may be one too
+        x[e] = fabsf(x[e]) == INFINITY ? copysignf(448.f, x[e]) : quotient(x[e], scale, inv);
     }
   };
   if (!is_v) {
