@@ -408,23 +408,38 @@ static hipError_t launch_rows_hd(const KvRowsArgs &a, bool f32, bool f8, hipStre
 
 // Which kernel: 0: that of few rows; else the waves that share a column of that of many.
 // The kernel of few rows reads a KV head's cache for every 16 columns, that of many for 64
-// or 128, with more to do before and after: the one loses from a size of the query on,
-// whatever the lengths.  us, few rows / many (two waves a column), causal, short and long
-// histories:
-//   query elements  head dim 256             128                       64                        128, 8 bits
-//   65k to 130k     20.7 / 20.9, 40.8 / 33   11.9 / 15.3, 23.4 / 24.8  12.6 / 14.4, 24.7 / 23.1  18.2 / 26.1
-//   260k            14.9 / 15.9, 40.5 / 27   16.1 / 15.6, 40.7 / 28.2  6.6 / 8.2,   21.0 / 23.6  12.7 / 16.5, 30.3 / 29.6
-//   520k            38.6 / 25.2, 97.9 / 43   8.8 / 11.7,  62.5 / 25.6  22.0 / 17.6, 62.9 / 34.0  10.3 / 12.3, 45.4 / 27.7
-//   1000k           37.3 / 22.9, 173 / 50    42.6 / 23.4, 126 / 57     45.0 / 24.5, 118 / 54     35.5 / 26.0, 79 / 67
-// At head dim 256, where the kernel of few rows spills, 130k elements are enough; 33k, 16 rows
-// of 8 heads on 4000 tokens, take 28.0 us for 32.4.
+// or 128, with more to do before and after: the one loses from a size of the query on, the
+// sooner the longer the histories are, which the launch does not know.  us, few rows / many
+// (two waves a column): one causal sequence with nothing, 1500 and 8000 tokens before its
+// rows, 16/2 heads of 256 and 32/8 of 128 and 64; last, their ratio over these, 8 sequences of
+// an eighth of the rows, and other heads (8/1, 12/2, 4/4):
+//   query    bf16                                          8 bits
+//   256
+//    65k     11.9 / 15.5   25.1 / 27.4   40.3 / 48.3  0.90  14.7 / 15.8   22.0 / 29.0   32.9 / 50.1  0.83
+//   130k     12.1 / 15.4   27.8 / 28.3   60.4 / 44.1  1.05  14.7 / 15.9   22.8 / 29.7   44.1 / 47.7  0.91
+//   260k     12.9 / 15.5   36.8 / 29.3  100.8 / 45.4  1.35  15.0 / 16.0   29.7 / 31.9   67.3 / 49.7  1.07
+//   520k     15.3 / 17.8   53.3 / 29.5  182.9 / 65.1  1.68  15.8 / 19.0   41.0 / 32.5  115.1 / 70.1  1.23
+//   128
+//   130k      7.6 / 11.0   17.9 / 20.9   40.6 / 31.0  0.92   9.4 / 11.1   17.5 / 21.8   30.8 / 33.8  0.84
+//   260k      8.0 / 11.1   24.2 / 21.3   68.9 / 43.1  1.07   9.4 / 11.2   21.2 / 22.8   45.1 / 46.8  0.87
+//   520k      8.9 / 12.6   33.5 / 24.5  122.9 / 66.1  1.33   9.8 / 13.4   24.5 / 28.0   72.4 / 76.3  0.93
+//  1040k     20.8 / 16.2   64.0 / 34.6  241.7 / 117   1.75  19.2 / 17.7   43.6 / 39.9  139.2 / 137.6 1.16
+//   64
+//   130k      6.4 /  8.7   16.4 / 19.4   39.0 / 30.7  0.94   7.7 /  8.8   17.3 / 20.3   31.3 / 33.8  0.85
+//   260k      6.8 / 10.0   22.2 / 20.0   67.9 / 41.6  1.15   7.8 / 10.3   21.8 / 21.7   50.8 / 47.9  0.96
+//   520k     10.6 / 12.5   31.9 / 23.7  122.9 / 69.1  1.37  10.4 / 13.6   27.1 / 26.6   87.8 / 80.6  1.02
+// The kernel of many takes over where that ratio passes 1.  Prompts without a history lose by
+// that up to a million elements, 3 to 5 us of 9 to 18.
 // With fewer than 16 columns a sequence its units would be mostly empty.  Two waves share a
-// column where units of 128 columns would be too few to fill the chip or half empty (25 and
-// 30 us at 64 columns a sequence); from 256 full ones on one wave takes 69 us for 100 at head
-// dim 256, at 128 and 512 units 198 for 214, of 8 bits 225 for 268.
-static int prompt_key_waves(const KvRowsArgs &a) {
+// column where units of 128 columns would be half empty or too few to fill the chip: from 256
+// full ones on one wave a column is as fast or faster, but for a single sequence's causal rows
+// at 256 of them (two waves / one: 256, 400 and 1024 units of 16/2 heads of 256, one sequence
+// with 1500 tokens before its rows 222 / 242, 456 / 386, 1795 / 1560; of 32/8 of 128 124 /
+// 139, 247 / 189, 785 / 600; of 64 71 / 80, 128 / 118, 408 / 343; 16 sequences of 32/8 of 128
+// 104 / 96, 194 / 138, 404 / 291; below 256 of them, 128 full ones, 61 / 113).
+static int prompt_key_waves(const KvRowsArgs &a, bool f8) {
   const int64_t columns = (int64_t)a.n_rows * a.group;
-  const int64_t few = a.d.head_dim == 256 ? 130000 : 250000;
+  const int64_t few = a.d.head_dim == 256 ? (f8 ? 200000 : 130000) : !f8 ? 250000 : a.d.head_dim == 128 ? 650000 : 500000;
   if (!a.row_start || columns < 16 * (int64_t)a.n_seqs || columns * a.d.n_kv_heads * a.d.head_dim < few) return 0;
   return columns < 128 * (int64_t)a.n_seqs || columns / 128 * a.d.n_kv_heads < 256 ? 2 : 1;
 }
@@ -434,7 +449,7 @@ hipError_t launch_kv_rows(const KvRowsArgs &a, bool f32, bool f8, hipStream_t s)
       a.target < 1 || a.slots < max_slots(a.target) || a.d.page_shift < 4 || a.window < 0 || a.sinks < 0 ||
       (!a.row_start && a.n_rows != a.n_seqs) || (!f8 && a.k_scales))
     return hipErrorInvalidValue;
-  const int key_waves = prompt_key_waves(a);
+  const int key_waves = prompt_key_waves(a, f8);
   if (key_waves) return launch_kv_prompt(a, key_waves, f32, f8, s);
   if (a.d.head_dim == 64) return launch_rows_hd<64>(a, f32, f8, s);
   if (a.d.head_dim == 128) return launch_rows_hd<128>(a, f32, f8, s);
