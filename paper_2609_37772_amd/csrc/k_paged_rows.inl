@@ -430,17 +430,22 @@ static hipError_t launch_rows_hd(const KvRowsArgs &a, bool f32, bool f8, hipStre
 //   520k     10.6 / 12.5   31.9 / 23.7  122.9 / 69.1  1.37  10.4 / 13.6   27.1 / 26.6   87.8 / 80.6  1.02
 // The kernel of many takes over where that ratio passes 1.  Prompts without a history lose by
 // that up to a million elements, 3 to 5 us of 9 to 18.
-// With fewer than 16 columns a sequence its units would be mostly empty.  Two waves share a
-// column where units of 128 columns would be half empty or too few to fill the chip: from 256
-// full ones on one wave a column is as fast or faster, but for a single sequence's causal rows
-// at 256 of them (two waves / one: 256, 400 and 1024 units of 16/2 heads of 256, one sequence
-// with 1500 tokens before its rows 222 / 242, 456 / 386, 1795 / 1560; of 32/8 of 128 124 /
-// 139, 247 / 189, 785 / 600; of 64 71 / 80, 128 / 118, 408 / 343; 16 sequences of 32/8 of 128
-// 104 / 96, 194 / 138, 404 / 291; below 256 of them, 128 full ones, 61 / 113).
+// With few columns a sequence its units would be mostly empty.  64 sequences with 1000 tokens
+// before their rows, few / many: of 16 columns 54.1 / 83.9 (32/8 heads of 128), 35.3 / 44.6 (of
+// 64), 50.8 / 37.6 (16/2 of 256); of 32 96.8 / 85.9, 46.4 / 45.9, 118 / 39; in 8 bits of 32 76 /
+// 93, 39.1 / 50.6, 52.4 / 42.0; of 64 141 / 99, 69.5 / 53.3, 97.9 / 52.
+// Two waves share a column where units of 128 columns would be half empty or too few to fill
+// the chip: from 256 full ones on one wave a column is as fast or faster, but for a single
+// sequence's causal rows at 256 of them (two waves / one: 256, 400 and 1024 units of 16/2 heads
+// of 256, one sequence with 1500 tokens before its rows 222 / 242, 456 / 386, 1795 / 1560; of
+// 32/8 of 128 124 / 139, 247 / 189, 785 / 600; of 64 71 / 80, 128 / 118, 408 / 343; 16
+// sequences of 32/8 of 128 104 / 96, 194 / 138, 404 / 291; below 256 of them, 128 full ones, 61
+// / 113).
 static int prompt_key_waves(const KvRowsArgs &a, bool f8) {
   const int64_t columns = (int64_t)a.n_rows * a.group;
   const int64_t few = a.d.head_dim == 256 ? (f8 ? 200000 : 130000) : !f8 ? 250000 : a.d.head_dim == 128 ? 650000 : 500000;
-  if (!a.row_start || columns < 16 * (int64_t)a.n_seqs || columns * a.d.n_kv_heads * a.d.head_dim < few) return 0;
+  const int least = a.d.head_dim == 256 ? 16 : f8 ? 33 : 17;  // columns of a sequence, on average
+  if (!a.row_start || columns < least * (int64_t)a.n_seqs || columns * a.d.n_kv_heads * a.d.head_dim < few) return 0;
   return columns < 128 * (int64_t)a.n_seqs || columns / 128 * a.d.n_kv_heads < 256 ? 2 : 1;
 }
 

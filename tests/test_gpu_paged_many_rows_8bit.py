@@ -24,7 +24,10 @@ MANY = [
     (6, 3, 64, 16, [450], [460], BF16, "blocks", 32, True, 0, 0, True),
     (2, 150, 64, 32, [25, 2], [300, 1000], F32, F8, 64, False, 100, 7, True),
     (1, 200, 128, 16, [31], [500], BF16, "blocks", 128, False, 0, 0, True),
-    (8, 4, 128, 64, [i % 13 for i in range(130)], [i % 13 + (3000 if i == 77 else 5) for i in range(130)], BF16, "blocks", 128, False, 33, 2, True),
+    # sequences beyond a thread each
+    (8, 4, 128, 64, [5 + i % 17 for i in range(130)], [5 + i % 17 + (3000 if i == 77 else 5) for i in range(130)], BF16, "blocks", 128, False, 33, 2, True),
+    (2, 16, 128, 16, [3 + i % 4 for i in range(700)], [3 + i % 4 + (900 if i == 650 else i % 9) for i in range(700)], BF16, "blocks", 128, False, 20, 3, True),
+    (8, 4, 64, 16, [9 + i % 13 for i in range(130)], [9 + i % 13 + (3000 if i == 77 else 5) for i in range(130)], F32, "blocks", 64, False, 0, 0, True),
 ]
 
 
