@@ -16,9 +16,12 @@ namespace uad {
 //
 // Bound by memory with many rows: 64 prompts of 816 rows, head dim 256, read 53 MB and write
 // 27 in 21.4 us, 3.8 TB/s of the 5.4 that a copy reaches.  A block's rows must all be there
-// before the first is stored, and the table's entry before that: what hides those waits is
-// the other waves alone.  With few rows, by the chain of loads (length, page, rows): 64
-// sequences with a token each 4.1 us, 16 uneven prompts of 64 columns 5.1.
+// before the first is stored, and the table's entry before that.  Of the 1660 workgroups with
+// work two are on a CU at once (115 registers: four waves on a SIMD), so three to four come
+// one after the other, each with that whole chain; the next block's rows, on their way
+// meanwhile, would be 16 registers more (32 of fp32) and leave one workgroup a CU.  With few
+// rows, by the chain of loads (length, page, rows): 64 sequences with a token each 4.1 us, 16
+// uneven prompts of 64 columns 5.2.
 // ---------------------------------------------------------------------------
 // 4 e4m3 values times `ratio`, rounded anew.
 __device__ __forceinline__ uint32_t rescaled4(uint32_t w, float ratio) {
@@ -314,9 +317,12 @@ hipError_t launch_kv_append_blocks(const KvAppendArgs &a, bool f32, hipStream_t 
 // into LDS (up to kSumEntries of them; with more sequences an entry stands for a run), and
 // fills its share of the table's entries and of the slots, eight rows a thread.  Lengths
 // and the free pages' number may be written where the others read them: then by the last
-// workgroup to be done.  64 sequences with a token each: 4.5 us a call in a graph, four
-// dependent loads and four scans; 1024 prompts with 484 176 rows, whose 3.9 MB of slots
-// are the most of it: 10.5 us.
+// workgroup to be done.  64 sequences with a token each: 4.5 us a call in a graph: lengths,
+// the ids for the table and then, though they need not wait for those, the ids for the slots,
+// between four scans (without slots 0.8 us less).  1024 prompts with 484 176 rows: 10.1 us; as
+// many sequences with a row each take 6.5, the same rows of 8 sequences 8.9, the slots' 3.9 MB
+// at a copy's rate 0.8.  Without slots the launch has no measure of the rows, and a few
+// workgroups fill all of the table: 30 000 entries 65 us.
 // ---------------------------------------------------------------------------
 constexpr int kSumEntries = 2048, kSumsPerThread = kSumEntries / 256;
 

@@ -21,10 +21,10 @@ namespace uad {
 // value), as in the kernel of few rows: a row is held in no fewer bits for others that its
 // call has.  Keys and values as stored.
 //
-// Measured: one causal prompt of 8191 rows, 32/8 heads of 128: 1357 us, with three terms 1.2
-// PFLOP/s of the 1.3 to 1.4 that a library's large products reach; 816 rows that all see
-// each other, 8/1 heads of 256: 35 us; 16 prompts of up to 1024 rows in 8 bits, 12/2 heads of
-// 128: 92 us, not much more than the one unit with the most tiles takes.
+// Measured: one causal prompt of 8191 rows, 32/8 heads of 128: 1300 to 1360 us, with three
+// terms 1.2 to 1.27 PFLOP/s of the 1.3 to 1.4 that a library's large products reach; 816 rows
+// that all see each other, 8/1 heads of 256: 35 us; 16 prompts of up to 1024 rows in 8 bits,
+// 12/2 heads of 128: 91 us, not much more than the one unit with the most tiles takes.
 //
 // Masks as in the kernel of few rows: what no column sees is zero in V, and values that are
 // not finite where some columns do not see them are taken out of LDS and noted for those
@@ -33,7 +33,7 @@ namespace uad {
 constexpr int kPromptTile = 64;
 // Tiles of a split at least, and those up to which a unit stays whole: a split costs the query
 // anew and a join, which take as long as 3 tiles.  102 units of 13 tiles at head dim 256:
-// 36.0 us whole, 31.5 us in two; 16 units of 63: 130 whole, 43 split.
+// 43.6 us whole, 35.1 us in two; 32 units of 63: 158 whole, 46 split.
 template <int KW>
 __host__ __device__ constexpr RowsKind many_rows() { return {kPromptTile, 128 / KW, 6, 3, true}; }
 
@@ -41,7 +41,7 @@ __host__ __device__ constexpr RowsKind many_rows() { return {kPromptTile, 128 / 
 // and two waves are to share a SIMD's 512 registers.  At head dim 128 32 columns leave 18 of
 // the query's registers (28 with 8-bit pools) to be read again from memory for every tile, and
 // are faster all the same than 16, which read each operand from LDS for half as many columns:
-// a prompt of 8191 rows 1357 us for 1433, the fleet of 16 in 8 bits 92 for 99.  Where
+// a prompt of 8191 rows 1357 us for 1433, 16 of up to 1024 rows in 8 bits 92 for 99.  Where
 // workgroups are too few to fill the chip, 16 columns give each of them twice the waves: 8
 // sequences of 64 rows in 8 bits 73 us for 81; at 64 a tile of 8 bits has fewer pieces than
 // twice the threads.
@@ -180,7 +180,7 @@ __global__ __launch_bounds__((kPromptThreads<HD, KW>), 2) void kv_prompt_kernel(
   const int v_row = threadIdx.x / VP, v_key = ((threadIdx.x % VP) ^ v_bits(v_row)) * PIECE;
   const uint32_t v_offset = (((uint32_t)v_row << a.d.page_shift) + (v_key & 15)) * ESZ;
   // The loads of a tile are shared out over the products of the one before: issued all at
-  // once they held a wave up for 1000 to 1800 of the 5000 to 9000 clocks of a tile.
+  // once they held a wave up for 1000 to 1800 clocks a tile.
   int next_k0 = 0, next_pages = 0;  // pages in lanes 0 .. 3
   const char *next_v = nullptr;     // this thread's first piece of V^T
   uint32_t next_to = 0;

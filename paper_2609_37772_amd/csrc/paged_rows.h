@@ -67,7 +67,7 @@ __device__ __forceinline__ bool plan_rows(RowsKind k, const KvRowsArgs &a, int w
   int seq = b0;  // whose s0 is
   if (k.one_round && !scan.block && __ballot(b0 < a.n_seqs && s0.tiles.count != __builtin_amdgcn_readfirstlane(s0.tiles.count))) {
     // the longest first, so that none of theirs is left for the end (16 sequences of up to
-    // 1024 rows: 82.6 -> 69.2 us; where all are alike it would cost up to 5 of 100)
+    // 1024 rows: 109 -> 91 us; where they differ little it costs up to 4 of 100)
     const int key = s0.tiles.count << 6 | (63 - scan.me);  // below 2^31: such tiles have 64 keys
     int rank = 0;
     for (int j = 0; j < a.n_seqs; ++j) rank += __builtin_amdgcn_readlane(key, j) > key;
