@@ -402,7 +402,9 @@ uad_status uad_kv_set_stream(uad_kv *kv, void *hip_stream);
  *               lens[b] - n + j.
  * Errors: UAD_E_INVALID (null pointer, bad layer, dtype or row length),
  * UAD_E_SHAPE (n_seqs beyond max_seqs, n_rows != n_seqs without row_start, a page
- * table of more than 2^30 tokens per sequence), UAD_E_HIP. */
+ * table of more than 2^30 tokens per sequence; with row_start 2^31 runs of 64 tokens,
+ * or of a smaller page, that n_seqs sequences of up to n_rows new tokens each may
+ * touch), UAD_E_HIP. */
 uad_status uad_kv_append(uad_kv *kv, int32_t layer, const void *k, const void *v, int32_t dtype, int64_t ldk,
                          int64_t ldv, int32_t n_rows, const int32_t *row_start, const int32_t *lens,
                          const int32_t *positions, const int32_t *page_table, int32_t pages_per_seq, int32_t n_seqs);

@@ -161,6 +161,8 @@ uad_status uad_kv_append(uad_kv *kv, int32_t layer, const void *k, const void *v
     return kv_fail(kv, UAD_E_INVALID, fn, "ldk / ldv below n_kv_heads * head_dim or above 2^30");
   if (!row_start && n_rows != n_seqs) return kv_fail(kv, UAD_E_SHAPE, fn, "n_rows != n_seqs without row_start");
   if (none || n_seqs == 0) return UAD_OK;
+  if (row_start && append_tiles_overflow(n_rows, n_seqs, pages_per_seq, dims_of(kv).page_shift))
+    return kv_fail(kv, UAD_E_SHAPE, fn, "n_seqs times the rows that a sequence may have is too large");
   OnDevice on(kv->device);
   if (on.err() != hipSuccess) return kv_hip_fail(kv, on.err(), fn, "hipSetDevice");
   KvAppendArgs a{};

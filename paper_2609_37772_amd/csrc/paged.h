@@ -91,6 +91,12 @@ UAD_HD int64_t append_grid(int n_rows, int n_seqs, int shift) {
   const int64_t most = ((int64_t)n_rows >> shift) + 2 * (int64_t)n_seqs;
   return most < n_rows ? most : n_rows;
 }
+// Whether all sequences together can have more tiles than 32 bits count: only where starts
+// fall, so that several take the same rows, and a page table has 2^29 entries or more.
+UAD_HD bool append_tiles_overflow(int n_rows, int n_seqs, int pages_per_seq, int page_shift) {
+  const int64_t tokens = (int64_t)pages_per_seq << page_shift, rows = tokens < n_rows ? tokens : n_rows;
+  return n_seqs * ((rows >> append_tile_shift(page_shift)) + 2) > 0x7FFFFFFF;
+}
 // New rows of a sequence at row_start[b] .. row_start[b + 1]: usable, or an error.
 UAD_HD bool rows_ok(int from, int to, int n_rows) { return from >= 0 && from <= to && to <= n_rows; }
 // The same of sequence b whose length with them is `len`: all of its new rows can be
